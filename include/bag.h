@@ -328,6 +328,111 @@ bag_status bag_rel_l1(bag_ctx* ctx, const void* a, const void* b, int dtype, lon
 bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows, long cols,
                               float* out, void* cuda_stream);
 
+/* ---- 8-bit operands with a scale for each block of 128 ----
+ *
+ * An encoded matrix [rows, cols] is two device buffers: codes, one float8 e4m3 byte an element
+ * (row stride ldc bytes), and scales, one byte b for each row and block of 128 consecutive
+ * columns (row stride lds bytes), standing for 2^(b - 127) (E8M0, as the tensor cores read it;
+ * 255 is NaN).  An element is code * scale.  codes: 16-byte aligned, ldc >= cols and a multiple
+ * of 16; scales: 4-byte aligned, lds >= ceil(cols / 128) and a multiple of 4.  Bytes past the
+ * last column or block are neither read as values nor written. */
+
+/* Encode rows: each block of 128 columns (the last one of a row may be shorter) takes the least
+ * power of two with amax / scale <= 448 (not below 2^-127, which an all-zero block has), and
+ * each element is rounded to the nearest code, ties to even.  A block that holds an infinity
+ * or NaN takes scale 255, so that everything made from it is NaN.  x: device [rows, cols] of
+ * dtype BAG_F32 or BAG_BF16 with row stride ldx elements (>= cols; any alignment). */
+bag_status bag_quant_fp8(bag_ctx* ctx, const void* x, int dtype, long ldx, long rows, long cols,
+                         void* codes, long ldc, void* scales, long lds);
+
+/* bag_ln_mod encoded: (1 + scale) * LayerNorm(x) + shift row-wise (eps 1e-6), rounded from fp32
+ * straight to codes and scales.  x fp32 device [rows, cols], row stride ldx elements; cols a
+ * multiple of 4 up to 6144, x 16-byte aligned and ldx a multiple of 4 (else EUNSUPPORTED);
+ * shift / scale fp32 device [cols], 16-byte aligned (null = plain LayerNorm). */
+bag_status bag_ln_mod_fp8(bag_ctx* ctx, const float* x, long ldx, const float* shift,
+                          const float* scale, long rows, long cols, void* codes, long ldc,
+                          void* scales, long lds);
+
+/* What bag_gemm_fp8 does with y = A W^T + bias. */
+enum {
+  BAG_FP8_F32 = 0,   /* out fp32 [M, N] = act(y) */
+  BAG_FP8_BF16 = 1,  /* out bf16 [M, N] = act(y) */
+  BAG_FP8_CODES = 2, /* out codes and out_scales = act(y) encoded as by bag_quant_fp8 */
+  BAG_FP8_RESID = 3  /* out fp32 [M, N] += gate * y (gate [N], null = 1); act must be 0 */
+};
+/* Product of two encoded matrices on the tensor cores: A [M, K] (codes a, scales a_s), W [N, K]
+ * (codes w, scales w_s); products and their scales are summed over K in fp32.  bias: fp32
+ * device [N] or null.  act: 0 none, 1 GELU (tanh).  ldo: row stride of out in elements; any
+ * alignment of out, bias and gate (16-byte aligned rows are stored fastest), except codes, which
+ * keep an encoded matrix's rules (ldo bytes, out_s / ldos its scales; ignored otherwise).
+ * Any M >= 0, N >= 1, K >= 1.  The sums of a row do not depend on M's other rows, but their
+ * order (the split of K) may depend on M, N and K. */
+bag_status bag_gemm_fp8(bag_ctx* ctx, const void* a, long lda, const void* a_s, long ldas,
+                        const void* w, long ldw, const void* w_s, long ldws, const float* bias,
+                        long M, long N, long K, int act, int kind, const float* gate, void* out,
+                        long ldo, void* out_s, long ldos);
+
+/* ---- quantised cache ----
+ *
+ * A cache holds `capacity` rows of cols elements as integer codes with a bf16 scale for each
+ * group of consecutive columns: bits = 8, one byte an element (-127 .. 127), groups of 128;
+ * bits = 4, two elements a byte (-7 .. 7 in two's complement, the even column in the low half),
+ * groups of 32.  codes: 16-byte aligned, row stride ldc bytes, a multiple of 16 and at least a
+ * row's codes; scales: row stride lds elements, at least a row's groups.  Row r of a call lives
+ * in cache row slots[r] (device int32), or r where slots is null (then capacity >= rows).  A slot
+ * outside [0, capacity) is skipped by the write, and reads as zeros.  The slots of one write
+ * have to be distinct. */
+
+/* Keep rows of x - base (base null: of x): scale = bf16(amax / top) (top 127 or 7, amax times
+ * the rounded reciprocal), code = round(element / scale), ties to even.  A group whose scale
+ * would be below 2^-126 is kept as zeros; one that holds an infinity or NaN keeps a NaN scale
+ * and reads as NaN.  x, base: device fp32 [rows, cols], row strides ldx, ldb elements; any
+ * alignment (16-byte aligned rows are fastest). */
+bag_status bag_cache_write(bag_ctx* ctx, const float* x, long ldx, const float* base, long ldb,
+                           const int32_t* slots, long rows, long cols, int bits, void* codes,
+                           long ldc, void* scales, long lds, long capacity);
+
+/* out = base + code * scale (base null: code * scale), fp32 [rows, cols], row stride ldo
+ * elements; out may be base. */
+bag_status bag_cache_read(bag_ctx* ctx, const void* codes, long ldc, const void* scales, long lds,
+                          long capacity, const int32_t* slots, long rows, long cols, int bits,
+                          const float* base, long ldb, float* out, long ldo);
+
+/* ---- attention over selected blocks ----
+ *
+ * Queries and keys are taken in blocks of 128 consecutive rows (the last may be shorter), heads
+ * of 128 columns; type BAG_BF16 or BAG_F16 (fp16).  heads query heads share kv_heads key heads,
+ * heads a multiple of kv_heads, consecutive query heads sharing one. */
+enum { BAG_F16 = 2 };
+
+/* Pooled vectors of the blocks of x [rows, ld] (head h at columns [128 h, 128 h + 128)): the
+ * mean of a block's rows (fp32, summed in halves: row r + row r + 64, then r + 32, ...), rounded
+ * to 8-bit integers: codes int8 device [heads][ldb][128], scales fp32 device [heads][ldb]
+ * (amax / 127 of each vector, amax times the rounded reciprocal), ldb >= ceil(rows / 128).
+ * A vector that is not finite keeps codes and scale 0. */
+bag_status bag_block_pool(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads,
+                          void* codes, float* scales, long ldb);
+
+/* For each head and block of queries the `keep` of nkb key blocks with the highest score (the
+ * pooled query's codes times the pooled key's codes, summed exactly, times the key's scale; the
+ * query's own scale would not change the order), ties to the lower index: blocks int32 device
+ * [heads][ceil(nq / 128)][keep], each list ascending.  codes / scales / ldb: the keys' pooled
+ * vectors (kv_heads of them); 1 <= keep <= nkb <= 8192 (else EUNSUPPORTED). */
+bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, long nq, int heads,
+                            const void* codes, const float* scales, long ldb, long nkb,
+                            int kv_heads, int keep, int32_t* blocks);
+
+/* softmax(q k^T / sqrt(128)) v over the keys of each query block's listed key blocks, on the
+ * tensor cores.  q [nq, ldq], k [nk, ldk], v transposed per key head [kv_heads][128][vpad] (vpad
+ * >= nk, a multiple of 8), all of `type`, 16-byte aligned, row strides multiples of 8; o bf16
+ * [nq, ldo], 16-byte aligned, ldo a multiple of 8.  blocks: int32 device
+ * [heads][ceil(nq / 128)][keep]; a list ends at its first entry outside [0, ceil(nk / 128)), so
+ * shorter ones end in -1, and a block of queries with an empty list gets zeros.  An index listed
+ * twice counts twice. */
+bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const void* k, long ldk,
+                                const void* v, long vpad, int type, long nq, long nk, int heads,
+                                int kv_heads, const int32_t* blocks, int keep, void* o, long ldo);
+
 /* Failure-path check: launches one kernel whose mbarrier wait can never complete (no
  * thread arrives on it), so its bounded wait gives up after the library's wait limit
  * (about 2 s), records the sticky device error and returns; nothing faults or hangs.

@@ -23,6 +23,11 @@ SAMPLER = {"euler": 0, "unipc": 1}
 OBSERVABLE = {"modulated": 0, "embedded": 1}
 POLICY_BAG, POLICY_FULL, POLICY_MASK, POLICY_STATIC_UNIFORM, POLICY_THRESHOLD = 0, 1, 2, 3, 4
 LOG_FLOATS = 16
+# Output kinds of gemm_fp8
+FP8_F32, FP8_BF16, FP8_CODES, FP8_RESID = 0, 1, 2, 3
+SCALE_BLOCK = 128                  # columns of one scale of an encoded matrix
+CACHE_GROUP = {8: 128, 4: 32}      # columns of one scale of a quantised cache, by bits
+ATTN_BLOCK = 128                   # rows of a block of queries or keys
 STATUS = {0: "BAG_OK", 1: "BAG_EINVAL", 2: "BAG_ENOMEM", 3: "BAG_ECUDA", 4: "BAG_EORDER",
           5: "BAG_EDEVICE_TIMEOUT", 6: "BAG_ESTATE", 7: "BAG_EUNSUPPORTED"}
 
@@ -31,7 +36,9 @@ EXPORTS = ["bag_create", "bag_destroy", "bag_last_error", "bag_set_stream", "bag
            "bag_get_weight", "bag_forward_block", "bag_prepare", "bag_launch_count",
            "bag_gemm_bf16", "bag_attention_bf16", "bag_attention_f16", "bag_ln_mod", "bag_residual_add",
            "bag_profile_run", "bag_profile_launches", "bag_rel_l1", "bag_rel_l1_noalloc",
-           "bag_check_wait_timeout"]
+           "bag_check_wait_timeout", "bag_quant_fp8", "bag_ln_mod_fp8", "bag_gemm_fp8",
+           "bag_cache_write", "bag_cache_read", "bag_block_pool", "bag_block_select",
+           "bag_attention_blocks"]
 
 PROF_KINDS = ["gemm", "attention", "norm", "signal", "gate", "cache"]
 
@@ -113,6 +120,15 @@ def load(path=None):
         "bag_attention_f16": ([_P, _P, _P, _P, _P, _L, _I, _I, _I, _I, _L], _I),
         "bag_ln_mod": ([_P, _P, _P, _P, _P, _I, _I], _I),
         "bag_residual_add": ([_P, _P, _P, _P, _L], _I),
+        "bag_quant_fp8": ([_P, _P, _I, _L, _L, _L, _P, _L, _P, _L], _I),
+        "bag_ln_mod_fp8": ([_P, _P, _L, _P, _P, _L, _L, _P, _L, _P, _L], _I),
+        "bag_gemm_fp8": ([_P, _P, _L, _P, _L, _P, _L, _P, _L, _P, _L, _L, _L, _I, _I, _P, _P, _L,
+                          _P, _L], _I),
+        "bag_cache_write": ([_P, _P, _L, _P, _L, _P, _L, _L, _I, _P, _L, _P, _L, _L], _I),
+        "bag_cache_read": ([_P, _P, _L, _P, _L, _L, _P, _L, _L, _I, _P, _L, _P, _L], _I),
+        "bag_block_pool": ([_P, _P, _I, _L, _L, _I, _P, _P, _L], _I),
+        "bag_block_select": ([_P, _P, _I, _L, _L, _I, _P, _P, _L, _L, _I, _I, _P], _I),
+        "bag_attention_blocks": ([_P, _P, _L, _P, _L, _P, _L, _I, _L, _L, _I, _I, _P, _I, _P, _L], _I),
         "bag_rel_l1": ([_P, _P, _P, _I, _L, _L, _P, _P], _I),
         "bag_rel_l1_noalloc": ([_P, _P, _I, _L, _L, _P, _P], _I),
         "bag_profile_run": ([_P, _P, ctypes.POINTER(Cond), ctypes.POINTER(Stats),
@@ -313,6 +329,187 @@ class Context:
 
     def residual_add(self, out, h_in, R, n):
         self._chk(self.lib.bag_residual_add(self.h, _ptr(out), _ptr(h_in), _ptr(R), n))
+
+    # --- 8-bit operands, quantised cache, block-sparse attention (see include/bag.h) ----
+    def quant_fp8(self, x, codes, scales):
+        """Rows of x (fp32 or bf16 [rows, cols]) as e4m3 codes and power-of-two scales."""
+        _rows(x, "x", _itemsize(_is(x, "x", "float32", "bfloat16")))
+        rows, cols = x.shape
+        self._chk(self.lib.bag_quant_fp8(self.h, _ptr(x), int(_itemsize(x) == 2), _ld(x), rows, cols,
+                                         *_encoded(codes, scales, "codes", rows, cols)))
+
+    def ln_mod_fp8(self, x, shift, scale, codes, scales):
+        """ln_mod of fp32 rows, encoded as by quant_fp8."""
+        _rows(_is(x, "x", "float32"), "x", 4)
+        rows, cols = x.shape
+        self._chk(self.lib.bag_ln_mod_fp8(self.h, _ptr(x), _ld(x), _vector(shift, "shift", cols),
+                                          _vector(scale, "scale", cols), rows, cols,
+                                          *_encoded(codes, scales, "codes", rows, cols)))
+
+    def gemm_fp8(self, a, a_scales, w, w_scales, out, K, bias=None, gelu=False, gate=None, residual=False,
+                 out_scales=None, N=None):
+        """Product of encoded a [M, K] and w [N, K]: out fp32 or bf16 [M, N]; encoded, where
+        out_scales is given (N then says how many columns, default w's rows); or, with residual,
+        fp32 out += gate * (product + bias)."""
+        M, N = a.shape[0], w.shape[0] if N is None else N
+        if out_scales is not None:
+            kind = FP8_CODES
+            o, ldo, os, ldos = _encoded(out, out_scales, "out", M, N)
+        else:
+            _rows(_is(out, "out", "float32", "bfloat16"), "out", _itemsize(out))
+            if out.shape[0] < M or out.shape[1] < N:
+                raise ValueError(f"out: {tuple(out.shape)} does not hold {M} x {N} elements")
+            kind = FP8_BF16 if _itemsize(out) == 2 else (FP8_RESID if residual else FP8_F32)
+            o, ldo, os, ldos = _ptr(out), _ld(out), None, 0
+        if residual and kind != FP8_RESID:
+            raise ValueError("a residual update needs an fp32 out")
+        self._chk(self.lib.bag_gemm_fp8(self.h, *_encoded(a, a_scales, "a", M, K), *_encoded(w, w_scales, "w", N, K),
+                                        _vector(bias, "bias", N), M, N, K, int(gelu), kind,
+                                        _vector(gate, "gate", N), o, ldo, os, ldos))
+
+    def _cache(self, codes, scales, bits, base, slots, rows, cols):
+        group = CACHE_GROUP.get(bits, 128)
+        _rows(codes, "codes", 1)
+        _rows(_is(scales, "scales", "bfloat16"), "scales", 2)
+        if codes.shape[1] * 8 < cols * bits or scales.shape[1] * group < cols or codes.shape[0] != scales.shape[0]:
+            raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} hold no rows of {cols}")
+        if base is not None:
+            _rows(_is(base, "base", "float32"), "base", 4)
+            if tuple(base.shape) != (rows, cols):
+                raise ValueError(f"base: {rows} x {cols} elements are needed, got {tuple(base.shape)}")
+        if slots is not None:
+            _is(slots, "slots", "int32")
+            if not slots.is_cuda or slots.dim() != 1 or slots.shape[0] != rows or (rows > 1 and slots.stride(0) != 1):
+                raise ValueError(f"slots: {rows} dense int32 on the device are needed, got {tuple(slots.shape)}")
+        return _ptr(base), 0 if base is None else _ld(base), _ptr(slots)
+
+    def cache_write(self, x, codes, scales, bits, base=None, slots=None):
+        """Keep rows of x - base (or of x) in slots of a quantised cache."""
+        _rows(_is(x, "x", "float32"), "x", 4)
+        rows, cols = x.shape
+        b, ldb, s = self._cache(codes, scales, bits, base, slots, rows, cols)
+        self._chk(self.lib.bag_cache_write(self.h, _ptr(x), _ld(x), b, ldb, s, rows, cols, bits, _ptr(codes),
+                                           _ld(codes), _ptr(scales), _ld(scales), codes.shape[0]))
+
+    def cache_read(self, codes, scales, out, bits, base=None, slots=None):
+        """out = base + the cache's rows (or the rows alone)."""
+        _rows(_is(out, "out", "float32"), "out", 4)
+        rows, cols = out.shape
+        b, ldb, s = self._cache(codes, scales, bits, base, slots, rows, cols)
+        self._chk(self.lib.bag_cache_read(self.h, _ptr(codes), _ld(codes), _ptr(scales), _ld(scales), codes.shape[0],
+                                          s, rows, cols, bits, b, ldb, _ptr(out), _ld(out)))
+
+    def _pooled(self, codes, scales):
+        _is(_rows(codes, "codes", 1, 3), "codes", "int8")
+        _is(scales, "scales", "float32")
+        heads, blocks = codes.shape[:2]
+        if (codes.shape[2] != 128 or tuple(scales.shape) != (heads, blocks) or not scales.is_cuda
+                or not codes.is_contiguous() or not scales.is_contiguous()):
+            raise ValueError("pooled vectors: dense int8 [heads, blocks, 128] and fp32 [heads, blocks] are needed, got "
+                             f"{tuple(codes.shape)} and {tuple(scales.shape)}")
+        return heads, blocks
+
+    def block_pool(self, x, codes, scales):
+        """Pooled vectors of the blocks of 128 rows of x [rows, 128 * heads]."""
+        _rows(_is(x, "x", "float16", "bfloat16"), "x", 2)
+        heads, blocks = self._pooled(codes, scales)
+        if x.shape[1] != 128 * heads:
+            raise ValueError(f"x: {heads} heads of 128 columns are needed, got {tuple(x.shape)}")
+        self._chk(self.lib.bag_block_pool(self.h, _ptr(x), _type16(x), _ld(x), x.shape[0], heads, _ptr(codes),
+                                          _ptr(scales), blocks))
+
+    def _lists(self, blocks, nq):
+        if not blocks.is_cuda or blocks.dim() != 3 or not blocks.is_contiguous() or \
+                blocks.shape[1] != (nq + ATTN_BLOCK - 1) // ATTN_BLOCK:
+            raise ValueError("blocks: dense int32 [heads, query blocks, keep] is needed, got "
+                             f"{tuple(blocks.shape)} for {nq} queries")
+        _is(blocks, "blocks", "int32")
+        return blocks.shape[0], blocks.shape[2]
+
+    def block_select(self, q, codes, scales, blocks, nkb=None):
+        """The key blocks (pooled vectors codes, scales; the first nkb of them) of highest score for
+        each head and block of queries of q, into blocks [heads, query blocks, keep]."""
+        _rows(_is(q, "q", "float16", "bfloat16"), "q", 2)
+        kv_heads, ldb = self._pooled(codes, scales)
+        heads, keep = self._lists(blocks, q.shape[0])
+        if q.shape[1] != 128 * heads:
+            raise ValueError(f"q: {heads} heads of 128 columns are needed, got {tuple(q.shape)}")
+        if nkb is not None and nkb > ldb:
+            raise ValueError(f"nkb: the pooled vectors are {ldb} blocks, not {nkb}")
+        self._chk(self.lib.bag_block_select(self.h, _ptr(q), _type16(q), _ld(q), q.shape[0], heads, _ptr(codes),
+                                            _ptr(scales), ldb, ldb if nkb is None else nkb, kv_heads, keep,
+                                            _ptr(blocks)))
+
+    def attention_blocks(self, q, k, vt, o, blocks, heads, kv_heads=None):
+        """Attention of q [nq, 128 * heads] over the listed blocks of k [nk, 128 * kv_heads]; vt
+        [kv_heads, 128, vpad] of the same type; o bf16 [nq, 128 * heads]."""
+        kv_heads = heads if kv_heads is None else kv_heads
+        _rows(_is(q, "q", "float16", "bfloat16"), "q", 2)
+        _rows(_is(k, "k", _name(q)), "k", 2)
+        _rows(_is(o, "o", "bfloat16"), "o", 2)
+        _rows(_is(vt, "vt", _name(q)), "vt", 2, 3)
+        lists, keep = self._lists(blocks, q.shape[0])
+        if lists != heads or q.shape[1] != 128 * heads or k.shape[1] != 128 * kv_heads or \
+                tuple(o.shape) != tuple(q.shape) or tuple(vt.shape[:2]) != (kv_heads, 128) or not vt.is_contiguous():
+            raise ValueError(f"{heads} heads over {kv_heads}: q {tuple(q.shape)}, k {tuple(k.shape)}, vt "
+                             f"{tuple(vt.shape)}, o {tuple(o.shape)}, blocks {tuple(blocks.shape)} do not fit")
+        self._chk(self.lib.bag_attention_blocks(self.h, _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(vt), vt.shape[2],
+                                                _type16(q), q.shape[0], k.shape[0], heads, kv_heads, _ptr(blocks),
+                                                keep, _ptr(o), _ld(o)))
+
+
+# --- shapes and types of tensors handed to the low-precision operators -------------------
+# Checked here, because a wrong stride or element type would reach the kernels as a plausible
+# pointer; sizes, alignment and everything else are checked by the library.
+def _itemsize(t):
+    return t.dtype.itemsize
+
+
+def _rows(t, name, size, dims=2):
+    """A device tensor whose last dimension is dense and whose elements have `size` bytes."""
+    if not t.is_cuda or t.dim() != dims or _itemsize(t) != size or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: a {dims}-dimensional device tensor of {size}-byte elements with dense rows is "
+                         f"needed, got {tuple(t.shape)} {t.dtype} strides {t.stride()}")
+    return t
+
+
+def _ld(t):
+    """Row stride (of one row: its length)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _name(t):
+    return str(t.dtype).replace("torch.", "")
+
+
+def _is(t, name, *types):
+    if _name(t) not in types:
+        raise ValueError(f"{name}: {' or '.join(types)} is needed, got {t.dtype}")
+    return t
+
+
+def _type16(t):
+    return 2 if _name(t) == "float16" else DTYPE["bf16"]
+
+
+def _vector(t, name, n):
+    if t is None:
+        return None
+    _is(t, name, "float32")
+    if not t.is_cuda or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: {n} dense floats on the device are needed, got {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _encoded(codes, scales, name, rows, cols):
+    """Pointers and strides of an encoded matrix [rows, cols]."""
+    _rows(codes, name, 1)
+    _rows(scales, name + " scales", 1)
+    blocks = (cols + SCALE_BLOCK - 1) // SCALE_BLOCK
+    if codes.shape[0] < rows or codes.shape[1] < cols or scales.shape[0] < rows or scales.shape[1] < blocks:
+        raise ValueError(f"{name}: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not hold "
+                         f"{rows} x {cols} elements")
+    return _ptr(codes), _ld(codes), _ptr(scales), _ld(scales)
 
 
 def rel_l1_noalloc(a, b, rows, cols, out, stream=0, bf16=None):

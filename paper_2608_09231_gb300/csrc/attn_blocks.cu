@@ -1,0 +1,525 @@
+// Attention over selected blocks of keys, on the 5th-generation tensor cores (heads of 128, 16-bit
+// operands): softmax(q k^T / sqrt(128)) v for each block of 128 queries over the key blocks of its
+// own list.
+//
+// One CTA works on two slots, each a block of queries with a list of key blocks:
+//   warp 0       TMA producer: the queries, then K and V^T blocks of both slots through one ring,
+//                in the order in which the MMAs consume them
+//   warp 1       MMA issuer, in turn between the slots:
+//                  S_A,0  S_B,0 | PV_A,j  S_A,j+1 | PV_B,j  S_B,j+1 | ...
+//                so that one slot's products run beside the other's softmax
+//   warps 4..7   softmax of slot A, 8..11 of slot B: thread = query row; the row's scores are read
+//                from TMEM at once, P = exp2(s - m) goes back over them in 16 bits and enters the
+//                PV product from TMEM; O stays in TMEM and is rescaled only when the running
+//                maximum has grown by more than 8 (in log2 units)
+// PAIR: the slots are two (head, query block) units.  Otherwise a cluster of C CTAs shares one
+// unit: its list is cut into 2 C parts, and rank r merges 128 / C rows of the 2 C partial outputs
+// through distributed shared memory.
+#include <algorithm>
+#include <cmath>
+
+#include "attn_common.cuh"
+#include "epilogue.cuh"
+#include "kernels.h"
+
+namespace bag {
+
+namespace {
+constexpr int BT = 128;                    // queries, keys and columns of a tile
+constexpr int BT_CHUNK = BT * 64 * 2;      // 128 rows x 64 columns: one 128-byte swizzle column
+constexpr int BT_TILE = 2 * BT_CHUNK;
+constexpr int BT_STAGES = 5;               // of the ring (a K or V^T tile each)
+constexpr int BT_OFF_RING = 2 * BT_TILE;   // after the slots' queries
+constexpr int BT_OFF_BAR = BT_OFF_RING + BT_STAGES * BT_TILE;
+constexpr int BT_SMEM = BT_OFF_BAR + 256 + 1024;
+constexpr int BT_TMEM_COLS = 512;          // S_A [0,128) S_B [128,256) O_A [256,384) O_B [384,512)
+constexpr int BT_THREADS = 384;
+// registers a thread: 168 at launch; 128 * 72 + 256 * 216 = 384 * 168
+constexpr int BT_REGS_ISSUE = 72, BT_REGS_SOFTMAX = 216;
+constexpr int BT_OLD = 36;                 // floats a row in the output transpose
+// exchange of partial outputs over the tiles: 256 rows of 128 floats (4 more a row against
+// bank conflicts), then (maximum, sum) of each
+constexpr int BT_XLD = BT + 4;
+constexpr int BT_OFF_ML = 2 * BT * BT_XLD * 4;
+static_assert(BT_OFF_ML + 2 * BT * 8 <= BT_OFF_BAR, "the exchange fits the operand tiles");
+
+struct BlockAttnParams {
+  int nq, nk, nqb, nkb, keep, group;  // group: query heads of a key head
+  long units;                         // heads * nqb
+  const int* blocks;
+  __nv_bfloat16* o;
+  long ldo;
+  float scale_log2;
+  int c;                              // CTAs of a unit (not PAIR)
+  int* err;
+};
+}  // namespace
+
+template <bool F16, bool PAIR>
+__global__ void __launch_bounds__(BT_THREADS, 1)
+    attn_blocks_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                       const __grid_constant__ CUtensorMap tmV, const BlockAttnParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* ring = smem + BT_OFF_RING;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + BT_OFF_BAR);
+  uint64_t* q_full = bars;
+  uint64_t* full = bars + 1;               // [BT_STAGES]
+  uint64_t* empty = full + BT_STAGES;      // [BT_STAGES]
+  uint64_t* s_full = empty + BT_STAGES;    // [2] per slot
+  uint64_t* p_full = s_full + 2;           // [2]
+  uint64_t* o_done = p_full + 2;           // [2]
+  uint64_t* drain = o_done + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* length = reinterpret_cast<int*>(tmem_slot + 2);  // [2] of the slots' lists
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int C = PAIR ? 1 : p.c;
+  const int rank = !PAIR && C > 1 ? (int)cluster_ctarank() : 0;
+  const long u0 = PAIR ? 2L * blockIdx.x : (long)blockIdx.x / C;
+  auto unit_of = [&](int x) { return PAIR ? u0 + x : u0; };
+  auto list_of = [&](int x) { return p.blocks + unit_of(x) * p.keep; };
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    for (int i = 0; i < BT_STAGES; ++i) {
+      mbar_init(full + i, 1);
+      mbar_init(empty + i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + i, 1);
+      mbar_init(p_full + i, 4);  // one arrival per softmax warp of the slot
+      mbar_init(o_done + i, 1);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    length[0] = unit_of(0) < p.units ? p.keep : 0;
+    length[1] = unit_of(1) < p.units ? p.keep : 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  grid_dep_sync();
+  __syncthreads();
+  // a list ends at its first entry that names no block
+  for (int x = 0; x < (PAIR ? 2 : 1); ++x) {
+    if (unit_of(x) >= p.units) continue;
+    const int* list = list_of(x);
+    for (int i = threadIdx.x; i < p.keep; i += BT_THREADS)
+      if ((unsigned)__ldg(list + i) >= (unsigned)p.nkb) atomicMin(length + x, i);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, BT_TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // slot x works on entries [first[x], first[x] + n[x]) of its list
+  int first[2], n[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    if (PAIR) {
+      first[x] = 0;
+      n[x] = length[x];
+    } else {
+      const long part = 2 * rank + x, all = length[0];
+      first[x] = (int)(part * all / (2 * C));
+      n[x] = (int)((part + 1) * all / (2 * C)) - first[x];
+    }
+  }
+  const int most = max(n[0], n[1]);
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(BT_REGS_ISSUE));
+    if (warp == 0 && lane == 0 && most > 0) {
+      // ---------------- TMA producer ----------------
+      int kvx[2], qx[2], qy[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const long u = min(unit_of(x), p.units - 1);
+        const int head = (int)(u / p.nqb);
+        kvx[x] = head / p.group * BT;
+        qx[x] = head * BT;
+        qy[x] = (int)(u % p.nqb) * BT;
+      }
+      constexpr int QT = PAIR ? 2 : 1;
+      mbar_arrive_expect_tx(q_full, QT * BT_TILE);
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        tma_load_2d(smem + x * BT_TILE, &tmQ, qx[x], qy[x], q_full);
+        tma_load_2d(smem + x * BT_TILE + BT_CHUNK, &tmQ, qx[x] + 64, qy[x], q_full);
+      }
+      int s = 0, issued = 0;
+      uint32_t ph = 1;
+      bool ok = true;
+      auto stage = [&]() {
+        if (!(ok = ok && mbar_wait(empty + s, ph, abort_flag))) return false;
+        mbar_arrive_expect_tx(full + s, BT_TILE);
+        return true;
+      };
+      auto next = [&]() {
+        ++issued;
+        if (++s == BT_STAGES) {
+          s = 0;
+          ph ^= 1;
+        }
+      };
+      auto load_k = [&](int x, int b) {
+        if (!stage()) return;
+        uint8_t* t = ring + s * BT_TILE;
+        tma_load_2d(t, &tmK, kvx[x], b * BT, full + s);
+        tma_load_2d(t + BT_CHUNK, &tmK, kvx[x] + 64, b * BT, full + s);
+        next();
+      };
+      auto load_v = [&](int x, int b) {
+        if (!stage()) return;
+        uint8_t* t = ring + s * BT_TILE;
+        tma_load_2d(t, &tmV, b * BT, kvx[x], full + s);
+        tma_load_2d(t + BT_CHUNK, &tmV, b * BT + 64, kvx[x], full + s);
+        next();
+      };
+      int now[2] = {0, 0};  // the block whose K was loaded last
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (n[x] > 0) {
+          now[x] = __ldg(list_of(x) + first[x]);
+          load_k(x, now[x]);
+        }
+      for (int j = 0; j < most && ok; ++j) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (j >= n[x]) continue;
+          const int b = j + 1 < n[x] ? __ldg(list_of(x) + first[x] + j + 1) : 0;
+          load_v(x, now[x]);
+          if (j + 1 < n[x]) load_k(x, now[x] = b);
+        }
+      }
+      if (!ok) {
+        // wait (bounded) for copies still in flight before the CTA may exit
+        const uint64_t t0 = global_ns();
+        auto landed = [&](uint64_t* bar, uint32_t parity) {
+          while (!mbar_try_wait(bar, parity) && global_ns() - t0 < kWaitLimitNs) {
+          }
+        };
+        landed(q_full, 0);
+        for (int i = max(0, issued - BT_STAGES); i < issued; ++i) landed(full + i % BT_STAGES, (i / BT_STAGES) & 1);
+      }
+    } else if (warp == 1 && most > 0) {
+      // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
+      constexpr uint32_t idesc = F16 ? idesc_f16_f32(BT, BT) : idesc_bf16_f32(BT, BT);
+      const uint32_t q_addr = smem_u32(smem), r_addr = smem_u32(ring);
+      // K step kk of a tile: 64-column chunk kk / 4, 32 bytes per step inside it (16-byte units)
+      auto koff = [](int kk) { return (uint64_t)(((kk >> 2) * BT_CHUNK + (kk & 3) * 32) >> 4); };
+      int s = 0;
+      uint32_t ph = 0;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        const bool w = mbar_wait_warp(bar, parity, abort_flag);
+        tc_fence_after();
+        return w;
+      };
+      auto next = [&]() {
+        if (++s == BT_STAGES) {
+          s = 0;
+          ph ^= 1;
+        }
+      };
+      auto issue_s = [&](int x) {  // scores of the ring's next tile
+        if (!wait(full + s, ph)) return false;
+        const uint64_t qd = sw128_desc(q_addr + (PAIR ? x * BT_TILE : 0));
+        const uint64_t kd = sw128_desc(r_addr + s * BT_TILE);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < BT / 16; ++kk)
+            mma_bf16(tmem + x * 128, qd + koff(kk), kd + koff(kk), idesc, kk > 0 ? 1u : 0u);
+          mma_commit(s_full + x);
+          mma_commit(empty + s);
+        }
+        __syncwarp();
+        next();
+        return true;
+      };
+      auto issue_pv = [&](int x, int j) {
+        if (!wait(full + s, ph)) return false;
+        const uint64_t vd = sw128_desc(r_addr + s * BT_TILE);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < BT / 16; ++kk)
+            mma_bf16_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + koff(kk), idesc,
+                        (j > 0 || kk > 0) ? 1u : 0u);
+          mma_commit(empty + s);
+          if (j + 1 == n[x]) mma_commit(o_done + x);
+        }
+        __syncwarp();
+        next();
+        return true;
+      };
+      bool ok = wait(q_full, 0);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (n[x] > 0) ok = ok && issue_s(x);
+      for (int j = 0; j < most && ok; ++j) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (j >= n[x] || !ok) continue;
+          ok = wait(p_full + x, j & 1) && issue_pv(x, j);
+          if (ok && j + 1 < n[x]) ok = issue_s(x);
+        }
+      }
+      if (elect_one()) {
+        mma_commit(drain);
+        const uint64_t t0 = global_ns();
+        while (!mbar_try_wait(drain, 0) && global_ns() - t0 < kWaitLimitNs) {
+        }
+      }
+    }
+    __syncwarp();
+    if (!PAIR) {  // the two barriers of the exchange
+      if (C > 1) {
+        cluster_sync_all();
+        cluster_sync_all();
+      } else {
+        __syncthreads();
+        __syncthreads();
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(BT_REGS_SOFTMAX));
+    // ---------------- softmax warpgroups ----------------
+    const int x = (warp - 4) >> 2;
+    const int quad = warp & 3;
+    const int mine = x ? n[1] : n[0];
+    const int* list = list_of(x) + (x ? first[1] : first[0]);
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    const uint32_t s_addr = tmem + lane_base + x * 128;
+    const uint32_t o_addr = tmem + lane_base + 256 + x * 128;
+    float m_use = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < mine; ++j) {
+      const int kvalid = p.nk - __ldg(list + j) * BT;  // keys of this block (< 128 only at the end)
+      const bool w = mbar_wait(s_full + x, j & 1, abort_flag);
+      if (!__all_sync(0xffffffffu, w)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      uint32_t r[BT];
+#pragma unroll
+      for (int c = 0; c < BT / 32; ++c) tmem_ld32_nowait(s_addr + c * 32, r + c * 32);
+      tmem_ld_wait();
+      if (kvalid < BT) {
+#pragma unroll
+        for (int i = 0; i < BT; ++i)
+          if (i >= kvalid) r[i] = __float_as_uint(-INFINITY);
+      }
+      // row maximum: four independent chains of three-input maxima
+      float mq[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) mq[u] = fmaxf(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
+#pragma unroll
+      for (int i = 8; i < BT; i += 8)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          mq[u] = max3(mq[u], __uint_as_float(r[i + 2 * u]), __uint_as_float(r[i + 2 * u + 1]));
+      const float mx2 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * p.scale_log2;
+      float alpha = 1.f;
+      if (mx2 > m_use + 8.f) {
+        alpha = ex2(m_use - mx2);
+        m_use = mx2;
+        l *= alpha;
+      }
+      // a tile of nothing but -inf scores before any other weighs nothing
+      const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
+      float ls0 = 0.f, ls1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < BT / 32; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          float x0, x1;
+          fma2(x0, x1, __uint_as_float(r[c * 32 + i]), __uint_as_float(r[c * 32 + i + 1]), p.scale_log2, neg_m);
+          const float a0 = ex2(x0), a1 = ex2(x1);
+          add2(ls0, ls1, a0, a1);
+          pk[i / 2] = F16 ? pack_f16x2(a0, a1) : pack_bf16x2(a0, a1);
+        }
+        tmem_st16(s_addr + c * 16, pk);
+      }
+      l += ls0 + ls1;
+      // O holds PV of every earlier tile; rescale it before this tile's PV is issued
+      if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+        for (int c = 0; c < BT / 32; ++c) {
+          float o[32];
+          tmem_ld32(o_addr + c * 32, o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] *= alpha;
+          tmem_st32(o_addr + c * 32, o);
+        }
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + x);
+    }
+    if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(o_done + x, 0, abort_flag));
+    tc_fence_after();
+    if (PAIR) {
+      const long u = unit_of(x);
+      if (ok && u < p.units) {
+        const int head = (int)(u / p.nqb), q0 = (int)(u % p.nqb) * BT;
+        const float inv = 1.f / l;
+        // through shared memory (this slot's queries, which no product reads any more): four
+        // lanes hold 32 consecutive columns of a row, so a store covers eight rows' 64-byte runs.
+        // An empty list's zeros stay out of it: its queries may still be landing there.
+        float* buf = reinterpret_cast<float*>(smem + x * BT_TILE) + quad * 32 * BT_OLD;
+        const int r = lane >> 2, c8 = (lane & 3) * 8;
+        const int qw = q0 + quad * 32 + r;
+#pragma unroll 1
+        for (int c = 0; c < BT; c += 32) {
+          float o[32];
+          if (mine > 0) {
+            tmem_ld32(o_addr + c, o);
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              *reinterpret_cast<float4*>(buf + lane * BT_OLD + i) =
+                  make_float4(o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int q = qw + 8 * i;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (mine > 0) ld_chunk<8>(buf + (8 * i + r) * BT_OLD + c8, v);
+            if (q < p.nq) store_vals<8>(p.o, (long)q * p.ldo + head * BT + c + c8, v, kStoreBF16);
+          }
+          __syncwarp();
+        }
+      }
+    } else {
+      const int rpo = BT / C;  // rows a rank merges
+      __syncwarp();
+      if (C > 1)
+        cluster_sync_all();  // every CTA's products are done: the operand tiles are free
+      else
+        __syncthreads();
+      if (ok) {
+        const int R = quad * 32 + lane;
+        const int at = (2 * rank + x) * rpo + R % rpo;
+        const uint32_t here = smem_u32(smem);
+        const uint32_t dst = C > 1 ? mapa_shared(here, (uint32_t)(R / rpo)) : here;
+#pragma unroll 1
+        for (int c = 0; c < BT; c += 32) {
+          float o[32];
+          if (mine > 0) tmem_ld32(o_addr + c, o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = mine > 0 ? o[i] : 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            st_cluster4(dst + (uint32_t)(at * BT_XLD + c + i) * 4, o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+        st_cluster2(dst + BT_OFF_ML + (uint32_t)at * 8, m_use, l);
+      }
+      __syncwarp();
+      if (C > 1)
+        cluster_sync_all();  // every part has arrived; no access to another CTA follows
+      else
+        __syncthreads();
+      const float* part = reinterpret_cast<const float*>(smem);
+      const float2* ml = reinterpret_cast<const float2*>(smem + BT_OFF_ML);
+      const int head = (int)(u0 / p.nqb), q0 = (int)(u0 % p.nqb) * BT;
+      for (int lr = warp - 4; lr < rpo; lr += 8) {  // a warp a row, four columns a lane
+        const int q = q0 + rank * rpo + lr;
+        if (q >= p.nq) break;
+        float m = -INFINITY, den = 0.f;
+        for (int s = 0; s < 2 * C; ++s) m = fmaxf(m, ml[s * rpo + lr].x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < 2 * C; ++s) {
+          const float2 f = ml[s * rpo + lr];
+          const float w = f.x == -INFINITY ? 0.f : ex2(f.x - m);
+          const float4 o = *reinterpret_cast<const float4*>(part + (s * rpo + lr) * BT_XLD + lane * 4);
+          den += w * f.y;
+          acc.x += w * o.x;
+          acc.y += w * o.y;
+          acc.z += w * o.z;
+          acc.w += w * o.w;
+        }
+        const float inv = length[0] > 0 ? 1.f / den : 0.f;
+        uint2 u;
+        u.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+        u.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2*>(p.o + (long)q * p.ldo + head * BT + lane * 4) = u;
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag && p.err) atomicOr(p.err, 1);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, BT_TMEM_COLS);
+  }
+}
+
+cudaError_t attention_blocks_init() {
+  const void* kernels[] = {(const void*)attn_blocks_kernel<false, false>, (const void*)attn_blocks_kernel<false, true>,
+                           (const void*)attn_blocks_kernel<true, false>, (const void*)attn_blocks_kernel<true, true>};
+  cudaError_t r = cudaSuccess;
+  for (const void* k : kernels)
+    if (r == cudaSuccess) r = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, BT_SMEM);
+  return r;
+}
+
+// CTAs that share a unit (0: a CTA takes two units), by the time each way would take: a wave of
+// CTAs that walk k blocks on each slot takes about 1.45 us x k, and sharing about 7 us.
+static int blocks_split(long units, int keep) {
+  const int sms = sm_count();
+  auto waves = [&](long ctas) { return (double)((ctas + sms - 1) / sms); };
+  double best = waves((units + 1) / 2) * keep * 1.45;
+  int c = 0;
+  for (int k = 1; k <= 8 && 2 * k <= keep; k *= 2) {
+    const double t = waves(units * k) * ((keep + 2 * k - 1) / (2 * k)) * 1.45 + 7.0;
+    if (t < best) {
+      best = t;
+      c = k;
+    }
+  }
+  return c;
+}
+
+cudaError_t attention_blocks(const BlockAttnArgs& a, cudaStream_t s) {
+  if (a.nq <= 0) return cudaSuccess;
+  CUtensorMap tq, tk, tv;
+  const uint64_t kw = (uint64_t)a.kv_heads * BT;
+  if (encode_tmap_2d_bf16(&tq, a.q, (uint64_t)a.heads * BT, (uint64_t)a.nq, (uint64_t)a.ldq * 2, 64, BT) ||
+      encode_tmap_2d_bf16(&tk, a.k, kw, (uint64_t)a.nk, (uint64_t)a.ldk * 2, 64, BT) ||
+      encode_tmap_2d_bf16(&tv, a.v, (uint64_t)a.nk, kw, (uint64_t)a.vpad * 2, 64, BT))
+    return cudaErrorInvalidValue;
+  BlockAttnParams p;
+  p.nq = a.nq;
+  p.nk = a.nk;
+  p.nqb = (a.nq + BT - 1) / BT;
+  p.nkb = (a.nk + BT - 1) / BT;
+  p.keep = a.keep;
+  p.group = a.heads / a.kv_heads;
+  p.units = (long)a.heads * p.nqb;
+  p.blocks = a.blocks;
+  p.o = reinterpret_cast<__nv_bfloat16*>(a.o);
+  p.ldo = a.ldo;
+  p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)BT));
+  p.err = a.err;
+  const int c = blocks_split(p.units, a.keep);
+  p.c = std::max(1, c);
+  const long ctas = c ? p.units * c : (p.units + 1) / 2;
+  if (ctas > 0x7fffffffL) return cudaErrorInvalidConfiguration;
+  auto launch = [&](auto kernel) {
+    return launch_cluster(kernel, c > 1 ? (unsigned)c : 0u, (unsigned)ctas, BT_THREADS, BT_SMEM, s, tq, tk, tv, p);
+  };
+  if (a.f16) return c ? launch(attn_blocks_kernel<true, false>) : launch(attn_blocks_kernel<true, true>);
+  return c ? launch(attn_blocks_kernel<false, false>) : launch(attn_blocks_kernel<false, true>);
+}
+
+}  // namespace bag

@@ -1791,6 +1791,207 @@ static bag_status bag_rel_l1_impl(bag_ctx* ctx, const void* a, const void* b, in
   return BAG_OK;
 }
 
+// ---- 8-bit operands, quantised cache, block-sparse attention ----
+static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// An encoded matrix's buffers: null, alignment and strides.
+static bag_status check_encoded(bag_ctx* ctx, const char* name, const void* codes, long ldc, const void* scales,
+                                long lds, long cols) {
+  if (!codes || !scales) return fail(ctx, BAG_EINVAL, std::string("null pointer: ") + name);
+  if (ldc < cols || ldc % 16 || !aligned(codes, 16))
+    return fail(ctx, BAG_EINVAL, std::string(name) + " codes need 16-byte aligned rows of at least cols bytes");
+  if (lds < (cols + 127) / 128 || lds % 4 || !aligned(scales, 4))
+    return fail(ctx, BAG_EINVAL, std::string(name) + " scales need 4-byte aligned rows of a byte for each 128 columns");
+  return BAG_OK;
+}
+
+static bag_status bag_quant_fp8_impl(bag_ctx* ctx, const void* x, int dtype, long ldx, long rows, long cols,
+                                     void* codes, long ldc, void* scales, long lds) {
+  if (rows < 0 || cols <= 0 || ldx < cols || (dtype != BAG_F32 && dtype != BAG_BF16))
+    return fail(ctx, BAG_EINVAL, "bad quant_fp8 shape or dtype");
+  if (rows == 0) return BAG_OK;
+  if (!x || !aligned(x, dtype == BAG_BF16 ? 2 : 4)) return fail(ctx, BAG_EINVAL, "x is null or not aligned to its type");
+  CKS(check_encoded(ctx, "output", codes, ldc, scales, lds, cols));
+  CK(quant_fp8(x, dtype == BAG_BF16, ldx, rows, cols, codes, ldc, scales, lds, ctx->stream));
+  return BAG_OK;
+}
+
+static bag_status bag_ln_mod_fp8_impl(bag_ctx* ctx, const float* x, long ldx, const float* shift, const float* scale,
+                                      long rows, long cols, void* codes, long ldc, void* scales, long lds) {
+  if (rows < 0 || cols <= 0 || ldx < cols) return fail(ctx, BAG_EINVAL, "bad ln_mod_fp8 shape");
+  if (rows == 0) return BAG_OK;
+  if (!x) return fail(ctx, BAG_EINVAL, "x is null");
+  CKS(check_encoded(ctx, "output", codes, ldc, scales, lds, cols));
+  if (cols % 4 || cols > 6144 || ldx % 4 || !aligned(x, 16) || !aligned(shift, 16) || !aligned(scale, 16))
+    return fail(ctx, BAG_EUNSUPPORTED, "ln_mod_fp8 needs 16-byte aligned rows of a multiple of 4 up to 6144 columns");
+  CK(ln_mod_fp8(x, ldx, shift, scale, rows, (int)cols, codes, ldc, scales, lds, ctx->stream));
+  return BAG_OK;
+}
+
+static bag_status bag_gemm_fp8_impl(bag_ctx* ctx, const void* a, long lda, const void* a_s, long ldas, const void* w,
+                                    long ldw, const void* w_s, long ldws, const float* bias, long M, long N, long K,
+                                    int act, int kind, const float* gate, void* out, long ldo, void* out_s, long ldos) {
+  const long most = 0x7fffff00L;
+  if (M < 0 || N < 1 || K < 1 || M > most || N > most || K > most) return fail(ctx, BAG_EINVAL, "bad gemm_fp8 shape");
+  if (kind < BAG_FP8_F32 || kind > BAG_FP8_RESID || act < 0 || act > 1 || (kind == BAG_FP8_RESID && act))
+    return fail(ctx, BAG_EINVAL, "bad gemm_fp8 output kind or activation");
+  if (gate && kind != BAG_FP8_RESID) return fail(ctx, BAG_EINVAL, "gate goes with BAG_FP8_RESID only");
+  if (M == 0) return BAG_OK;
+  CKS(check_encoded(ctx, "A", a, lda, a_s, ldas, K));
+  CKS(check_encoded(ctx, "W", w, ldw, w_s, ldws, K));
+  if (kind == BAG_FP8_CODES) {
+    CKS(check_encoded(ctx, "output", out, ldo, out_s, ldos, N));
+  } else if (!out || ldo < N || !aligned(out, kind == BAG_FP8_BF16 ? 2 : 4)) {
+    return fail(ctx, BAG_EINVAL, "out is null, not aligned to its type or its rows overlap");
+  }
+  if (!aligned(bias, 4) || !aligned(gate, 4)) return fail(ctx, BAG_EINVAL, "bias or gate is not aligned to its type");
+  Fp8Gemm g{};
+  g.a = reinterpret_cast<const uint8_t*>(a);
+  g.lda = lda;
+  g.a_s = reinterpret_cast<const uint8_t*>(a_s);
+  g.ldas = ldas;
+  g.w = reinterpret_cast<const uint8_t*>(w);
+  g.ldw = ldw;
+  g.w_s = reinterpret_cast<const uint8_t*>(w_s);
+  g.ldws = ldws;
+  g.M = (int)M;
+  g.N = (int)N;
+  g.K = (int)K;
+  g.bias = bias;
+  g.gate = gate;
+  g.act = act;
+  g.kind = kind;
+  g.out = out;
+  g.ldo = ldo;
+  g.out_s = reinterpret_cast<uint8_t*>(out_s);
+  g.ldos = ldos;
+  g.err = &ctx->st_op->err;
+  CK(gemm_fp8(g, ctx->stream));
+  return BAG_OK;
+}
+
+// What a write and a read of the cache have in common.
+static bag_status check_cache(bag_ctx* ctx, const void* codes, long ldc, const void* scales, long lds, long capacity,
+                              const int32_t* slots, long rows, long cols, int bits, const float* base, long ldb) {
+  if (bits != 8 && bits != 4) return fail(ctx, BAG_EINVAL, "bits must be 8 or 4");
+  if (rows < 0 || cols <= 0 || capacity < 0 || (!slots && capacity < rows)) return fail(ctx, BAG_EINVAL, "bad cache shape");
+  if (rows == 0) return BAG_OK;
+  const int group = bits == 8 ? 128 : 32;
+  if (!codes || ldc < (cols * bits + 7) / 8 || ldc % 16 || !aligned(codes, 16))
+    return fail(ctx, BAG_EINVAL, "cache codes need 16-byte aligned rows of at least a row's codes");
+  if (!scales || lds < (cols + group - 1) / group || !aligned(scales, 2))
+    return fail(ctx, BAG_EINVAL, "cache scales need rows of a bf16 for each group");
+  if (!aligned(slots, 4) || !aligned(base, 4) || (base && ldb < cols))
+    return fail(ctx, BAG_EINVAL, "slots or base is not aligned to its type, or base's rows overlap");
+  return BAG_OK;
+}
+
+static CacheArgs cache_args(const void* codes, long ldc, const void* scales, long lds, long capacity,
+                            const int32_t* slots, long rows, long cols, const float* base, long ldb) {
+  CacheArgs a{};
+  a.base = base;
+  a.ldb = ldb;
+  a.slots = slots;
+  a.rows = rows;
+  a.cols = cols;
+  a.capacity = capacity;
+  a.codes = reinterpret_cast<uint8_t*>(const_cast<void*>(codes));
+  a.ldc = ldc;
+  a.scales = const_cast<void*>(scales);
+  a.lds = lds;
+  return a;
+}
+
+static bag_status bag_cache_write_impl(bag_ctx* ctx, const float* x, long ldx, const float* base, long ldb,
+                                       const int32_t* slots, long rows, long cols, int bits, void* codes, long ldc,
+                                       void* scales, long lds, long capacity) {
+  CKS(check_cache(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb));
+  if (rows == 0) return BAG_OK;
+  if (!x || ldx < cols || !aligned(x, 4)) return fail(ctx, BAG_EINVAL, "x is null, not aligned or its rows overlap");
+  CacheArgs a = cache_args(codes, ldc, scales, lds, capacity, slots, rows, cols, base, ldb);
+  a.x = x;
+  a.ldx = ldx;
+  CK(cache_write(a, bits, ctx->stream));
+  return BAG_OK;
+}
+
+static bag_status bag_cache_read_impl(bag_ctx* ctx, const void* codes, long ldc, const void* scales, long lds,
+                                      long capacity, const int32_t* slots, long rows, long cols, int bits,
+                                      const float* base, long ldb, float* out, long ldo) {
+  CKS(check_cache(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb));
+  if (rows == 0) return BAG_OK;
+  if (!out || ldo < cols || !aligned(out, 4)) return fail(ctx, BAG_EINVAL, "out is null, not aligned or its rows overlap");
+  CacheArgs a = cache_args(codes, ldc, scales, lds, capacity, slots, rows, cols, base, ldb);
+  a.out = out;
+  a.ldo = ldo;
+  CK(cache_read(a, bits, ctx->stream));
+  return BAG_OK;
+}
+
+constexpr long kMaxRows = 0x7fffff00L;  // row counts are ints in the kernels
+constexpr int kMaxHeads = 65535;        // a grid dimension
+
+static bag_status bag_block_pool_impl(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads,
+                                      void* codes, float* scales, long ldb) {
+  if (rows < 0 || rows > kMaxRows || heads <= 0 || heads > kMaxHeads || ld < 128L * heads ||
+      (type != BAG_BF16 && type != BAG_F16) || ldb < (rows + 127) / 128)
+    return fail(ctx, BAG_EINVAL, "bad block_pool shape or type");
+  if (rows == 0) return BAG_OK;
+  if (!x || !codes || !scales || !aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, 4))
+    return fail(ctx, BAG_EINVAL, "x, codes (16-byte aligned) or scales is null or not aligned");
+  CK(block_pool(x, type == BAG_F16, ld, rows, heads, codes, scales, ldb, ctx->stream));
+  return BAG_OK;
+}
+
+static bag_status bag_block_select_impl(bag_ctx* ctx, const void* q, int type, long ldq, long nq, int heads,
+                                        const void* codes, const float* scales, long ldb, long nkb, int kv_heads,
+                                        int keep, int32_t* blocks) {
+  if (nq < 0 || nq > kMaxRows || heads <= 0 || heads > kMaxHeads || kv_heads <= 0 || heads % kv_heads ||
+      ldq < 128L * heads || (type != BAG_BF16 && type != BAG_F16) || ldb < nkb || keep < 1 || keep > nkb)
+    return fail(ctx, BAG_EINVAL, "bad block_select shape or type");
+  if (nkb > 8192) return fail(ctx, BAG_EUNSUPPORTED, "block_select takes up to 8192 key blocks");
+  if (nq == 0) return BAG_OK;
+  if (!q || !codes || !scales || !blocks || !aligned(q, 2) || !aligned(codes, 16) || !aligned(scales, 4) ||
+      !aligned(blocks, 4))
+    return fail(ctx, BAG_EINVAL, "q, codes (16-byte aligned), scales or blocks is null or not aligned");
+  CK(block_select(q, type == BAG_F16, ldq, nq, heads, codes, scales, ldb, (int)nkb, kv_heads, keep, blocks, ctx->stream));
+  return BAG_OK;
+}
+
+static bag_status bag_attention_blocks_impl(bag_ctx* ctx, const void* q, long ldq, const void* k, long ldk,
+                                            const void* v, long vpad, int type, long nq, long nk, int heads,
+                                            int kv_heads, const int32_t* blocks, int keep, void* o, long ldo) {
+  if (nq < 0 || nk < 0 || nq > kMaxRows || nk > kMaxRows || heads <= 0 || heads > kMaxHeads || kv_heads <= 0 ||
+      heads % kv_heads || ldq < 128L * heads || ldk < 128L * kv_heads || ldo < 128L * heads || keep < 1 ||
+      (type != BAG_BF16 && type != BAG_F16) || vpad < nk)
+    return fail(ctx, BAG_EINVAL, "bad attention_blocks shape or type");
+  if (nq == 0) return BAG_OK;
+  if (!q || !k || !v || !blocks || !o) return fail(ctx, BAG_EINVAL, "null pointer");
+  if (ldq % 8 || ldk % 8 || vpad % 8 || ldo % 8 || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) ||
+      !aligned(o, 16) || !aligned(blocks, 4))
+    return fail(ctx, BAG_EUNSUPPORTED, "attention_blocks needs 16-byte aligned rows");
+  if (nk == 0) return fail(ctx, BAG_EUNSUPPORTED, "attention_blocks needs a key");
+  BlockAttnArgs a{};
+  a.q = q;
+  a.ldq = ldq;
+  a.k = k;
+  a.ldk = ldk;
+  a.v = v;
+  a.vpad = vpad;
+  a.f16 = type == BAG_F16;
+  a.nq = (int)nq;
+  a.nk = (int)nk;
+  a.heads = heads;
+  a.kv_heads = kv_heads;
+  a.keep = keep;
+  a.blocks = blocks;
+  a.o = o;
+  a.ldo = ldo;
+  a.err = &ctx->st_op->err;
+  CK(attention_blocks(a, ctx->stream));
+  return BAG_OK;
+}
+
 static bag_status bag_residual_add_impl(bag_ctx* ctx, float* out, const float* h_in, const float* R, long n) {
   if (!ctx || !out || !h_in || !R) return BAG_EINVAL;
   if (n < 0 || n % 4) return fail(ctx, BAG_EINVAL, "n must be a multiple of 4");
@@ -2066,6 +2267,71 @@ bag_status bag_residual_add(bag_ctx* ctx, float* out, const float* h_in, const f
   if (!ctx) return BAG_EINVAL;
   CKS(enter(ctx));
   return leave(ctx, bag_residual_add_impl(ctx, out, h_in, R, n));
+}
+
+bag_status bag_quant_fp8(bag_ctx* ctx, const void* x, int dtype, long ldx, long rows, long cols, void* codes, long
+                         ldc, void* scales, long lds) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_quant_fp8_impl(ctx, x, dtype, ldx, rows, cols, codes, ldc, scales, lds));
+}
+
+bag_status bag_ln_mod_fp8(bag_ctx* ctx, const float* x, long ldx, const float* shift, const float* scale, long rows,
+                          long cols, void* codes, long ldc, void* scales, long lds) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_ln_mod_fp8_impl(ctx, x, ldx, shift, scale, rows, cols, codes, ldc, scales, lds));
+}
+
+bag_status bag_gemm_fp8(bag_ctx* ctx, const void* a, long lda, const void* a_s, long ldas, const void* w, long ldw,
+                        const void* w_s, long ldws, const float* bias, long M, long N, long K, int act, int kind,
+                        const float* gate, void* out, long ldo, void* out_s, long ldos) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_gemm_fp8_impl(ctx, a, lda, a_s, ldas, w, ldw, w_s, ldws, bias, M, N, K, act, kind, gate, out,
+                                    ldo, out_s, ldos));
+}
+
+bag_status bag_cache_write(bag_ctx* ctx, const float* x, long ldx, const float* base, long ldb, const int32_t* slots,
+                           long rows, long cols, int bits, void* codes, long ldc, void* scales, long lds, long
+                           capacity) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_cache_write_impl(ctx, x, ldx, base, ldb, slots, rows, cols, bits, codes, ldc, scales, lds,
+                                       capacity));
+}
+
+bag_status bag_cache_read(bag_ctx* ctx, const void* codes, long ldc, const void* scales, long lds, long capacity,
+                          const int32_t* slots, long rows, long cols, int bits, const float* base, long ldb, float*
+                          out, long ldo) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_cache_read_impl(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb,
+                                      out, ldo));
+}
+
+bag_status bag_block_pool(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads, void* codes, float*
+                          scales, long ldb) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_block_pool_impl(ctx, x, type, ld, rows, heads, codes, scales, ldb));
+}
+
+bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, long nq, int heads, const void* codes,
+                            const float* scales, long ldb, long nkb, int kv_heads, int keep, int32_t* blocks) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_block_select_impl(ctx, q, type, ldq, nq, heads, codes, scales, ldb, nkb, kv_heads, keep,
+                                        blocks));
+}
+
+bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const void* k, long ldk, const void* v, long
+                                vpad, int type, long nq, long nk, int heads, int kv_heads, const int32_t* blocks, int
+                                keep, void* o, long ldo) {
+  if (!ctx) return BAG_EINVAL;
+  CKS(enter(ctx));
+  return leave(ctx, bag_attention_blocks_impl(ctx, q, ldq, k, ldk, v, vpad, type, nq, nk, heads, kv_heads, blocks,
+                                            keep, o, ldo));
 }
 
 }  // extern "C"

@@ -264,6 +264,59 @@ cudaError_t residual_add(float* out, const float* a, const float* b, long n, cud
 cudaError_t rel_l1(const void* a, const void* b, int bf16, long rows, long cols, float* scratch, float* out, int pdl,
                    cudaStream_t s);
 
+// ---- 8-bit operands with block scales (see bag.h), quantised cache, block-sparse attention ----
+cudaError_t quant_fp8(const void* x, int bf16, long ldx, long rows, long cols, void* codes, long ldc, void* scales,
+                      long lds, cudaStream_t s);
+cudaError_t ln_mod_fp8(const float* x, long ldx, const float* shift, const float* scale, long rows, int cols,
+                       void* codes, long ldc, void* scales, long lds, cudaStream_t s);
+
+// Product of two encoded matrices; kind / act / gate as for bag_gemm_fp8.
+struct Fp8Gemm {
+  const uint8_t* a; long lda; const uint8_t* a_s; long ldas;
+  const uint8_t* w; long ldw; const uint8_t* w_s; long ldws;
+  int M, N, K;
+  const float* bias;
+  const float* gate;
+  int act, kind;
+  void* out; long ldo;
+  uint8_t* out_s; long ldos;
+  int vec;   // rows of out (and bias, gate) are 16-byte aligned (set by the launcher)
+  int* err;
+};
+cudaError_t gemm_fp8(Fp8Gemm g, cudaStream_t s);
+cudaError_t gemm_fp8_init();  // part of kernels_init
+
+struct CacheArgs {
+  const float* x; long ldx;        // write: rows to keep
+  const float* base; long ldb;     // null = none
+  const int32_t* slots;            // null = row r in cache row r
+  long rows, cols, capacity;
+  uint8_t* codes; long ldc;
+  void* scales; long lds;
+  float* out; long ldo;            // read
+  int segs, vec;                   // set by the launcher
+};
+cudaError_t cache_write(CacheArgs a, int bits, cudaStream_t s);
+cudaError_t cache_read(CacheArgs a, int bits, cudaStream_t s);
+
+cudaError_t block_pool(const void* x, int f16, long ld, long rows, int heads, void* codes, float* scales, long ldb,
+                       cudaStream_t s);
+cudaError_t block_select(const void* q, int f16, long ldq, long nq, int heads, const void* codes, const float* scales,
+                         long ldb, int nkb, int kv_heads, int keep, int* blocks, cudaStream_t s);
+
+struct BlockAttnArgs {
+  const void* q; long ldq;
+  const void* k; long ldk;
+  const void* v; long vpad;        // [kv_heads][128][vpad]
+  int f16;
+  int nq, nk, heads, kv_heads, keep;
+  const int* blocks;               // [heads][query blocks][keep]
+  void* o; long ldo;
+  int* err;
+};
+cudaError_t attention_blocks(const BlockAttnArgs& a, cudaStream_t s);
+cudaError_t attention_blocks_init();
+
 // message returned by bag_last_error(NULL) (entry points without a context)
 }  // namespace bag
 #include <string>
@@ -276,5 +329,7 @@ cudaError_t kernels_init();
 // host-side TMA descriptor encoding (driver entry point resolved at run time)
 int encode_tmap_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                         uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer);
+int encode_tmap_2d_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride_bytes,
+                      uint32_t box_inner, uint32_t box_outer);
 
 }  // namespace bag
