@@ -330,6 +330,10 @@ bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows
 
 /* ---- 8-bit operands with a scale for each block of 128 ----
  *
+ * The operations from here to bag_attention_blocks use nothing of the context but its stream and
+ * error text: they run on the caller's stream itself (in order with the context's other calls,
+ * also across bag_set_stream), never synchronise, and may be captured into a CUDA graph.
+ *
  * An encoded matrix [rows, cols] is two device buffers: codes, one float8 e4m3 byte an element
  * (row stride ldc bytes), and scales, one byte b for each row and block of 128 consecutive
  * columns (row stride lds bytes), standing for 2^(b - 127) (E8M0, as the tensor cores read it;

@@ -333,183 +333,170 @@ class Context:
     # --- 8-bit operands, quantised cache, block-sparse attention (see include/bag.h) ----
     def quant_fp8(self, x, codes, scales):
         """Rows of x (fp32 or bf16 [rows, cols]) as e4m3 codes and power-of-two scales."""
-        _rows(x, "x", _itemsize(_is(x, "x", "float32", "bfloat16")))
-        rows, cols = x.shape
-        self._chk(self.lib.bag_quant_fp8(self.h, _ptr(x), int(_itemsize(x) == 2), _ld(x), rows, cols,
+        p, ld, rows, cols, kind = _mat(x, "x", ("float32", "bfloat16"))
+        self._chk(self.lib.bag_quant_fp8(self.h, p, int(kind == "bfloat16"), ld, rows, cols,
                                          *_encoded(codes, scales, "codes", rows, cols)))
 
     def ln_mod_fp8(self, x, shift, scale, codes, scales):
         """ln_mod of fp32 rows, encoded as by quant_fp8."""
-        _rows(_is(x, "x", "float32"), "x", 4)
-        rows, cols = x.shape
-        self._chk(self.lib.bag_ln_mod_fp8(self.h, _ptr(x), _ld(x), _vector(shift, "shift", cols),
-                                          _vector(scale, "scale", cols), rows, cols,
-                                          *_encoded(codes, scales, "codes", rows, cols)))
+        p, ld, rows, cols, _ = _mat(x, "x", ("float32",))
+        self._chk(self.lib.bag_ln_mod_fp8(self.h, p, ld, _vec(shift, "shift", cols), _vec(scale, "scale", cols),
+                                          rows, cols, *_encoded(codes, scales, "codes", rows, cols)))
 
     def gemm_fp8(self, a, a_scales, w, w_scales, out, K, bias=None, gelu=False, gate=None, residual=False,
                  out_scales=None, N=None):
         """Product of encoded a [M, K] and w [N, K]: out fp32 or bf16 [M, N]; encoded, where
-        out_scales is given (N then says how many columns, default w's rows); or, with residual,
-        fp32 out += gate * (product + bias)."""
+        out_scales is given; or, with residual, fp32 out += gate * (product + bias).  N: how many
+        rows of w (default all)."""
         M, N = a.shape[0], w.shape[0] if N is None else N
         if out_scales is not None:
             kind = FP8_CODES
             o, ldo, os, ldos = _encoded(out, out_scales, "out", M, N)
         else:
-            _rows(_is(out, "out", "float32", "bfloat16"), "out", _itemsize(out))
-            if out.shape[0] < M or out.shape[1] < N:
+            o, ldo, rows, cols, name = _mat(out, "out", ("float32", "bfloat16"))
+            os, ldos = None, 0
+            kind = FP8_BF16 if name == "bfloat16" else (FP8_RESID if residual else FP8_F32)
+            if rows < M or cols < N:
                 raise ValueError(f"out: {tuple(out.shape)} does not hold {M} x {N} elements")
-            kind = FP8_BF16 if _itemsize(out) == 2 else (FP8_RESID if residual else FP8_F32)
-            o, ldo, os, ldos = _ptr(out), _ld(out), None, 0
         if residual and kind != FP8_RESID:
             raise ValueError("a residual update needs an fp32 out")
         self._chk(self.lib.bag_gemm_fp8(self.h, *_encoded(a, a_scales, "a", M, K), *_encoded(w, w_scales, "w", N, K),
-                                        _vector(bias, "bias", N), M, N, K, int(gelu), kind,
-                                        _vector(gate, "gate", N), o, ldo, os, ldos))
+                                        _vec(bias, "bias", N), M, N, K, int(gelu), kind, _vec(gate, "gate", N), o, ldo,
+                                        os, ldos))
 
-    def _cache(self, codes, scales, bits, base, slots, rows, cols):
-        group = CACHE_GROUP.get(bits, 128)
-        _rows(codes, "codes", 1)
-        _rows(_is(scales, "scales", "bfloat16"), "scales", 2)
-        if codes.shape[1] * 8 < cols * bits or scales.shape[1] * group < cols or codes.shape[0] != scales.shape[0]:
+    @staticmethod
+    def _cache(codes, scales, bits, base, slots, rows, cols):
+        c, ldc, cap, nc, _ = _mat(codes, "codes")
+        s, lds, ns, ng, _ = _mat(scales, "scales", ("bfloat16",))
+        if nc * 8 < cols * bits or ng * CACHE_GROUP.get(bits, 128) < cols or cap != ns:
             raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} hold no rows of {cols}")
+        b, ldb = None, 0
         if base is not None:
-            _rows(_is(base, "base", "float32"), "base", 4)
-            if tuple(base.shape) != (rows, cols):
-                raise ValueError(f"base: {rows} x {cols} elements are needed, got {tuple(base.shape)}")
-        if slots is not None:
-            _is(slots, "slots", "int32")
-            if not slots.is_cuda or slots.dim() != 1 or slots.shape[0] != rows or (rows > 1 and slots.stride(0) != 1):
-                raise ValueError(f"slots: {rows} dense int32 on the device are needed, got {tuple(slots.shape)}")
-        return _ptr(base), 0 if base is None else _ld(base), _ptr(slots)
+            b, ldb, br, bc, _ = _mat(base, "base", ("float32",))
+            if br != rows or bc != cols:
+                _want(base, "base", f"a matrix of {rows} x {cols}")
+        return c, ldc, s, lds, cap, b, ldb, _vec(slots, "slots", rows, "int32")
 
     def cache_write(self, x, codes, scales, bits, base=None, slots=None):
         """Keep rows of x - base (or of x) in slots of a quantised cache."""
-        _rows(_is(x, "x", "float32"), "x", 4)
-        rows, cols = x.shape
-        b, ldb, s = self._cache(codes, scales, bits, base, slots, rows, cols)
-        self._chk(self.lib.bag_cache_write(self.h, _ptr(x), _ld(x), b, ldb, s, rows, cols, bits, _ptr(codes),
-                                           _ld(codes), _ptr(scales), _ld(scales), codes.shape[0]))
+        p, ld, rows, cols, _ = _mat(x, "x", ("float32",))
+        c, ldc, s, lds, cap, b, ldb, at = self._cache(codes, scales, bits, base, slots, rows, cols)
+        self._chk(self.lib.bag_cache_write(self.h, p, ld, b, ldb, at, rows, cols, bits, c, ldc, s, lds, cap))
 
     def cache_read(self, codes, scales, out, bits, base=None, slots=None):
         """out = base + the cache's rows (or the rows alone)."""
-        _rows(_is(out, "out", "float32"), "out", 4)
-        rows, cols = out.shape
-        b, ldb, s = self._cache(codes, scales, bits, base, slots, rows, cols)
-        self._chk(self.lib.bag_cache_read(self.h, _ptr(codes), _ld(codes), _ptr(scales), _ld(scales), codes.shape[0],
-                                          s, rows, cols, bits, b, ldb, _ptr(out), _ld(out)))
+        p, ld, rows, cols, _ = _mat(out, "out", ("float32",))
+        c, ldc, s, lds, cap, b, ldb, at = self._cache(codes, scales, bits, base, slots, rows, cols)
+        self._chk(self.lib.bag_cache_read(self.h, c, ldc, s, lds, cap, at, rows, cols, bits, b, ldb, p, ld))
 
-    def _pooled(self, codes, scales):
-        _is(_rows(codes, "codes", 1, 3), "codes", "int8")
-        _is(scales, "scales", "float32")
+    @staticmethod
+    def _pooled(codes, scales):
+        if codes.dim() != 3 or codes.shape[2] != 128 or _type(codes)[0] != "int8" or not codes.is_cuda or \
+                not codes.is_contiguous():
+            _want(codes, "codes", "dense int8 [heads, blocks, 128] on the device")
         heads, blocks = codes.shape[:2]
-        if (codes.shape[2] != 128 or tuple(scales.shape) != (heads, blocks) or not scales.is_cuda
-                or not codes.is_contiguous() or not scales.is_contiguous()):
-            raise ValueError("pooled vectors: dense int8 [heads, blocks, 128] and fp32 [heads, blocks] are needed, got "
-                             f"{tuple(codes.shape)} and {tuple(scales.shape)}")
-        return heads, blocks
+        if scales.shape != (heads, blocks) or _type(scales)[0] != "float32" or not scales.is_cuda or \
+                not scales.is_contiguous():
+            _want(scales, "scales", f"dense float32 [{heads}, {blocks}] on the device")
+        return codes.data_ptr(), scales.data_ptr(), heads, blocks
+
+    @staticmethod
+    def _heads16(x, name, heads, types=("float16", "bfloat16")):
+        p, ld, rows, cols, kind = _mat(x, name, types)
+        if cols != 128 * heads:
+            _want(x, name, f"{heads} heads of 128 columns")
+        return p, ld, rows, kind
 
     def block_pool(self, x, codes, scales):
         """Pooled vectors of the blocks of 128 rows of x [rows, 128 * heads]."""
-        _rows(_is(x, "x", "float16", "bfloat16"), "x", 2)
-        heads, blocks = self._pooled(codes, scales)
-        if x.shape[1] != 128 * heads:
-            raise ValueError(f"x: {heads} heads of 128 columns are needed, got {tuple(x.shape)}")
-        self._chk(self.lib.bag_block_pool(self.h, _ptr(x), _type16(x), _ld(x), x.shape[0], heads, _ptr(codes),
-                                          _ptr(scales), blocks))
+        c, s, heads, blocks = self._pooled(codes, scales)
+        p, ld, rows, kind = self._heads16(x, "x", heads)
+        self._chk(self.lib.bag_block_pool(self.h, p, _T16[kind], ld, rows, heads, c, s, blocks))
 
-    def _lists(self, blocks, nq):
-        if not blocks.is_cuda or blocks.dim() != 3 or not blocks.is_contiguous() or \
-                blocks.shape[1] != (nq + ATTN_BLOCK - 1) // ATTN_BLOCK:
-            raise ValueError("blocks: dense int32 [heads, query blocks, keep] is needed, got "
-                             f"{tuple(blocks.shape)} for {nq} queries")
-        _is(blocks, "blocks", "int32")
-        return blocks.shape[0], blocks.shape[2]
+    @staticmethod
+    def _lists(blocks, nq):
+        if blocks.dim() != 3 or blocks.shape[1] != (nq + ATTN_BLOCK - 1) // ATTN_BLOCK or not blocks.is_cuda or \
+                not blocks.is_contiguous() or _type(blocks)[0] != "int32":
+            _want(blocks, "blocks", f"dense int32 [heads, query blocks, keep] for {nq} queries on the device")
+        return blocks.data_ptr(), blocks.shape[0], blocks.shape[2]
 
     def block_select(self, q, codes, scales, blocks, nkb=None):
         """The key blocks (pooled vectors codes, scales; the first nkb of them) of highest score for
         each head and block of queries of q, into blocks [heads, query blocks, keep]."""
-        _rows(_is(q, "q", "float16", "bfloat16"), "q", 2)
-        kv_heads, ldb = self._pooled(codes, scales)
-        heads, keep = self._lists(blocks, q.shape[0])
-        if q.shape[1] != 128 * heads:
-            raise ValueError(f"q: {heads} heads of 128 columns are needed, got {tuple(q.shape)}")
-        if nkb is not None and nkb > ldb:
-            raise ValueError(f"nkb: the pooled vectors are {ldb} blocks, not {nkb}")
-        self._chk(self.lib.bag_block_select(self.h, _ptr(q), _type16(q), _ld(q), q.shape[0], heads, _ptr(codes),
-                                            _ptr(scales), ldb, ldb if nkb is None else nkb, kv_heads, keep,
-                                            _ptr(blocks)))
+        c, s, kv_heads, ldb = self._pooled(codes, scales)
+        at, heads, keep = self._lists(blocks, q.shape[0])
+        p, ld, nq, kind = self._heads16(q, "q", heads)
+        self._chk(self.lib.bag_block_select(self.h, p, _T16[kind], ld, nq, heads, c, s, ldb,
+                                            ldb if nkb is None else nkb, kv_heads, keep, at))
 
     def attention_blocks(self, q, k, vt, o, blocks, heads, kv_heads=None):
         """Attention of q [nq, 128 * heads] over the listed blocks of k [nk, 128 * kv_heads]; vt
         [kv_heads, 128, vpad] of the same type; o bf16 [nq, 128 * heads]."""
         kv_heads = heads if kv_heads is None else kv_heads
-        _rows(_is(q, "q", "float16", "bfloat16"), "q", 2)
-        _rows(_is(k, "k", _name(q)), "k", 2)
-        _rows(_is(o, "o", "bfloat16"), "o", 2)
-        _rows(_is(vt, "vt", _name(q)), "vt", 2, 3)
-        lists, keep = self._lists(blocks, q.shape[0])
-        if lists != heads or q.shape[1] != 128 * heads or k.shape[1] != 128 * kv_heads or \
-                tuple(o.shape) != tuple(q.shape) or tuple(vt.shape[:2]) != (kv_heads, 128) or not vt.is_contiguous():
-            raise ValueError(f"{heads} heads over {kv_heads}: q {tuple(q.shape)}, k {tuple(k.shape)}, vt "
-                             f"{tuple(vt.shape)}, o {tuple(o.shape)}, blocks {tuple(blocks.shape)} do not fit")
-        self._chk(self.lib.bag_attention_blocks(self.h, _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(vt), vt.shape[2],
-                                                _type16(q), q.shape[0], k.shape[0], heads, kv_heads, _ptr(blocks),
-                                                keep, _ptr(o), _ld(o)))
+        qp, ldq, nq, kind = self._heads16(q, "q", heads)
+        kp, ldk, nk, _ = self._heads16(k, "k", kv_heads, (kind,))
+        op, ldo, no, _ = self._heads16(o, "o", heads, ("bfloat16",))
+        at, lists, keep = self._lists(blocks, nq)
+        if vt.dim() != 3 or vt.shape[0] != kv_heads or vt.shape[1] != 128 or _type(vt)[0] != kind or \
+                not vt.is_cuda or not vt.is_contiguous():
+            _want(vt, "vt", f"dense {kind} [{kv_heads}, 128, vpad] on the device")
+        if no != nq or lists != heads:
+            raise ValueError(f"o {tuple(o.shape)} or blocks {tuple(blocks.shape)} does not fit {nq} queries of {heads} heads")
+        self._chk(self.lib.bag_attention_blocks(self.h, qp, ldq, kp, ldk, vt.data_ptr(), vt.shape[2], _T16[kind], nq, nk,
+                                                heads, kv_heads, at, keep, op, ldo))
 
 
-# --- shapes and types of tensors handed to the low-precision operators -------------------
-# Checked here, because a wrong stride or element type would reach the kernels as a plausible
-# pointer; sizes, alignment and everything else are checked by the library.
-def _itemsize(t):
-    return t.dtype.itemsize
+# --- tensors handed to the low-precision operators ---------------------------------------
+# A wrong element type or a row whose elements are not dense would reach the kernels as a
+# plausible pointer, so these are checked here; sizes, strides and alignment are checked by the
+# library as well.
+_TYPES = {}  # dtype -> (name, bytes)
 
 
-def _rows(t, name, size, dims=2):
-    """A device tensor whose last dimension is dense and whose elements have `size` bytes."""
-    if not t.is_cuda or t.dim() != dims or _itemsize(t) != size or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name}: a {dims}-dimensional device tensor of {size}-byte elements with dense rows is "
-                         f"needed, got {tuple(t.shape)} {t.dtype} strides {t.stride()}")
-    return t
+def _type(t):
+    d = t.dtype
+    r = _TYPES.get(d)
+    if r is None:
+        r = _TYPES[d] = (str(d).replace("torch.", ""), d.itemsize)
+    return r
 
 
-def _ld(t):
-    """Row stride (of one row: its length)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _want(t, name, what):
+    raise ValueError(f"{name}: {what} is needed, got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
 
 
-def _name(t):
-    return str(t.dtype).replace("torch.", "")
+def _mat(t, name, types=None):
+    """(pointer, row stride, rows, columns, type name) of a device matrix with dense rows, of one
+    of `types` (None: of one-byte elements)."""
+    shape, (kind, size) = t.shape, _type(t)
+    if len(shape) != 2 or not t.is_cuda or (size != 1 if types is None else kind not in types):
+        _want(t, name, f"a device matrix of {types or 'one-byte elements'}")
+    rows, cols = shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        _want(t, name, "a matrix with dense rows")
+    return t.data_ptr(), ld if rows > 1 else max(ld, cols), rows, cols, kind
 
 
-def _is(t, name, *types):
-    if _name(t) not in types:
-        raise ValueError(f"{name}: {' or '.join(types)} is needed, got {t.dtype}")
-    return t
-
-
-def _type16(t):
-    return 2 if _name(t) == "float16" else DTYPE["bf16"]
-
-
-def _vector(t, name, n):
+def _vec(t, name, n, kind="float32"):
     if t is None:
         return None
-    _is(t, name, "float32")
-    if not t.is_cuda or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: {n} dense floats on the device are needed, got {tuple(t.shape)}")
-    return _ptr(t)
+    if t.shape != (n,) or _type(t)[0] != kind or not t.is_cuda or (n > 1 and t.stride(0) != 1):
+        _want(t, name, f"a dense device vector of {n} {kind}")
+    return t.data_ptr()
 
 
 def _encoded(codes, scales, name, rows, cols):
     """Pointers and strides of an encoded matrix [rows, cols]."""
-    _rows(codes, name, 1)
-    _rows(scales, name + " scales", 1)
-    blocks = (cols + SCALE_BLOCK - 1) // SCALE_BLOCK
-    if codes.shape[0] < rows or codes.shape[1] < cols or scales.shape[0] < rows or scales.shape[1] < blocks:
+    c, ldc, rc, cc, _ = _mat(codes, name)
+    s, lds, rs, cs, _ = _mat(scales, name)
+    if rc < rows or cc < cols or rs < rows or cs * SCALE_BLOCK < cols:
         raise ValueError(f"{name}: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not hold "
                          f"{rows} x {cols} elements")
-    return _ptr(codes), _ld(codes), _ptr(scales), _ld(scales)
+    return c, ldc, s, lds
+
+
+_T16 = {"float16": 2, "bfloat16": 1}  # BAG_F16, BAG_BF16
 
 
 def rel_l1_noalloc(a, b, rows, cols, out, stream=0, bf16=None):

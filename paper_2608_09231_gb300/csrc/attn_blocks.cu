@@ -21,6 +21,7 @@
 #include "attn_common.cuh"
 #include "epilogue.cuh"
 #include "kernels.h"
+#include "peer.cuh"
 
 namespace bag {
 
@@ -420,9 +421,9 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
           for (int i = 0; i < 32; ++i) o[i] = mine > 0 ? o[i] : 0.f;
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
-            st_cluster4(dst + (uint32_t)(at * BT_XLD + c + i) * 4, o[i], o[i + 1], o[i + 2], o[i + 3]);
+            peer_store4(dst + (uint32_t)(at * BT_XLD + c + i) * 4, o[i], o[i + 1], o[i + 2], o[i + 3]);
         }
-        st_cluster2(dst + BT_OFF_ML + (uint32_t)at * 8, m_use, l);
+        peer_store2(dst + BT_OFF_ML + (uint32_t)at * 8, m_use, l);
       }
       __syncwarp();
       if (C > 1)

@@ -104,6 +104,8 @@ struct bag_ctx {
   cudaStream_t stream = nullptr;       // internal stream: all work and graph capture
   cudaStream_t user_stream = nullptr;  // caller's stream (bag_set_stream), bridged by events
   cudaEvent_t ev_in = nullptr, ev_out = nullptr;
+  cudaEvent_t ev_op = nullptr;        // after the last operation that ran on user_stream itself
+  bool stream_changed = false;        // since the last call
   std::string err;
 
   // weights
@@ -1586,6 +1588,8 @@ static bag_status reset_state(bag_ctx* ctx) {
 // Order the internal stream after the caller's stream, and the caller's stream after
 // the work just enqueued.
 static bag_status enter(bag_ctx* ctx) {
+  if (ctx->stream_changed) CK(cudaStreamWaitEvent(ctx->stream, ctx->ev_op, 0));
+  ctx->stream_changed = false;
   CK(cudaEventRecord(ctx->ev_in, ctx->user_stream));
   CK(cudaStreamWaitEvent(ctx->stream, ctx->ev_in, 0));
   return BAG_OK;
@@ -1593,6 +1597,29 @@ static bag_status enter(bag_ctx* ctx) {
 static bag_status leave(bag_ctx* ctx, bag_status s) {
   if (cudaEventRecord(ctx->ev_out, ctx->stream) == cudaSuccess)
     cudaStreamWaitEvent(ctx->user_stream, ctx->ev_out, 0);
+  return s;
+}
+
+// Operations that use nothing of the context run on the caller's stream itself, which spares
+// them the bridge (four event calls, and two cross-stream waits on the device: together about
+// half of a small call).  The order of a context's calls holds all the same when the caller
+// changes streams: the first call on another stream waits for the last one before it.  Inside a
+// stream capture no event of the context is waited for or recorded, so that these calls can be
+// captured; the capture is ordered by whoever launches its graph.
+static bool capturing(bag_ctx* ctx) {
+  cudaStreamCaptureStatus c = cudaStreamCaptureStatusNone;
+  return cudaStreamIsCapturing(ctx->user_stream, &c) != cudaSuccess || c != cudaStreamCaptureStatusNone;
+}
+static bag_status enter_op(bag_ctx* ctx) {
+  if (!ctx->stream_changed || capturing(ctx)) return BAG_OK;
+  CK(cudaStreamWaitEvent(ctx->user_stream, ctx->ev_out, 0));
+  CK(cudaStreamWaitEvent(ctx->user_stream, ctx->ev_op, 0));
+  ctx->stream_changed = false;
+  return BAG_OK;
+}
+static bag_status leave_op(bag_ctx* ctx, bag_status s) {
+  if (!capturing(ctx)) cudaEventRecord(ctx->ev_op, ctx->user_stream);
+  if (s == BAG_ECUDA) cudaGetLastError();  // reported: off the thread, or the next check reports it again
   return s;
 }
 
@@ -1812,7 +1839,7 @@ static bag_status bag_quant_fp8_impl(bag_ctx* ctx, const void* x, int dtype, lon
   if (rows == 0) return BAG_OK;
   if (!x || !aligned(x, dtype == BAG_BF16 ? 2 : 4)) return fail(ctx, BAG_EINVAL, "x is null or not aligned to its type");
   CKS(check_encoded(ctx, "output", codes, ldc, scales, lds, cols));
-  CK(quant_fp8(x, dtype == BAG_BF16, ldx, rows, cols, codes, ldc, scales, lds, ctx->stream));
+  CK(quant_fp8(x, dtype == BAG_BF16, ldx, rows, cols, codes, ldc, scales, lds, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1824,7 +1851,7 @@ static bag_status bag_ln_mod_fp8_impl(bag_ctx* ctx, const float* x, long ldx, co
   CKS(check_encoded(ctx, "output", codes, ldc, scales, lds, cols));
   if (cols % 4 || cols > 6144 || ldx % 4 || !aligned(x, 16) || !aligned(shift, 16) || !aligned(scale, 16))
     return fail(ctx, BAG_EUNSUPPORTED, "ln_mod_fp8 needs 16-byte aligned rows of a multiple of 4 up to 6144 columns");
-  CK(ln_mod_fp8(x, ldx, shift, scale, rows, (int)cols, codes, ldc, scales, lds, ctx->stream));
+  CK(ln_mod_fp8(x, ldx, shift, scale, rows, (int)cols, codes, ldc, scales, lds, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1866,7 +1893,7 @@ static bag_status bag_gemm_fp8_impl(bag_ctx* ctx, const void* a, long lda, const
   g.out_s = reinterpret_cast<uint8_t*>(out_s);
   g.ldos = ldos;
   g.err = &ctx->st_op->err;
-  CK(gemm_fp8(g, ctx->stream));
+  CK(gemm_fp8(g, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1911,7 +1938,7 @@ static bag_status bag_cache_write_impl(bag_ctx* ctx, const float* x, long ldx, c
   CacheArgs a = cache_args(codes, ldc, scales, lds, capacity, slots, rows, cols, base, ldb);
   a.x = x;
   a.ldx = ldx;
-  CK(cache_write(a, bits, ctx->stream));
+  CK(cache_write(a, bits, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1924,7 +1951,7 @@ static bag_status bag_cache_read_impl(bag_ctx* ctx, const void* codes, long ldc,
   CacheArgs a = cache_args(codes, ldc, scales, lds, capacity, slots, rows, cols, base, ldb);
   a.out = out;
   a.ldo = ldo;
-  CK(cache_read(a, bits, ctx->stream));
+  CK(cache_read(a, bits, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1939,7 +1966,7 @@ static bag_status bag_block_pool_impl(bag_ctx* ctx, const void* x, int type, lon
   if (rows == 0) return BAG_OK;
   if (!x || !codes || !scales || !aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, 4))
     return fail(ctx, BAG_EINVAL, "x, codes (16-byte aligned) or scales is null or not aligned");
-  CK(block_pool(x, type == BAG_F16, ld, rows, heads, codes, scales, ldb, ctx->stream));
+  CK(block_pool(x, type == BAG_F16, ld, rows, heads, codes, scales, ldb, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1954,7 +1981,7 @@ static bag_status bag_block_select_impl(bag_ctx* ctx, const void* q, int type, l
   if (!q || !codes || !scales || !blocks || !aligned(q, 2) || !aligned(codes, 16) || !aligned(scales, 4) ||
       !aligned(blocks, 4))
     return fail(ctx, BAG_EINVAL, "q, codes (16-byte aligned), scales or blocks is null or not aligned");
-  CK(block_select(q, type == BAG_F16, ldq, nq, heads, codes, scales, ldb, (int)nkb, kv_heads, keep, blocks, ctx->stream));
+  CK(block_select(q, type == BAG_F16, ldq, nq, heads, codes, scales, ldb, (int)nkb, kv_heads, keep, blocks, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -1988,7 +2015,7 @@ static bag_status bag_attention_blocks_impl(bag_ctx* ctx, const void* q, long ld
   a.o = o;
   a.ldo = ldo;
   a.err = &ctx->st_op->err;
-  CK(attention_blocks(a, ctx->stream));
+  CK(attention_blocks(a, ctx->user_stream));
   return BAG_OK;
 }
 
@@ -2034,7 +2061,8 @@ bag_status bag_create(const bag_arch* arch, int T, int B, bag_ctx** out) {
   bag_status s = BAG_OK;
   if (cudaStreamCreateWithFlags(&ctx->stream, cudaStreamNonBlocking) != cudaSuccess ||
       cudaEventCreateWithFlags(&ctx->ev_in, cudaEventDisableTiming) != cudaSuccess ||
-      cudaEventCreateWithFlags(&ctx->ev_out, cudaEventDisableTiming) != cudaSuccess)
+      cudaEventCreateWithFlags(&ctx->ev_out, cudaEventDisableTiming) != cudaSuccess ||
+      cudaEventCreateWithFlags(&ctx->ev_op, cudaEventDisableTiming) != cudaSuccess)
     s = fail(ctx, BAG_ECUDA, "stream/event creation failed");
   if (s == BAG_OK && kernels_init() != cudaSuccess) s = fail(ctx, BAG_ECUDA, "kernel attribute setup failed");
   if (s == BAG_OK) s = alloc_weights(ctx);
@@ -2060,6 +2088,7 @@ void bag_destroy(bag_ctx* ctx) {
   if (ctx->aarena) cudaFree(ctx->aarena);
   if (ctx->ev_in) cudaEventDestroy(ctx->ev_in);
   if (ctx->ev_out) cudaEventDestroy(ctx->ev_out);
+  if (ctx->ev_op) cudaEventDestroy(ctx->ev_op);
   for (auto ev : ctx->ev_pool) cudaEventDestroy(ev);
   if (ctx->stream) cudaStreamDestroy(ctx->stream);
   delete ctx;
@@ -2069,6 +2098,7 @@ const char* bag_last_error(bag_ctx* ctx) { return ctx ? ctx->err.c_str() : g_cre
 
 bag_status bag_set_stream(bag_ctx* ctx, void* stream) {
   if (!ctx) return BAG_EINVAL;
+  if (ctx->user_stream != (cudaStream_t)stream) ctx->stream_changed = true;
   ctx->user_stream = (cudaStream_t)stream;
   return BAG_OK;
 }
@@ -2272,23 +2302,23 @@ bag_status bag_residual_add(bag_ctx* ctx, float* out, const float* h_in, const f
 bag_status bag_quant_fp8(bag_ctx* ctx, const void* x, int dtype, long ldx, long rows, long cols, void* codes, long
                          ldc, void* scales, long lds) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_quant_fp8_impl(ctx, x, dtype, ldx, rows, cols, codes, ldc, scales, lds));
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_quant_fp8_impl(ctx, x, dtype, ldx, rows, cols, codes, ldc, scales, lds));
 }
 
 bag_status bag_ln_mod_fp8(bag_ctx* ctx, const float* x, long ldx, const float* shift, const float* scale, long rows,
                           long cols, void* codes, long ldc, void* scales, long lds) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_ln_mod_fp8_impl(ctx, x, ldx, shift, scale, rows, cols, codes, ldc, scales, lds));
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_ln_mod_fp8_impl(ctx, x, ldx, shift, scale, rows, cols, codes, ldc, scales, lds));
 }
 
 bag_status bag_gemm_fp8(bag_ctx* ctx, const void* a, long lda, const void* a_s, long ldas, const void* w, long ldw,
                         const void* w_s, long ldws, const float* bias, long M, long N, long K, int act, int kind,
                         const float* gate, void* out, long ldo, void* out_s, long ldos) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_gemm_fp8_impl(ctx, a, lda, a_s, ldas, w, ldw, w_s, ldws, bias, M, N, K, act, kind, gate, out,
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_gemm_fp8_impl(ctx, a, lda, a_s, ldas, w, ldw, w_s, ldws, bias, M, N, K, act, kind, gate, out,
                                     ldo, out_s, ldos));
 }
 
@@ -2296,8 +2326,8 @@ bag_status bag_cache_write(bag_ctx* ctx, const float* x, long ldx, const float* 
                            long rows, long cols, int bits, void* codes, long ldc, void* scales, long lds, long
                            capacity) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_cache_write_impl(ctx, x, ldx, base, ldb, slots, rows, cols, bits, codes, ldc, scales, lds,
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_cache_write_impl(ctx, x, ldx, base, ldb, slots, rows, cols, bits, codes, ldc, scales, lds,
                                        capacity));
 }
 
@@ -2305,23 +2335,23 @@ bag_status bag_cache_read(bag_ctx* ctx, const void* codes, long ldc, const void*
                           const int32_t* slots, long rows, long cols, int bits, const float* base, long ldb, float*
                           out, long ldo) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_cache_read_impl(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb,
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_cache_read_impl(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb,
                                       out, ldo));
 }
 
 bag_status bag_block_pool(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads, void* codes, float*
                           scales, long ldb) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_block_pool_impl(ctx, x, type, ld, rows, heads, codes, scales, ldb));
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_block_pool_impl(ctx, x, type, ld, rows, heads, codes, scales, ldb));
 }
 
 bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, long nq, int heads, const void* codes,
                             const float* scales, long ldb, long nkb, int kv_heads, int keep, int32_t* blocks) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_block_select_impl(ctx, q, type, ldq, nq, heads, codes, scales, ldb, nkb, kv_heads, keep,
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_block_select_impl(ctx, q, type, ldq, nq, heads, codes, scales, ldb, nkb, kv_heads, keep,
                                         blocks));
 }
 
@@ -2329,8 +2359,8 @@ bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const voi
                                 vpad, int type, long nq, long nk, int heads, int kv_heads, const int32_t* blocks, int
                                 keep, void* o, long ldo) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter(ctx));
-  return leave(ctx, bag_attention_blocks_impl(ctx, q, ldq, k, ldk, v, vpad, type, nq, nk, heads, kv_heads, blocks,
+  CKS(enter_op(ctx));
+  return leave_op(ctx, bag_attention_blocks_impl(ctx, q, ldq, k, ldk, v, vpad, type, nq, nk, heads, kv_heads, blocks,
                                             keep, o, ldo));
 }
 

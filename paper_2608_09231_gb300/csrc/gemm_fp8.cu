@@ -12,6 +12,7 @@
 #include "lowbit.cuh"
 #include "bag.h"
 #include "kernels.h"
+#include "peer.cuh"
 
 namespace bag {
 
@@ -69,10 +70,6 @@ BAG_DEV uint4 scale_words(const uint8_t* __restrict__ s, long lds, int row0, int
     return row < rows ? __ldg(reinterpret_cast<const uint32_t*>(s + (long)row * lds) + g) : 0x7f7f7f7fu;
   };
   return make_uint4(at(r), at(r + 32), at(r + 64), at(r + 96));
-}
-
-BAG_DEV void st_cluster1(uint32_t addr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 }  // namespace
@@ -281,7 +278,7 @@ __global__ void __launch_bounds__(256)
       for (int j = 0; j < 16; ++j)
         if (c + j < cols) {
           const uint32_t at = here + (uint32_t)((c + j) / S * 128) * 4u;
-          st_cluster1(S > 1 ? mapa_shared(at, (uint32_t)((c + j) % S)) : at, v[j]);
+          peer_store1(S > 1 ? mapa_shared(at, (uint32_t)((c + j) % S)) : at, v[j]);
         }
     }
   }
