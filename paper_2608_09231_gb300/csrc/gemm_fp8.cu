@@ -85,7 +85,7 @@ BAG_DEV uint4 scale_words(const uint8_t* __restrict__ s, long lds, int row0, int
 template <int BN>
 struct FewCfg {
   static constexpr int STAGE = F8_TILE + BN * F8_BK;
-  static constexpr int STAGES = BN == 16 ? 6 : (BN == 32 ? 5 : (BN == 64 ? 4 : 3));
+  static constexpr int STAGES = BN <= 32 ? 4 : 3;
   static constexpr int OFF_SF = STAGES * STAGE;              // two stages of W's and A's scale words
   static constexpr int OFF_RED = OFF_SF + 2 * 2 * F8_ATOM;   // [BN][4] block maxima of warps
   static constexpr int OFF_BAR = OFF_RED + BN * 16;
@@ -99,7 +99,7 @@ struct FewCfg {
 template <int BN>
 __global__ void __launch_bounds__(256)
     gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
-                        const __grid_constant__ Fp8Gemm g, int S) {
+                        const __grid_constant__ Fp8Gemm g, int logS) {
   using C = FewCfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(256)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int rank = S > 1 ? (int)cluster_ctarank() : 0;
-  const int mt = (g.M + BN - 1) / BN, unit = blockIdx.x / S;
+  const int S = 1 << logS, rank = logS > 0 ? (int)cluster_ctarank() : 0;
+  const int mt = (g.M + BN - 1) / BN, unit = (int)(blockIdx.x >> logS);
   const int m0 = unit % mt * BN, n0 = unit / mt * 128;
   const int nkb = (g.K + F8_BK - 1) / F8_BK;
   const int kb0 = (int)((long)rank * nkb / S), kb1 = (int)((long)(rank + 1) * nkb / S);
@@ -254,76 +254,100 @@ __global__ void __launch_bounds__(256)
   const bool epi = warp >= 4;
   const int row = (int)threadIdx.x - 128, n = n0 + row;  // of an epilogue thread
   const int cols = min(BN, g.M - m0);
-  const int per = BN / S;                                // rows m of the tile a rank finishes
+  const int per = BN >> logS;                            // rows m of the tile a rank finishes
   float* part = reinterpret_cast<float*>(smem);          // [S][per][128]
   if (epi) mbar_wait(tfull, 0, abort_flag);
   __syncwarp();
   tc_fence_before();
   // every product is done, here and in the cluster: the rings are free.  No role waits after
   // this, so all threads see the same abort flag.
-  if (S > 1)
+  if (logS > 0)
     cluster_sync_all();
   else
     __syncthreads();
   tc_fence_after();
   const bool ok = !*abort_flag;
-  if (epi && ok) {
-    const uint32_t tb = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t here = smem_u32(part) + (uint32_t)(rank * per * 128 + row) * 4u;
+  const uint32_t tb = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  if (logS > 0) {
+    if (epi && ok) {
+      const uint32_t here = smem_u32(part) + (uint32_t)((rank * per * 128 + row) * 4);
 #pragma unroll 1
-    for (int c = 0; c < cols; c += 16) {
-      float v[16];
-      tmem_ld16(tb + (uint32_t)c, v);
+      for (int c = 0; c < cols; c += 16) {
+        float v[16];
+        tmem_ld16(tb + (uint32_t)c, v);
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (c + j < cols) {
-          const uint32_t at = here + (uint32_t)((c + j) / S * 128) * 4u;
-          peer_store1(S > 1 ? mapa_shared(at, (uint32_t)((c + j) % S)) : at, v[j]);
-        }
+        for (int j = 0; j < 16; ++j)
+          if (c + j < cols)
+            peer_store1(mapa_shared(here + (uint32_t)((c + j) >> logS) * 512u, (uint32_t)((c + j) & (S - 1))), v[j]);
+      }
     }
+    __syncwarp();
+    cluster_sync_all();  // every part has arrived; no access to another CTA follows
   }
-  tc_fence_before();
-  __syncwarp();
-  if (S > 1) cluster_sync_all();  // every part has arrived; no access to another CTA follows
   if (epi && ok) {
     const bool in = n < g.N;
     const float bias = in && g.bias ? __ldg(g.bias + n) : 0.f;
     const float gate = in && g.gate ? __ldg(g.gate + n) : 1.f;
-    const int mine = (cols - rank + S - 1) / S;
-    uint32_t* red = reinterpret_cast<uint32_t*>(smem + C::OFF_RED);
+    const int mine = (cols - rank + S - 1) >> logS;
+    uint4* red = reinterpret_cast<uint4*>(smem + C::OFF_RED);  // [row m of the tile]: the warps' maxima
 #pragma unroll 1
-    for (int j = 0; j < mine; ++j) {
-      float y = part[j * 128 + row];
-      for (int p = 1; p < S; ++p) y += part[(p * per + j) * 128 + row];
-      y += bias;
-      if (g.act) y = gelu_sigmoid(y);
-      const long at = (long)(m0 + j * S + rank) * g.ldo + n;
+    for (int j0 = 0; j0 < mine; j0 += 16) {
+      float y[16];
+      if (logS == 0) {
+        tmem_ld16(tb + (uint32_t)j0, y);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = j0 + j < mine ? part[(j0 + j) * 128 + row] : 0.f;
+        for (int p = 1; p < S; ++p)
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (j0 + j < mine) y[j] += part[(p * per + j0 + j) * 128 + row];
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) y[j] += bias;
+      if (g.act) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = gelu_sigmoid(y[j]);
+      }
+      const long m = m0 + rank + ((long)j0 << logS);  // of y[0]; the others S rows apart
+      const long at = m * g.ldo + n, step = g.ldo << logS;
       if (g.kind == BAG_FP8_CODES) {
-        y = in ? y : 0.f;
-        part[j * 128 + row] = y;  // this thread's own word
-        const uint32_t m = group_max<32>(abs_bits(y));
-        if (lane == 0) red[j * 4 + (warp & 3)] = m;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint32_t top = group_max<32>(in ? abs_bits(y[j]) : 0u);
+          if (lane == 0) reinterpret_cast<uint32_t*>(red + j0 + j)[warp & 3] = top;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // the four epilogue warps
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (j0 + j >= mine) break;
+          const uint4 r = red[j0 + j];
+          const uint32_t b = e8m0_of(max(max(r.x, r.y), max(r.z, r.w)));
+          if (in)
+            reinterpret_cast<uint8_t*>(g.out)[at + j * step] =
+                __nv_cvt_float_to_fp8(y[j] * e8m0_inverse(b), __NV_SATFINITE, __NV_E4M3);
+          if (row == 0) g.out_s[(m + ((long)j << logS)) * g.ldos + n0 / kScaleBlock] = (uint8_t)b;
+        }
       } else if (in) {
-        if (g.kind == BAG_FP8_F32)
-          reinterpret_cast<float*>(g.out)[at] = y;
-        else if (g.kind == BAG_FP8_BF16)
-          reinterpret_cast<__nv_bfloat16*>(g.out)[at] = __float2bfloat16_rn(y);
-        else
-          reinterpret_cast<float*>(g.out)[at] += gate * y;
+        if (g.kind == BAG_FP8_BF16) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (j0 + j < mine) reinterpret_cast<__nv_bfloat16*>(g.out)[at + j * step] = __float2bfloat16_rn(y[j]);
+        } else {
+          float* o = reinterpret_cast<float*>(g.out) + at;
+          if (g.kind == BAG_FP8_RESID) {
+            float h[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) h[j] = j0 + j < mine ? o[j * step] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) y[j] = h[j] + gate * y[j];
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (j0 + j < mine) o[j * step] = y[j];
+        }
       }
-    }
-    if (g.kind == BAG_FP8_CODES) {
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-#pragma unroll 1
-      for (int j = 0; j < mine; ++j) {
-        const uint4 r = *reinterpret_cast<const uint4*>(red + j * 4);
-        const uint32_t b = e8m0_of(max(max(r.x, r.y), max(r.z, r.w)));
-        const float y = part[j * 128 + row] * e8m0_inverse(b);
-        const long m = m0 + j * S + rank;
-        if (in)
-          reinterpret_cast<uint8_t*>(g.out)[m * g.ldo + n] = __nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3);
-        if (row == 0) g.out_s[m * g.ldos + n0 / kScaleBlock] = (uint8_t)b;
-      }
+      __syncwarp();
     }
   }
   __syncthreads();
@@ -335,15 +359,511 @@ __global__ void __launch_bounds__(256)
 }
 
 template <int BN>
-static cudaError_t launch_few(const Fp8Gemm& g, int S, cudaStream_t s) {
+static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
   CUtensorMap tw, ta;
   if (encode_tmap_2d_u8(&tw, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128) ||
       encode_tmap_2d_u8(&ta, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, BN))
     return cudaErrorInvalidValue;
   const long units = (long)((g.M + BN - 1) / BN) * ((g.N + 127) / 128);
-  if (units * S > 0x7fffffffL) return cudaErrorInvalidConfiguration;
-  return launch_cluster(gemm_fp8_few_kernel<BN>, S > 1 ? (unsigned)S : 0u, (unsigned)(units * S), 256,
-                        FewCfg<BN>::SMEM, s, tw, ta, g, S);
+  if (units << logS > 0x7fffffffL) return cudaErrorInvalidConfiguration;
+  return launch_cluster(gemm_fp8_few_kernel<BN>, logS > 0 ? 1u << logS : 0u, (unsigned)(units << logS), 256,
+                        FewCfg<BN>::SMEM, s, tw, ta, g, logS);
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: CTA pairs
+// ---------------------------------------------------------------------------
+// Clusters of two CTAs compute 256 x 256 tiles (M = 256, N = 256, K = 32 an instruction), each CTA
+// staging its 128 rows of A and of W and receiving its 128 rows of the accumulator; both hold the
+// scales of all 256 columns.  Persistent, in an order that shares A's rows in L2.
+// Two accumulators of 256 columns fill tensor memory, which the scales need a little of: the second
+// one starts 32 columns inside the first (columns 224 .. 479), and the tile after this one waits
+// only for this one's drain of the shared 32 columns, which the epilogue reads first.
+// warp 0: TMA producer; 1: MMA (even CTA); 2: scale words; 4 .. 11: epilogue, two warps to each lane
+// quarter, 128 columns (one output block) each.
+constexpr int F8P_STAGES = 5, F8P_STAGE = 2 * F8_TILE;
+constexpr int F8P_SHARED = 32, F8P_ACC1 = 256 - F8P_SHARED;  // TMEM columns
+constexpr int F8P_SF_COL = F8P_ACC1 + 256, F8P_SF_COLS = 12;  // A's 4 columns, W's 8
+constexpr int F8P_LD = 36;  // floats of a row in an epilogue warp's transpose tile
+constexpr int F8P_OFF_SF = F8P_STAGES * F8P_STAGE;
+constexpr int F8P_OFF_EPI = F8P_OFF_SF + 2 * 3 * F8_ATOM;
+constexpr int F8P_OFF_BAR = F8P_OFF_EPI + 8 * 32 * F8P_LD * 4;
+constexpr int F8P_SMEM = F8P_OFF_BAR + 256 + 1024;
+constexpr int F8P_THREADS = 384;
+// registers a thread: 168 at launch; 128 * 72 + 256 * 216 = 384 * 168
+constexpr int F8P_REGS_ISSUE = 72, F8P_REGS_EPI = 216;
+static_assert(F8P_SF_COL + 2 * F8P_SF_COLS <= 512, "tensor memory");
+static_assert(F8P_SMEM <= 232448, "shared memory");
+
+namespace {
+
+BAG_DEV void copy_scales_pair(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+BAG_DEV void pair_mma_mxf8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                           uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)
+      : "memory");
+}
+
+// n <= 16 bytes of v to p (16-byte aligned).
+BAG_DEV void store_bytes16(uint8_t* p, uint4 v, int n) {
+  if (n >= 16) {
+    *reinterpret_cast<uint4*>(p) = v;
+  } else {
+    store_bytes(p, v.x, n);
+    if (n > 4) store_bytes(p + 4, v.y, n - 4);
+    if (n > 8) store_bytes(p + 8, v.z, n - 8);
+    if (n > 12) store_bytes(p + 12, v.w, n - 12);
+  }
+}
+
+// N consecutive floats, zeros past `valid`.
+template <int N>
+BAG_DEV void load_row(const float* p, int valid, float* v) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = i < valid ? __ldg(p + i) : 0.f;
+}
+
+// 32 x 32 accumulators of a warp (v: a row a lane) to fp32 or bf16 rows or the residual stream,
+// through shared memory, so that a warp access covers whole 64- or 128-byte runs of a row.
+template <int KIND>
+BAG_DEV void store_chunk(const Fp8Gemm& g, int row0, int col0, const float* v, float* buf) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int j = 0; j < 32; j += 4)
+    *reinterpret_cast<float4*>(buf + lane * F8P_LD + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  constexpr int NV = KIND == BAG_FP8_BF16 ? 8 : 4;  // 16 bytes of columns a lane
+  constexpr int LANES = 32 / NV, RPP = 32 / LANES, P = 32 / RPP;
+  const int r = lane / LANES, c = lane % LANES * NV, col = col0 + c;
+  const int valid = min(NV, g.N - col);
+  float b[NV];
+  load_row<NV>(g.bias + col, g.bias ? valid : 0, b);
+  __syncwarp();
+  float y[P][NV];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int j = 0; j < NV; j += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(buf + (p * RPP + r) * F8P_LD + c + j);
+      y[p][j] = f.x + b[j];
+      y[p][j + 1] = f.y + b[j + 1];
+      y[p][j + 2] = f.z + b[j + 2];
+      y[p][j + 3] = f.w + b[j + 3];
+    }
+  __syncwarp();  // the tile may be overwritten
+  if (g.act) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) y[p][j] = gelu_sigmoid(y[p][j]);
+  }
+  if (valid <= 0) return;
+  const int row = row0 + r;
+  if constexpr (KIND == BAG_FP8_BF16) {
+    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(g.out) + (long)row * g.ldo + col;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if (row + p * RPP >= g.M) break;
+      if (g.vec && valid == NV) {
+        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(y[p][0], y[p][1]), pack_bf16x2(y[p][2], y[p][3]),
+                                                  pack_bf16x2(y[p][4], y[p][5]), pack_bf16x2(y[p][6], y[p][7]));
+      } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (j < valid) o[j] = __float2bfloat16_rn(y[p][j]);
+      }
+      o += RPP * g.ldo;
+    }
+  } else {
+    float* o = reinterpret_cast<float*>(g.out) + (long)row * g.ldo + col;
+    if constexpr (KIND == BAG_FP8_RESID) {
+      float gt[NV];
+      if (g.gate)
+        load_row<NV>(g.gate + col, valid, gt);
+      else
+        gt[0] = gt[1] = gt[2] = gt[3] = 1.f;
+      float4 h[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        h[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float* q = o + (long)(p * RPP) * g.ldo;
+        if (row + p * RPP >= g.M) continue;
+        if (g.vec && valid == NV) {
+          h[p] = *reinterpret_cast<const float4*>(q);
+        } else {
+          h[p].x = q[0];
+          if (valid > 1) h[p].y = q[1];
+          if (valid > 2) h[p].z = q[2];
+          if (valid > 3) h[p].w = q[3];
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        y[p][0] = h[p].x + gt[0] * y[p][0];
+        y[p][1] = h[p].y + gt[1] * y[p][1];
+        y[p][2] = h[p].z + gt[2] * y[p][2];
+        y[p][3] = h[p].w + gt[3] * y[p][3];
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if (row + p * RPP >= g.M) break;
+      if (g.vec && valid == NV) {
+        *reinterpret_cast<float4*>(o) = make_float4(y[p][0], y[p][1], y[p][2], y[p][3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (j < valid) o[j] = y[p][j];
+      }
+      o += RPP * g.ldo;
+    }
+  }
+}
+
+// A thread's row of 128 accumulated columns (one block) encoded: the largest magnitude is its own
+// to find; the codes pass through shared memory, so that eight lanes store a row's 128 bytes.
+BAG_DEV void encode_block(const Fp8Gemm& g, int row, int col0, float* v, float* buf) {
+  const int lane = threadIdx.x & 31, valid = g.N - col0;
+  if (valid <= 0) return;  // a warp's columns are the same
+  if (g.bias) {
+    const bool whole = valid >= 128 && (reinterpret_cast<uintptr_t>(g.bias + col0) & 15) == 0;
+    if (whole) {
+#pragma unroll
+      for (int j = 0; j < 128; j += 4) {
+        const float4 b = __ldg(reinterpret_cast<const float4*>(g.bias + col0 + j));
+        v[j] += b.x;
+        v[j + 1] += b.y;
+        v[j + 2] += b.z;
+        v[j + 3] += b.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 128; ++j)
+        if (j < valid) v[j] += __ldg(g.bias + col0 + j);
+    }
+  }
+  if (g.act) {
+#pragma unroll
+    for (int j = 0; j < 128; ++j) v[j] = gelu_sigmoid(v[j]);
+  }
+  uint32_t m[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 128; ++j)
+    if (j < valid) m[j & 3] = max(m[j & 3], abs_bits(v[j]));
+  const uint32_t b = e8m0_of(max(max(m[0], m[1]), max(m[2], m[3])));
+  const float inv = e8m0_inverse(b);
+  if (row < g.M) g.out_s[(long)row * g.ldos + col0 / kScaleBlock] = (uint8_t)b;
+  uint4* line = reinterpret_cast<uint4*>(buf + lane * F8P_LD);
+#pragma unroll
+  for (int j = 0; j < 128; j += 16) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = pack_e4m3x4(v[j + 4 * i] * inv, v[j + 4 * i + 1] * inv, v[j + 4 * i + 2] * inv, v[j + 4 * i + 3] * inv);
+    line[j / 16] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __syncwarp();
+  const int r = lane >> 3, c = (lane & 7) * 16;
+  uint8_t* o = reinterpret_cast<uint8_t*>(g.out) + (long)(row - lane + r) * g.ldo + col0 + c;
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    if (row - lane + r + 4 * p < g.M && c < valid)
+      store_bytes16(o, reinterpret_cast<const uint4*>(buf + (4 * p + r) * F8P_LD)[lane & 7], valid - c);
+    o += 4 * g.ldo;
+  }
+  __syncwarp();  // the tile may be overwritten
+}
+
+}  // namespace
+
+template <int KIND>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
+    gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                         const __grid_constant__ Fp8Gemm g, int group_rows) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + F8P_OFF_BAR);
+  uint64_t* empty = full + F8P_STAGES;
+  uint64_t* sf_full = empty + F8P_STAGES;
+  uint64_t* sf_empty = sf_full + 2;
+  uint64_t* tfull = sf_empty + 2;
+  uint64_t* tempty = tfull + 2;
+  uint64_t* shared_free = tempty + 2;  // [2]: accumulator b's columns that the other one shares are drained
+  uint64_t* drain = shared_free + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
+  const long tiles = (long)num_m * num_n;
+  const int nkb = (g.K + F8_BK - 1) / F8_BK, ng = (nkb + F8_GROUP - 1) / F8_GROUP;
+  // groups of group_rows row tiles visit every column tile, the row tile varying fastest
+  auto decode = [&](long tile, int& mt, int& nt) {
+    const long per = (long)group_rows * num_n;
+    const int gr = (int)(tile / per);
+    const int i = (int)(tile - gr * per), rows = min(group_rows, num_m - gr * group_rows);
+    mt = gr * group_rows + i % rows;
+    nt = i / rows;
+  };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F8P_STAGES; ++s) {
+      mbar_init(full + s, 1);   // even CTA: its producer's expect_tx; both CTAs' bytes
+      mbar_init(empty + s, 1);  // both CTAs: one multicast commit per consumed stage
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(sf_full + s, 2);       // even CTA: both CTAs' scale warps
+      mbar_init(sf_empty + s, 1);      // both CTAs: multicast commit
+      mbar_init(tfull + s, 1);         // both CTAs: multicast commit
+      mbar_init(tempty + s, 16);       // even CTA: every epilogue warp of both CTAs
+      mbar_init(shared_free + s, 8);   // even CTA: the warps that hold the shared columns
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmW);
+  }
+  grid_dep_sync();
+  __syncwarp();
+  if (warp == 1) {
+    tmem_alloc_pair(tmem_slot, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();  // barriers of both CTAs initialised, tensor memory allocated
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F8P_REGS_ISSUE));
+    if (warp == 0) {
+      if (lane == 0) {
+        // ---------------- TMA producer (both CTAs: their own halves) ----------------
+        int s = 0;
+        uint32_t ph = 0;
+        long issued = 0;
+        bool ok = true;
+        for (long tile = pair; tile < tiles && ok; tile += npairs) {
+          int mt, nt;
+          decode(tile, mt, nt);
+          for (int kb = 0; kb < nkb; ++kb) {
+            if (!mbar_wait(empty + s, ph ^ 1, abort_flag)) {
+              ok = false;
+              break;
+            }
+            if (rank == 0) mbar_arrive_expect_tx(full + s, 2 * F8P_STAGE);
+            const uint32_t fb = mapa_shared(smem_u32(full + s), 0);
+            pair_load_2d(smem + s * F8P_STAGE, &tmA, kb * F8_BK, mt * 256 + (int)rank * 128, fb);
+            pair_load_2d(smem + s * F8P_STAGE + F8_TILE, &tmW, kb * F8_BK, nt * 256 + (int)rank * 128, fb);
+            ++issued;
+            if (++s == F8P_STAGES) {
+              s = 0;
+              ph ^= 1;
+            }
+          }
+        }
+        if (!ok && rank == 0) {
+          // wait (bounded): both CTAs' copies in flight complete on this CTA's barriers
+          const uint64_t t0 = global_ns();
+          for (int i = 0; i < F8P_STAGES && i < issued; ++i) {
+            if (--s < 0) {
+              s = F8P_STAGES - 1;
+              ph ^= 1;
+            }
+            while (!mbar_try_wait(full + s, ph) && global_ns() - t0 < kWaitLimitNs) {
+            }
+          }
+        }
+      }
+    } else if (warp == 1) {
+      if (rank == 0) {
+        // -------- MMA issuer (even CTA; converged warp, one elected lane issues) --------
+        const uint32_t base = smem_u32(smem);
+        int s = 0, ss = 0;
+        uint32_t ph = 0, sph = 0;
+        long i = 0;  // tiles of this pair so far
+        bool ok = true;
+        for (long tile = pair; tile < tiles && ok; tile += npairs, ++i) {
+          const int acc = (int)(i & 1);
+          const uint32_t dt = tmem + (acc ? F8P_ACC1 : 0);
+          // the accumulator's last tile is drained, and the other one's shared columns
+          if (!mbar_wait_warp(tempty + acc, (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag)) break;
+          if (i > 0 && !mbar_wait_warp(shared_free + (acc ^ 1), (uint32_t)(((i - 1) >> 1) & 1), abort_flag)) break;
+          tc_fence_after();
+          for (int kb = 0; kb < nkb; ++kb) {
+            const uint32_t sa = tmem + F8P_SF_COL + ss * F8P_SF_COLS;
+            if (kb % F8_GROUP == 0) {
+              if (!(ok = wait_warp_cluster(sf_full + ss, sph, abort_flag))) break;
+              tc_fence_after();
+              const uint64_t d = scale_desc(base + F8P_OFF_SF + ss * 3 * F8_ATOM);
+              if (elect_one()) {
+#pragma unroll
+                for (int a = 0; a < 3; ++a) copy_scales_pair(sa + 4 * a, d + a * (F8_ATOM >> 4));
+              }
+              __syncwarp();
+            }
+            if (!(ok = mbar_wait_warp(full + s, ph, abort_flag))) break;
+            tc_fence_after();
+            const uint64_t ad = sw128_desc(base + s * F8P_STAGE);
+            const uint64_t wd = sw128_desc(base + s * F8P_STAGE + F8_TILE);
+            const uint32_t idesc = idesc_mxf8(256, 256) | scale_byte((uint32_t)(kb % F8_GROUP));
+            const bool last = kb + 1 == nkb || (kb + 1) % F8_GROUP == 0;
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
+                pair_mma_mxf8(dt, ad + 2 * k, wd + 2 * k, idesc, sa, sa + 4, (kb | k) != 0 ? 1u : 0u);
+              pair_commit(empty + s, 3);
+              if (last) pair_commit(sf_empty + ss, 3);
+            }
+            __syncwarp();
+            if (++s == F8P_STAGES) {
+              s = 0;
+              ph ^= 1;
+            }
+            if (last && (ss ^= 1) == 0) sph ^= 1;
+          }
+          if (!ok) break;
+          if (elect_one()) pair_commit(tfull + acc, 3);
+          __syncwarp();
+        }
+        // every issued MMA has finished before tensor memory is released
+        if (elect_one()) {
+          pair_commit(drain, 1);
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(drain, 0) && global_ns() - t0 < kWaitLimitNs) {
+          }
+        }
+        __syncwarp();
+      }
+    } else if (warp == 2) {
+      // ---------------- scale words (both CTAs: A's own rows, all 256 of W) ----------------
+      int ss = 0, mt = 0, nt = 0, gi = 0;
+      uint32_t sph = 0;
+      const uint32_t full_even = mapa_shared(smem_u32(sf_full), 0);
+      uint4 w[3];
+      auto fetch = [&]() {
+        w[0] = scale_words(g.a_s, g.ldas, mt * 256 + (int)rank * 128, g.M, gi);
+        w[1] = scale_words(g.w_s, g.ldws, nt * 256, g.N, gi);
+        w[2] = scale_words(g.w_s, g.ldws, nt * 256 + 128, g.N, gi);
+      };
+      long tile = pair;
+      if (tile < tiles) {
+        decode(tile, mt, nt);
+        fetch();
+      }
+      while (tile < tiles) {
+        if (!mbar_wait_warp(sf_empty + ss, sph ^ 1, abort_flag)) break;
+        uint4* d = reinterpret_cast<uint4*>(smem + F8P_OFF_SF + ss * 3 * F8_ATOM);
+#pragma unroll
+        for (int a = 0; a < 3; ++a) d[a * 32 + lane] = w[a];
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) peer_arrive(full_even + (uint32_t)(ss * sizeof(uint64_t)));
+        if (++gi == ng) {
+          gi = 0;
+          tile += npairs;
+          if (tile < tiles) decode(tile, mt, nt);
+        }
+        if (tile < tiles) fetch();
+        if ((ss ^= 1) == 0) sph ^= 1;
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F8P_REGS_EPI));
+    // ---------------- epilogue (both CTAs: their 128 rows of each tile) ----------------
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    float* buf = reinterpret_cast<float*>(smem + F8P_OFF_EPI) + (warp - 4) * 32 * F8P_LD;
+    const uint32_t tempty_even = mapa_shared(smem_u32(tempty), 0), free_even = mapa_shared(smem_u32(shared_free), 0);
+    long i = 0;
+    for (long tile = pair; tile < tiles; tile += npairs, ++i) {
+      const int acc = (int)(i & 1);
+      int mt, nt;
+      decode(tile, mt, nt);
+      const bool ok = mbar_wait(tfull + acc, (uint32_t)((i >> 1) & 1), abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after();
+      const int row = mt * 256 + (int)rank * 128 + q * 32 + lane, col0 = nt * 256 + half * 128;
+      const uint32_t tb = tmem + (uint32_t)((acc ? F8P_ACC1 : 0) + half * 128) + ((uint32_t)(q * 32) << 16);
+      // the shared columns are the last 32 of accumulator 0 and the first 32 of accumulator 1
+      const bool shares = half == (acc ^ 1);
+      const int first = acc ? 0 : 3;
+      auto release_shared = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) peer_arrive(free_even + (uint32_t)(acc * sizeof(uint64_t)));
+      };
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) peer_arrive(tempty_even + (uint32_t)(acc * sizeof(uint64_t)));
+      };
+      if constexpr (KIND == BAG_FP8_CODES) {
+        float v[128];
+        if (shares && first == 3) {
+          tmem_ld32(tb + 96, v + 96);
+          release_shared();
+        }
+        tmem_ld32(tb, v);
+        if (shares && first == 0) release_shared();
+        tmem_ld32(tb + 32, v + 32);
+        tmem_ld32(tb + 64, v + 64);
+        if (!(shares && first == 3)) tmem_ld32(tb + 96, v + 96);
+        release();
+        encode_block(g, row, col0, v, buf);
+      } else {
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+          const int c = ((k + first) & 3) * 32;
+          float v[32];
+          tmem_ld32(tb + (uint32_t)c, v);
+          if (k == 0 && shares) release_shared();
+          if (k == 3) release();
+          store_chunk<KIND>(g, row - lane, col0 + c, v, buf);
+          __syncwarp();
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();  // no CTA of the pair still uses the pair's tensor memory
+  if (threadIdx.x == 0 && *abort_flag && g.err) atomicOr(g.err, 1);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
+  }
+}
+
+static cudaError_t launch_pair(Fp8Gemm g, cudaStream_t s) {
+  CUtensorMap ta, tw;
+  if (encode_tmap_2d_u8(&ta, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, 128) ||
+      encode_tmap_2d_u8(&tw, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128))
+    return cudaErrorInvalidValue;
+  const int size = g.kind == BAG_FP8_BF16 ? 2 : 4;
+  g.vec = ((reinterpret_cast<uintptr_t>(g.out) | (uintptr_t)(g.ldo * size)) & 15) == 0;
+  const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
+  const int pairs = (int)std::min((long)num_m * num_n, (long)sm_count() / 2);
+  const int rows = (int)std::max(1.0, std::min((double)num_m, 40.0 * 1048576.0 / (256.0 * g.K)));
+  auto launch = [&](auto kernel) {
+    return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, g, rows);
+  };
+  switch (g.kind) {
+    case BAG_FP8_F32: return launch(gemm_fp8_pair_kernel<BAG_FP8_F32>);
+    case BAG_FP8_BF16: return launch(gemm_fp8_pair_kernel<BAG_FP8_BF16>);
+    case BAG_FP8_CODES: return launch(gemm_fp8_pair_kernel<BAG_FP8_CODES>);
+    default: return launch(gemm_fp8_pair_kernel<BAG_FP8_RESID>);
+  }
 }
 
 cudaError_t gemm_fp8_init() {
@@ -355,20 +875,27 @@ cudaError_t gemm_fp8_init() {
   smem(gemm_fp8_few_kernel<32>, FewCfg<32>::SMEM);
   smem(gemm_fp8_few_kernel<64>, FewCfg<64>::SMEM);
   smem(gemm_fp8_few_kernel<128>, FewCfg<128>::SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_F32>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_BF16>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_CODES>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_RESID>, F8P_SMEM);
   return r;
 }
 
 cudaError_t gemm_fp8(Fp8Gemm g, cudaStream_t s) {
   if (g.M <= 0 || g.N <= 0) return cudaSuccess;
+  const long tiles = (long)((g.M + 255) / 256) * ((g.N + 255) / 256);
+  if (tiles * 2 >= sm_count()) return launch_pair(g, s);
   const int BN = g.M <= 16 ? 16 : (g.M <= 32 ? 32 : (g.M <= 64 ? 64 : 128));
   const long units = (long)((g.M + BN - 1) / BN) * ((g.N + 127) / 128);
   const int nkb = (g.K + F8_BK - 1) / F8_BK;
-  int S = 1;
-  while (S < 8 && units * S * 2 <= sm_count() && nkb >= S * 2 * 4) S *= 2;
-  if (BN == 16) return launch_few<16>(g, S, s);
-  if (BN == 32) return launch_few<32>(g, S, s);
-  if (BN == 64) return launch_few<64>(g, S, s);
-  return launch_few<128>(g, S, s);
+  const int fit = BN <= 32 ? 3 : 2;  // CTAs that an SM holds
+  int logS = 0;
+  while (logS < 3 && units << (logS + 1) <= (long)sm_count() * fit && nkb >= 8 << logS) ++logS;
+  if (BN == 16) return launch_few<16>(g, logS, s);
+  if (BN == 32) return launch_few<32>(g, logS, s);
+  if (BN == 64) return launch_few<64>(g, logS, s);
+  return launch_few<128>(g, logS, s);
 }
 
 }  // namespace bag

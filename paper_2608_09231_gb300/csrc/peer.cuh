@@ -12,5 +12,27 @@ BAG_DEV void peer_store2(uint32_t addr, float a, float b) { st_cluster2(addr, a,
 BAG_DEV void peer_store1(uint32_t addr, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
+BAG_DEV void peer_arrive(uint32_t mbar_cluster) { mbar_arrive_remote(mbar_cluster); }
+BAG_DEV void pair_load_2d(void* smem_dst, const CUtensorMap* map, int x, int y, uint32_t mbar_cluster) {
+  tma_load_2d_pair(smem_dst, map, x, y, mbar_cluster);
+}
+BAG_DEV void pair_commit(uint64_t* bar, uint16_t mask) { mma_commit_pair(bar, mask); }
+
+// mbar_wait_warp for a barrier that the peer arrives on after writing its own shared memory: the
+// wait acquires at the cluster's scope.
+BAG_DEV bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+BAG_DEV bool wait_warp_cluster(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return mbar_wait_warp(bar, parity, abort) && __all_sync(0xffffffffu, try_wait_cluster(bar, parity));
+}
 
 }  // namespace bag
