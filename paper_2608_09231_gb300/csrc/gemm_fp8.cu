@@ -22,6 +22,7 @@ constexpr int F8_BK = kScaleBlock;      // K columns (bytes) of a pipeline stage
 constexpr int F8_TILE = 128 * F8_BK;    // bytes of 128 rows
 constexpr int F8_GROUP = 4;             // K blocks whose scale bytes share a word
 constexpr int F8_ATOM = 512;            // bytes of 128 rows' scale words
+constexpr int F8_RUN = 4;               // groups that are fetched and handed over together (16 bytes a row)
 
 // Shared-memory descriptor of a scale atom: 16-byte rows, groups of eight 128 bytes apart.
 BAG_DEV uint64_t scale_desc(uint32_t saddr) {
@@ -62,14 +63,46 @@ BAG_DEV void tmem_ld16(uint32_t taddr, float* v) {
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// The scale words of K blocks 4 g .. 4 g + 3 for rows row0 + 32 c + lane (c = 0 .. 3); rows past
-// the end have scale 1 (their codes are zeros).
-BAG_DEV uint4 scale_words(const uint8_t* __restrict__ s, long lds, int row0, int rows, int g) {
-  const int r = row0 + (int)(threadIdx.x & 31);
-  auto at = [&](int row) {
-    return row < rows ? __ldg(reinterpret_cast<const uint32_t*>(s + (long)row * lds) + g) : 0x7f7f7f7fu;
-  };
-  return make_uint4(at(r), at(r + 32), at(r + 64), at(r + 96));
+// The scale words of one run of groups (run r: K blocks 16 r .. 16 r + 15) for the 128 rows from
+// row0 on: rows row0 + 32 c + lane, c = 0 .. 3.  Rows past the end have scale 1 (their codes are
+// zeros).  16-byte loads where the rows allow them: a row's words of a run lie in one sector, and
+// with word loads every group would fetch it again (the ring leaves L1 too small to keep it).
+struct ScaleRun {
+  uint4 w[4];
+  BAG_DEV void fetch(const uint8_t* __restrict__ s, long lds, bool wide, int row0, int rows, int run) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int row = row0 + 32 * c + (int)(threadIdx.x & 31);
+      w[c] = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+      if (row >= rows) continue;
+      const uint8_t* p = s + (long)row * lds + run * 16;
+      if (wide) {
+        w[c] = __ldg(reinterpret_cast<const uint4*>(p));
+      } else {
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+        const long left = lds / 4 - run * 4;  // words of the row from here on
+        if (left > 0) w[c].x = __ldg(q);
+        if (left > 1) w[c].y = __ldg(q + 1);
+        if (left > 2) w[c].z = __ldg(q + 2);
+        if (left > 3) w[c].w = __ldg(q + 3);
+      }
+    }
+  }
+  // to shared memory, group after group `step` bytes apart: lane i's 16 bytes are the words of rows
+  // i, 32 + i, 64 + i and 96 + i
+  BAG_DEV void put(uint8_t* dst, int step) const {
+    const int lane = threadIdx.x & 31;
+    auto at = [&](int j) -> uint4& { return reinterpret_cast<uint4*>(dst + j * step)[lane]; };
+    at(0) = make_uint4(w[0].x, w[1].x, w[2].x, w[3].x);
+    at(1) = make_uint4(w[0].y, w[1].y, w[2].y, w[3].y);
+    at(2) = make_uint4(w[0].z, w[1].z, w[2].z, w[3].z);
+    at(3) = make_uint4(w[0].w, w[1].w, w[2].w, w[3].w);
+  }
+};
+
+// Whether rows of scale bytes are whole 16-byte units.
+__host__ __device__ __forceinline__ bool wide_scales(const uint8_t* s, long lds) {
+  return ((reinterpret_cast<uintptr_t>(s) | (uintptr_t)lds) & 15) == 0;
 }
 
 }  // namespace
@@ -85,9 +118,10 @@ BAG_DEV uint4 scale_words(const uint8_t* __restrict__ s, long lds, int row0, int
 template <int BN>
 struct FewCfg {
   static constexpr int STAGE = F8_TILE + BN * F8_BK;
-  static constexpr int STAGES = BN <= 32 ? 4 : 3;
-  static constexpr int OFF_SF = STAGES * STAGE;              // two stages of W's and A's scale words
-  static constexpr int OFF_RED = OFF_SF + 2 * 2 * F8_ATOM;   // [BN][4] block maxima of warps
+  static constexpr int STAGES = 3;
+  static constexpr int OFF_SF = STAGES * STAGE;              // two runs of W's and A's scale words
+  static constexpr int SF_GROUP = 2 * F8_ATOM, SF_STAGE = F8_RUN * SF_GROUP;
+  static constexpr int OFF_RED = OFF_SF + 2 * SF_STAGE;      // [BN][4] block maxima of warps
   static constexpr int OFF_BAR = OFF_RED + BN * 16;
   static constexpr int SMEM = OFF_BAR + 256 + 1024;
   static constexpr int SF_COL = BN;                          // 8 TMEM columns a scale stage
@@ -108,7 +142,8 @@ __global__ void __launch_bounds__(256)
   uint64_t* empty = full + C::STAGES;
   uint64_t* sf_full = empty + C::STAGES;
   uint64_t* sf_empty = sf_full + 2;
-  uint64_t* tfull = sf_empty + 2;
+  uint64_t* sf_used = sf_empty + 2;  // [2]: a group's products are done, its TMEM columns free
+  uint64_t* tfull = sf_used + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tfull + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -127,6 +162,7 @@ __global__ void __launch_bounds__(256)
     for (int s = 0; s < 2; ++s) {
       mbar_init(sf_full + s, 1);
       mbar_init(sf_empty + s, 1);
+      mbar_init(sf_used + s, 1);
     }
     mbar_init(tfull, 1);
     *abort_flag = 0;
@@ -182,14 +218,19 @@ __global__ void __launch_bounds__(256)
   } else if (warp == 1) {
     // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
     const uint32_t base = smem_u32(smem);
-    int s = 0, ss = 0;
-    uint32_t ph = 0, sph = 0;
+    int s = 0, run = 0, grp = 0;  // ring stage; runs and groups handled so far
+    uint32_t ph = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
-      const uint32_t sw = tmem + C::SF_COL + ss * 8;
+      if (kb == kb0 || kb % (F8_GROUP * F8_RUN) == 0) {
+        if (!mbar_wait_warp(sf_full + (run & 1), (uint32_t)(run >> 1) & 1u, abort_flag)) break;
+        ++run;
+      }
+      const uint32_t sw = tmem + C::SF_COL + (grp & 1) * 8;
       if (kb == kb0 || kb % F8_GROUP == 0) {
-        if (!mbar_wait_warp(sf_full + ss, sph, abort_flag)) break;
+        if (!mbar_wait_warp(sf_used + (grp & 1), ((uint32_t)(grp >> 1) & 1u) ^ 1u, abort_flag)) break;
         tc_fence_after();
-        const uint64_t d = scale_desc(base + C::OFF_SF + ss * 2 * F8_ATOM);
+        const uint64_t d = scale_desc(base + C::OFF_SF + ((run - 1) & 1) * C::SF_STAGE +
+                                      kb / F8_GROUP % F8_RUN * C::SF_GROUP);
         if (elect_one()) {
           copy_scales(sw, d);
           copy_scales(sw + 4, d + (F8_ATOM >> 4));
@@ -202,19 +243,21 @@ __global__ void __launch_bounds__(256)
       const uint64_t ad = sw128_desc(base + s * C::STAGE + F8_TILE);
       const uint32_t idesc = idesc_mxf8(128, BN) | scale_byte((uint32_t)(kb % F8_GROUP));
       const bool last = kb + 1 == kb1 || (kb + 1) % F8_GROUP == 0;
+      const bool last_run = kb + 1 == kb1 || (kb + 1) % (F8_GROUP * F8_RUN) == 0;
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
           mma_mxf8(tmem, wd + 2 * k, ad + 2 * k, idesc, sw, sw + 4, (kb > kb0 || k > 0) ? 1u : 0u);
         mma_commit(empty + s);
-        if (last) mma_commit(sf_empty + ss);
+        if (last) mma_commit(sf_used + (grp & 1));
+        if (last_run) mma_commit(sf_empty + ((run - 1) & 1));
       }
       __syncwarp();
       if (++s == C::STAGES) {
         s = 0;
         ph ^= 1;
       }
-      if (last && (ss ^= 1) == 0) sph ^= 1;
+      grp += last;
     }
     // all MMAs issued so far (whatever happened above) finish before tfull completes, and
     // the bounded wait keeps tensor memory until then
@@ -226,28 +269,27 @@ __global__ void __launch_bounds__(256)
     }
     __syncwarp();
   } else if (warp == 2) {
-    // ---------------- scale words, a group of four K blocks at a time ----------------
-    const int g0 = kb0 / F8_GROUP, g1 = (kb1 + F8_GROUP - 1) / F8_GROUP;
-    uint4 w = make_uint4(0u, 0u, 0u, 0u), a = w;
-    auto fetch = [&](int gi) {
-      if (gi < g1) {
-        w = scale_words(g.w_s, g.ldws, n0, g.N, gi);
-        a = scale_words(g.a_s, g.ldas, m0, min(g.M, m0 + BN), gi);
+    // ---------------- scale words, a run of groups at a time ----------------
+    const int r0 = kb0 / (F8_GROUP * F8_RUN), r1 = (kb1 + F8_GROUP * F8_RUN - 1) / (F8_GROUP * F8_RUN);
+    const bool wide_w = wide_scales(g.w_s, g.ldws), wide_a = wide_scales(g.a_s, g.ldas);
+    ScaleRun w, a;
+    auto fetch = [&](int r) {
+      if (r < r1) {
+        w.fetch(g.w_s, g.ldws, wide_w, n0, g.N, r);
+        a.fetch(g.a_s, g.ldas, wide_a, m0, min(g.M, m0 + BN), r);
       }
     };
-    fetch(g0);
-    int ss = 0;
-    uint32_t sph = 0;
-    for (int gi = g0; gi < g1 && kb0 < kb1; ++gi) {
-      if (!mbar_wait_warp(sf_empty + ss, sph ^ 1, abort_flag)) break;
-      uint4* d = reinterpret_cast<uint4*>(smem + C::OFF_SF + ss * 2 * F8_ATOM);
-      d[lane] = w;
-      d[32 + lane] = a;
+    fetch(r0);
+    for (int r = r0; r < r1; ++r) {
+      const int i = r - r0, st = i & 1;
+      if (!mbar_wait_warp(sf_empty + st, ((uint32_t)(i >> 1) & 1u) ^ 1u, abort_flag)) break;
+      uint8_t* d = smem + C::OFF_SF + st * C::SF_STAGE;
+      w.put(d, C::SF_GROUP);
+      a.put(d + F8_ATOM, C::SF_GROUP);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(sf_full + ss);
-      fetch(gi + 1);
-      if ((ss ^= 1) == 0) sph ^= 1;
+      if (lane == 0) mbar_arrive(sf_full + st);
+      fetch(r + 1);
     }
   }
   // ---------------- epilogue ----------------
@@ -361,8 +403,8 @@ __global__ void __launch_bounds__(256)
 template <int BN>
 static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
   CUtensorMap tw, ta;
-  if (encode_tmap_2d_u8(&tw, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128) ||
-      encode_tmap_2d_u8(&ta, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, BN))
+  if (encode_tmap_2d_bytes(&tw, 1, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128) ||
+      encode_tmap_2d_bytes(&ta, 1, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, BN))
     return cudaErrorInvalidValue;
   const long units = (long)((g.M + BN - 1) / BN) * ((g.N + 127) / 128);
   if (units << logS > 0x7fffffffL) return cudaErrorInvalidConfiguration;
@@ -381,17 +423,22 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // only for this one's drain of the shared 32 columns, which the epilogue reads first.
 // warp 0: TMA producer; 1: MMA (even CTA); 2: scale words; 4 .. 11: epilogue, two warps to each lane
 // quarter, 128 columns (one output block) each.
+// The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a
+// row a thread, with bias and gate broadcast from shared memory, and its output leaves by TMA:
+// stores, or for the residual stream an add that L2 carries out, so that the stream is not read.
 constexpr int F8P_STAGES = 5, F8P_STAGE = 2 * F8_TILE;
 constexpr int F8P_SHARED = 32, F8P_ACC1 = 256 - F8P_SHARED;  // TMEM columns
 constexpr int F8P_SF_COL = F8P_ACC1 + 256, F8P_SF_COLS = 12;  // A's 4 columns, W's 8
-constexpr int F8P_LD = 36;  // floats of a row in an epilogue warp's transpose tile
-constexpr int F8P_OFF_SF = F8P_STAGES * F8P_STAGE;
-constexpr int F8P_OFF_EPI = F8P_OFF_SF + 2 * 3 * F8_ATOM;
-constexpr int F8P_OFF_BAR = F8P_OFF_EPI + 8 * 32 * F8P_LD * 4;
+constexpr int F8P_SF_GROUP = 3 * F8_ATOM, F8P_SF_STAGE = F8_RUN * F8P_SF_GROUP;
+constexpr int F8P_BUF = 32 * 128;    // bytes of an epilogue warp's staged output: 32 rows of 128 bytes
+constexpr int F8P_OFF_BUF = F8P_STAGES * F8P_STAGE;
+constexpr int F8P_OFF_SF = F8P_OFF_BUF + 8 * F8P_BUF;
+constexpr int F8P_OFF_VEC = F8P_OFF_SF + 2 * F8P_SF_STAGE;  // bias and gate of each warp's 128 columns
+constexpr int F8P_OFF_BAR = F8P_OFF_VEC + 8 * 2 * 512;
 constexpr int F8P_SMEM = F8P_OFF_BAR + 256 + 1024;
 constexpr int F8P_THREADS = 384;
-// registers a thread: 168 at launch; 128 * 72 + 256 * 216 = 384 * 168
-constexpr int F8P_REGS_ISSUE = 72, F8P_REGS_EPI = 216;
+// registers a thread: 168 at launch; 128 * 88 + 256 * 208 = 384 * 168
+constexpr int F8P_REGS_ISSUE = 88, F8P_REGS_EPI = 208;
 static_assert(F8P_SF_COL + 2 * F8P_SF_COLS <= 512, "tensor memory");
 static_assert(F8P_SMEM <= 232448, "shared memory");
 
@@ -411,173 +458,66 @@ BAG_DEV void pair_mma_mxf8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, u
       : "memory");
 }
 
-// n <= 16 bytes of v to p (16-byte aligned).
-BAG_DEV void store_bytes16(uint8_t* p, uint4 v, int n) {
-  if (n >= 16) {
-    *reinterpret_cast<uint4*>(p) = v;
-  } else {
-    store_bytes(p, v.x, n);
-    if (n > 4) store_bytes(p + 4, v.y, n - 4);
-    if (n > 8) store_bytes(p + 8, v.z, n - 8);
-    if (n > 12) store_bytes(p + 12, v.w, n - 12);
+// A tile in shared memory to (or added to) the tensor of `map` at column x, row y; rows past its
+// last are left out.
+BAG_DEV void tma_store_2d(const CUtensorMap* map, const void* smem, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(smem_u32(smem))
+               : "memory");
+}
+BAG_DEV void tma_add_2d(const CUtensorMap* map, const void* smem, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(smem_u32(smem))
+               : "memory");
+}
+BAG_DEV void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+BAG_DEV void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+BAG_DEV void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// Column-wise vectors: entry j of 32 columns to v (16-byte broadcasts from shared memory).
+template <typename F>
+BAG_DEV void with_vector(const float* s, float* v, F f) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    const float4 b = *reinterpret_cast<const float4*>(s + j);
+    v[j] = f(v[j], b.x);
+    v[j + 1] = f(v[j + 1], b.y);
+    v[j + 2] = f(v[j + 2], b.z);
+    v[j + 3] = f(v[j + 3], b.w);
   }
 }
 
-// N consecutive floats, zeros past `valid`.
-template <int N>
-BAG_DEV void load_row(const float* p, int valid, float* v) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = i < valid ? __ldg(p + i) : 0.f;
-}
-
-// 32 x 32 accumulators of a warp (v: a row a lane) to fp32 or bf16 rows or the residual stream,
-// through shared memory, so that a warp access covers whole 64- or 128-byte runs of a row.
-template <int KIND>
-BAG_DEV void store_chunk(const Fp8Gemm& g, int row0, int col0, const float* v, float* buf) {
+// 16-byte unit u of this lane's 128-byte row in a staged tile (the 128-byte swizzle of TMA).
+BAG_DEV uint4& staged(uint8_t* buf, int u) {
   const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int j = 0; j < 32; j += 4)
-    *reinterpret_cast<float4*>(buf + lane * F8P_LD + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-  constexpr int NV = KIND == BAG_FP8_BF16 ? 8 : 4;  // 16 bytes of columns a lane
-  constexpr int LANES = 32 / NV, RPP = 32 / LANES, P = 32 / RPP;
-  const int r = lane / LANES, c = lane % LANES * NV, col = col0 + c;
-  const int valid = min(NV, g.N - col);
-  float b[NV];
-  load_row<NV>(g.bias + col, g.bias ? valid : 0, b);
-  __syncwarp();
-  float y[P][NV];
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int j = 0; j < NV; j += 4) {
-      const float4 f = *reinterpret_cast<const float4*>(buf + (p * RPP + r) * F8P_LD + c + j);
-      y[p][j] = f.x + b[j];
-      y[p][j + 1] = f.y + b[j + 1];
-      y[p][j + 2] = f.z + b[j + 2];
-      y[p][j + 3] = f.w + b[j + 3];
-    }
-  __syncwarp();  // the tile may be overwritten
-  if (g.act) {
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int j = 0; j < NV; ++j) y[p][j] = gelu_sigmoid(y[p][j]);
-  }
-  if (valid <= 0) return;
-  const int row = row0 + r;
-  if constexpr (KIND == BAG_FP8_BF16) {
-    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(g.out) + (long)row * g.ldo + col;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if (row + p * RPP >= g.M) break;
-      if (g.vec && valid == NV) {
-        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(y[p][0], y[p][1]), pack_bf16x2(y[p][2], y[p][3]),
-                                                  pack_bf16x2(y[p][4], y[p][5]), pack_bf16x2(y[p][6], y[p][7]));
-      } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          if (j < valid) o[j] = __float2bfloat16_rn(y[p][j]);
-      }
-      o += RPP * g.ldo;
-    }
-  } else {
-    float* o = reinterpret_cast<float*>(g.out) + (long)row * g.ldo + col;
-    if constexpr (KIND == BAG_FP8_RESID) {
-      float gt[NV];
-      if (g.gate)
-        load_row<NV>(g.gate + col, valid, gt);
-      else
-        gt[0] = gt[1] = gt[2] = gt[3] = 1.f;
-      float4 h[P];
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        h[p] = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float* q = o + (long)(p * RPP) * g.ldo;
-        if (row + p * RPP >= g.M) continue;
-        if (g.vec && valid == NV) {
-          h[p] = *reinterpret_cast<const float4*>(q);
-        } else {
-          h[p].x = q[0];
-          if (valid > 1) h[p].y = q[1];
-          if (valid > 2) h[p].z = q[2];
-          if (valid > 3) h[p].w = q[3];
-        }
-      }
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        y[p][0] = h[p].x + gt[0] * y[p][0];
-        y[p][1] = h[p].y + gt[1] * y[p][1];
-        y[p][2] = h[p].z + gt[2] * y[p][2];
-        y[p][3] = h[p].w + gt[3] * y[p][3];
-      }
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if (row + p * RPP >= g.M) break;
-      if (g.vec && valid == NV) {
-        *reinterpret_cast<float4*>(o) = make_float4(y[p][0], y[p][1], y[p][2], y[p][3]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          if (j < valid) o[j] = y[p][j];
-      }
-      o += RPP * g.ldo;
-    }
-  }
+  return *reinterpret_cast<uint4*>(buf + lane * 128 + ((u ^ (lane & 7)) << 4));
 }
 
-// A thread's row of 128 accumulated columns (one block) encoded: the largest magnitude is its own
-// to find; the codes pass through shared memory, so that eight lanes store a row's 128 bytes.
-BAG_DEV void encode_block(const Fp8Gemm& g, int row, int col0, float* v, float* buf) {
-  const int lane = threadIdx.x & 31, valid = g.N - col0;
-  if (valid <= 0) return;  // a warp's columns are the same
-  if (g.bias) {
-    const bool whole = valid >= 128 && (reinterpret_cast<uintptr_t>(g.bias + col0) & 15) == 0;
-    if (whole) {
+// A staged tile (32 rows of 128 bytes: W columns of T) to rows that TMA cannot address or past whose
+// end it would write, a row at a time, lane after lane along it.
+template <typename T, bool ADD>
+BAG_DEV void store_rows(const Fp8Gemm& g, const uint8_t* buf, int row0, int col0) {
+  constexpr int W = 128 / (int)sizeof(T);
+  const int lane = threadIdx.x & 31;
+  T* o = reinterpret_cast<T*>(g.out) + (long)row0 * g.ldo + col0;
+  const int rows = min(32, g.M - row0);
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r) {
 #pragma unroll
-      for (int j = 0; j < 128; j += 4) {
-        const float4 b = __ldg(reinterpret_cast<const float4*>(g.bias + col0 + j));
-        v[j] += b.x;
-        v[j + 1] += b.y;
-        v[j + 2] += b.z;
-        v[j + 3] += b.w;
+    for (int c = lane; c < W; c += 32) {
+      const int byte = c * (int)sizeof(T);
+      const T v = *reinterpret_cast<const T*>(buf + r * 128 + ((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)));
+      if (col0 + c < g.N) {
+        T* p = o + (long)r * g.ldo + c;
+        if constexpr (ADD)
+          *p += v;
+        else
+          *p = v;
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 128; ++j)
-        if (j < valid) v[j] += __ldg(g.bias + col0 + j);
     }
   }
-  if (g.act) {
-#pragma unroll
-    for (int j = 0; j < 128; ++j) v[j] = gelu_sigmoid(v[j]);
-  }
-  uint32_t m[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int j = 0; j < 128; ++j)
-    if (j < valid) m[j & 3] = max(m[j & 3], abs_bits(v[j]));
-  const uint32_t b = e8m0_of(max(max(m[0], m[1]), max(m[2], m[3])));
-  const float inv = e8m0_inverse(b);
-  if (row < g.M) g.out_s[(long)row * g.ldos + col0 / kScaleBlock] = (uint8_t)b;
-  uint4* line = reinterpret_cast<uint4*>(buf + lane * F8P_LD);
-#pragma unroll
-  for (int j = 0; j < 128; j += 16) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = pack_e4m3x4(v[j + 4 * i] * inv, v[j + 4 * i + 1] * inv, v[j + 4 * i + 2] * inv, v[j + 4 * i + 3] * inv);
-    line[j / 16] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  __syncwarp();
-  const int r = lane >> 3, c = (lane & 7) * 16;
-  uint8_t* o = reinterpret_cast<uint8_t*>(g.out) + (long)(row - lane + r) * g.ldo + col0 + c;
-#pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    if (row - lane + r + 4 * p < g.M && c < valid)
-      store_bytes16(o, reinterpret_cast<const uint4*>(buf + (4 * p + r) * F8P_LD)[lane & 7], valid - c);
-    o += 4 * g.ldo;
-  }
-  __syncwarp();  // the tile may be overwritten
 }
 
 }  // namespace
@@ -585,7 +525,8 @@ BAG_DEV void encode_block(const Fp8Gemm& g, int row, int col0, float* v, float* 
 template <int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
-                         const __grid_constant__ Fp8Gemm g, int group_rows) {
+                         const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ Fp8Gemm g,
+                         int group_rows) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -593,7 +534,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   uint64_t* empty = full + F8P_STAGES;
   uint64_t* sf_full = empty + F8P_STAGES;
   uint64_t* sf_empty = sf_full + 2;
-  uint64_t* tfull = sf_empty + 2;
+  uint64_t* sf_used = sf_empty + 2;    // [2], even CTA: a group's products are done, its TMEM columns free
+  uint64_t* tfull = sf_used + 2;
   uint64_t* tempty = tfull + 2;
   uint64_t* shared_free = tempty + 2;  // [2]: accumulator b's columns that the other one shares are drained
   uint64_t* drain = shared_free + 2;
@@ -605,7 +547,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
   const long tiles = (long)num_m * num_n;
-  const int nkb = (g.K + F8_BK - 1) / F8_BK, ng = (nkb + F8_GROUP - 1) / F8_GROUP;
+  const int nkb = (g.K + F8_BK - 1) / F8_BK, nruns = (nkb + F8_GROUP * F8_RUN - 1) / (F8_GROUP * F8_RUN);
   // groups of group_rows row tiles visit every column tile, the row tile varying fastest
   auto decode = [&](long tile, int& mt, int& nt) {
     const long per = (long)group_rows * num_n;
@@ -623,6 +565,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     for (int s = 0; s < 2; ++s) {
       mbar_init(sf_full + s, 2);       // even CTA: both CTAs' scale warps
       mbar_init(sf_empty + s, 1);      // both CTAs: multicast commit
+      mbar_init(sf_used + s, 1);
       mbar_init(tfull + s, 1);         // both CTAs: multicast commit
       mbar_init(tempty + s, 16);       // even CTA: every epilogue warp of both CTAs
       mbar_init(shared_free + s, 8);   // even CTA: the warps that hold the shared columns
@@ -690,9 +633,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
       if (rank == 0) {
         // -------- MMA issuer (even CTA; converged warp, one elected lane issues) --------
         const uint32_t base = smem_u32(smem);
-        int s = 0, ss = 0;
-        uint32_t ph = 0, sph = 0;
-        long i = 0;  // tiles of this pair so far
+        int s = 0;
+        uint32_t ph = 0;
+        uint32_t run = 0, grp = 0;  // runs and groups of scales handled so far
+        long i = 0;                 // tiles of this pair so far
         bool ok = true;
         for (long tile = pair; tile < tiles && ok; tile += npairs, ++i) {
           const int acc = (int)(i & 1);
@@ -702,11 +646,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
           if (i > 0 && !mbar_wait_warp(shared_free + (acc ^ 1), (uint32_t)(((i - 1) >> 1) & 1), abort_flag)) break;
           tc_fence_after();
           for (int kb = 0; kb < nkb; ++kb) {
-            const uint32_t sa = tmem + F8P_SF_COL + ss * F8P_SF_COLS;
+            if (kb % (F8_GROUP * F8_RUN) == 0) {
+              if (!(ok = wait_warp_cluster(sf_full + (run & 1), (run >> 1) & 1u, abort_flag))) break;
+              ++run;
+            }
+            const uint32_t sa = tmem + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
             if (kb % F8_GROUP == 0) {
-              if (!(ok = wait_warp_cluster(sf_full + ss, sph, abort_flag))) break;
+              if (!(ok = mbar_wait_warp(sf_used + (grp & 1), ((grp >> 1) & 1u) ^ 1u, abort_flag))) break;
               tc_fence_after();
-              const uint64_t d = scale_desc(base + F8P_OFF_SF + ss * 3 * F8_ATOM);
+              const uint64_t d = scale_desc(base + F8P_OFF_SF + ((run - 1) & 1) * F8P_SF_STAGE +
+                                            kb / F8_GROUP % F8_RUN * F8P_SF_GROUP);
               if (elect_one()) {
 #pragma unroll
                 for (int a = 0; a < 3; ++a) copy_scales_pair(sa + 4 * a, d + a * (F8_ATOM >> 4));
@@ -719,19 +668,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
             const uint64_t wd = sw128_desc(base + s * F8P_STAGE + F8_TILE);
             const uint32_t idesc = idesc_mxf8(256, 256) | scale_byte((uint32_t)(kb % F8_GROUP));
             const bool last = kb + 1 == nkb || (kb + 1) % F8_GROUP == 0;
+            const bool last_run = kb + 1 == nkb || (kb + 1) % (F8_GROUP * F8_RUN) == 0;
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
                 pair_mma_mxf8(dt, ad + 2 * k, wd + 2 * k, idesc, sa, sa + 4, (kb | k) != 0 ? 1u : 0u);
               pair_commit(empty + s, 3);
-              if (last) pair_commit(sf_empty + ss, 3);
+              if (last) pair_commit(sf_used + (grp & 1), 1);
+              if (last_run) pair_commit(sf_empty + ((run - 1) & 1), 3);
             }
             __syncwarp();
             if (++s == F8P_STAGES) {
               s = 0;
               ph ^= 1;
             }
-            if (last && (ss ^= 1) == 0) sph ^= 1;
+            grp += last;
           }
           if (!ok) break;
           if (elect_one()) pair_commit(tfull + acc, 3);
@@ -748,92 +699,169 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
       }
     } else if (warp == 2) {
       // ---------------- scale words (both CTAs: A's own rows, all 256 of W) ----------------
-      int ss = 0, mt = 0, nt = 0, gi = 0;
-      uint32_t sph = 0;
+      int mt = 0, nt = 0, r = 0;
       const uint32_t full_even = mapa_shared(smem_u32(sf_full), 0);
-      uint4 w[3];
+      const bool wide_a = wide_scales(g.a_s, g.ldas), wide_w = wide_scales(g.w_s, g.ldws);
+      ScaleRun w[3];
       auto fetch = [&]() {
-        w[0] = scale_words(g.a_s, g.ldas, mt * 256 + (int)rank * 128, g.M, gi);
-        w[1] = scale_words(g.w_s, g.ldws, nt * 256, g.N, gi);
-        w[2] = scale_words(g.w_s, g.ldws, nt * 256 + 128, g.N, gi);
+        w[0].fetch(g.a_s, g.ldas, wide_a, mt * 256 + (int)rank * 128, g.M, r);
+        w[1].fetch(g.w_s, g.ldws, wide_w, nt * 256, g.N, r);
+        w[2].fetch(g.w_s, g.ldws, wide_w, nt * 256 + 128, g.N, r);
       };
       long tile = pair;
       if (tile < tiles) {
         decode(tile, mt, nt);
         fetch();
       }
-      while (tile < tiles) {
-        if (!mbar_wait_warp(sf_empty + ss, sph ^ 1, abort_flag)) break;
-        uint4* d = reinterpret_cast<uint4*>(smem + F8P_OFF_SF + ss * 3 * F8_ATOM);
+      for (uint32_t i = 0; tile < tiles; ++i) {
+        if (!mbar_wait_warp(sf_empty + (i & 1), ((i >> 1) & 1u) ^ 1u, abort_flag)) break;
+        uint8_t* d = smem + F8P_OFF_SF + (i & 1) * F8P_SF_STAGE;
 #pragma unroll
-        for (int a = 0; a < 3; ++a) d[a * 32 + lane] = w[a];
+        for (int a = 0; a < 3; ++a) w[a].put(d + a * F8_ATOM, F8P_SF_GROUP);
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) peer_arrive(full_even + (uint32_t)(ss * sizeof(uint64_t)));
-        if (++gi == ng) {
-          gi = 0;
+        if (lane == 0) peer_arrive(full_even + (uint32_t)((i & 1) * sizeof(uint64_t)));
+        if (++r == nruns) {
+          r = 0;
           tile += npairs;
           if (tile < tiles) decode(tile, mt, nt);
         }
         if (tile < tiles) fetch();
-        if ((ss ^= 1) == 0) sph ^= 1;
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F8P_REGS_EPI));
     // ---------------- epilogue (both CTAs: their 128 rows of each tile) ----------------
     const int q = warp & 3, half = (warp - 4) >> 2;
-    float* buf = reinterpret_cast<float*>(smem + F8P_OFF_EPI) + (warp - 4) * 32 * F8P_LD;
+    uint8_t* buf = smem + F8P_OFF_BUF + (warp - 4) * F8P_BUF;
+    float* sbias = reinterpret_cast<float*>(smem + F8P_OFF_VEC) + (warp - 4) * 256;
+    float* sgate = sbias + 128;
     const uint32_t tempty_even = mapa_shared(smem_u32(tempty), 0), free_even = mapa_shared(smem_u32(shared_free), 0);
+    constexpr int CW = KIND == BAG_FP8_BF16 ? 64 : (KIND == BAG_FP8_CODES ? 128 : 32);  // columns of a staged row
+    constexpr int NC = 128 / CW;
     long i = 0;
     for (long tile = pair; tile < tiles; tile += npairs, ++i) {
       const int acc = (int)(i & 1);
       int mt, nt;
       decode(tile, mt, nt);
+      const int row0 = mt * 256 + (int)rank * 128 + q * 32, col0 = nt * 256 + half * 128;
+      {
+        float b[4], t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = col0 + lane * 4 + j;
+          b[j] = g.bias && c < g.N ? __ldg(g.bias + c) : 0.f;
+          t[j] = KIND == BAG_FP8_RESID && g.gate && c < g.N ? __ldg(g.gate + c) : 1.f;
+        }
+        reinterpret_cast<float4*>(sbias)[lane] = make_float4(b[0], b[1], b[2], b[3]);
+        if (KIND == BAG_FP8_RESID) reinterpret_cast<float4*>(sgate)[lane] = make_float4(t[0], t[1], t[2], t[3]);
+        __syncwarp();
+      }
       const bool ok = mbar_wait(tfull + acc, (uint32_t)((i >> 1) & 1), abort_flag);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
-      const int row = mt * 256 + (int)rank * 128 + q * 32 + lane, col0 = nt * 256 + half * 128;
       const uint32_t tb = tmem + (uint32_t)((acc ? F8P_ACC1 : 0) + half * 128) + ((uint32_t)(q * 32) << 16);
       // the shared columns are the last 32 of accumulator 0 and the first 32 of accumulator 1
       const bool shares = half == (acc ^ 1);
-      const int first = acc ? 0 : 3;
-      auto release_shared = [&]() {
+      auto release = [&](uint32_t bar) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) peer_arrive(free_even + (uint32_t)(acc * sizeof(uint64_t)));
+        if (lane == 0) peer_arrive(bar + (uint32_t)(acc * sizeof(uint64_t)));
       };
-      auto release = [&]() {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) peer_arrive(tempty_even + (uint32_t)(acc * sizeof(uint64_t)));
-      };
-      if constexpr (KIND == BAG_FP8_CODES) {
-        float v[128];
-        if (shares && first == 3) {
-          tmem_ld32(tb + 96, v + 96);
-          release_shared();
-        }
-        tmem_ld32(tb, v);
-        if (shares && first == 0) release_shared();
-        tmem_ld32(tb + 32, v + 32);
-        tmem_ld32(tb + 64, v + 64);
-        if (!(shares && first == 3)) tmem_ld32(tb + 96, v + 96);
-        release();
-        encode_block(g, row, col0, v, buf);
-      } else {
 #pragma unroll 1
-        for (int k = 0; k < 4; ++k) {
-          const int c = ((k + first) & 3) * 32;
-          float v[32];
-          tmem_ld32(tb + (uint32_t)c, v);
-          if (k == 0 && shares) release_shared();
-          if (k == 3) release();
-          store_chunk<KIND>(g, row - lane, col0 + c, v, buf);
+      for (int k = 0; k < NC; ++k) {
+        const int c = (acc ? k : NC - 1 - k) * CW;  // the shared columns' part first
+        float v[CW];
+        // whole 32-column loads, the shared columns' first
+        if (!acc) tmem_ld32(tb + (uint32_t)(c + CW - 32), v + CW - 32);
+        if (acc) tmem_ld32(tb + (uint32_t)c, v);
+        if (k == 0 && shares) release(free_even);
+#pragma unroll
+        for (int j = 0; j < CW; j += 32) {
+          if (j > 0 && j < CW - 32) tmem_ld32(tb + (uint32_t)(c + j), v + j);
+        }
+        if (CW > 32) {
+          if (acc)
+            tmem_ld32(tb + (uint32_t)(c + CW - 32), v + CW - 32);
+          else
+            tmem_ld32(tb + (uint32_t)c, v);
+        }
+        if (k == NC - 1) release(tempty_even);
+        if (g.bias) {
+#pragma unroll
+          for (int j = 0; j < CW; j += 32) with_vector(sbias + c + j, v + j, [](float x, float y) { return x + y; });
+        }
+        if (g.act) {
+#pragma unroll
+          for (int j = 0; j < CW; ++j) v[j] = gelu_sigmoid(v[j]);
+        }
+        if (KIND == BAG_FP8_RESID) with_vector(sgate + c, v, [](float x, float y) { return x * y; });
+        // the staged tile's last store has read it
+        if (lane == 0) bulk_wait_read();
+        __syncwarp();
+        if constexpr (KIND == BAG_FP8_CODES) {
+          const int valid = g.N - col0;
+          uint32_t m[4] = {0u, 0u, 0u, 0u};
+          if (valid >= 128) {
+#pragma unroll
+            for (int j = 0; j < 128; ++j) m[j & 3] = max(m[j & 3], abs_bits(v[j]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 128; ++j) m[j & 3] = max(m[j & 3], j < valid ? abs_bits(v[j]) : 0u);
+          }
+          const uint32_t b = e8m0_of(max(max(m[0], m[1]), max(m[2], m[3])));
+          const float inv = e8m0_inverse(b);
+          if (valid > 0 && row0 + lane < g.M) g.out_s[(long)(row0 + lane) * g.ldos + col0 / kScaleBlock] = (uint8_t)b;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float* x = v + 16 * u + 4 * e;
+              w[e] = pack_e4m3x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+            }
+            staged(buf, u) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else if constexpr (KIND == BAG_FP8_BF16) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float* x = v + 8 * u;
+            staged(buf, u) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                        pack_bf16x2(x[6], x[7]));
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            staged(buf, u) = make_uint4(__float_as_uint(v[4 * u]), __float_as_uint(v[4 * u + 1]),
+                                        __float_as_uint(v[4 * u + 2]), __float_as_uint(v[4 * u + 3]));
+        }
+        // TMA writes whole 16-byte units, also where the tensor ends inside one: the last columns
+        // go the other way
+        if (g.vec && col0 + c + CW <= g.N) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && row0 < g.M) {
+            if (KIND == BAG_FP8_RESID)
+              tma_add_2d(&tmOut, buf, col0 + c, row0);
+            else
+              tma_store_2d(&tmOut, buf, col0 + c, row0);
+            bulk_commit();
+          }
+        } else {
+          __syncwarp();
+          if constexpr (KIND == BAG_FP8_CODES)
+            store_rows<uint8_t, false>(g, buf, row0, col0 + c);
+          else if constexpr (KIND == BAG_FP8_BF16)
+            store_rows<__nv_bfloat16, false>(g, buf, row0, col0 + c);
+          else
+            store_rows<float, KIND == BAG_FP8_RESID>(g, buf, row0, col0 + c);
           __syncwarp();
         }
+        __syncwarp();
       }
     }
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
   }
   tc_fence_before();
   __syncwarp();
@@ -847,16 +875,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
 
 static cudaError_t launch_pair(Fp8Gemm g, cudaStream_t s) {
   CUtensorMap ta, tw;
-  if (encode_tmap_2d_u8(&ta, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, 128) ||
-      encode_tmap_2d_u8(&tw, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128))
+  if (encode_tmap_2d_bytes(&ta, 1, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, 128) ||
+      encode_tmap_2d_bytes(&tw, 1, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128))
     return cudaErrorInvalidValue;
-  const int size = g.kind == BAG_FP8_BF16 ? 2 : 4;
+  // the output map: boxes of 32 rows of 128 bytes; rows that TMA cannot address are stored otherwise
+  CUtensorMap to = ta;
+  const int size = g.kind == BAG_FP8_CODES ? 1 : (g.kind == BAG_FP8_BF16 ? 2 : 4);
   g.vec = ((reinterpret_cast<uintptr_t>(g.out) | (uintptr_t)(g.ldo * size)) & 15) == 0;
+  if (g.vec && encode_tmap_2d_bytes(&to, size, g.out, (uint64_t)g.N, (uint64_t)g.M, (uint64_t)(g.ldo * size),
+                                    128u / (unsigned)size, 32))
+    return cudaErrorInvalidValue;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
   const int pairs = (int)std::min((long)num_m * num_n, (long)sm_count() / 2);
   const int rows = (int)std::max(1.0, std::min((double)num_m, 40.0 * 1048576.0 / (256.0 * g.K)));
   auto launch = [&](auto kernel) {
-    return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, g, rows);
+    return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, to, g, rows);
   };
   switch (g.kind) {
     case BAG_FP8_F32: return launch(gemm_fp8_pair_kernel<BAG_FP8_F32>);

@@ -201,6 +201,56 @@ def g_first(M, N, K):
     return g.integers(121, 134, (M, -(-K // 128))).astype(np.uint8)[0, 0]
 
 
+@pytest.mark.parametrize("M,N,K", [(2500, 2304, 640), (2433, 2309, 1040), (2305, 2050, 127), (4700, 1156, 2176),
+                                   (130, 19500, 384), (19500, 136, 4224), (5000, 2500, 13824)])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "fp8", "resid"])
+@pytest.mark.parametrize("aligned", [True, False])
+def test_gemm_fp8_of_many_tiles(M, N, K, kind, aligned, ctx):
+    """Enough 256 x 256 tiles for a CTA pair each and more, ragged in M, N and K, one to seven runs of
+    scale words, scale rows of whole 16-byte units and not, output rows that TMA can address and rows
+    that it cannot.  Bounds as in test_gemm_fp8."""
+    if kind == "fp8" and not aligned:
+        pytest.skip("code rows are always aligned")
+    g = rng(M, N, K)
+    a, a_s, A = operand(g, M, K)
+    w, w_s, W = operand(g, N, K)
+    if aligned:  # 16-byte scale rows
+        nb = -(-K // 128)
+        t = torch.full((M, R.up(nb, 16)), 255, device=DEV, dtype=torch.uint8)
+        t[:, :nb], a_s = a_s[:, :nb], t
+    bias, gate = (dev(g.standard_normal(N).astype(np.float32)) for _ in range(2))
+    y = A @ W.T + bias.double()
+    eps = 4 * K * 2.0 ** -24 * (A.abs() @ W.abs().T + bias.double().abs())
+    if kind == "fp8":
+        c, s = encoded(M, N)
+        ctx.gemm_fp8(a, a_s, w, w_s, c[1:M + 1], K, bias=bias, out_scales=s[1:M + 1])
+        nb = -(-N // 128)
+        codes, sc = c[1:M + 1, :N].contiguous(), s[1:M + 1, :nb].double()
+        step = torch.exp2(sc - 127).repeat_interleave(128, 1)[:, :N]
+        got = codes.view(torch.float8_e4m3fn).double() * step
+        assert bool(((got - y).abs() <= 2.0 ** -4 * y.abs() + 2.0 ** -10 * step + 1.1 * eps).all())
+        top = torch.nn.functional.pad(y.abs(), (0, nb * 128 - N)).view(M, nb, 128).amax(2)
+        more = torch.nn.functional.pad(eps, (0, nb * 128 - N)).view(M, nb, 128).amax(2)
+        assert bool((top <= 448 * step[:, ::128] + more).all() and (top >= 224 * step[:, ::128] - more).all())
+        untouched(c, s, M, N)
+        return
+    width = R.up(N, 8) + 8 if aligned else R.up(N, 8) + 1
+    out = torch.full((M + 2, width), 7.0, device=DEV, dtype=torch.bfloat16 if kind == "bf16" else torch.float32)
+    o = out[1:M + 1, :N]
+    if kind == "resid":
+        h = dev(g.standard_normal((M, N)).astype(np.float32))
+        o.copy_(h)
+        ctx.gemm_fp8(a, a_s, w, w_s, o, K, bias=bias, gate=gate, residual=True)
+        ref = h.double() + gate.double() * y
+        eps = eps * gate.double().abs() + 2.0 ** -22 * (ref.abs() + h.double().abs())
+    else:
+        ctx.gemm_fp8(a, a_s, w, w_s, o, K, bias=bias)
+        ref, eps = y, eps + 2.0 ** (-8 if kind == "bf16" else -22) * y.abs()
+    assert bool(((o.double() - ref).abs() <= eps).all()), float(((o.double() - ref).abs() / eps).max())
+    out[1:M + 1, :N] = 7.0
+    assert bool((out == 7.0).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 300, 640), (600, 1024, 512), (3000, 2048, 640)])
 def test_gemm_fp8_without_bias_or_gate(M, N, K, ctx):
     g = rng(M, N)
