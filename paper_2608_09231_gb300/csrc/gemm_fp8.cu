@@ -349,7 +349,11 @@ __global__ void __launch_bounds__(256)
       for (int j = 0; j < 16; ++j) y[j] += bias;
       if (g.act) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = gelu_sigmoid(y[j]);
+        for (int j = 0; j < 16; j += 2) {
+          const float2 t = gelu2(make_float2(y[j], y[j + 1]));
+          y[j] = t.x;
+          y[j + 1] = t.y;
+        }
       }
       const long m = m0 + rank + ((long)j0 << logS);  // of y[0]; the others S rows apart
       const long at = m * g.ldo + n, step = g.ldo << logS;
@@ -476,16 +480,18 @@ BAG_DEV void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "mem
 BAG_DEV void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 BAG_DEV void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
-// Column-wise vectors: entry j of 32 columns to v (16-byte broadcasts from shared memory).
+// f(v[j], s[j]) of 32 columns, two at a time (16-byte broadcasts from shared memory).
 template <typename F>
 BAG_DEV void with_vector(const float* s, float* v, F f) {
 #pragma unroll
   for (int j = 0; j < 32; j += 4) {
     const float4 b = *reinterpret_cast<const float4*>(s + j);
-    v[j] = f(v[j], b.x);
-    v[j + 1] = f(v[j + 1], b.y);
-    v[j + 2] = f(v[j + 2], b.z);
-    v[j + 3] = f(v[j + 3], b.w);
+    const float2 x = f(make_float2(v[j], v[j + 1]), make_float2(b.x, b.y));
+    const float2 y = f(make_float2(v[j + 2], v[j + 3]), make_float2(b.z, b.w));
+    v[j] = x.x;
+    v[j + 1] = x.y;
+    v[j + 2] = y.x;
+    v[j + 3] = y.y;
   }
 }
 
@@ -645,44 +651,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
           if (!mbar_wait_warp(tempty + acc, (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag)) break;
           if (i > 0 && !mbar_wait_warp(shared_free + (acc ^ 1), (uint32_t)(((i - 1) >> 1) & 1), abort_flag)) break;
           tc_fence_after();
-          for (int kb = 0; kb < nkb; ++kb) {
-            if (kb % (F8_GROUP * F8_RUN) == 0) {
+          uint32_t add = 0;  // the tile's first product overwrites the accumulator
+          for (int kb0 = 0; kb0 < nkb && ok; kb0 += F8_GROUP) {
+            if (kb0 % (F8_GROUP * F8_RUN) == 0) {
               if (!(ok = wait_warp_cluster(sf_full + (run & 1), (run >> 1) & 1u, abort_flag))) break;
               ++run;
             }
             const uint32_t sa = tmem + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
-            if (kb % F8_GROUP == 0) {
-              if (!(ok = mbar_wait_warp(sf_used + (grp & 1), ((grp >> 1) & 1u) ^ 1u, abort_flag))) break;
-              tc_fence_after();
-              const uint64_t d = scale_desc(base + F8P_OFF_SF + ((run - 1) & 1) * F8P_SF_STAGE +
-                                            kb / F8_GROUP % F8_RUN * F8P_SF_GROUP);
-              if (elect_one()) {
-#pragma unroll
-                for (int a = 0; a < 3; ++a) copy_scales_pair(sa + 4 * a, d + a * (F8_ATOM >> 4));
-              }
-              __syncwarp();
-            }
-            if (!(ok = mbar_wait_warp(full + s, ph, abort_flag))) break;
+            if (!(ok = mbar_wait_warp(sf_used + (grp & 1), ((grp >> 1) & 1u) ^ 1u, abort_flag))) break;
             tc_fence_after();
-            const uint64_t ad = sw128_desc(base + s * F8P_STAGE);
-            const uint64_t wd = sw128_desc(base + s * F8P_STAGE + F8_TILE);
-            const uint32_t idesc = idesc_mxf8(256, 256) | scale_byte((uint32_t)(kb % F8_GROUP));
-            const bool last = kb + 1 == nkb || (kb + 1) % F8_GROUP == 0;
-            const bool last_run = kb + 1 == nkb || (kb + 1) % (F8_GROUP * F8_RUN) == 0;
+            const uint64_t d = scale_desc(base + F8P_OFF_SF + ((run - 1) & 1) * F8P_SF_STAGE +
+                                          kb0 / F8_GROUP % F8_RUN * F8P_SF_GROUP);
             if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
-                pair_mma_mxf8(dt, ad + 2 * k, wd + 2 * k, idesc, sa, sa + 4, (kb | k) != 0 ? 1u : 0u);
-              pair_commit(empty + s, 3);
-              if (last) pair_commit(sf_used + (grp & 1), 1);
-              if (last_run) pair_commit(sf_empty + ((run - 1) & 1), 3);
+              for (int a = 0; a < 3; ++a) copy_scales_pair(sa + 4 * a, d + a * (F8_ATOM >> 4));
             }
             __syncwarp();
-            if (++s == F8P_STAGES) {
-              s = 0;
-              ph ^= 1;
+#pragma unroll
+            for (int b = 0; b < F8_GROUP; ++b) {
+              if (kb0 + b >= nkb) break;
+              if (!(ok = mbar_wait_warp(full + s, ph, abort_flag))) break;
+              tc_fence_after();
+              const uint64_t ad = sw128_desc(base + s * F8P_STAGE);
+              const uint64_t wd = ad + (F8_TILE >> 4);
+              if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
+                  pair_mma_mxf8(dt, ad + 2 * k, wd + 2 * k, idesc_mxf8(256, 256) | scale_byte(b), sa, sa + 4,
+                                k > 0 ? 1u : add);
+                pair_commit(empty + s, 3);
+              }
+              __syncwarp();
+              add = 1;
+              if (++s == F8P_STAGES) {
+                s = 0;
+                ph ^= 1;
+              }
             }
-            grp += last;
+            if (elect_one()) {
+              pair_commit(sf_used + (grp & 1), 1);
+              if (kb0 + F8_GROUP >= nkb || (kb0 / F8_GROUP + 1) % F8_RUN == 0) pair_commit(sf_empty + ((run - 1) & 1), 3);
+            }
+            __syncwarp();
+            ++grp;
           }
           if (!ok) break;
           if (elect_one()) pair_commit(tfull + acc, 3);
@@ -766,7 +777,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
       auto release = [&](uint32_t bar) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) peer_arrive(bar + (uint32_t)(acc * sizeof(uint64_t)));
+        if (lane == 0) peer_signal(bar + (uint32_t)(acc * sizeof(uint64_t)));
       };
 #pragma unroll 1
       for (int k = 0; k < NC; ++k) {
@@ -789,27 +800,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
         if (k == NC - 1) release(tempty_even);
         if (g.bias) {
 #pragma unroll
-          for (int j = 0; j < CW; j += 32) with_vector(sbias + c + j, v + j, [](float x, float y) { return x + y; });
+          for (int j = 0; j < CW; j += 32) with_vector(sbias + c + j, v + j, sum2);
         }
         if (g.act) {
 #pragma unroll
-          for (int j = 0; j < CW; ++j) v[j] = gelu_sigmoid(v[j]);
+          for (int j = 0; j < CW; j += 2) {
+            const float2 t = gelu2(make_float2(v[j], v[j + 1]));
+            v[j] = t.x;
+            v[j + 1] = t.y;
+          }
         }
-        if (KIND == BAG_FP8_RESID) with_vector(sgate + c, v, [](float x, float y) { return x * y; });
+        if (KIND == BAG_FP8_RESID) with_vector(sgate + c, v, mul2);
         // the staged tile's last store has read it
         if (lane == 0) bulk_wait_read();
         __syncwarp();
         if constexpr (KIND == BAG_FP8_CODES) {
           const int valid = g.N - col0;
-          uint32_t m[4] = {0u, 0u, 0u, 0u};
-          if (valid >= 128) {
+          float m[4] = {0.f, 0.f, 0.f, 0.f};
+          if (valid < 128) {  // columns past the end count as zeros
 #pragma unroll
-            for (int j = 0; j < 128; ++j) m[j & 3] = max(m[j & 3], abs_bits(v[j]));
-          } else {
-#pragma unroll
-            for (int j = 0; j < 128; ++j) m[j & 3] = max(m[j & 3], j < valid ? abs_bits(v[j]) : 0u);
+            for (int j = 0; j < 128; ++j) v[j] = j < valid ? v[j] : 0.f;
           }
-          const uint32_t b = e8m0_of(max(max(m[0], m[1]), max(m[2], m[3])));
+#pragma unroll
+          for (int j = 0; j < 128; j += 2) m[(j >> 1) & 3] = max3_abs(m[(j >> 1) & 3], v[j], v[j + 1]);
+          const uint32_t b = e8m0_of(abs_bits(max3_abs(max3_abs(m[0], m[1], m[2]), m[3], 0.f)));
           const float inv = e8m0_inverse(b);
           if (valid > 0 && row0 + lane < g.M) g.out_s[(long)(row0 + lane) * g.ldos + col0 / kScaleBlock] = (uint8_t)b;
 #pragma unroll
@@ -818,7 +832,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float* x = v + 16 * u + 4 * e;
-              w[e] = pack_e4m3x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+              const float2 lo = mul2(make_float2(x[0], x[1]), make_float2(inv, inv));
+              const float2 hi = mul2(make_float2(x[2], x[3]), make_float2(inv, inv));
+              w[e] = pack_e4m3x4(lo.x, lo.y, hi.x, hi.y);
             }
             staged(buf, u) = make_uint4(w[0], w[1], w[2], w[3]);
           }

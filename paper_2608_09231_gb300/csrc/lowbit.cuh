@@ -58,12 +58,52 @@ BAG_DEV void store_bytes(uint8_t* p, uint32_t v, int n) {
   }
 }
 
-// GELU (tanh form): y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3), the same function as
-// 0.5 y (1 + tanh u).  exp2 and the reciprocal of the special-function unit: relative error about
-// 2^-20, below every rounding that follows and below fp32's own at the sums this is applied to.
-BAG_DEV float gelu_sigmoid(float y) {
-  const float k = -2.0f * 0.7978845608028654f;
-  return __fdividef(y, 1.0f + __expf(k * (y + 0.044715f * y * y * y)));
+// Two fp32 operations in one instruction.
+BAG_DEV float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+BAG_DEV float2 sum2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+BAG_DEV float2 muladd2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
+// GELU (tanh form) of two values: y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3), the same
+// function as 0.5 y (1 + tanh u).  exp2 and the reciprocal of the special-function unit: relative
+// error about 2^-20, below every rounding that follows and below fp32's own at the sums this is
+// applied to.  (A power that overflows gives 1 / inf = 0.)
+BAG_DEV float2 gelu2(float2 y) {
+  const float k = -2.0f * 0.7978845608028654f * 1.4426950408889634f;  // exp(-2u) = 2^(y (k + k' y^2))
+  float2 e = mul2(y, muladd2(mul2(y, y), make_float2(k * 0.044715f, k * 0.044715f), make_float2(k, k)));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+  e = sum2(e, make_float2(1.f, 1.f));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+  return mul2(y, e);
+}
+
+// Largest magnitude of three values (a NaN if there is one).
+BAG_DEV float max3_abs(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 }  // namespace bag
