@@ -330,9 +330,9 @@ bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows
 
 /* ---- 8-bit operands with a scale for each block of 128 ----
  *
- * The operations from here to bag_attention_blocks use nothing of the context but its stream and
- * error text: they run on the caller's stream itself (in order with the context's other calls,
- * also across bag_set_stream), never synchronise, and may be captured into a CUDA graph.
+ * The operations from here to bag_attention_blocks use nothing of the context but its error text:
+ * they are kernels on the caller's stream itself (the one of bag_set_stream), ordered like any
+ * other work that the caller puts there, never synchronise, and may be captured into a CUDA graph.
  *
  * An encoded matrix [rows, cols] is two device buffers: codes, one float8 e4m3 byte an element
  * (row stride ldc bytes), and scales, one byte b for each row and block of 128 consecutive

@@ -104,8 +104,6 @@ struct bag_ctx {
   cudaStream_t stream = nullptr;       // internal stream: all work and graph capture
   cudaStream_t user_stream = nullptr;  // caller's stream (bag_set_stream), bridged by events
   cudaEvent_t ev_in = nullptr, ev_out = nullptr;
-  cudaEvent_t ev_op = nullptr;        // after the last operation that ran on user_stream itself
-  bool stream_changed = false;        // since the last call
   std::string err;
 
   // weights
@@ -1588,8 +1586,6 @@ static bag_status reset_state(bag_ctx* ctx) {
 // Order the internal stream after the caller's stream, and the caller's stream after
 // the work just enqueued.
 static bag_status enter(bag_ctx* ctx) {
-  if (ctx->stream_changed) CK(cudaStreamWaitEvent(ctx->stream, ctx->ev_op, 0));
-  ctx->stream_changed = false;
   CK(cudaEventRecord(ctx->ev_in, ctx->user_stream));
   CK(cudaStreamWaitEvent(ctx->stream, ctx->ev_in, 0));
   return BAG_OK;
@@ -1600,25 +1596,15 @@ static bag_status leave(bag_ctx* ctx, bag_status s) {
   return s;
 }
 
-// Operations that use nothing of the context run on the caller's stream itself, which spares
-// them the bridge (four event calls, and two cross-stream waits on the device: together about
-// half of a small call).  The order of a context's calls holds all the same when the caller
-// changes streams: the first call on another stream waits for the last one before it.  Inside a
-// stream capture no event of the context is waited for or recorded, so that these calls can be
-// captured; the capture is ordered by whoever launches its graph.
-static bool capturing(bag_ctx* ctx) {
-  cudaStreamCaptureStatus c = cudaStreamCaptureStatusNone;
-  return cudaStreamIsCapturing(ctx->user_stream, &c) != cudaSuccess || c != cudaStreamCaptureStatusNone;
-}
-static bag_status enter_op(bag_ctx* ctx) {
-  if (!ctx->stream_changed || capturing(ctx)) return BAG_OK;
-  CK(cudaStreamWaitEvent(ctx->user_stream, ctx->ev_out, 0));
-  CK(cudaStreamWaitEvent(ctx->user_stream, ctx->ev_op, 0));
-  ctx->stream_changed = false;
-  return BAG_OK;
-}
-static bag_status leave_op(bag_ctx* ctx, bag_status s) {
-  if (!capturing(ctx)) cudaEventRecord(ctx->ev_op, ctx->user_stream);
+// Operations that use nothing of the context run on the caller's stream itself, which spares them
+// the bridge's event calls and lets them be captured.  Their kernels are launched with programmatic
+// stream serialization (unless BAG_PDL=0): all of them wait for the kernel before (grid_dep_sync)
+// ahead of their first access to global memory, so a chain of them overlaps launches with ends.
+struct OpScope {
+  explicit OpScope(bag_ctx* ctx) { g_pdl = ctx->pdl; }
+  ~OpScope() { g_pdl = false; }
+};
+static bag_status leave_op(bag_status s) {
   if (s == BAG_ECUDA) cudaGetLastError();  // reported: off the thread, or the next check reports it again
   return s;
 }
@@ -2061,8 +2047,7 @@ bag_status bag_create(const bag_arch* arch, int T, int B, bag_ctx** out) {
   bag_status s = BAG_OK;
   if (cudaStreamCreateWithFlags(&ctx->stream, cudaStreamNonBlocking) != cudaSuccess ||
       cudaEventCreateWithFlags(&ctx->ev_in, cudaEventDisableTiming) != cudaSuccess ||
-      cudaEventCreateWithFlags(&ctx->ev_out, cudaEventDisableTiming) != cudaSuccess ||
-      cudaEventCreateWithFlags(&ctx->ev_op, cudaEventDisableTiming) != cudaSuccess)
+      cudaEventCreateWithFlags(&ctx->ev_out, cudaEventDisableTiming) != cudaSuccess)
     s = fail(ctx, BAG_ECUDA, "stream/event creation failed");
   if (s == BAG_OK && kernels_init() != cudaSuccess) s = fail(ctx, BAG_ECUDA, "kernel attribute setup failed");
   if (s == BAG_OK) s = alloc_weights(ctx);
@@ -2088,7 +2073,6 @@ void bag_destroy(bag_ctx* ctx) {
   if (ctx->aarena) cudaFree(ctx->aarena);
   if (ctx->ev_in) cudaEventDestroy(ctx->ev_in);
   if (ctx->ev_out) cudaEventDestroy(ctx->ev_out);
-  if (ctx->ev_op) cudaEventDestroy(ctx->ev_op);
   for (auto ev : ctx->ev_pool) cudaEventDestroy(ev);
   if (ctx->stream) cudaStreamDestroy(ctx->stream);
   delete ctx;
@@ -2098,7 +2082,6 @@ const char* bag_last_error(bag_ctx* ctx) { return ctx ? ctx->err.c_str() : g_cre
 
 bag_status bag_set_stream(bag_ctx* ctx, void* stream) {
   if (!ctx) return BAG_EINVAL;
-  if (ctx->user_stream != (cudaStream_t)stream) ctx->stream_changed = true;
   ctx->user_stream = (cudaStream_t)stream;
   return BAG_OK;
 }
@@ -2302,23 +2285,23 @@ bag_status bag_residual_add(bag_ctx* ctx, float* out, const float* h_in, const f
 bag_status bag_quant_fp8(bag_ctx* ctx, const void* x, int dtype, long ldx, long rows, long cols, void* codes, long
                          ldc, void* scales, long lds) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_quant_fp8_impl(ctx, x, dtype, ldx, rows, cols, codes, ldc, scales, lds));
+  const OpScope scope(ctx);
+  return leave_op(bag_quant_fp8_impl(ctx, x, dtype, ldx, rows, cols, codes, ldc, scales, lds));
 }
 
 bag_status bag_ln_mod_fp8(bag_ctx* ctx, const float* x, long ldx, const float* shift, const float* scale, long rows,
                           long cols, void* codes, long ldc, void* scales, long lds) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_ln_mod_fp8_impl(ctx, x, ldx, shift, scale, rows, cols, codes, ldc, scales, lds));
+  const OpScope scope(ctx);
+  return leave_op(bag_ln_mod_fp8_impl(ctx, x, ldx, shift, scale, rows, cols, codes, ldc, scales, lds));
 }
 
 bag_status bag_gemm_fp8(bag_ctx* ctx, const void* a, long lda, const void* a_s, long ldas, const void* w, long ldw,
                         const void* w_s, long ldws, const float* bias, long M, long N, long K, int act, int kind,
                         const float* gate, void* out, long ldo, void* out_s, long ldos) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_gemm_fp8_impl(ctx, a, lda, a_s, ldas, w, ldw, w_s, ldws, bias, M, N, K, act, kind, gate, out,
+  const OpScope scope(ctx);
+  return leave_op(bag_gemm_fp8_impl(ctx, a, lda, a_s, ldas, w, ldw, w_s, ldws, bias, M, N, K, act, kind, gate, out,
                                     ldo, out_s, ldos));
 }
 
@@ -2326,8 +2309,8 @@ bag_status bag_cache_write(bag_ctx* ctx, const float* x, long ldx, const float* 
                            long rows, long cols, int bits, void* codes, long ldc, void* scales, long lds, long
                            capacity) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_cache_write_impl(ctx, x, ldx, base, ldb, slots, rows, cols, bits, codes, ldc, scales, lds,
+  const OpScope scope(ctx);
+  return leave_op(bag_cache_write_impl(ctx, x, ldx, base, ldb, slots, rows, cols, bits, codes, ldc, scales, lds,
                                        capacity));
 }
 
@@ -2335,23 +2318,23 @@ bag_status bag_cache_read(bag_ctx* ctx, const void* codes, long ldc, const void*
                           const int32_t* slots, long rows, long cols, int bits, const float* base, long ldb, float*
                           out, long ldo) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_cache_read_impl(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb,
+  const OpScope scope(ctx);
+  return leave_op(bag_cache_read_impl(ctx, codes, ldc, scales, lds, capacity, slots, rows, cols, bits, base, ldb,
                                       out, ldo));
 }
 
 bag_status bag_block_pool(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads, void* codes, float*
                           scales, long ldb) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_block_pool_impl(ctx, x, type, ld, rows, heads, codes, scales, ldb));
+  const OpScope scope(ctx);
+  return leave_op(bag_block_pool_impl(ctx, x, type, ld, rows, heads, codes, scales, ldb));
 }
 
 bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, long nq, int heads, const void* codes,
                             const float* scales, long ldb, long nkb, int kv_heads, int keep, int32_t* blocks) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_block_select_impl(ctx, q, type, ldq, nq, heads, codes, scales, ldb, nkb, kv_heads, keep,
+  const OpScope scope(ctx);
+  return leave_op(bag_block_select_impl(ctx, q, type, ldq, nq, heads, codes, scales, ldb, nkb, kv_heads, keep,
                                         blocks));
 }
 
@@ -2359,8 +2342,8 @@ bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const voi
                                 vpad, int type, long nq, long nk, int heads, int kv_heads, const int32_t* blocks, int
                                 keep, void* o, long ldo) {
   if (!ctx) return BAG_EINVAL;
-  CKS(enter_op(ctx));
-  return leave_op(ctx, bag_attention_blocks_impl(ctx, q, ldq, k, ldk, v, vpad, type, nq, nk, heads, kv_heads, blocks,
+  const OpScope scope(ctx);
+  return leave_op(bag_attention_blocks_impl(ctx, q, ldq, k, ldk, v, vpad, type, nq, nk, heads, kv_heads, blocks,
                                             keep, o, ldo));
 }
 

@@ -115,32 +115,39 @@ __host__ __device__ __forceinline__ bool wide_scales(const uint8_t* s, long lds)
 // their parts through distributed shared memory in rank order (rank r finishes rows m = r, r + S,
 // ... of the tile).
 // warp 0: TMA producer; 1: MMA; 2: scale words; 4 .. 7: epilogue, thread = column n.
+// The ring is as deep as the CTAs that share an SM leave room for (`stages`, at most F8F_MAX).
+constexpr int F8F_MAX = 10;
 template <int BN>
 struct FewCfg {
   static constexpr int STAGE = F8_TILE + BN * F8_BK;
-  static constexpr int STAGES = 3;
-  static constexpr int OFF_SF = STAGES * STAGE;              // two runs of W's and A's scale words
   static constexpr int SF_GROUP = 2 * F8_ATOM, SF_STAGE = F8_RUN * SF_GROUP;
-  static constexpr int OFF_RED = OFF_SF + 2 * SF_STAGE;      // [BN][4] block maxima of warps
+  // after the ring: two runs of W's and A's scale words, [BN][4] block maxima of warps, barriers
+  static constexpr int OFF_RED = 2 * SF_STAGE;
   static constexpr int OFF_BAR = OFF_RED + BN * 16;
-  static constexpr int SMEM = OFF_BAR + 256 + 1024;
+  static constexpr int REST = OFF_BAR + 256 + 1024;
+  static constexpr int MIN_STAGES = 3;
   static constexpr int SF_COL = BN;                          // 8 TMEM columns a scale stage
   static constexpr int TMEM_COLS = 2 * BN;
   static_assert(BN + 16 <= TMEM_COLS, "accumulator and two scale stages");
-  static_assert(128 * BN * 4 <= OFF_SF, "the exchange fits the ring");
+  static_assert(128 * BN * 4 <= MIN_STAGES * STAGE, "the exchange fits the ring");
+  // ring depth where `ctas` share an SM (each takes 1 KB of it besides its own)
+  static int stages(int ctas) {
+    return std::max(MIN_STAGES, std::min(F8F_MAX, (228 * 1024 / ctas - 1024 - REST) / STAGE));
+  }
 };
 
 template <int BN>
 __global__ void __launch_bounds__(256)
     gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
-                        const __grid_constant__ Fp8Gemm g, int logS) {
+                        const __grid_constant__ Fp8Gemm g, int logS, int stages) {
   using C = FewCfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
-  uint64_t* empty = full + C::STAGES;
-  uint64_t* sf_full = empty + C::STAGES;
+  uint8_t* rest = smem + stages * C::STAGE;
+  uint64_t* full = reinterpret_cast<uint64_t*>(rest + C::OFF_BAR);
+  uint64_t* empty = full + F8F_MAX;
+  uint64_t* sf_full = empty + F8F_MAX;
   uint64_t* sf_empty = sf_full + 2;
   uint64_t* sf_used = sf_empty + 2;  // [2]: a group's products are done, its TMEM columns free
   uint64_t* tfull = sf_used + 2;
@@ -155,7 +162,7 @@ __global__ void __launch_bounds__(256)
   const int kb0 = (int)((long)rank * nkb / S), kb1 = (int)((long)(rank + 1) * nkb / S);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::STAGES; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(full + s, 1);
       mbar_init(empty + s, 1);
     }
@@ -197,7 +204,7 @@ __global__ void __launch_bounds__(256)
         tma_load_2d(smem + s * C::STAGE, &tmW, kb * F8_BK, n0, full + s);
         tma_load_2d(smem + s * C::STAGE + F8_TILE, &tmA, kb * F8_BK, m0, full + s);
         ++issued;
-        if (++s == C::STAGES) {
+        if (++s == stages) {
           s = 0;
           ph ^= 1;
         }
@@ -205,9 +212,9 @@ __global__ void __launch_bounds__(256)
       if (!ok) {
         // wait (bounded) for the copies this thread may still have in flight
         const uint64_t t0 = global_ns();
-        for (int i = 0; i < C::STAGES && i < issued; ++i) {
+        for (int i = 0; i < stages && i < issued; ++i) {
           if (--s < 0) {
-            s = C::STAGES - 1;
+            s = stages - 1;
             ph ^= 1;
           }
           while (!mbar_try_wait(full + s, ph) && global_ns() - t0 < kWaitLimitNs) {
@@ -217,47 +224,50 @@ __global__ void __launch_bounds__(256)
     }
   } else if (warp == 1) {
     // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
-    const uint32_t base = smem_u32(smem);
+    const uint32_t base = smem_u32(smem), sf = smem_u32(rest);
     int s = 0, run = 0, grp = 0;  // ring stage; runs and groups handled so far
-    uint32_t ph = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      if (kb == kb0 || kb % (F8_GROUP * F8_RUN) == 0) {
-        if (!mbar_wait_warp(sf_full + (run & 1), (uint32_t)(run >> 1) & 1u, abort_flag)) break;
+    uint32_t ph = 0, add = 0;     // the first product overwrites the accumulator
+    bool good = true;
+    for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1 && good; kg += F8_GROUP) {  // groups, maybe cut at the ends
+      if (run == 0 || kg % (F8_GROUP * F8_RUN) == 0) {
+        if (!(good = mbar_wait_warp(sf_full + (run & 1), (uint32_t)(run >> 1) & 1u, abort_flag))) break;
         ++run;
       }
       const uint32_t sw = tmem + C::SF_COL + (grp & 1) * 8;
-      if (kb == kb0 || kb % F8_GROUP == 0) {
-        if (!mbar_wait_warp(sf_used + (grp & 1), ((uint32_t)(grp >> 1) & 1u) ^ 1u, abort_flag)) break;
-        tc_fence_after();
-        const uint64_t d = scale_desc(base + C::OFF_SF + ((run - 1) & 1) * C::SF_STAGE +
-                                      kb / F8_GROUP % F8_RUN * C::SF_GROUP);
-        if (elect_one()) {
-          copy_scales(sw, d);
-          copy_scales(sw + 4, d + (F8_ATOM >> 4));
-        }
-        __syncwarp();
-      }
-      if (!mbar_wait_warp(full + s, ph, abort_flag)) break;
+      if (!(good = mbar_wait_warp(sf_used + (grp & 1), ((uint32_t)(grp >> 1) & 1u) ^ 1u, abort_flag))) break;
       tc_fence_after();
-      const uint64_t wd = sw128_desc(base + s * C::STAGE);
-      const uint64_t ad = sw128_desc(base + s * C::STAGE + F8_TILE);
-      const uint32_t idesc = idesc_mxf8(128, BN) | scale_byte((uint32_t)(kb % F8_GROUP));
-      const bool last = kb + 1 == kb1 || (kb + 1) % F8_GROUP == 0;
-      const bool last_run = kb + 1 == kb1 || (kb + 1) % (F8_GROUP * F8_RUN) == 0;
+      const uint64_t d = scale_desc(sf + ((run - 1) & 1) * C::SF_STAGE + kg / F8_GROUP % F8_RUN * C::SF_GROUP);
       if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
-          mma_mxf8(tmem, wd + 2 * k, ad + 2 * k, idesc, sw, sw + 4, (kb > kb0 || k > 0) ? 1u : 0u);
-        mma_commit(empty + s);
-        if (last) mma_commit(sf_used + (grp & 1));
-        if (last_run) mma_commit(sf_empty + ((run - 1) & 1));
+        copy_scales(sw, d);
+        copy_scales(sw + 4, d + (F8_ATOM >> 4));
       }
       __syncwarp();
-      if (++s == C::STAGES) {
-        s = 0;
-        ph ^= 1;
+#pragma unroll
+      for (int b = 0; b < F8_GROUP; ++b) {
+        if (kg + b < kb0 || kg + b >= kb1) continue;
+        if (!(good = good && mbar_wait_warp(full + s, ph, abort_flag))) break;
+        tc_fence_after();
+        const uint64_t wd = sw128_desc(base + s * C::STAGE);
+        const uint64_t ad = wd + (F8_TILE >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
+            mma_mxf8(tmem, wd + 2 * k, ad + 2 * k, idesc_mxf8(128, BN) | scale_byte(b), sw, sw + 4, k > 0 ? 1u : add);
+          mma_commit(empty + s);
+        }
+        __syncwarp();
+        add = 1;
+        if (++s == stages) {
+          s = 0;
+          ph ^= 1;
+        }
       }
-      grp += last;
+      if (elect_one()) {
+        mma_commit(sf_used + (grp & 1));
+        if (kg + F8_GROUP >= kb1 || (kg / F8_GROUP + 1) % F8_RUN == 0) mma_commit(sf_empty + ((run - 1) & 1));
+      }
+      __syncwarp();
+      ++grp;
     }
     // all MMAs issued so far (whatever happened above) finish before tfull completes, and
     // the bounded wait keeps tensor memory until then
@@ -283,7 +293,7 @@ __global__ void __launch_bounds__(256)
     for (int r = r0; r < r1; ++r) {
       const int i = r - r0, st = i & 1;
       if (!mbar_wait_warp(sf_empty + st, ((uint32_t)(i >> 1) & 1u) ^ 1u, abort_flag)) break;
-      uint8_t* d = smem + C::OFF_SF + st * C::SF_STAGE;
+      uint8_t* d = rest + st * C::SF_STAGE;
       w.put(d, C::SF_GROUP);
       a.put(d + F8_ATOM, C::SF_GROUP);
       fence_proxy_async_smem();
@@ -331,7 +341,7 @@ __global__ void __launch_bounds__(256)
     const float bias = in && g.bias ? __ldg(g.bias + n) : 0.f;
     const float gate = in && g.gate ? __ldg(g.gate + n) : 1.f;
     const int mine = (cols - rank + S - 1) >> logS;
-    uint4* red = reinterpret_cast<uint4*>(smem + C::OFF_RED);  // [row m of the tile]: the warps' maxima
+    uint4* red = reinterpret_cast<uint4*>(rest + C::OFF_RED);  // [row m of the tile]: the warps' maxima
 #pragma unroll 1
     for (int j0 = 0; j0 < mine; j0 += 16) {
       float y[16];
@@ -412,8 +422,10 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
     return cudaErrorInvalidValue;
   const long units = (long)((g.M + BN - 1) / BN) * ((g.N + 127) / 128);
   if (units << logS > 0x7fffffffL) return cudaErrorInvalidConfiguration;
-  return launch_cluster(gemm_fp8_few_kernel<BN>, logS > 0 ? 1u << logS : 0u, (unsigned)(units << logS), 256,
-                        FewCfg<BN>::SMEM, s, tw, ta, g, logS);
+  const long sms = sm_count(), ctas = units << logS;
+  const int stages = FewCfg<BN>::stages(ctas <= sms ? 1 : (ctas <= 2 * sms ? 2 : 3));
+  return launch_cluster(gemm_fp8_few_kernel<BN>, logS > 0 ? 1u << logS : 0u, (unsigned)ctas, 256,
+                        stages * FewCfg<BN>::STAGE + FewCfg<BN>::REST, s, tw, ta, g, logS, stages);
 }
 
 // ---------------------------------------------------------------------------
@@ -920,10 +932,10 @@ cudaError_t gemm_fp8_init() {
   auto smem = [&](auto kernel, int bytes) {
     if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  smem(gemm_fp8_few_kernel<16>, FewCfg<16>::SMEM);
-  smem(gemm_fp8_few_kernel<32>, FewCfg<32>::SMEM);
-  smem(gemm_fp8_few_kernel<64>, FewCfg<64>::SMEM);
-  smem(gemm_fp8_few_kernel<128>, FewCfg<128>::SMEM);
+  smem(gemm_fp8_few_kernel<16>, FewCfg<16>::stages(1) * FewCfg<16>::STAGE + FewCfg<16>::REST);
+  smem(gemm_fp8_few_kernel<32>, FewCfg<32>::stages(1) * FewCfg<32>::STAGE + FewCfg<32>::REST);
+  smem(gemm_fp8_few_kernel<64>, FewCfg<64>::stages(1) * FewCfg<64>::STAGE + FewCfg<64>::REST);
+  smem(gemm_fp8_few_kernel<128>, FewCfg<128>::stages(1) * FewCfg<128>::STAGE + FewCfg<128>::REST);
   smem(gemm_fp8_pair_kernel<BAG_FP8_F32>, F8P_SMEM);
   smem(gemm_fp8_pair_kernel<BAG_FP8_BF16>, F8P_SMEM);
   smem(gemm_fp8_pair_kernel<BAG_FP8_CODES>, F8P_SMEM);

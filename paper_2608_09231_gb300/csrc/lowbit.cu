@@ -40,6 +40,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(Q_WARPS * 32) quant_kernel(const T* __restrict__ x, long ldx, long rows, long cols,
                                                              uint8_t* __restrict__ codes, long ldc,
                                                              uint8_t* __restrict__ scales, long lds, int segs) {
+  grid_dep_sync();
   constexpr int N = 16 / sizeof(T), STEP = 32 * N, LANES = kScaleBlock / N;
   const long item = (long)blockIdx.x * Q_WARPS + threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
@@ -93,6 +94,7 @@ __global__ void __launch_bounds__(TH) ln_fp8_kernel(const float* __restrict__ x,
                                                     const float* __restrict__ shift, const float* __restrict__ scale,
                                                     int cols, uint8_t* __restrict__ codes, long ldc,
                                                     uint8_t* __restrict__ scales, long lds) {
+  grid_dep_sync();
   __shared__ float red_mean[TH / 32], red_var[TH / 32];
   const long row = blockIdx.x;
   const float4* xr = reinterpret_cast<const float4*>(x + row * ldx);
@@ -165,6 +167,7 @@ BAG_DEV float4 load_cols(const float* p, int valid, bool vec) {
 
 template <int BITS>
 __global__ void __launch_bounds__(C_WARPS * 32) cache_write_kernel(const CacheArgs a) {
+  grid_dep_sync();
   using F = CacheFmt<BITS>;
   const long item = (long)blockIdx.x * C_WARPS + threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
@@ -223,6 +226,7 @@ __global__ void __launch_bounds__(C_WARPS * 32) cache_write_kernel(const CacheAr
 
 template <int BITS>
 __global__ void __launch_bounds__(C_WARPS * 32) cache_read_kernel(const CacheArgs a) {
+  grid_dep_sync();
   using F = CacheFmt<BITS>;
   const long item = (long)blockIdx.x * C_WARPS + threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
@@ -334,6 +338,7 @@ template <typename T>
 __global__ void __launch_bounds__(P_TH) block_pool_kernel(const T* __restrict__ x, long ld, long rows, int vec,
                                                           int8_t* __restrict__ codes, float* __restrict__ scales,
                                                           long ldb) {
+  grid_dep_sync();
   __shared__ float sums[16][128];
   __shared__ uint32_t red[4];
   const long b = blockIdx.x, h = blockIdx.y;
@@ -352,6 +357,7 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
                                                             const int8_t* __restrict__ codes,
                                                             const float* __restrict__ scales, long ldb, int nkb,
                                                             int group, int keep, int* __restrict__ blocks) {
+  grid_dep_sync();
   extern __shared__ uint32_t keys[];
   __shared__ float sums[16][128];
   __shared__ uint32_t red[4];
