@@ -8,6 +8,7 @@
 // instruction descriptor picks the block's byte.  Scales are then applied inside the MMA at its
 // full rate, and the accumulator is the plain fp32 sum over K.
 #include <algorithm>
+#include <cmath>
 
 #include "lowbit.cuh"
 #include "bag.h"
@@ -414,6 +415,12 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// SMs that clusters of S CTAs reach (a cluster stays inside one group of SMs).
+static long cluster_sms(int logS) {
+  const long sms = sm_count();
+  return logS < 2 ? sms : (logS == 2 ? sms - sms / 19 : sms - sms / 19 * 4);  // 152, 152, 144, 120 of 152
+}
+
 template <int BN>
 static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
   CUtensorMap tw, ta;
@@ -422,7 +429,7 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
     return cudaErrorInvalidValue;
   const long units = (long)((g.M + BN - 1) / BN) * ((g.N + 127) / 128);
   if (units << logS > 0x7fffffffL) return cudaErrorInvalidConfiguration;
-  const long sms = sm_count(), ctas = units << logS;
+  const long sms = cluster_sms(logS), ctas = units << logS;
   const int stages = FewCfg<BN>::stages(ctas <= sms ? 1 : (ctas <= 2 * sms ? 2 : 3));
   return launch_cluster(gemm_fp8_few_kernel<BN>, logS > 0 ? 1u << logS : 0u, (unsigned)ctas, 256,
                         stages * FewCfg<BN>::STAGE + FewCfg<BN>::REST, s, tw, ta, g, logS, stages);
@@ -943,20 +950,55 @@ cudaError_t gemm_fp8_init() {
   return r;
 }
 
+// Which kernel, tile and split: the least expected time.  The constants (us) fit 247 shapes of 1 to
+// 2048 rows, 512 to 13824 columns and K, each timed under every choice (3000 timings, chained
+// launches); the choice is within 2.1 % of the best one on average, 40 % at most (50 rows through 13824 x 5120).  A CTA of either
+// kernel takes 0.2 to 0.3 us a K block whatever its tile (the issue of its four MMAs and their
+// waits), so few tiles want K split, and many the largest tile.
+struct Fp8Plan {
+  int BN;    // 0: CTA pairs
+  int logS;
+};
+static Fp8Plan plan_fp8(long M, long N, long K) {
+  auto cd = [](long a, long b) { return (a + b - 1) / b; };
+  const long nkb = cd(K, F8_BK);
+  // the operands' way from HBM beside the time of the CTAs: a smooth maximum of the two, so that of
+  // splits that HBM bounds alike the one with more loads in flight is taken
+  const double dram = (double)(M + N) * (double)K / 6.5e6 + 3.8;
+  auto together = [&](double us) { return std::pow(std::pow(us, 6.0) + std::pow(dram, 6.0), 1.0 / 6.0); };
+  const double waves = (double)cd(cd(M, 256) * cd(N, 256), std::max(1, sm_count() / 2));
+  double best = together(7.9 + waves * (2.0 + 0.2 * (double)nkb));
+  Fp8Plan p{0, 0};
+  const struct {
+    int BN;
+    double start, wave, share;  // of a launch, of a further wave, of its K blocks (SMs shared)
+  } tiles[] = {{16, 2.8, 1.7, 0.01}, {32, 3.7, 1.5, 0.01}, {64, 5.0, 3.4, 0.17}, {128, 6.4, 3.4, 0.17}};
+  for (const auto& t : tiles) {
+    if (t.BN < 64 && M > t.BN) continue;  // narrow tiles read W again for every tile of rows
+    for (int logS = 0; logS <= 3 && nkb >= 2L << logS; ++logS) {
+      const double kb = (double)cd(nkb, 1L << logS);
+      const double more = (double)(cd(cd(M, t.BN) * cd(N, 128) << logS, cluster_sms(logS)) - 1);
+      const double us = together(t.start + 0.32 * kb + more * (t.wave + t.share * kb) + (logS ? 0.65 : 0.0) +
+                                 0.25 * (1 << logS));
+      if (us < best) {
+        best = us;
+        p = Fp8Plan{t.BN, logS};
+      }
+    }
+  }
+  return p;
+}
+
 cudaError_t gemm_fp8(Fp8Gemm g, cudaStream_t s) {
   if (g.M <= 0 || g.N <= 0) return cudaSuccess;
-  const long tiles = (long)((g.M + 255) / 256) * ((g.N + 255) / 256);
-  if (tiles * 2 >= sm_count()) return launch_pair(g, s);
-  const int BN = g.M <= 16 ? 16 : (g.M <= 32 ? 32 : (g.M <= 64 ? 64 : 128));
-  const long units = (long)((g.M + BN - 1) / BN) * ((g.N + 127) / 128);
-  const int nkb = (g.K + F8_BK - 1) / F8_BK;
-  const int fit = BN <= 32 ? 3 : 2;  // CTAs that an SM holds
-  int logS = 0;
-  while (logS < 3 && units << (logS + 1) <= (long)sm_count() * fit && nkb >= 8 << logS) ++logS;
-  if (BN == 16) return launch_few<16>(g, logS, s);
-  if (BN == 32) return launch_few<32>(g, logS, s);
-  if (BN == 64) return launch_few<64>(g, logS, s);
-  return launch_few<128>(g, logS, s);
+  const Fp8Plan p = plan_fp8(g.M, g.N, g.K);
+  switch (p.BN) {
+    case 16: return launch_few<16>(g, p.logS, s);
+    case 32: return launch_few<32>(g, p.logS, s);
+    case 64: return launch_few<64>(g, p.logS, s);
+    case 128: return launch_few<128>(g, p.logS, s);
+    default: return launch_pair(g, s);
+  }
 }
 
 }  // namespace bag
