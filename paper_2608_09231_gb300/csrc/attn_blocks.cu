@@ -12,9 +12,10 @@
 //                from TMEM at once, P = exp2(s - m) goes back over them in 16 bits and enters the
 //                PV product from TMEM; O stays in TMEM and is rescaled only when the running
 //                maximum has grown by more than 8 (in log2 units)
-// PAIR: the slots are two (head, query block) units.  Otherwise a cluster of C CTAs shares one
-// unit: its list is cut into 2 C parts, and rank r merges 128 / C rows of the 2 C partial outputs
-// through distributed shared memory.
+// The slots are two (head, query block) units, or one unit is shared: its list is cut into 2 C
+// parts for a cluster of C CTAs, and rank r merges 128 / C rows of the 2 C partial outputs through
+// distributed shared memory.  A launch in pairs shares (C = 1) the units of its last wave where
+// they would leave half of the slots idle.
 #include <algorithm>
 #include <cmath>
 
@@ -51,7 +52,8 @@ struct BlockAttnParams {
   __nv_bfloat16* o;
   long ldo;
   float scale_log2;
-  int c;                              // CTAs of a unit (not PAIR)
+  int c;                              // CTAs of a shared unit (PAIR: 1)
+  int pairs;                          // PAIR: CTAs that work on two units; later ones share one each
   int* err;
 };
 }  // namespace
@@ -77,10 +79,11 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
   int* length = reinterpret_cast<int*>(tmem_slot + 2);  // [2] of the slots' lists
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const bool pair = PAIR && (int)blockIdx.x < p.pairs;  // two units
   const int C = PAIR ? 1 : p.c;
   const int rank = !PAIR && C > 1 ? (int)cluster_ctarank() : 0;
-  const long u0 = PAIR ? 2L * blockIdx.x : (long)blockIdx.x / C;
-  auto unit_of = [&](int x) { return PAIR ? u0 + x : u0; };
+  const long u0 = PAIR ? (pair ? 2L * blockIdx.x : (long)blockIdx.x + p.pairs) : (long)blockIdx.x / C;
+  auto unit_of = [&](int x) { return pair ? u0 + x : u0; };
   auto list_of = [&](int x) { return p.blocks + unit_of(x) * p.keep; };
 
   if (threadIdx.x == 0) {
@@ -106,7 +109,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
   grid_dep_sync();
   __syncthreads();
   // a list ends at its first entry that names no block
-  for (int x = 0; x < (PAIR ? 2 : 1); ++x) {
+  for (int x = 0; x < (pair ? 2 : 1); ++x) {
     if (unit_of(x) >= p.units) continue;
     const int* list = list_of(x);
     for (int i = threadIdx.x; i < p.keep; i += BT_THREADS)
@@ -125,7 +128,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
   int first[2], n[2];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    if (PAIR) {
+    if (pair) {
       first[x] = 0;
       n[x] = length[x];
     } else {
@@ -149,10 +152,9 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
         qx[x] = head * BT;
         qy[x] = (int)(u % p.nqb) * BT;
       }
-      constexpr int QT = PAIR ? 2 : 1;
-      mbar_arrive_expect_tx(q_full, QT * BT_TILE);
-#pragma unroll
-      for (int x = 0; x < QT; ++x) {
+      const int qt = pair ? 2 : 1;
+      mbar_arrive_expect_tx(q_full, qt * BT_TILE);
+      for (int x = 0; x < qt; ++x) {
         tma_load_2d(smem + x * BT_TILE, &tmQ, qx[x], qy[x], q_full);
         tma_load_2d(smem + x * BT_TILE + BT_CHUNK, &tmQ, qx[x] + 64, qy[x], q_full);
       }
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
       };
       auto issue_s = [&](int x) {  // scores of the ring's next tile
         if (!wait(full + s, ph)) return false;
-        const uint64_t qd = sw128_desc(q_addr + (PAIR ? x * BT_TILE : 0));
+        const uint64_t qd = sw128_desc(q_addr + (pair ? x * BT_TILE : 0));
         const uint64_t kd = sw128_desc(r_addr + s * BT_TILE);
         if (elect_one()) {
 #pragma unroll
@@ -280,8 +282,8 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
       }
     }
     __syncwarp();
-    if (!PAIR) {  // the two barriers of the exchange
-      if (C > 1) {
+    if (!pair) {  // the two barriers of the exchange
+      if (!PAIR && C > 1) {
         cluster_sync_all();
         cluster_sync_all();
       } else {
@@ -369,7 +371,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
     }
     if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(o_done + x, 0, abort_flag));
     tc_fence_after();
-    if (PAIR) {
+    if (pair) {
       const long u = unit_of(x);
       if (ok && u < p.units) {
         const int head = (int)(u / p.nqb), q0 = (int)(u % p.nqb) * BT;
@@ -404,7 +406,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
     } else {
       const int rpo = BT / C;  // rows a rank merges
       __syncwarp();
-      if (C > 1)
+      if (!PAIR && C > 1)
         cluster_sync_all();  // every CTA's products are done: the operand tiles are free
       else
         __syncthreads();
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
         const int R = quad * 32 + lane;
         const int at = (2 * rank + x) * rpo + R % rpo;
         const uint32_t here = smem_u32(smem);
-        const uint32_t dst = C > 1 ? mapa_shared(here, (uint32_t)(R / rpo)) : here;
+        const uint32_t dst = !PAIR && C > 1 ? mapa_shared(here, (uint32_t)(R / rpo)) : here;
 #pragma unroll 1
         for (int c = 0; c < BT; c += 32) {
           float o[32];
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
         peer_store2(dst + BT_OFF_ML + (uint32_t)at * 8, m_use, l);
       }
       __syncwarp();
-      if (C > 1)
+      if (!PAIR && C > 1)
         cluster_sync_all();  // every part has arrived; no access to another CTA follows
       else
         __syncthreads();
@@ -474,19 +476,37 @@ cudaError_t attention_blocks_init() {
   return r;
 }
 
-// CTAs that share a unit (0: a CTA takes two units), by the time each way would take: a wave of
-// CTAs that walk k blocks on each slot takes about 1.45 us x k, and sharing about 7 us.
-static int blocks_split(long units, int keep) {
-  const int sms = sm_count();
-  auto waves = [&](long ctas) { return (double)((ctas + sms - 1) / sms); };
-  double best = waves((units + 1) / 2) * keep * 1.45;
+// CTAs that share a unit (0: a CTA takes two units, and *pairs CTAs do; units of the last wave
+// follow alone), by the time each way would take (us; 15 shapes of 1 to 32,760 queries and 2 to
+// 2560 units, each timed in every way): a wave of CTAs that walk k blocks on each slot takes 1.7 k,
+// and 5 more where the slots are units of their own, 9 to 13 with the exchange.  32,760 queries x 4
+// heads x 64 of 256 blocks: 449 us in pairs, 452, 541, 748 and 1371 shared by 1, 2, 4 and 8; one
+// query x 40 heads x 32 blocks: 59 in pairs, 33, 24, 37 and 49.
+static int blocks_split(long units, int keep, long* pairs) {
+  const long sms = sm_count();
+  auto cd = [](long a, long b) { return (a + b - 1) / b; };
+  auto shared = [&](long n, int log) {
+    const long reach = log < 2 ? sms : (log == 2 ? sms - sms / 19 : sms - sms / 19 * 4);  // by clusters of 2^log
+    return (double)cd(n << log, reach) * (1.7 * (double)cd(keep, 2L << log) + 9.0 + 1.3 * log);
+  };
+  const double wave = 1.7 * keep + 5.0;
+  *pairs = cd(units, 2);
+  double best = (double)cd(*pairs, sms) * wave;
+  const long full = units / (2 * sms), rest = units - full * 2 * sms;
+  if (full > 0 && rest > 0 && shared(rest, 0) < wave) {
+    *pairs = full * sms;
+    best = (double)full * wave + shared(rest, 0);
+  }
   int c = 0;
-  for (int k = 1; k <= 8 && 2 * k <= keep; k *= 2) {
-    const double t = waves(units * k) * ((keep + 2 * k - 1) / (2 * k)) * 1.45 + 7.0;
-    if (t < best) {
-      best = t;
-      c = k;
+  for (int log = 0; log <= 3 && (log == 0 || 2 << log <= keep); ++log) {
+    if (shared(units, log) < best) {
+      best = shared(units, log);
+      c = 1 << log;
     }
+  }
+  if (c == 1) {  // the same kernel as pairs, with none
+    c = 0;
+    *pairs = 0;
   }
   return c;
 }
@@ -512,9 +532,11 @@ cudaError_t attention_blocks(const BlockAttnArgs& a, cudaStream_t s) {
   p.ldo = a.ldo;
   p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)BT));
   p.err = a.err;
-  const int c = blocks_split(p.units, a.keep);
+  long pairs;
+  const int c = blocks_split(p.units, a.keep, &pairs);
   p.c = std::max(1, c);
-  const long ctas = c ? p.units * c : (p.units + 1) / 2;
+  const long ctas = c ? p.units * c : pairs + std::max(0L, p.units - 2 * pairs);
+  p.pairs = (int)std::min(pairs, 0x7fffffffL);
   if (ctas > 0x7fffffffL) return cudaErrorInvalidConfiguration;
   auto launch = [&](auto kernel) {
     return launch_cluster(kernel, c > 1 ? (unsigned)c : 0u, (unsigned)ctas, BT_THREADS, BT_SMEM, s, tq, tk, tv, p);

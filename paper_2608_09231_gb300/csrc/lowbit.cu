@@ -284,34 +284,46 @@ __global__ void __launch_bounds__(C_WARPS * 32) cache_read_kernel(const CacheArg
 // ---------------------------------------------------------------------------
 constexpr int P_TH = 256;
 
+// Eight elements of a row as 16 bytes, zeros where there is no row.
+template <typename T>
+BAG_DEV uint4 raw8(const T* p, bool row, bool vec) {
+  uint4 u = make_uint4(0u, 0u, 0u, 0u);
+  if (!row) return u;
+  if (vec) return __ldg(reinterpret_cast<const uint4*>(p));
+  const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+  uint32_t w[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = __ldg(q + j);
+  return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+
 // Mean of up to 128 rows of 128 columns by all P_TH threads, as 8-bit codes of threads 0 .. 127
 // (thread = column); returns the vector's scale to every thread.  Thread (rg, cg) holds rows rg
 // + 16 i of eight columns, so the first three halvings (64, 32 and 16 rows apart) are its own;
-// the other four pass through shared memory.
+// the other four pass through shared memory.  All eight rows are loaded before the first is
+// converted, and kept as 16 bits until then (eight rows in fp32 would halve the CTAs on an SM).
 template <typename T>
 BAG_DEV float pool_block(const T* __restrict__ x, long ld, int rows, bool vec, float (*sums)[128], uint32_t* red,
                          int* code) {
   const int rg = threadIdx.x / 16, c = (threadIdx.x % 16) * 8;
-  float v[8][8];
+  uint4 u[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = rg + 16 * i;
-    const T* p = x + (long)r * ld + c;
-    if (r < rows && vec) {
-      load_n<T, 8, true>(p, 8, v[i]);
-    } else {
+  for (int i = 0; i < 8; ++i) u[i] = raw8<T>(x + (long)(rg + 16 * i) * ld + c, rg + 16 * i < rows, vec);
+  float v[4][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = r < rows ? to_f32(p[j]) : 0.f;
-    }
+  for (int i = 0; i < 4; ++i) {
+    const T *a = reinterpret_cast<const T*>(&u[i]), *b = reinterpret_cast<const T*>(&u[i + 4]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = to_f32(a[j]) + to_f32(b[j]);
   }
 #pragma unroll
-  for (int h = 4; h > 0; h /= 2)
+  for (int h = 2; h > 0; h /= 2)
 #pragma unroll
     for (int i = 0; i < h; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] += v[i + h][j];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sums[rg][c + j] = v[0][j];
+  *reinterpret_cast<float4*>(&sums[rg][c]) = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+  *reinterpret_cast<float4*>(&sums[rg][c + 4]) = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);
   __syncthreads();
   float mean = 0.f;
   if (threadIdx.x < 128) {
@@ -335,11 +347,11 @@ BAG_DEV float pool_block(const T* __restrict__ x, long ld, int rows, bool vec, f
 }
 
 template <typename T>
-__global__ void __launch_bounds__(P_TH) block_pool_kernel(const T* __restrict__ x, long ld, long rows, int vec,
+__global__ void __launch_bounds__(P_TH, 4) block_pool_kernel(const T* __restrict__ x, long ld, long rows, int vec,
                                                           int8_t* __restrict__ codes, float* __restrict__ scales,
                                                           long ldb) {
   grid_dep_sync();
-  __shared__ float sums[16][128];
+  __shared__ __align__(16) float sums[16][128];
   __shared__ uint32_t red[4];
   const long b = blockIdx.x, h = blockIdx.y;
   int code;
@@ -359,7 +371,7 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
                                                             int group, int keep, int* __restrict__ blocks) {
   grid_dep_sync();
   extern __shared__ uint32_t keys[];
-  __shared__ float sums[16][128];
+  __shared__ __align__(16) float sums[16][128];
   __shared__ uint32_t red[4];
   __shared__ __align__(16) int8_t qc[128];
   __shared__ int hist[256], warp_sum[P_TH / 32];
@@ -372,18 +384,27 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
   __syncthreads();
   const long kh = h / group;
   const int4 a = reinterpret_cast<const int4*>(qc)[lane % 8];
-  for (int j0 = warp * 4; j0 < nkb; j0 += P_TH / 8) {
-    const int j = j0 + lane / 8;
-    int dot = 0;
-    if (j < nkb) {
-      const int4 k = __ldg(reinterpret_cast<const int4*>(codes + (kh * ldb + j) * 128) + lane % 8);
-      dot = __dp4a(a.x, k.x, __dp4a(a.y, k.y, __dp4a(a.z, k.z, __dp4a(a.w, k.w, 0))));
+  const int4* kc = reinterpret_cast<const int4*>(codes + kh * ldb * 128) + lane % 8;
+  constexpr int KU = 8;  // steps whose loads are in flight together
+  for (int j0 = warp * 4 + lane / 8; j0 - lane / 8 < nkb; j0 += KU * P_TH / 8) {
+    int4 k[KU];
+    float sc[KU];
+#pragma unroll
+    for (int i = 0; i < KU; ++i) {
+      const int j = min(j0 + i * (P_TH / 8), nkb - 1);
+      k[i] = __ldg(kc + (long)j * 8);
+      sc[i] = __ldg(scales + kh * ldb + j);
     }
 #pragma unroll
-    for (int o = 4; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-    if (j < nkb && lane % 8 == 0) {
-      const uint32_t u = __float_as_uint((float)dot * __ldg(scales + kh * ldb + j) + 0.f);  // no -0
-      keys[j] = u & 0x80000000u ? ~u : u | 0x80000000u;
+    for (int i = 0; i < KU; ++i) {
+      const int j = j0 + i * (P_TH / 8);
+      int dot = __dp4a(a.x, k[i].x, __dp4a(a.y, k[i].y, __dp4a(a.z, k[i].z, __dp4a(a.w, k[i].w, 0))));
+#pragma unroll
+      for (int o = 4; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      if (j < nkb && lane % 8 == 0) {
+        const uint32_t u = __float_as_uint((float)dot * sc[i] + 0.f);  // no -0
+        keys[j] = u & 0x80000000u ? ~u : u | 0x80000000u;
+      }
     }
   }
   uint32_t top = 0, mask = 0;  // the digits found so far, and where they are
