@@ -431,8 +431,8 @@ bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, lon
  * >= nk, a multiple of 8), all of `type`, 16-byte aligned, row strides multiples of 8; o bf16
  * [nq, ldo], 16-byte aligned, ldo a multiple of 8.  blocks: int32 device
  * [heads][ceil(nq / 128)][keep]; a list ends at its first entry outside [0, ceil(nk / 128)), so
- * shorter ones end in -1, and a block of queries with an empty list gets zeros.  An index listed
- * twice counts twice. */
+ * shorter ones end in -1, and a block of queries with an empty list gets zeros (all of them where
+ * nk = 0).  An index listed twice counts twice. */
 bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const void* k, long ldk,
                                 const void* v, long vpad, int type, long nq, long nk, int heads,
                                 int kv_heads, const int32_t* blocks, int keep, void* o, long ldo);

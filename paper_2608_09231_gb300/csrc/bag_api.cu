@@ -1979,11 +1979,14 @@ static bag_status bag_attention_blocks_impl(bag_ctx* ctx, const void* q, long ld
       (type != BAG_BF16 && type != BAG_F16) || vpad < nk)
     return fail(ctx, BAG_EINVAL, "bad attention_blocks shape or type");
   if (nq == 0) return BAG_OK;
-  if (!q || !k || !v || !blocks || !o) return fail(ctx, BAG_EINVAL, "null pointer");
+  if (!q || !o || (nk > 0 && (!k || !v || !blocks))) return fail(ctx, BAG_EINVAL, "null pointer");
   if (ldq % 8 || ldk % 8 || vpad % 8 || ldo % 8 || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) ||
       !aligned(o, 16) || !aligned(blocks, 4))
     return fail(ctx, BAG_EUNSUPPORTED, "attention_blocks needs 16-byte aligned rows");
-  if (nk == 0) return fail(ctx, BAG_EUNSUPPORTED, "attention_blocks needs a key");
+  if (nk == 0) {  // no list names a block
+    CK(cudaMemset2DAsync(o, (size_t)ldo * 2, 0, (size_t)heads * 256, (size_t)nq, ctx->user_stream));
+    return BAG_OK;
+  }
   BlockAttnArgs a{};
   a.q = q;
   a.ldq = ldq;
