@@ -467,6 +467,193 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
   }
 }
 
+// ---------------------------------------------------------------------------
+// One query
+// ---------------------------------------------------------------------------
+// The scores of one query row are no matrix product: its keys and values are read once and used
+// once, 64 KB a block, so the row is bound by HBM and by how many of those bytes are in flight.  A
+// cluster of C CTAs shares a head's list; a CTA walks its part block by block on CUDA cores, with
+// fp32 products, sums and probabilities.  Sixteen lanes hold a row of K (16 bytes each), or of V^T;
+// eight rows a lane, so a warp takes 16 keys, then 16 columns of the output.  The values of a block
+// are in flight while its scores are taken, the next block's keys while the values are summed.
+// Rank 0 merges the ranks' sums in order.
+constexpr int TK_TH = 256, TK_MAX_C = 8;
+
+// Element pairs of 16 bytes.
+template <bool F16>
+BAG_DEV float2 pair_of(uint32_t u) {
+  if constexpr (F16)
+    return __half22float2(*reinterpret_cast<const __half2*>(&u));
+  else
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+template <bool F16>
+BAG_DEV float dot8(uint4 u, const float* w) {
+  const float2 a = pair_of<F16>(u.x), b = pair_of<F16>(u.y), c = pair_of<F16>(u.z), d = pair_of<F16>(u.w);
+  float s = a.x * w[0];
+  s = fmaf(a.y, w[1], s);
+  s = fmaf(b.x, w[2], s);
+  s = fmaf(b.y, w[3], s);
+  s = fmaf(c.x, w[4], s);
+  s = fmaf(c.y, w[5], s);
+  s = fmaf(d.x, w[6], s);
+  return fmaf(d.y, w[7], s);
+}
+
+// Sums of eight values over sixteen lanes, half of the values handed over in each step: the lane's
+// result is value (its index within the sixteen) / 2.
+BAG_DEV float sum_16lanes(float* v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int n = 4; n > 0; n /= 2) {  // lanes 2 n apart
+    const bool up = lane & (2 * n);
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+      const float give = up ? v[j] : v[j + n], keep = up ? v[j + n] : v[j];
+      v[j] = keep + __shfl_xor_sync(0xffffffffu, give, 2 * n);
+    }
+  }
+  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(TK_TH, 2)
+    attn_token_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, long ldk,
+                      const uint16_t* __restrict__ v, long vpad, const BlockAttnParams p) {
+  __shared__ __align__(16) float sc[2][BT];
+  __shared__ float part[TK_MAX_C][BT];
+  __shared__ float2 ml[TK_MAX_C];
+  __shared__ int length;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, li = lane % 16, hl = lane / 16;
+  const int C = p.c, rank = C > 1 ? (int)cluster_ctarank() : 0;
+  const int head = (int)(blockIdx.x / C), kh = head / p.group;
+  const int* list = p.blocks + (long)head * p.keep;
+  if (threadIdx.x == 0) length = p.keep;
+  if (C > 1)
+    cluster_sync_all();  // every CTA has started
+  else
+    __syncthreads();
+  grid_dep_sync();
+  // a list ends at its first entry that names no block
+  for (int i = threadIdx.x; i < p.keep; i += TK_TH)
+    if ((unsigned)__ldg(list + i) >= (unsigned)p.nkb) atomicMin(&length, i);
+  float qv[8];
+  {
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(q + head * BT) + li);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = pair_of<F16>(w[i]);
+      qv[2 * i] = t.x * p.scale_log2;
+      qv[2 * i + 1] = t.y * p.scale_log2;
+    }
+  }
+  __syncthreads();
+  const int first = (int)((long)rank * length / C), last = (int)((long)(rank + 1) * length / C);
+  uint4 kr[8], vr[8];
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  auto load_k = [&](int b) {  // rows 2 i + hl of the warp's 16 keys
+    const int key = b * BT + warp * 16 + hl;
+    const uint16_t* r = k + (long)key * ldk + kh * BT + li * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      kr[i] = key + 2 * i < p.nk ? __ldg(reinterpret_cast<const uint4*>(r + (long)(2 * i) * ldk)) : zero;
+  };
+  auto load_v = [&](int b) {  // columns 2 i + hl of the warp's 16
+    const int key = b * BT + li * 8;
+    const uint16_t* r = v + ((long)kh * BT + warp * 16 + hl) * vpad + key;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vr[i] = key < p.nk ? __ldg(reinterpret_cast<const uint4*>(r + (long)(2 * i) * vpad)) : zero;
+    const int left = p.nk - key;
+    if (left > 0 && left < 8) {  // what lies past the last key may be anything
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint16_t* t = reinterpret_cast<uint16_t*>(&vr[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = j < left ? t[j] : (uint16_t)0;
+      }
+    }
+  };
+  float m = -INFINITY, l = 0.f, acc[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  int b = first < last ? __ldg(list + first) : 0;
+  if (first < last) load_k(b);
+  for (int j = first; j < last; ++j) {
+    float* s = sc[j & 1];
+    load_v(b);
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = dot8<F16>(kr[i], qv);
+    const float mine = sum_16lanes(t);
+    const int key = warp * 16 + (li >> 1) * 2 + hl;
+    if ((li & 1) == 0) s[key] = b * BT + key < p.nk ? mine : -INFINITY;
+    if (j + 1 < last) {
+      b = __ldg(list + j + 1);
+      load_k(b);
+    }
+    __syncthreads();  // (the other buffer was read before this barrier's predecessor)
+    float w[8];
+    ld_chunk<8>(s + li * 8, w);
+    float mx = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float m1 = fmaxf(m, mx);
+    const float ref = m1 == -INFINITY ? 0.f : m1;  // nothing but -inf so far weighs nothing
+    const float alpha = ex2(m - ref);
+    m = m1;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[i] = ex2(w[i] - ref);
+      sum += w[i];
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    l = l * alpha + sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = fmaf(acc[i], alpha, dot8<F16>(vr[i], w));
+  }
+  const float o = sum_16lanes(acc);
+  const int col = warp * 16 + (li >> 1) * 2 + hl;
+  if (C > 1) {
+    if ((li & 1) == 0) peer_store1(mapa_shared(smem_u32(&part[rank][col]), 0), o);
+    if (threadIdx.x == 0) peer_store2(mapa_shared(smem_u32(&ml[rank]), 0), m, l);
+    __syncwarp();
+    cluster_sync_all();  // every part has arrived; no access to another CTA follows
+    if (rank == 0 && threadIdx.x < BT) {
+      float top = -INFINITY, den = 0.f, num = 0.f;
+      for (int r = 0; r < C; ++r) top = fmaxf(top, ml[r].x);
+      for (int r = 0; r < C; ++r) {
+        const float w = ml[r].x == -INFINITY ? 0.f : ex2(ml[r].x - top);
+        den += w * ml[r].y;
+        num += w * part[r][threadIdx.x];
+      }
+      p.o[head * BT + threadIdx.x] = __float2bfloat16_rn(length > 0 ? num / den : 0.f);
+    }
+  } else if ((li & 1) == 0) {
+    p.o[head * BT + col] = __float2bfloat16_rn(length > 0 ? o / l : 0.f);
+  }
+}
+
+// CTAs that share a head: as many as two to an SM leave room for, up to eight and a block each.
+static int token_split(int heads, int keep) {
+  const long sms = sm_count();
+  int c = 1;
+  while (c < TK_MAX_C && 2 * c <= keep && (long)heads * 2 * c <= 2 * (sms - sms / 19 * (c >= 4 ? 4 : 1))) c *= 2;
+  return c;
+}
+
+static cudaError_t attention_token(const BlockAttnArgs& a, BlockAttnParams p, cudaStream_t s) {
+  p.c = token_split(a.heads, a.keep);
+  auto launch = [&](auto kernel) {
+    return launch_cluster(kernel, p.c > 1 ? (unsigned)p.c : 0u, (unsigned)(a.heads * p.c), TK_TH, 0, s,
+                          reinterpret_cast<const uint16_t*>(a.q), reinterpret_cast<const uint16_t*>(a.k), a.ldk,
+                          reinterpret_cast<const uint16_t*>(a.v), a.vpad, p);
+  };
+  return a.f16 ? launch(attn_token_kernel<true>) : launch(attn_token_kernel<false>);
+}
+
 cudaError_t attention_blocks_init() {
   const void* kernels[] = {(const void*)attn_blocks_kernel<false, false>, (const void*)attn_blocks_kernel<false, true>,
                            (const void*)attn_blocks_kernel<true, false>, (const void*)attn_blocks_kernel<true, true>};
@@ -515,10 +702,6 @@ cudaError_t attention_blocks(const BlockAttnArgs& a, cudaStream_t s) {
   if (a.nq <= 0) return cudaSuccess;
   CUtensorMap tq, tk, tv;
   const uint64_t kw = (uint64_t)a.kv_heads * BT;
-  if (encode_tmap_2d_bf16(&tq, a.q, (uint64_t)a.heads * BT, (uint64_t)a.nq, (uint64_t)a.ldq * 2, 64, BT) ||
-      encode_tmap_2d_bf16(&tk, a.k, kw, (uint64_t)a.nk, (uint64_t)a.ldk * 2, 64, BT) ||
-      encode_tmap_2d_bf16(&tv, a.v, (uint64_t)a.nk, kw, (uint64_t)a.vpad * 2, 64, BT))
-    return cudaErrorInvalidValue;
   BlockAttnParams p;
   p.nq = a.nq;
   p.nk = a.nk;
@@ -531,7 +714,14 @@ cudaError_t attention_blocks(const BlockAttnArgs& a, cudaStream_t s) {
   p.o = reinterpret_cast<__nv_bfloat16*>(a.o);
   p.ldo = a.ldo;
   p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)BT));
+  p.c = 1;
+  p.pairs = 0;
   p.err = a.err;
+  if (a.nq == 1) return attention_token(a, p, s);
+  if (encode_tmap_2d_bf16(&tq, a.q, (uint64_t)a.heads * BT, (uint64_t)a.nq, (uint64_t)a.ldq * 2, 64, BT) ||
+      encode_tmap_2d_bf16(&tk, a.k, kw, (uint64_t)a.nk, (uint64_t)a.ldk * 2, 64, BT) ||
+      encode_tmap_2d_bf16(&tv, a.v, (uint64_t)a.nk, kw, (uint64_t)a.vpad * 2, 64, BT))
+    return cudaErrorInvalidValue;
   long pairs;
   const int c = blocks_split(p.units, a.keep, &pairs);
   p.c = std::max(1, c);
