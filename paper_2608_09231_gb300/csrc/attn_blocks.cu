@@ -636,12 +636,26 @@ __global__ void __launch_bounds__(TK_TH, 2)
   }
 }
 
-// CTAs that share a head: as many as two to an SM leave room for, up to eight and a block each.
+static int g_token_clusters[TK_MAX_C + 1];  // clusters of 1 .. TK_MAX_C CTAs that run at once
+
+// CTAs that share a head, by the expected time (us; 12 shapes of 8 to 192 heads and 8 to 200 blocks
+// under every split): a CTA takes 1.5 a block, 2.1 where an SM holds two of them, and 2.5 go to the
+// start and the merge.  40 heads x 32 blocks: 49.1, 26.9, 19.8, 18.8, 17.3, 15.3, 22.8 and 20.4
+// shared by 1 .. 8.
 static int token_split(int heads, int keep) {
-  const long sms = sm_count();
-  int c = 1;
-  while (c < TK_MAX_C && 2 * c <= keep && (long)heads * 2 * c <= 2 * (sms - sms / 19 * (c >= 4 ? 4 : 1))) c *= 2;
-  return c;
+  int best = 1;
+  double least = 1e30;
+  for (int c = 1; c <= TK_MAX_C && c <= keep; ++c) {
+    const int at_once = std::max(1, g_token_clusters[c]);
+    const long waves = ((long)heads + at_once - 1) / at_once;
+    const double block = (long)std::min(heads, at_once) * c <= sm_count() ? 1.5 : 2.1;
+    const double us = (double)waves * ((keep + c - 1) / c) * block + 2.5;
+    if (us < least) {
+      least = us;
+      best = c;
+    }
+  }
+  return best;
 }
 
 static cudaError_t attention_token(const BlockAttnArgs& a, BlockAttnParams p, cudaStream_t s) {
@@ -660,6 +674,18 @@ cudaError_t attention_blocks_init() {
   cudaError_t r = cudaSuccess;
   for (const void* k : kernels)
     if (r == cudaSuccess) r = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, BT_SMEM);
+  for (int c = 1; c <= TK_MAX_C && r == cudaSuccess; ++c) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)c;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = (unsigned)(c * 1024);
+    cfg.blockDim = TK_TH;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    r = cudaOccupancyMaxActiveClusters(&g_token_clusters[c], attn_token_kernel<true>, &cfg);
+  }
   return r;
 }
 
