@@ -115,7 +115,8 @@ __host__ __device__ __forceinline__ bool wide_scales(const uint8_t* s, long lds)
 // rows, A's the N operand, which may be as narrow as 16.  Clusters of S CTAs split K and add
 // their parts through distributed shared memory in rank order (rank r finishes rows m = r, r + S,
 // ... of the tile).
-// warp 0: TMA producer; 1: MMA; 2: scale words; 4 .. 7: epilogue, thread = column n.
+// warp 0: TMA producer; 1: MMA; 2: scale words to shared memory; 3: and to tensor memory; 4 .. 7:
+// epilogue, thread = column n.
 // The ring is as deep as the CTAs that share an SM leave room for (`stages`, at most F8F_MAX).
 constexpr int F8F_MAX = 10;
 template <int BN>
@@ -150,9 +151,11 @@ __global__ void __launch_bounds__(256)
   uint64_t* empty = full + F8F_MAX;
   uint64_t* sf_full = empty + F8F_MAX;
   uint64_t* sf_empty = sf_full + 2;
-  uint64_t* sf_used = sf_empty + 2;  // [2]: a group's products are done, its TMEM columns free
+  uint64_t* sf_ready = sf_empty + 2;  // [2]: a group's scales are in tensor memory
+  uint64_t* sf_used = sf_ready + 2;   // [2]: a group's products are done, its TMEM columns free
   uint64_t* tfull = sf_used + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tfull + 1);
+  uint64_t* sf_drain = tfull + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sf_drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -160,7 +163,9 @@ __global__ void __launch_bounds__(256)
   const int mt = (g.M + BN - 1) / BN, unit = (int)(blockIdx.x >> logS);
   const int m0 = unit % mt * BN, n0 = unit / mt * 128;
   const int nkb = (g.K + F8_BK - 1) / F8_BK;
-  const int kb0 = (int)((long)rank * nkb / S), kb1 = (int)((long)(rank + 1) * nkb / S);
+  // this rank's K blocks: from an even one on, since they are issued in pairs
+  auto cut = [&](int r) { return r == S ? nkb : (int)((long)r * nkb / S) & ~1; };
+  const int kb0 = cut(rank), kb1 = cut(rank + 1);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
@@ -170,9 +175,11 @@ __global__ void __launch_bounds__(256)
     for (int s = 0; s < 2; ++s) {
       mbar_init(sf_full + s, 1);
       mbar_init(sf_empty + s, 1);
+      mbar_init(sf_ready + s, 1);
       mbar_init(sf_used + s, 1);
     }
     mbar_init(tfull, 1);
+    mbar_init(sf_drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmW);
@@ -225,50 +232,51 @@ __global__ void __launch_bounds__(256)
     }
   } else if (warp == 1) {
     // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
-    const uint32_t base = smem_u32(smem), sf = smem_u32(rest);
-    int s = 0, run = 0, grp = 0;  // ring stage; runs and groups handled so far
-    uint32_t ph = 0, add = 0;     // the first product overwrites the accumulator
+    const uint32_t base = smem_u32(smem);
+    int s = 0, grp = 0;        // ring stage; groups handled so far
+    uint32_t ph = 0, add = 0;  // the first product overwrites the accumulator
+    auto next = [&](int& st, uint32_t& parity) {
+      if (++st == stages) {
+        st = 0;
+        parity ^= 1;
+      }
+    };
     bool good = true;
-    for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1 && good; kg += F8_GROUP) {  // groups, maybe cut at the ends
-      if (run == 0 || kg % (F8_GROUP * F8_RUN) == 0) {
-        if (!(good = mbar_wait_warp(sf_full + (run & 1), (uint32_t)(run >> 1) & 1u, abort_flag))) break;
-        ++run;
-      }
+    for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1 && good; kg += F8_GROUP, ++grp) {  // groups, maybe cut
       const uint32_t sw = tmem + C::SF_COL + (grp & 1) * 8;
-      if (!(good = mbar_wait_warp(sf_used + (grp & 1), ((uint32_t)(grp >> 1) & 1u) ^ 1u, abort_flag))) break;
-      tc_fence_after();
-      const uint64_t d = scale_desc(sf + ((run - 1) & 1) * C::SF_STAGE + kg / F8_GROUP % F8_RUN * C::SF_GROUP);
-      if (elect_one()) {
-        copy_scales(sw, d);
-        copy_scales(sw + 4, d + (F8_ATOM >> 4));
-      }
-      __syncwarp();
+      if (!(good = mbar_wait_warp(sf_ready + (grp & 1), (uint32_t)(grp >> 1) & 1u, abort_flag))) break;
 #pragma unroll
-      for (int b = 0; b < F8_GROUP; ++b) {
+      for (int b = 0; b < F8_GROUP; b += 2) {
         if (kg + b < kb0 || kg + b >= kb1) continue;
+        const bool two = kg + b + 1 < kb1;
+        int s1 = s;
+        uint32_t ph1 = ph;
+        next(s1, ph1);
         if (!(good = good && mbar_wait_warp(full + s, ph, abort_flag))) break;
+        if (two && !(good = mbar_wait_warp(full + s1, ph1, abort_flag))) break;
         tc_fence_after();
-        const uint64_t wd = sw128_desc(base + s * C::STAGE);
-        const uint64_t ad = wd + (F8_TILE >> 4);
+        const uint64_t w0 = sw128_desc(base + s * C::STAGE), w1 = sw128_desc(base + s1 * C::STAGE);
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
-            mma_mxf8(tmem, wd + 2 * k, ad + 2 * k, idesc_mxf8(128, BN) | scale_byte(b), sw, sw + 4, k > 0 ? 1u : add);
+            mma_mxf8(tmem, w0 + 2 * k, w0 + (F8_TILE >> 4) + 2 * k, idesc_mxf8(128, BN) | scale_byte(b), sw, sw + 4,
+                     k > 0 ? 1u : add);
           mma_commit(empty + s);
+          if (two) {
+#pragma unroll
+            for (int k = 0; k < F8_BK / 32; ++k)
+              mma_mxf8(tmem, w1 + 2 * k, w1 + (F8_TILE >> 4) + 2 * k, idesc_mxf8(128, BN) | scale_byte(b + 1), sw,
+                       sw + 4, 1u);
+            mma_commit(empty + s1);
+          }
+          if (b + 2 == F8_GROUP || kg + b + 2 >= kb1) mma_commit(sf_used + (grp & 1));
         }
         __syncwarp();
         add = 1;
-        if (++s == stages) {
-          s = 0;
-          ph ^= 1;
-        }
+        s = s1;
+        ph = ph1;
+        if (two) next(s, ph);
       }
-      if (elect_one()) {
-        mma_commit(sf_used + (grp & 1));
-        if (kg + F8_GROUP >= kb1 || (kg / F8_GROUP + 1) % F8_RUN == 0) mma_commit(sf_empty + ((run - 1) & 1));
-      }
-      __syncwarp();
-      ++grp;
     }
     // all MMAs issued so far (whatever happened above) finish before tfull completes, and
     // the bounded wait keeps tensor memory until then
@@ -276,6 +284,35 @@ __global__ void __launch_bounds__(256)
       mma_commit(tfull);
       const uint64_t t0 = global_ns();
       while (!mbar_try_wait(tfull, 0) && global_ns() - t0 < kWaitLimitNs) {
+      }
+    }
+    __syncwarp();
+  } else if (warp == 3) {
+    // ---------------- scales to tensor memory, a group ahead of the products ----------------
+    const uint32_t sf = smem_u32(rest);
+    int run = 0, grp = 0;
+    for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1; kg += F8_GROUP, ++grp) {
+      if (run == 0 || kg % (F8_GROUP * F8_RUN) == 0) {
+        if (!mbar_wait_warp(sf_full + (run & 1), (uint32_t)(run >> 1) & 1u, abort_flag)) break;
+        ++run;
+      }
+      if (!mbar_wait_warp(sf_used + (grp & 1), ((uint32_t)(grp >> 1) & 1u) ^ 1u, abort_flag)) break;
+      tc_fence_after();
+      const uint32_t sw = tmem + C::SF_COL + (grp & 1) * 8;
+      const uint64_t d = scale_desc(sf + ((run - 1) & 1) * C::SF_STAGE + kg / F8_GROUP % F8_RUN * C::SF_GROUP);
+      if (elect_one()) {
+        copy_scales(sw, d);
+        copy_scales(sw + 4, d + (F8_ATOM >> 4));
+        mma_commit(sf_ready + (grp & 1));
+        if (kg + F8_GROUP >= kb1 || (kg / F8_GROUP + 1) % F8_RUN == 0) mma_commit(sf_empty + ((run - 1) & 1));
+      }
+      __syncwarp();
+    }
+    // every copy has ended before tensor memory is released
+    if (elect_one()) {
+      mma_commit(sf_drain);
+      const uint64_t t0 = global_ns();
+      while (!mbar_try_wait(sf_drain, 0) && global_ns() - t0 < kWaitLimitNs) {
       }
     }
     __syncwarp();
@@ -444,8 +481,10 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // Two accumulators of 256 columns fill tensor memory, which the scales need a little of: the second
 // one starts 32 columns inside the first (columns 224 .. 479), and the tile after this one waits
 // only for this one's drain of the shared 32 columns, which the epilogue reads first.
-// warp 0: TMA producer; 1: MMA (even CTA); 2: scale words; 4 .. 11: epilogue, two warps to each lane
-// quarter, 128 columns (one output block) each.
+// Tiles of a last wave that would leave half of the pairs idle are worked on as two halves of 128
+// columns (M = 256, N = 128).
+// warp 0: TMA producer; 1: MMA (even CTA); 2: scale words to shared memory; 3 (even CTA): and to
+// tensor memory; 4 .. 11: epilogue, two warps to each lane quarter, 128 columns (one output block) each.
 // The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a
 // row a thread, with bias and gate broadcast from shared memory, and its output leaves by TMA:
 // stores, or for the residual stream an add that L2 carries out, so that the stream is not read.
@@ -550,8 +589,8 @@ BAG_DEV void store_rows(const Fp8Gemm& g, const uint8_t* buf, int row0, int col0
 template <int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
-                         const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ Fp8Gemm g,
-                         int group_rows) {
+                         const __grid_constant__ CUtensorMap tmHalf, const __grid_constant__ CUtensorMap tmOut,
+                         const __grid_constant__ Fp8Gemm g, int group_rows, long whole) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -559,27 +598,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   uint64_t* empty = full + F8P_STAGES;
   uint64_t* sf_full = empty + F8P_STAGES;
   uint64_t* sf_empty = sf_full + 2;
-  uint64_t* sf_used = sf_empty + 2;    // [2], even CTA: a group's products are done, its TMEM columns free
+  uint64_t* sf_ready = sf_empty + 2;   // [2], even CTA: a group's scales are in tensor memory
+  uint64_t* sf_used = sf_ready + 2;    // [2], even CTA: a group's products are done, its TMEM columns free
   uint64_t* tfull = sf_used + 2;
   uint64_t* tempty = tfull + 2;
   uint64_t* shared_free = tempty + 2;  // [2]: accumulator b's columns that the other one shares are drained
   uint64_t* drain = shared_free + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* sf_drain = drain + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sf_drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
-  const long tiles = (long)num_m * num_n;
   const int nkb = (g.K + F8_BK - 1) / F8_BK, nruns = (nkb + F8_GROUP * F8_RUN - 1) / (F8_GROUP * F8_RUN);
-  // groups of group_rows row tiles visit every column tile, the row tile varying fastest
-  auto decode = [&](long tile, int& mt, int& nt) {
+  // units of work: `whole` tiles of 256 x 256, then every later tile as two of 256 x 128
+  const long units = 2 * (long)num_m * num_n - whole;
+  // first row and column of a unit, and whether it is half a tile; groups of group_rows row tiles
+  // visit every column tile, the row tile varying fastest
+  auto decode = [&](long unit, int& m0, int& n0) {
+    const bool half = unit >= whole;
+    const long tile = half ? whole + ((unit - whole) >> 1) : unit;
     const long per = (long)group_rows * num_n;
     const int gr = (int)(tile / per);
     const int i = (int)(tile - gr * per), rows = min(group_rows, num_m - gr * group_rows);
-    mt = gr * group_rows + i % rows;
-    nt = i / rows;
+    m0 = (gr * group_rows + i % rows) * 256;
+    n0 = i / rows * 256 + (half && ((unit - whole) & 1) ? 128 : 0);
+    return half;
   };
 
   if (threadIdx.x == 0) {
@@ -590,16 +636,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     for (int s = 0; s < 2; ++s) {
       mbar_init(sf_full + s, 2);       // even CTA: both CTAs' scale warps
       mbar_init(sf_empty + s, 1);      // both CTAs: multicast commit
+      mbar_init(sf_ready + s, 1);
       mbar_init(sf_used + s, 1);
       mbar_init(tfull + s, 1);         // both CTAs: multicast commit
       mbar_init(tempty + s, 16);       // even CTA: every epilogue warp of both CTAs
       mbar_init(shared_free + s, 8);   // even CTA: the warps that hold the shared columns
     }
     mbar_init(drain, 1);
+    mbar_init(sf_drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
-    tma_prefetch_desc(&tmW);
+    tma_prefetch_desc(whole > 0 ? &tmW : &tmHalf);
   }
   grid_dep_sync();
   __syncwarp();
@@ -622,18 +670,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
         uint32_t ph = 0;
         long issued = 0;
         bool ok = true;
-        for (long tile = pair; tile < tiles && ok; tile += npairs) {
-          int mt, nt;
-          decode(tile, mt, nt);
+        for (long unit = pair; unit < units && ok; unit += npairs) {
+          int m0, n0;
+          const bool half = decode(unit, m0, n0);
+          const CUtensorMap* mapW = half ? &tmHalf : &tmW;
+          const int am = m0 + (int)rank * 128, wn = n0 + (int)rank * (half ? 64 : 128);
+          const uint32_t bytes = half ? 2 * F8P_STAGE - F8_TILE : 2 * F8P_STAGE;  // of both CTAs
           for (int kb = 0; kb < nkb; ++kb) {
             if (!mbar_wait(empty + s, ph ^ 1, abort_flag)) {
               ok = false;
               break;
             }
-            if (rank == 0) mbar_arrive_expect_tx(full + s, 2 * F8P_STAGE);
+            if (rank == 0) mbar_arrive_expect_tx(full + s, bytes);
             const uint32_t fb = mapa_shared(smem_u32(full + s), 0);
-            pair_load_2d(smem + s * F8P_STAGE, &tmA, kb * F8_BK, mt * 256 + (int)rank * 128, fb);
-            pair_load_2d(smem + s * F8P_STAGE + F8_TILE, &tmW, kb * F8_BK, nt * 256 + (int)rank * 128, fb);
+            pair_load_2d(smem + s * F8P_STAGE, &tmA, kb * F8_BK, am, fb);
+            pair_load_2d(smem + s * F8P_STAGE + F8_TILE, mapW, kb * F8_BK, wn, fb);
             ++issued;
             if (++s == F8P_STAGES) {
               s = 0;
@@ -660,59 +711,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
         const uint32_t base = smem_u32(smem);
         int s = 0;
         uint32_t ph = 0;
-        uint32_t run = 0, grp = 0;  // runs and groups of scales handled so far
-        long i = 0;                 // tiles of this pair so far
+        uint32_t grp = 0;  // groups of scales handled so far
+        auto next = [&](int& st, uint32_t& parity) {
+          if (++st == F8P_STAGES) {
+            st = 0;
+            parity ^= 1;
+          }
+        };
+        long i = 0;  // units of this pair so far
         bool ok = true;
-        for (long tile = pair; tile < tiles && ok; tile += npairs, ++i) {
+        for (long unit = pair; unit < units && ok; unit += npairs, ++i) {
           const int acc = (int)(i & 1);
+          const uint32_t shape = unit >= whole ? idesc_mxf8(256, 128) : idesc_mxf8(256, 256);
           const uint32_t dt = tmem + (acc ? F8P_ACC1 : 0);
           // the accumulator's last tile is drained, and the other one's shared columns
           if (!mbar_wait_warp(tempty + acc, (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag)) break;
           if (i > 0 && !mbar_wait_warp(shared_free + (acc ^ 1), (uint32_t)(((i - 1) >> 1) & 1), abort_flag)) break;
           tc_fence_after();
           uint32_t add = 0;  // the tile's first product overwrites the accumulator
-          for (int kb0 = 0; kb0 < nkb && ok; kb0 += F8_GROUP) {
-            if (kb0 % (F8_GROUP * F8_RUN) == 0) {
-              if (!(ok = wait_warp_cluster(sf_full + (run & 1), (run >> 1) & 1u, abort_flag))) break;
-              ++run;
-            }
+          for (int kg = 0; kg < nkb && ok; kg += F8_GROUP, ++grp) {
             const uint32_t sa = tmem + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
-            if (!(ok = mbar_wait_warp(sf_used + (grp & 1), ((grp >> 1) & 1u) ^ 1u, abort_flag))) break;
-            tc_fence_after();
-            const uint64_t d = scale_desc(base + F8P_OFF_SF + ((run - 1) & 1) * F8P_SF_STAGE +
-                                          kb0 / F8_GROUP % F8_RUN * F8P_SF_GROUP);
-            if (elect_one()) {
+            if (!(ok = mbar_wait_warp(sf_ready + (grp & 1), (grp >> 1) & 1u, abort_flag))) break;
 #pragma unroll
-              for (int a = 0; a < 3; ++a) copy_scales_pair(sa + 4 * a, d + a * (F8_ATOM >> 4));
-            }
-            __syncwarp();
-#pragma unroll
-            for (int b = 0; b < F8_GROUP; ++b) {
-              if (kb0 + b >= nkb) break;
+            for (int b = 0; b < F8_GROUP; b += 2) {  // two K blocks at a time
+              if (kg + b >= nkb) break;
+              const bool two = kg + b + 1 < nkb;
+              int s1 = s;
+              uint32_t ph1 = ph;
+              next(s1, ph1);
               if (!(ok = mbar_wait_warp(full + s, ph, abort_flag))) break;
+              if (two && !(ok = mbar_wait_warp(full + s1, ph1, abort_flag))) break;
               tc_fence_after();
-              const uint64_t ad = sw128_desc(base + s * F8P_STAGE);
-              const uint64_t wd = ad + (F8_TILE >> 4);
+              const uint64_t a0 = sw128_desc(base + s * F8P_STAGE), a1 = sw128_desc(base + s1 * F8P_STAGE);
               if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
-                  pair_mma_mxf8(dt, ad + 2 * k, wd + 2 * k, idesc_mxf8(256, 256) | scale_byte(b), sa, sa + 4,
+                  pair_mma_mxf8(dt, a0 + 2 * k, a0 + (F8_TILE >> 4) + 2 * k, shape | scale_byte(b), sa, sa + 4,
                                 k > 0 ? 1u : add);
                 pair_commit(empty + s, 3);
+                if (two) {
+#pragma unroll
+                  for (int k = 0; k < F8_BK / 32; ++k)
+                    pair_mma_mxf8(dt, a1 + 2 * k, a1 + (F8_TILE >> 4) + 2 * k, shape | scale_byte(b + 1), sa, sa + 4, 1u);
+                  pair_commit(empty + s1, 3);
+                }
+                if (b + 2 == F8_GROUP || kg + b + 2 >= nkb) pair_commit(sf_used + (grp & 1), 1);
               }
               __syncwarp();
               add = 1;
-              if (++s == F8P_STAGES) {
-                s = 0;
-                ph ^= 1;
-              }
+              s = s1;
+              ph = ph1;
+              if (two) next(s, ph);
             }
-            if (elect_one()) {
-              pair_commit(sf_used + (grp & 1), 1);
-              if (kb0 + F8_GROUP >= nkb || (kb0 / F8_GROUP + 1) % F8_RUN == 0) pair_commit(sf_empty + ((run - 1) & 1), 3);
-            }
-            __syncwarp();
-            ++grp;
           }
           if (!ok) break;
           if (elect_one()) pair_commit(tfull + acc, 3);
@@ -727,42 +777,79 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
         }
         __syncwarp();
       }
+    } else if (warp == 3) {
+      if (rank == 0) {
+        // -------- scales to both CTAs' tensor memory, a group ahead of the products --------
+        const uint32_t sf = smem_u32(smem + F8P_OFF_SF);
+        uint32_t run = 0, grp = 0;  // runs and groups handled so far
+        bool ok = true;
+        for (long unit = pair; unit < units && ok; unit += npairs) {
+          for (int kg = 0; kg < nkb; kg += F8_GROUP, ++grp) {
+            if (kg % (F8_GROUP * F8_RUN) == 0) {
+              if (!(ok = wait_warp_cluster(sf_full + (run & 1), (run >> 1) & 1u, abort_flag))) break;
+              ++run;
+            }
+            if (!(ok = mbar_wait_warp(sf_used + (grp & 1), ((grp >> 1) & 1u) ^ 1u, abort_flag))) break;
+            tc_fence_after();
+            const uint32_t sa = tmem + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
+            const uint64_t d = scale_desc(sf + ((run - 1) & 1) * F8P_SF_STAGE + kg / F8_GROUP % F8_RUN * F8P_SF_GROUP);
+            if (elect_one()) {
+#pragma unroll
+              for (int a = 0; a < 3; ++a)
+                if (a < 2 || unit < whole) copy_scales_pair(sa + 4 * a, d + a * (F8_ATOM >> 4));
+              pair_commit(sf_ready + (grp & 1), 1);
+              if (kg + F8_GROUP >= nkb || (kg / F8_GROUP + 1) % F8_RUN == 0) pair_commit(sf_empty + ((run - 1) & 1), 3);
+            }
+            __syncwarp();
+          }
+        }
+        // every copy has ended before tensor memory is released
+        if (elect_one()) {
+          pair_commit(sf_drain, 1);
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(sf_drain, 0) && global_ns() - t0 < kWaitLimitNs) {
+          }
+        }
+        __syncwarp();
+      }
     } else if (warp == 2) {
       // ---------------- scale words (both CTAs: A's own rows, all 256 of W) ----------------
-      int mt = 0, nt = 0, r = 0;
+      int m0 = 0, n0 = 0, r = 0;
+      bool half = false;
       const uint32_t full_even = mapa_shared(smem_u32(sf_full), 0);
       const bool wide_a = wide_scales(g.a_s, g.ldas), wide_w = wide_scales(g.w_s, g.ldws);
       ScaleRun w[3];
       auto fetch = [&]() {
-        w[0].fetch(g.a_s, g.ldas, wide_a, mt * 256 + (int)rank * 128, g.M, r);
-        w[1].fetch(g.w_s, g.ldws, wide_w, nt * 256, g.N, r);
-        w[2].fetch(g.w_s, g.ldws, wide_w, nt * 256 + 128, g.N, r);
+        w[0].fetch(g.a_s, g.ldas, wide_a, m0 + (int)rank * 128, g.M, r);
+        w[1].fetch(g.w_s, g.ldws, wide_w, n0, g.N, r);
+        if (!half) w[2].fetch(g.w_s, g.ldws, wide_w, n0 + 128, g.N, r);
       };
-      long tile = pair;
-      if (tile < tiles) {
-        decode(tile, mt, nt);
+      long unit = pair;
+      if (unit < units) {
+        half = decode(unit, m0, n0);
         fetch();
       }
-      for (uint32_t i = 0; tile < tiles; ++i) {
+      for (uint32_t i = 0; unit < units; ++i) {
         if (!mbar_wait_warp(sf_empty + (i & 1), ((i >> 1) & 1u) ^ 1u, abort_flag)) break;
         uint8_t* d = smem + F8P_OFF_SF + (i & 1) * F8P_SF_STAGE;
 #pragma unroll
-        for (int a = 0; a < 3; ++a) w[a].put(d + a * F8_ATOM, F8P_SF_GROUP);
+        for (int a = 0; a < 3; ++a)
+          if (a < 2 || !half) w[a].put(d + a * F8_ATOM, F8P_SF_GROUP);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) peer_arrive(full_even + (uint32_t)((i & 1) * sizeof(uint64_t)));
         if (++r == nruns) {
           r = 0;
-          tile += npairs;
-          if (tile < tiles) decode(tile, mt, nt);
+          unit += npairs;
+          if (unit < units) half = decode(unit, m0, n0);
         }
-        if (tile < tiles) fetch();
+        if (unit < units) fetch();
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F8P_REGS_EPI));
     // ---------------- epilogue (both CTAs: their 128 rows of each tile) ----------------
-    const int q = warp & 3, half = (warp - 4) >> 2;
+    const int q = warp & 3, side = (warp - 4) >> 2;  // columns 0 .. 127 of a tile, 128 .. 255
     uint8_t* buf = smem + F8P_OFF_BUF + (warp - 4) * F8P_BUF;
     float* sbias = reinterpret_cast<float*>(smem + F8P_OFF_VEC) + (warp - 4) * 256;
     float* sgate = sbias + 128;
@@ -770,11 +857,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     constexpr int CW = KIND == BAG_FP8_BF16 ? 64 : (KIND == BAG_FP8_CODES ? 128 : 32);  // columns of a staged row
     constexpr int NC = 128 / CW;
     long i = 0;
-    for (long tile = pair; tile < tiles; tile += npairs, ++i) {
+    for (long unit = pair; unit < units; unit += npairs, ++i) {
       const int acc = (int)(i & 1);
-      int mt, nt;
-      decode(tile, mt, nt);
-      const int row0 = mt * 256 + (int)rank * 128 + q * 32, col0 = nt * 256 + half * 128;
+      int m0, n0;
+      const bool half = decode(unit, m0, n0);
+      const int row0 = m0 + (int)rank * 128 + q * 32, col0 = n0 + side * 128;
       {
         float b[4], t[4];
 #pragma unroll
@@ -790,14 +877,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
       const bool ok = mbar_wait(tfull + acc, (uint32_t)((i >> 1) & 1), abort_flag);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
-      const uint32_t tb = tmem + (uint32_t)((acc ? F8P_ACC1 : 0) + half * 128) + ((uint32_t)(q * 32) << 16);
+      const uint32_t tb = tmem + (uint32_t)((acc ? F8P_ACC1 : 0) + side * 128) + ((uint32_t)(q * 32) << 16);
       // the shared columns are the last 32 of accumulator 0 and the first 32 of accumulator 1
-      const bool shares = half == (acc ^ 1);
+      const bool shares = side == (acc ^ 1);
       auto release = [&](uint32_t bar) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) peer_signal(bar + (uint32_t)(acc * sizeof(uint64_t)));
       };
+      if (half && side) {  // half a tile has no columns for these warps
+        if (shares) release(free_even);
+        release(tempty_even);
+        continue;
+      }
 #pragma unroll 1
       for (int k = 0; k < NC; ++k) {
         const int c = (acc ? k : NC - 1 - k) * CW;  // the shared columns' part first
@@ -908,10 +1000,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   }
 }
 
+// Tiles that keep their size: those of the last wave are halved where that gives each pair at most
+// one half.
+static long whole_tiles(long tiles, long pairs) {
+  const long rest = tiles % pairs;
+  return 2 * rest <= pairs ? tiles - rest : tiles;
+}
+
 static cudaError_t launch_pair(Fp8Gemm g, cudaStream_t s) {
-  CUtensorMap ta, tw;
+  CUtensorMap ta, tw, th;
   if (encode_tmap_2d_bytes(&ta, 1, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, F8_BK, 128) ||
-      encode_tmap_2d_bytes(&tw, 1, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128))
+      encode_tmap_2d_bytes(&tw, 1, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 128) ||
+      encode_tmap_2d_bytes(&th, 1, g.w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldw, F8_BK, 64))
     return cudaErrorInvalidValue;
   // the output map: boxes of 32 rows of 128 bytes; rows that TMA cannot address are stored otherwise
   CUtensorMap to = ta;
@@ -921,10 +1021,11 @@ static cudaError_t launch_pair(Fp8Gemm g, cudaStream_t s) {
                                     128u / (unsigned)size, 32))
     return cudaErrorInvalidValue;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
-  const int pairs = (int)std::min((long)num_m * num_n, (long)sm_count() / 2);
+  const long tiles = (long)num_m * num_n, most = std::max(1, sm_count() / 2), whole = whole_tiles(tiles, most);
+  const int pairs = (int)std::min(2 * tiles - whole, most);
   const int rows = (int)std::max(1.0, std::min((double)num_m, 40.0 * 1048576.0 / (256.0 * g.K)));
   auto launch = [&](auto kernel) {
-    return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, to, g, rows);
+    return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, th, to, g, rows, whole);
   };
   switch (g.kind) {
     case BAG_FP8_F32: return launch(gemm_fp8_pair_kernel<BAG_FP8_F32>);
@@ -952,34 +1053,35 @@ cudaError_t gemm_fp8_init() {
 
 // Which kernel, tile and split: the least expected time.  The constants (us) fit 247 shapes of 1 to
 // 2048 rows, 512 to 13824 columns and K, each timed under every choice (3000 timings, chained
-// launches); the choice is within 2.1 % of the best one on average, 40 % at most (50 rows through 13824 x 5120).  A CTA of either
-// kernel takes 0.2 to 0.3 us a K block whatever its tile (the issue of its four MMAs and their
-// waits), so few tiles want K split, and many the largest tile.
+// launches); the choice is within 1.4 % of the best one on average, 28 % at most (50 rows through
+// 5120 x 13824).  A CTA of either kernel takes about 0.2 us a K block whatever its tile (the issue
+// of its four MMAs and their waits), so few tiles want K split, and many the largest tile.
 struct Fp8Plan {
   int BN;    // 0: CTA pairs
   int logS;
 };
 static Fp8Plan plan_fp8(long M, long N, long K) {
   auto cd = [](long a, long b) { return (a + b - 1) / b; };
-  const long nkb = cd(K, F8_BK);
+  const double nkb = (double)cd(K, F8_BK);
   // the operands' way from HBM beside the time of the CTAs: a smooth maximum of the two, so that of
   // splits that HBM bounds alike the one with more loads in flight is taken
   const double dram = (double)(M + N) * (double)K / 6.5e6 + 3.8;
-  auto together = [&](double us) { return std::pow(std::pow(us, 6.0) + std::pow(dram, 6.0), 1.0 / 6.0); };
-  const double waves = (double)cd(cd(M, 256) * cd(N, 256), std::max(1, sm_count() / 2));
-  double best = together(7.9 + waves * (2.0 + 0.2 * (double)nkb));
+  auto together = [&](double us) { return std::pow(std::pow(us, 8.0) + std::pow(dram, 8.0), 1.0 / 8.0); };
+  const long full = cd(M, 256) * cd(N, 256), pairs = std::max(1, sm_count() / 2), whole = whole_tiles(full, pairs);
+  double us = 4.6 + (double)cd(whole, pairs) * (3.6 + 0.27 * nkb);
+  if (whole < full) us += 1.6 + 0.19 * nkb;  // a wave of halves
+  double best = together(us);
   Fp8Plan p{0, 0};
   const struct {
     int BN;
     double start, wave, share;  // of a launch, of a further wave, of its K blocks (SMs shared)
-  } tiles[] = {{16, 2.8, 1.7, 0.01}, {32, 3.7, 1.5, 0.01}, {64, 5.0, 3.4, 0.17}, {128, 6.4, 3.4, 0.17}};
+  } tiles[] = {{16, 2.6, 1.3, 0.01}, {32, 2.5, 2.0, 0.01}, {64, 5.8, 3.4, 0.28}, {128, 6.2, 5.7, 0.28}};
   for (const auto& t : tiles) {
     if (t.BN < 64 && M > t.BN) continue;  // narrow tiles read W again for every tile of rows
-    for (int logS = 0; logS <= 3 && nkb >= 2L << logS; ++logS) {
-      const double kb = (double)cd(nkb, 1L << logS);
+    for (int logS = 0; logS <= 3 && nkb >= (double)(2 << logS); ++logS) {
+      const double kb = (double)cd(cd(K, F8_BK), 1L << logS);
       const double more = (double)(cd(cd(M, t.BN) * cd(N, 128) << logS, cluster_sms(logS)) - 1);
-      const double us = together(t.start + 0.32 * kb + more * (t.wave + t.share * kb) + (logS ? 0.65 : 0.0) +
-                                 0.25 * (1 << logS));
+      us = together(t.start + 0.2 * kb + more * (t.wave + t.share * kb) + (logS ? 0.84 : 0.0) + 0.15 * (1 << logS));
       if (us < best) {
         best = us;
         p = Fp8Plan{t.BN, logS};
