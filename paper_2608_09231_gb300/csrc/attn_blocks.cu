@@ -216,7 +216,9 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
     } else if (warp == 1 && most > 0) {
       // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
       constexpr uint32_t idesc = F16 ? idesc_f16_f32(BT, BT) : idesc_bf16_f32(BT, BT);
-      const uint32_t q_addr = smem_u32(smem), r_addr = smem_u32(ring);
+      const uint32_t q_addr = smem_u32(smem), r_addr = smem_u32(ring), tm = uniform(tmem);
+      const int len[2] = {(int)uniform((uint32_t)n[0]), (int)uniform((uint32_t)n[1])};
+      const int longest = max(len[0], len[1]);
       // K step kk of a tile: 64-column chunk kk / 4, 32 bytes per step inside it (16-byte units)
       auto koff = [](int kk) { return (uint64_t)(((kk >> 2) * BT_CHUNK + (kk & 3) * 32) >> 4); };
       int s = 0;
@@ -239,7 +241,7 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < BT / 16; ++kk)
-            mma_bf16(tmem + x * 128, qd + koff(kk), kd + koff(kk), idesc, kk > 0 ? 1u : 0u);
+            mma_bf16(tm + x * 128, qd + koff(kk), kd + koff(kk), idesc, kk > 0 ? 1u : 0u);
           mma_commit(s_full + x);
           mma_commit(empty + s);
         }
@@ -253,10 +255,10 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < BT / 16; ++kk)
-            mma_bf16_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + koff(kk), idesc,
+            mma_bf16_ts(tm + 256 + x * 128, tm + x * 128 + kk * 8, vd + koff(kk), idesc,
                         (j > 0 || kk > 0) ? 1u : 0u);
           mma_commit(empty + s);
-          if (j + 1 == n[x]) mma_commit(o_done + x);
+          if (j + 1 == len[x]) mma_commit(o_done + x);
         }
         __syncwarp();
         next();
@@ -265,13 +267,13 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
       bool ok = wait(q_full, 0);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        if (n[x] > 0) ok = ok && issue_s(x);
-      for (int j = 0; j < most && ok; ++j) {
+        if (len[x] > 0) ok = ok && issue_s(x);
+      for (int j = 0; j < longest && ok; ++j) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          if (j >= n[x] || !ok) continue;
+          if (j >= len[x] || !ok) continue;
           ok = wait(p_full + x, j & 1) && issue_pv(x, j);
-          if (ok && j + 1 < n[x]) ok = issue_s(x);
+          if (ok && j + 1 < len[x]) ok = issue_s(x);
         }
       }
       if (elect_one()) {

@@ -5,6 +5,11 @@
 
 namespace bag {
 
+// A value that all lanes of a converged warp hold, in a uniform register: the reduction writes one,
+// and what is computed from it stays there.  For what comes out of shared memory (the address of
+// tensor memory, the length of a list) and goes into the operands of every MMA.
+BAG_DEV uint32_t uniform(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
+
 BAG_DEV float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attn_common.cuh"
 #include "lowbit.cuh"
 #include "bag.h"
 #include "kernels.h"
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(256)
     }
   } else if (warp == 1) {
     // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
-    const uint32_t base = smem_u32(smem);
+    const uint32_t base = smem_u32(smem), tm = uniform(tmem);
     int s = 0, grp = 0;        // ring stage; groups handled so far
     uint32_t ph = 0, add = 0;  // the first product overwrites the accumulator
     auto next = [&](int& st, uint32_t& parity) {
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(256)
     };
     bool good = true;
     for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1 && good; kg += F8_GROUP, ++grp) {  // groups, maybe cut
-      const uint32_t sw = tmem + C::SF_COL + (grp & 1) * 8;
+      const uint32_t sw = tm + C::SF_COL + (grp & 1) * 8;
       if (!(good = mbar_wait_warp(sf_ready + (grp & 1), (uint32_t)(grp >> 1) & 1u, abort_flag))) break;
 #pragma unroll
       for (int b = 0; b < F8_GROUP; b += 2) {
@@ -259,13 +260,13 @@ __global__ void __launch_bounds__(256)
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
-            mma_mxf8(tmem, w0 + 2 * k, w0 + (F8_TILE >> 4) + 2 * k, idesc_mxf8(128, BN) | scale_byte(b), sw, sw + 4,
+            mma_mxf8(tm, w0 + 2 * k, w0 + (F8_TILE >> 4) + 2 * k, idesc_mxf8(128, BN) | scale_byte(b), sw, sw + 4,
                      k > 0 ? 1u : add);
           mma_commit(empty + s);
           if (two) {
 #pragma unroll
             for (int k = 0; k < F8_BK / 32; ++k)
-              mma_mxf8(tmem, w1 + 2 * k, w1 + (F8_TILE >> 4) + 2 * k, idesc_mxf8(128, BN) | scale_byte(b + 1), sw,
+              mma_mxf8(tm, w1 + 2 * k, w1 + (F8_TILE >> 4) + 2 * k, idesc_mxf8(128, BN) | scale_byte(b + 1), sw,
                        sw + 4, 1u);
             mma_commit(empty + s1);
           }
@@ -708,7 +709,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     } else if (warp == 1) {
       if (rank == 0) {
         // -------- MMA issuer (even CTA; converged warp, one elected lane issues) --------
-        const uint32_t base = smem_u32(smem);
+        const uint32_t base = smem_u32(smem), tm = uniform(tmem);
         int s = 0;
         uint32_t ph = 0;
         uint32_t grp = 0;  // groups of scales handled so far
@@ -723,14 +724,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
         for (long unit = pair; unit < units && ok; unit += npairs, ++i) {
           const int acc = (int)(i & 1);
           const uint32_t shape = unit >= whole ? idesc_mxf8(256, 128) : idesc_mxf8(256, 256);
-          const uint32_t dt = tmem + (acc ? F8P_ACC1 : 0);
+          const uint32_t dt = tm + (acc ? F8P_ACC1 : 0);
           // the accumulator's last tile is drained, and the other one's shared columns
           if (!mbar_wait_warp(tempty + acc, (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag)) break;
           if (i > 0 && !mbar_wait_warp(shared_free + (acc ^ 1), (uint32_t)(((i - 1) >> 1) & 1), abort_flag)) break;
           tc_fence_after();
           uint32_t add = 0;  // the tile's first product overwrites the accumulator
           for (int kg = 0; kg < nkb && ok; kg += F8_GROUP, ++grp) {
-            const uint32_t sa = tmem + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
+            const uint32_t sa = tm + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
             if (!(ok = mbar_wait_warp(sf_ready + (grp & 1), (grp >> 1) & 1u, abort_flag))) break;
 #pragma unroll
             for (int b = 0; b < F8_GROUP; b += 2) {  // two K blocks at a time

@@ -141,6 +141,52 @@ def test_attention_blocks(nq, nk, heads, kv_heads, keep, dtype, pad, ctx):
     check(got, ref, dtype)
 
 
+@pytest.mark.parametrize("how", ["equal", "alike", "disjoint", "twice", "shorter"])
+@pytest.mark.parametrize("heads,kv_heads,nq,nk", [(40, 40, 1300, 2500), (44, 11, 1281, 2432)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_of_neighbouring_lists(how, heads, kv_heads, nq, nk, dtype, ctx):
+    """Two lists a CTA that hold the same blocks, some of them, or none (with an odd number of units,
+    whose last has no neighbour); one that lists a block twice; one that ends early.  With key heads
+    that four query heads share, neighbours are of other heads too.  The last key block is short or
+    whole, and among the common blocks or not."""
+    g = np.random.default_rng(heads + len(how))
+    nqb, nkb, keep = -(-nq // 128), -(-nk // 128), 9
+    flat = np.zeros((heads * nqb, keep), np.int32)
+    for u in range(len(flat)):
+        if u % 2 == 0 or how == "twice":
+            a = np.sort(g.permutation(nkb)[:keep])
+        if how == "equal":
+            flat[u] = a
+        elif how == "alike":
+            b = a.copy()
+            if u % 2:
+                b[g.integers(0, keep, 3)] = g.permutation(np.setdiff1d(np.arange(nkb), a))[0]
+                b = np.unique(b)
+                b = np.sort(np.concatenate([b, g.permutation(np.setdiff1d(np.arange(nkb), b))[:keep - len(b)]]))
+            flat[u] = b
+        elif how == "disjoint":
+            flat[u] = a if u % 2 == 0 else np.sort(g.permutation(np.setdiff1d(np.arange(nkb), a))[:keep])
+        elif how == "twice":
+            flat[u] = a
+            if u % 3 == 0:
+                flat[u, 4] = flat[u, 2]
+        else:
+            flat[u] = a
+            flat[u, g.integers(0, keep + 1):] = -1
+    got, ref = attend(ctx, nq, nk, heads, kv_heads, dtype, flat.reshape(heads, nqb, keep), heads)
+    check(got, ref, dtype)
+
+
+def test_attention_over_half_a_million_keys(ctx):
+    """4097 key blocks, the last one short and in every list."""
+    heads, nq, nk = 28, 1500, 4097 * 128 - 3
+    g = np.random.default_rng(0)
+    blocks = np.sort(g.integers(0, 4096, (heads, 12, 3)), axis=2).astype(np.int32)
+    blocks[:, :, 2] = 4096
+    got, ref = attend(ctx, nq, nk, heads, 1, "f16", blocks, 9)
+    check(got, ref, "f16")
+
+
 @pytest.mark.parametrize("nq,heads,keep", [(130, 2, 4), (700, 60, 4), (1, 3, 20), (257, 5, 1)])
 def test_attention_of_short_and_empty_lists(nq, heads, keep, ctx):
     """Lists that end early, at an index past the last block or at once: the last give zeros."""
