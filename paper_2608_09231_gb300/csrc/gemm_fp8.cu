@@ -482,6 +482,10 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // Two accumulators of 256 columns fill tensor memory, which the scales need a little of: the second
 // one starts 32 columns inside the first (columns 224 .. 479), and the tile after this one waits
 // only for this one's drain of the shared 32 columns, which the epilogue reads first.
+// The tensor core cuts what an addend has below the accumulator's last bits, towards zero, so the
+// error of a sum grows with K (1.4e-7 of the result at K = 3072, 9.3e-7 at 13824).  A unit of more
+// than F8P_PASS K blocks (LONG) is therefore computed in passes of at most that many, which the
+// epilogue adds in registers (rounded to nearest): 1.2e-6 -> 5.4e-7 at K = 13824, for 2 % more time.
 // Tiles of a last wave that would leave half of the pairs idle are worked on as two halves of 128
 // columns (M = 256, N = 128).
 // warp 0: TMA producer; 1: MMA (even CTA); 2: scale words to shared memory; 3 (even CTA): and to
@@ -489,6 +493,7 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a
 // row a thread, with bias and gate broadcast from shared memory, and its output leaves by TMA:
 // stores, or for the residual stream an add that L2 carries out, so that the stream is not read.
+constexpr int F8P_PASS = 64;  // most K blocks of a pass
 constexpr int F8P_STAGES = 5, F8P_STAGE = 2 * F8_TILE;
 constexpr int F8P_SHARED = 32, F8P_ACC1 = 256 - F8P_SHARED;  // TMEM columns
 constexpr int F8P_SF_COL = F8P_ACC1 + 256, F8P_SF_COLS = 12;  // A's 4 columns, W's 8
@@ -587,7 +592,7 @@ BAG_DEV void store_rows(const Fp8Gemm& g, const uint8_t* buf, int row0, int col0
 
 }  // namespace
 
-template <int KIND>
+template <int KIND, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                          const __grid_constant__ CUtensorMap tmHalf, const __grid_constant__ CUtensorMap tmOut,
@@ -614,6 +619,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
   const int nkb = (g.K + F8_BK - 1) / F8_BK, nruns = (nkb + F8_GROUP * F8_RUN - 1) / (F8_GROUP * F8_RUN);
+  // passes of about the same length, whole runs of scale words each
+  constexpr int RUN = F8_GROUP * F8_RUN;
+  const int passes = LONG ? (nkb + F8P_PASS - 1) / F8P_PASS : 1;
+  const int pass_kb = LONG ? ((nkb + passes - 1) / passes + RUN - 1) / RUN * RUN : nkb;
   // units of work: `whole` tiles of 256 x 256, then every later tile as two of 256 x 128
   const long units = 2 * (long)num_m * num_n - whole;
   // first row and column of a unit, and whether it is half a tile; groups of group_rows row tiles
@@ -719,24 +728,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
             parity ^= 1;
           }
         };
-        long i = 0;  // units of this pair so far
+        long i = 0;            // accumulators of this pair so far
+        int k0 = 0, k1 = 0;    // the pass's K blocks
         bool ok = true;
-        for (long unit = pair; unit < units && ok; unit += npairs, ++i) {
+        for (long unit = pair; unit < units && ok; unit += k1 == nkb ? npairs : 0, ++i) {
+          k0 = k1 == nkb ? 0 : k1;
+          k1 = min(nkb, k0 + pass_kb);
           const int acc = (int)(i & 1);
           const uint32_t shape = unit >= whole ? idesc_mxf8(256, 128) : idesc_mxf8(256, 256);
           const uint32_t dt = tm + (acc ? F8P_ACC1 : 0);
-          // the accumulator's last tile is drained, and the other one's shared columns
+          // the accumulator is drained, and the other one's shared columns
           if (!mbar_wait_warp(tempty + acc, (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag)) break;
           if (i > 0 && !mbar_wait_warp(shared_free + (acc ^ 1), (uint32_t)(((i - 1) >> 1) & 1), abort_flag)) break;
           tc_fence_after();
-          uint32_t add = 0;  // the tile's first product overwrites the accumulator
-          for (int kg = 0; kg < nkb && ok; kg += F8_GROUP, ++grp) {
+          uint32_t add = 0;  // the first product overwrites the accumulator
+          for (int kg = k0; kg < k1 && ok; kg += F8_GROUP, ++grp) {
             const uint32_t sa = tm + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
             if (!(ok = mbar_wait_warp(sf_ready + (grp & 1), (grp >> 1) & 1u, abort_flag))) break;
 #pragma unroll
             for (int b = 0; b < F8_GROUP; b += 2) {  // two K blocks at a time
-              if (kg + b >= nkb) break;
-              const bool two = kg + b + 1 < nkb;
+              if (kg + b >= k1) break;
+              const bool two = kg + b + 1 < k1;
               int s1 = s;
               uint32_t ph1 = ph;
               next(s1, ph1);
@@ -756,7 +768,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
                     pair_mma_mxf8(dt, a1 + 2 * k, a1 + (F8_TILE >> 4) + 2 * k, shape | scale_byte(b + 1), sa, sa + 4, 1u);
                   pair_commit(empty + s1, 3);
                 }
-                if (b + 2 == F8_GROUP || kg + b + 2 >= nkb) pair_commit(sf_used + (grp & 1), 1);
+                if (b + 2 == F8_GROUP || kg + b + 2 >= k1) pair_commit(sf_used + (grp & 1), 1);
               }
               __syncwarp();
               add = 1;
@@ -857,9 +869,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
     const uint32_t tempty_even = mapa_shared(smem_u32(tempty), 0), free_even = mapa_shared(smem_u32(shared_free), 0);
     constexpr int CW = KIND == BAG_FP8_BF16 ? 64 : (KIND == BAG_FP8_CODES ? 128 : 32);  // columns of a staged row
     constexpr int NC = 128 / CW;
-    long i = 0;
-    for (long unit = pair; unit < units; unit += npairs, ++i) {
-      const int acc = (int)(i & 1);
+    long i = 0;  // accumulators so far
+    for (long unit = pair; unit < units; unit += npairs) {
       int m0, n0;
       const bool half = decode(unit, m0, n0);
       const int row0 = m0 + (int)rank * 128 + q * 32, col0 = n0 + side * 128;
@@ -875,118 +886,165 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
         if (KIND == BAG_FP8_RESID) reinterpret_cast<float4*>(sgate)[lane] = make_float4(t[0], t[1], t[2], t[3]);
         __syncwarp();
       }
-      const bool ok = mbar_wait(tfull + acc, (uint32_t)((i >> 1) & 1), abort_flag);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      tc_fence_after();
-      const uint32_t tb = tmem + (uint32_t)((acc ? F8P_ACC1 : 0) + side * 128) + ((uint32_t)(q * 32) << 16);
-      // the shared columns are the last 32 of accumulator 0 and the first 32 of accumulator 1
-      const bool shares = side == (acc ^ 1);
+      uint32_t tb = 0;
+      int acc = 0;
+      bool shares = false;  // whether this warp's columns are shared: the last 32 of accumulator 0, the first 32 of 1
+      auto begin = [&]() {
+        acc = (int)(i & 1);
+        const bool ok = mbar_wait(tfull + acc, (uint32_t)((i >> 1) & 1), abort_flag);
+        ++i;
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        tc_fence_after();
+        tb = tmem + (uint32_t)((acc ? F8P_ACC1 : 0) + side * 128) + ((uint32_t)(q * 32) << 16);
+        shares = side == (acc ^ 1);
+        return true;
+      };
       auto release = [&](uint32_t bar) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) peer_signal(bar + (uint32_t)(acc * sizeof(uint64_t)));
       };
+      // CW finished sums from column c of this warp's 128 on, to where they go
+      auto finish = [&](float* v, int c) {
+      if (g.bias) {
+#pragma unroll
+        for (int j = 0; j < CW; j += 32) with_vector(sbias + c + j, v + j, sum2);
+      }
+      if (g.act) {
+#pragma unroll
+        for (int j = 0; j < CW; j += 2) {
+          const float2 t = gelu2(make_float2(v[j], v[j + 1]));
+          v[j] = t.x;
+          v[j + 1] = t.y;
+        }
+      }
+      if (KIND == BAG_FP8_RESID) with_vector(sgate + c, v, mul2);
+      // the staged tile's last store has read it
+      if (lane == 0) bulk_wait_read();
+      __syncwarp();
+      if constexpr (KIND == BAG_FP8_CODES) {
+        const int valid = g.N - col0;
+        float m[4] = {0.f, 0.f, 0.f, 0.f};
+        if (valid < 128) {  // columns past the end count as zeros
+#pragma unroll
+          for (int j = 0; j < 128; ++j) v[j] = j < valid ? v[j] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 128; j += 2) m[(j >> 1) & 3] = max3_abs(m[(j >> 1) & 3], v[j], v[j + 1]);
+        const uint32_t b = e8m0_of(abs_bits(max3_abs(max3_abs(m[0], m[1], m[2]), m[3], 0.f)));
+        const float inv = e8m0_inverse(b);
+        if (valid > 0 && row0 + lane < g.M) g.out_s[(long)(row0 + lane) * g.ldos + col0 / kScaleBlock] = (uint8_t)b;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float* x = v + 16 * u + 4 * e;
+            const float2 lo = mul2(make_float2(x[0], x[1]), make_float2(inv, inv));
+            const float2 hi = mul2(make_float2(x[2], x[3]), make_float2(inv, inv));
+            w[e] = pack_e4m3x4(lo.x, lo.y, hi.x, hi.y);
+          }
+          staged(buf, u) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      } else if constexpr (KIND == BAG_FP8_BF16) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float* x = v + 8 * u;
+          staged(buf, u) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                      pack_bf16x2(x[6], x[7]));
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          staged(buf, u) = make_uint4(__float_as_uint(v[4 * u]), __float_as_uint(v[4 * u + 1]),
+                                      __float_as_uint(v[4 * u + 2]), __float_as_uint(v[4 * u + 3]));
+      }
+      // TMA writes whole 16-byte units, also where the tensor ends inside one: the last columns
+      // go the other way
+      if (g.vec && col0 + c + CW <= g.N) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0 && row0 < g.M) {
+          if (KIND == BAG_FP8_RESID)
+            tma_add_2d(&tmOut, buf, col0 + c, row0);
+          else
+            tma_store_2d(&tmOut, buf, col0 + c, row0);
+          bulk_commit();
+        }
+      } else {
+        __syncwarp();
+        if constexpr (KIND == BAG_FP8_CODES)
+          store_rows<uint8_t, false>(g, buf, row0, col0 + c);
+        else if constexpr (KIND == BAG_FP8_BF16)
+          store_rows<__nv_bfloat16, false>(g, buf, row0, col0 + c);
+        else
+          store_rows<float, KIND == BAG_FP8_RESID>(g, buf, row0, col0 + c);
+        __syncwarp();
+      }
+        __syncwarp();
+      };
+      bool ok = true;
       if (half && side) {  // half a tile has no columns for these warps
-        if (shares) release(free_even);
-        release(tempty_even);
-        continue;
-      }
+        for (int pass = 0; pass < passes && (ok = begin()); ++pass) {
+          if (shares) release(free_even);
+          release(tempty_even);
+        }
+      } else if constexpr (LONG) {
+        float v[128];
+#pragma unroll
+        for (int j = 0; j < 128; ++j) v[j] = 0.f;
 #pragma unroll 1
-      for (int k = 0; k < NC; ++k) {
-        const int c = (acc ? k : NC - 1 - k) * CW;  // the shared columns' part first
-        float v[CW];
-        // whole 32-column loads, the shared columns' first
-        if (!acc) tmem_ld32(tb + (uint32_t)(c + CW - 32), v + CW - 32);
-        if (acc) tmem_ld32(tb + (uint32_t)c, v);
-        if (k == 0 && shares) release(free_even);
+        for (int pass = 0; pass < passes && (ok = begin()); ++pass) {
+          auto add = [&](int c) {
 #pragma unroll
-        for (int j = 0; j < CW; j += 32) {
-          if (j > 0 && j < CW - 32) tmem_ld32(tb + (uint32_t)(c + j), v + j);
-        }
-        if (CW > 32) {
-          if (acc)
-            tmem_ld32(tb + (uint32_t)(c + CW - 32), v + CW - 32);
-          else
-            tmem_ld32(tb + (uint32_t)c, v);
-        }
-        if (k == NC - 1) release(tempty_even);
-        if (g.bias) {
+            for (int h = c; h < c + 32; h += 16) {
+              float t[16];
+              tmem_ld16(tb + (uint32_t)h, t);
 #pragma unroll
-          for (int j = 0; j < CW; j += 32) with_vector(sbias + c + j, v + j, sum2);
-        }
-        if (g.act) {
-#pragma unroll
-          for (int j = 0; j < CW; j += 2) {
-            const float2 t = gelu2(make_float2(v[j], v[j + 1]));
-            v[j] = t.x;
-            v[j + 1] = t.y;
-          }
-        }
-        if (KIND == BAG_FP8_RESID) with_vector(sgate + c, v, mul2);
-        // the staged tile's last store has read it
-        if (lane == 0) bulk_wait_read();
-        __syncwarp();
-        if constexpr (KIND == BAG_FP8_CODES) {
-          const int valid = g.N - col0;
-          float m[4] = {0.f, 0.f, 0.f, 0.f};
-          if (valid < 128) {  // columns past the end count as zeros
-#pragma unroll
-            for (int j = 0; j < 128; ++j) v[j] = j < valid ? v[j] : 0.f;
-          }
-#pragma unroll
-          for (int j = 0; j < 128; j += 2) m[(j >> 1) & 3] = max3_abs(m[(j >> 1) & 3], v[j], v[j + 1]);
-          const uint32_t b = e8m0_of(abs_bits(max3_abs(max3_abs(m[0], m[1], m[2]), m[3], 0.f)));
-          const float inv = e8m0_inverse(b);
-          if (valid > 0 && row0 + lane < g.M) g.out_s[(long)(row0 + lane) * g.ldos + col0 / kScaleBlock] = (uint8_t)b;
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float* x = v + 16 * u + 4 * e;
-              const float2 lo = mul2(make_float2(x[0], x[1]), make_float2(inv, inv));
-              const float2 hi = mul2(make_float2(x[2], x[3]), make_float2(inv, inv));
-              w[e] = pack_e4m3x4(lo.x, lo.y, hi.x, hi.y);
+              for (int j = 0; j < 16; ++j) v[h + j] += t[j];
             }
-            staged(buf, u) = make_uint4(w[0], w[1], w[2], w[3]);
+          };
+          if (acc) {  // the shared columns first
+            add(0);
+            if (shares) release(free_even);
+            add(96);
+          } else {
+            add(96);
+            if (shares) release(free_even);
+            add(0);
           }
-        } else if constexpr (KIND == BAG_FP8_BF16) {
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float* x = v + 8 * u;
-            staged(buf, u) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                        pack_bf16x2(x[6], x[7]));
-          }
-        } else {
-#pragma unroll
-          for (int u = 0; u < 8; ++u)
-            staged(buf, u) = make_uint4(__float_as_uint(v[4 * u]), __float_as_uint(v[4 * u + 1]),
-                                        __float_as_uint(v[4 * u + 2]), __float_as_uint(v[4 * u + 3]));
+          add(32);
+          add(64);
+          release(tempty_even);
         }
-        // TMA writes whole 16-byte units, also where the tensor ends inside one: the last columns
-        // go the other way
-        if (g.vec && col0 + c + CW <= g.N) {
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0 && row0 < g.M) {
-            if (KIND == BAG_FP8_RESID)
-              tma_add_2d(&tmOut, buf, col0 + c, row0);
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < 128; c += CW) finish(v + c, c);
+      } else {
+        if (!(ok = begin())) break;
+#pragma unroll 1
+        for (int k = 0; k < NC; ++k) {
+          const int c = (acc ? k : NC - 1 - k) * CW;  // the shared columns' part first
+          float v[CW];
+          // whole 32-column loads, the shared columns' first
+          if (!acc) tmem_ld32(tb + (uint32_t)(c + CW - 32), v + CW - 32);
+          if (acc) tmem_ld32(tb + (uint32_t)c, v);
+          if (k == 0 && shares) release(free_even);
+#pragma unroll
+          for (int j = 0; j < CW; j += 32) {
+            if (j > 0 && j < CW - 32) tmem_ld32(tb + (uint32_t)(c + j), v + j);
+          }
+          if (CW > 32) {
+            if (acc)
+              tmem_ld32(tb + (uint32_t)(c + CW - 32), v + CW - 32);
             else
-              tma_store_2d(&tmOut, buf, col0 + c, row0);
-            bulk_commit();
+              tmem_ld32(tb + (uint32_t)c, v);
           }
-        } else {
-          __syncwarp();
-          if constexpr (KIND == BAG_FP8_CODES)
-            store_rows<uint8_t, false>(g, buf, row0, col0 + c);
-          else if constexpr (KIND == BAG_FP8_BF16)
-            store_rows<__nv_bfloat16, false>(g, buf, row0, col0 + c);
-          else
-            store_rows<float, KIND == BAG_FP8_RESID>(g, buf, row0, col0 + c);
-          __syncwarp();
+          if (k == NC - 1) release(tempty_even);
+          finish(v, c);
         }
-        __syncwarp();
       }
+      if (!ok) break;
     }
     if (lane == 0) bulk_wait_all();
     __syncwarp();
@@ -1028,11 +1086,12 @@ static cudaError_t launch_pair(Fp8Gemm g, cudaStream_t s) {
   auto launch = [&](auto kernel) {
     return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, th, to, g, rows, whole);
   };
+  const bool l = g.K > F8P_PASS * F8_BK;
   switch (g.kind) {
-    case BAG_FP8_F32: return launch(gemm_fp8_pair_kernel<BAG_FP8_F32>);
-    case BAG_FP8_BF16: return launch(gemm_fp8_pair_kernel<BAG_FP8_BF16>);
-    case BAG_FP8_CODES: return launch(gemm_fp8_pair_kernel<BAG_FP8_CODES>);
-    default: return launch(gemm_fp8_pair_kernel<BAG_FP8_RESID>);
+    case BAG_FP8_F32: return l ? launch(gemm_fp8_pair_kernel<BAG_FP8_F32, true>) : launch(gemm_fp8_pair_kernel<BAG_FP8_F32, false>);
+    case BAG_FP8_BF16: return l ? launch(gemm_fp8_pair_kernel<BAG_FP8_BF16, true>) : launch(gemm_fp8_pair_kernel<BAG_FP8_BF16, false>);
+    case BAG_FP8_CODES: return l ? launch(gemm_fp8_pair_kernel<BAG_FP8_CODES, true>) : launch(gemm_fp8_pair_kernel<BAG_FP8_CODES, false>);
+    default: return l ? launch(gemm_fp8_pair_kernel<BAG_FP8_RESID, true>) : launch(gemm_fp8_pair_kernel<BAG_FP8_RESID, false>);
   }
 }
 
@@ -1045,10 +1104,14 @@ cudaError_t gemm_fp8_init() {
   smem(gemm_fp8_few_kernel<32>, FewCfg<32>::stages(1) * FewCfg<32>::STAGE + FewCfg<32>::REST);
   smem(gemm_fp8_few_kernel<64>, FewCfg<64>::stages(1) * FewCfg<64>::STAGE + FewCfg<64>::REST);
   smem(gemm_fp8_few_kernel<128>, FewCfg<128>::stages(1) * FewCfg<128>::STAGE + FewCfg<128>::REST);
-  smem(gemm_fp8_pair_kernel<BAG_FP8_F32>, F8P_SMEM);
-  smem(gemm_fp8_pair_kernel<BAG_FP8_BF16>, F8P_SMEM);
-  smem(gemm_fp8_pair_kernel<BAG_FP8_CODES>, F8P_SMEM);
-  smem(gemm_fp8_pair_kernel<BAG_FP8_RESID>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_F32, false>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_F32, true>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_BF16, false>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_BF16, true>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_CODES, false>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_CODES, true>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_RESID, false>, F8P_SMEM);
+  smem(gemm_fp8_pair_kernel<BAG_FP8_RESID, true>, F8P_SMEM);
   return r;
 }
 
@@ -1081,6 +1144,7 @@ static Fp8Plan plan_fp8(long M, long N, long K) {
     if (t.BN < 64 && M > t.BN) continue;  // narrow tiles read W again for every tile of rows
     for (int logS = 0; logS <= 3 && nkb >= (double)(2 << logS); ++logS) {
       const double kb = (double)cd(cd(K, F8_BK), 1L << logS);
+      if (kb > F8P_PASS && logS < 3) continue;  // a longer sum on the tensor core loses precision (see LONG)
       const double more = (double)(cd(cd(M, t.BN) * cd(N, 128) << logS, cluster_sms(logS)) - 1);
       us = together(t.start + 0.2 * kb + more * (t.wave + t.share * kb) + (logS ? 0.84 : 0.0) + 0.15 * (1 << logS));
       if (us < best) {
