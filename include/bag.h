@@ -330,9 +330,11 @@ bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows
 
 /* ---- 8-bit operands with a scale for each block of 128 ----
  *
- * The operations from here to bag_attention_blocks use nothing of the context but its error text:
- * they are kernels on the caller's stream itself (the one of bag_set_stream), ordered like any
- * other work that the caller puts there, never synchronise, and may be captured into a CUDA graph.
+ * The operations from here to bag_attention_blocks use nothing of the context but its error text
+ * and its device error word (a wait that expired in one of them is reported by the next bag_step
+ * or bag_run, up to bag_reset): they are kernels on the caller's stream itself (the one of
+ * bag_set_stream), ordered like any other work that the caller puts there, never synchronise, and
+ * may be captured into a CUDA graph (which then must not outlive the context).
  *
  * An encoded matrix [rows, cols] is two device buffers: codes, one float8 e4m3 byte an element
  * (row stride ldc bytes), and scales, one byte b for each row and block of 128 consecutive

@@ -1878,7 +1878,7 @@ static bag_status bag_gemm_fp8_impl(bag_ctx* ctx, const void* a, long lda, const
   g.ldo = ldo;
   g.out_s = reinterpret_cast<uint8_t*>(out_s);
   g.ldos = ldos;
-  g.err = &ctx->st_op->err;
+  g.err = &ctx->st->err;
   CK(gemm_fp8(g, ctx->user_stream));
   return BAG_OK;
 }
@@ -2003,7 +2003,7 @@ static bag_status bag_attention_blocks_impl(bag_ctx* ctx, const void* q, long ld
   a.blocks = blocks;
   a.o = o;
   a.ldo = ldo;
-  a.err = &ctx->st_op->err;
+  a.err = &ctx->st->err;
   CK(attention_blocks(a, ctx->user_stream));
   return BAG_OK;
 }
