@@ -167,7 +167,7 @@ KERNEL_NAMES = {"gemm": "gemm_tc_kernel", "attention": "attn_tc_kernel",
                 "gate": "gate_kernel", "cache": "stream_init_kernel"}
 KERNEL_SOURCES = {"gemm_tc_kernel": ["gemm.cu", "epilogue.cuh", "common.cuh"],
                   "gemm_pair_kernel": ["gemm.cu", "epilogue.cuh", "common.cuh"],
-                  "attn_tc_kernel": ["attn_tc.cu", "common.cuh"]}
+                  "attn_tc_kernel": ["attn_tc.cu", "attn_common.cuh", "common.cuh"]}
 
 
 def source_sha1(kernel):
