@@ -331,8 +331,8 @@ bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows
 /* ---- 8-bit operands with a scale for each block of 128 ----
  *
  * The operations from here to bag_attention_blocks use nothing of the context but its error text
- * and its device error word (a wait that expired in one of them is reported by the next bag_step
- * or bag_run, up to bag_reset): they are kernels on the caller's stream itself (the one of
+ * and its device error word (a wait that expired in one of them is reported by bag_run, up to
+ * bag_reset): they are kernels on the caller's stream itself (the one of
  * bag_set_stream), ordered like any other work that the caller puts there, never synchronise, and
  * may be captured into a CUDA graph (which then must not outlive the context).
  *
@@ -390,10 +390,10 @@ bag_status bag_gemm_fp8(bag_ctx* ctx, const void* a, long lda, const void* a_s, 
  * have to be distinct. */
 
 /* Keep rows of x - base (base null: of x): scale = bf16(amax / top) (top 127 or 7, amax times
- * the rounded reciprocal), code = round(element / scale), ties to even.  A group whose scale
- * would be below 2^-126 is kept as zeros; one that holds an infinity or NaN keeps a NaN scale
- * and reads as NaN.  x, base: device fp32 [rows, cols], row strides ldx, ldb elements; any
- * alignment (16-byte aligned rows are fastest). */
+ * the rounded reciprocal), code = round(element * (1 / scale)), 1 / scale rounded to fp32, ties to
+ * even.  A group whose scale would be below 2^-126 is kept as zeros; one that holds an infinity or
+ * NaN keeps a NaN scale and reads as NaN.  x, base: device fp32 [rows, cols], row strides ldx,
+ * ldb elements; any alignment (16-byte aligned rows are fastest). */
 bag_status bag_cache_write(bag_ctx* ctx, const float* x, long ldx, const float* base, long ldb,
                            const int32_t* slots, long rows, long cols, int bits, void* codes,
                            long ldc, void* scales, long lds, long capacity);
@@ -414,8 +414,9 @@ enum { BAG_F16 = 2 };
 /* Pooled vectors of the blocks of x [rows, ld] (head h at columns [128 h, 128 h + 128)): the
  * mean of a block's rows (fp32, summed in halves: row r + row r + 64, then r + 32, ...), rounded
  * to 8-bit integers: codes int8 device [heads][ldb][128], scales fp32 device [heads][ldb]
- * (amax / 127 of each vector, amax times the rounded reciprocal), ldb >= ceil(rows / 128).
- * A vector that is not finite keeps codes and scale 0. */
+ * (amax / 127 of each vector, amax times the rounded reciprocal; codes as in a cache row), ldb >=
+ * ceil(rows / 128).  A vector that is not finite, or whose scale would be below 2^-126, keeps codes
+ * and scale 0. */
 bag_status bag_block_pool(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads,
                           void* codes, float* scales, long ldb);
 

@@ -1805,6 +1805,9 @@ static bag_status bag_rel_l1_impl(bag_ctx* ctx, const void* a, const void* b, in
 }
 
 // ---- 8-bit operands, quantised cache, block-sparse attention ----
+constexpr long kMaxRows = 0x7fffff00L;  // an int in the kernels, also after rounding up to a tile
+constexpr int kMaxHeads = 65535;        // a grid dimension
+
 static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 // An encoded matrix's buffers: null, alignment and strides.
@@ -1820,7 +1823,7 @@ static bag_status check_encoded(bag_ctx* ctx, const char* name, const void* code
 
 static bag_status bag_quant_fp8_impl(bag_ctx* ctx, const void* x, int dtype, long ldx, long rows, long cols,
                                      void* codes, long ldc, void* scales, long lds) {
-  if (rows < 0 || cols <= 0 || ldx < cols || (dtype != BAG_F32 && dtype != BAG_BF16))
+  if (rows < 0 || cols <= 0 || cols > kMaxRows || ldx < cols || (dtype != BAG_F32 && dtype != BAG_BF16))
     return fail(ctx, BAG_EINVAL, "bad quant_fp8 shape or dtype");
   if (rows == 0) return BAG_OK;
   if (!x || !aligned(x, dtype == BAG_BF16 ? 2 : 4)) return fail(ctx, BAG_EINVAL, "x is null or not aligned to its type");
@@ -1844,8 +1847,7 @@ static bag_status bag_ln_mod_fp8_impl(bag_ctx* ctx, const float* x, long ldx, co
 static bag_status bag_gemm_fp8_impl(bag_ctx* ctx, const void* a, long lda, const void* a_s, long ldas, const void* w,
                                     long ldw, const void* w_s, long ldws, const float* bias, long M, long N, long K,
                                     int act, int kind, const float* gate, void* out, long ldo, void* out_s, long ldos) {
-  const long most = 0x7fffff00L;
-  if (M < 0 || N < 1 || K < 1 || M > most || N > most || K > most) return fail(ctx, BAG_EINVAL, "bad gemm_fp8 shape");
+  if (M < 0 || N < 1 || K < 1 || M > kMaxRows || N > kMaxRows || K > kMaxRows) return fail(ctx, BAG_EINVAL, "bad gemm_fp8 shape");
   if (kind < BAG_FP8_F32 || kind > BAG_FP8_RESID || act < 0 || act > 1 || (kind == BAG_FP8_RESID && act))
     return fail(ctx, BAG_EINVAL, "bad gemm_fp8 output kind or activation");
   if (gate && kind != BAG_FP8_RESID) return fail(ctx, BAG_EINVAL, "gate goes with BAG_FP8_RESID only");
@@ -1887,7 +1889,8 @@ static bag_status bag_gemm_fp8_impl(bag_ctx* ctx, const void* a, long lda, const
 static bag_status check_cache(bag_ctx* ctx, const void* codes, long ldc, const void* scales, long lds, long capacity,
                               const int32_t* slots, long rows, long cols, int bits, const float* base, long ldb) {
   if (bits != 8 && bits != 4) return fail(ctx, BAG_EINVAL, "bits must be 8 or 4");
-  if (rows < 0 || cols <= 0 || capacity < 0 || (!slots && capacity < rows)) return fail(ctx, BAG_EINVAL, "bad cache shape");
+  if (rows < 0 || cols <= 0 || cols > kMaxRows || capacity < 0 || (!slots && capacity < rows))
+    return fail(ctx, BAG_EINVAL, "bad cache shape");
   if (rows == 0) return BAG_OK;
   const int group = bits == 8 ? 128 : 32;
   if (!codes || ldc < (cols * bits + 7) / 8 || ldc % 16 || !aligned(codes, 16))
@@ -1940,9 +1943,6 @@ static bag_status bag_cache_read_impl(bag_ctx* ctx, const void* codes, long ldc,
   CK(cache_read(a, bits, ctx->user_stream));
   return BAG_OK;
 }
-
-constexpr long kMaxRows = 0x7fffff00L;  // row counts are ints in the kernels
-constexpr int kMaxHeads = 65535;        // a grid dimension
 
 static bag_status bag_block_pool_impl(bag_ctx* ctx, const void* x, int type, long ld, long rows, int heads,
                                       void* codes, float* scales, long ldb) {

@@ -504,10 +504,10 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
 
 bool rows16(const void* p, long ld, int size) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0; }
 
-cudaError_t grid_of(long items, int per, unsigned* grid) {
-  const long n = (items + per - 1) / per;
-  if (n > 0x7fffffffL) return cudaErrorInvalidConfiguration;
-  *grid = (unsigned)n;
+// CTAs of `per` items for rows of segs items each (refused before the product could overflow).
+cudaError_t grid_of(long rows, long segs, int per, unsigned* grid) {
+  if (segs > 0x7fffffffL || rows > 0x7fffffffL * per / segs) return cudaErrorInvalidConfiguration;
+  *grid = (unsigned)((rows * segs + per - 1) / per);
   return cudaSuccess;
 }
 
@@ -518,9 +518,8 @@ cudaError_t quant_fp8(const void* x, int bf16, long ldx, long rows, long cols, v
   if (rows <= 0 || cols <= 0) return cudaSuccess;
   const int seg = QS * 32 * (bf16 ? 8 : 4);
   const long segs = (cols + seg - 1) / seg;
-  if (segs > 0x7fffffffL) return cudaErrorInvalidConfiguration;
   unsigned grid;
-  if (cudaError_t e = grid_of(rows * segs, Q_WARPS, &grid)) return e;
+  if (cudaError_t e = grid_of(rows, segs, Q_WARPS, &grid)) return e;
   auto launch = [&](auto kernel, auto type) {
     using T = decltype(type);
     return launch_kernel(kernel, grid, Q_WARPS * 32, 0, s, reinterpret_cast<const T*>(x), ldx, rows, cols,
@@ -547,9 +546,8 @@ cudaError_t ln_mod_fp8(const float* x, long ldx, const float* shift, const float
 
 static cudaError_t cache_grid(CacheArgs* a, unsigned* grid) {
   const long segs = (a->cols + C_SEG - 1) / C_SEG;
-  if (segs > 0x7fffffffL) return cudaErrorInvalidConfiguration;
   a->segs = (int)segs;
-  return grid_of(a->rows * segs, C_WARPS, grid);
+  return grid_of(a->rows, segs, C_WARPS, grid);
 }
 
 cudaError_t cache_write(CacheArgs a, int bits, cudaStream_t s) {

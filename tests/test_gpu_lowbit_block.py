@@ -208,3 +208,22 @@ def test_refusals_of_the_binding(ctx):
         with pytest.raises(ValueError):
             call()
             print("accepted:", i)
+
+
+def test_sizes_past_the_grid_are_refused(ctx):
+    """Rows whose count of work items passes a grid, or 64 bits, launch nothing."""
+    lib, h = ctx.lib, ctx.h
+    x, c, s = torch.ones(8, 2048, device=DEV), torch.zeros(8, 2048, device=DEV, dtype=torch.uint8), \
+        torch.zeros(8, 64, device=DEV, dtype=torch.bfloat16)
+    slots = torch.zeros(8, device=DEV, dtype=torch.int32)
+    p, pc, ps, pi = (t.data_ptr() for t in (x, c, s, slots))
+    for rows in (2 ** 35, 2 ** 62 + 2, 2 ** 63 - 1):
+        assert lib.bag_quant_fp8(h, p, 0, 2048, rows, 2048, pc, 2048, ps, 128) != 0
+        assert lib.bag_ln_mod_fp8(h, p, 2048, None, None, rows, 2048, pc, 2048, ps, 128) != 0
+        assert lib.bag_cache_write(h, p, 2048, None, 0, pi, rows, 2048, 8, pc, 2048, ps, 64, 8) != 0
+        assert lib.bag_cache_read(h, pc, 2048, ps, 64, 8, pi, rows, 2048, 8, None, 0, p, 2048) != 0
+    for cols in (2 ** 32, 2 ** 63 - 1):
+        assert lib.bag_quant_fp8(h, p, 0, cols, 1, cols, pc, cols & ~15, ps, 2 ** 60) != 0
+        assert lib.bag_cache_write(h, p, cols, None, 0, pi, 1, cols, 8, pc, cols & ~15, ps, 2 ** 60, 8) != 0
+    torch.cuda.synchronize()
+    assert bool((c == 0).all() and (s == 0).all() and (x == 1).all())
