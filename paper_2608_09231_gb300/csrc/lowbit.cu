@@ -59,7 +59,8 @@ struct Piece {
 // A warp takes QS steps of a row, each 32 lanes x 16 bytes (128 fp32 or 256 bf16 columns); a
 // block's largest magnitude passes between its 32 or 16 lanes.  Bound: HBM.  The steps' loads are
 // all in flight before the first reduction, and stay as loaded until then: 32,760 x 5120 bf16 took
-// 148 us with elements converted on arrival (40 % of HBM's rate), 82 so, 85 with five steps, 101 with eight.
+// 148 us with elements converted on arrival (40 % of HBM's rate), 80 so (6.3 TB/s; floor 74), 85 with
+// five steps, 101 with eight; 4608 x 3072 fp32 12.9 (floor 10.4).
 constexpr int QS = 4, Q_WARPS = 8;
 
 template <typename T, bool VEC>
@@ -120,10 +121,15 @@ BAG_DEV float block_sum(float v, float* red) {
   return s;
 }
 
-// A CTA a row; the row stays in registers (VPT float4 a thread).  A warp's 32 float4 are 128
-// consecutive columns, which is one scale block.
-template <int TH, int VPT>
-__global__ void __launch_bounds__(TH) ln_fp8_kernel(const float* __restrict__ x, long ldx,
+// A CTA a row; the row stays in registers (VPT float4 a thread, statistics in two passes over it), so
+// that x is read once.  A warp's 32 float4 are 128 consecutive columns, which is one scale block.
+// Bound: HBM behind the row's phases (load, two reductions, encode), which CTAS rows on an SM hide
+// from each other, and the issue of the encoding: packed arithmetic, one maximum of three and (at
+// 5120) CTAS held to 42 registers took 32,760 x 5120 from 155 to 132 us (floor 124: 6.4 TB/s), 4608 x
+// 3072 from 16.3 to 14.8 (10.4: three waves of rows and a start).  Two rows a CTA took 17.4 against
+// those 16.3, four 23.6; a row of 3072 on 192 threads 14.5 (7145 rows 20.8 against 20.5), on 96 16.2.
+template <int TH, int VPT, int CTAS>
+__global__ void __launch_bounds__(TH, CTAS) ln_fp8_kernel(const float* __restrict__ x, long ldx,
                                                     const float* __restrict__ shift, const float* __restrict__ scale,
                                                     int cols, uint8_t* __restrict__ codes, long ldc,
                                                     uint8_t* __restrict__ scales, long lds) {
@@ -132,48 +138,57 @@ __global__ void __launch_bounds__(TH) ln_fp8_kernel(const float* __restrict__ x,
   const long row = blockIdx.x;
   const float4* xr = reinterpret_cast<const float4*>(x + row * ldx);
   const int nv = cols / 4;
-  float4 v[VPT];
-  float s = 0.f;
+  float2 v[2 * VPT];
+  float2 s = make_float2(0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int c = threadIdx.x + i * TH;
-    v[i] = c < nv ? __ldcs(xr + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    s += (v[i].x + v[i].y) + (v[i].z + v[i].w);
+    const float4 f = c < nv ? __ldcs(xr + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    v[2 * i] = make_float2(f.x, f.y);
+    v[2 * i + 1] = make_float2(f.z, f.w);
   }
-  const float mean = block_sum<TH>(s, red_mean) / (float)cols;
-  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2 * VPT; ++i) s = sum2(s, v[i]);
+  const float mean = block_sum<TH>(s.x + s.y, red_mean) / (float)cols;
+  float2 q = make_float2(0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     if (threadIdx.x + i * TH < nv) {
-      v[i] = make_float4(v[i].x - mean, v[i].y - mean, v[i].z - mean, v[i].w - mean);
-      q += (v[i].x * v[i].x + v[i].y * v[i].y) + (v[i].z * v[i].z + v[i].w * v[i].w);
+#pragma unroll
+      for (int j = 2 * i; j < 2 * i + 2; ++j) {
+        v[j] = sum2(v[j], make_float2(-mean, -mean));
+        q = muladd2(v[j], v[j], q);
+      }
     }
   }
-  const float rstd = rsqrtf(block_sum<TH>(q, red_var) / (float)cols + 1e-6f);
+  const float rstd = rsqrtf(block_sum<TH>(q.x + q.y, red_var) / (float)cols + 1e-6f);
+  uint8_t* const to = codes + row * ldc;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int c = threadIdx.x + i * TH;
     const int c0 = c - (int)(threadIdx.x % 32);  // the warp's first float4: warp-uniform
     if (c0 >= nv) break;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    float2 y0 = mul2(v[2 * i], make_float2(rstd, rstd)), y1 = mul2(v[2 * i + 1], make_float2(rstd, rstd));
     if (c < nv) {
-      y = make_float4(v[i].x * rstd, v[i].y * rstd, v[i].z * rstd, v[i].w * rstd);
       if (scale) {
         const float4 g = __ldg(reinterpret_cast<const float4*>(scale) + c);
-        y = make_float4(y.x * (1.f + g.x), y.y * (1.f + g.y), y.z * (1.f + g.z), y.w * (1.f + g.w));
+        y0 = mul2(y0, sum2(make_float2(g.x, g.y), make_float2(1.f, 1.f)));
+        y1 = mul2(y1, sum2(make_float2(g.z, g.w), make_float2(1.f, 1.f)));
       }
       if (shift) {
         const float4 g = __ldg(reinterpret_cast<const float4*>(shift) + c);
-        y = make_float4(y.x + g.x, y.y + g.y, y.z + g.z, y.w + g.w);
+        y0 = sum2(y0, make_float2(g.x, g.y));
+        y1 = sum2(y1, make_float2(g.z, g.w));
       }
     }
-    const uint32_t m = max(max(abs_bits(y.x), abs_bits(y.y)), max(abs_bits(y.z), abs_bits(y.w)));
-    const uint32_t b = e8m0_of(group_max<32>(m));
+    const uint32_t b = e8m0_of(group_max<32>(abs_bits(max3_abs(max3_abs(y0.x, y0.y, y1.x), y1.y, 0.f))));
     const float inv = e8m0_inverse(b);
     if (c == c0) scales[row * lds + c / 32] = (uint8_t)b;
-    if (c < nv)
-      *reinterpret_cast<uint32_t*>(codes + row * ldc + 4 * c) =
-          pack_e4m3x4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+    if (c < nv) {
+      y0 = mul2(y0, make_float2(inv, inv));
+      y1 = mul2(y1, make_float2(inv, inv));
+      *reinterpret_cast<uint32_t*>(to + 4 * c) = pack_e4m3x4(y0.x, y0.y, y1.x, y1.y);
+    }
   }
 }
 
@@ -539,9 +554,10 @@ cudaError_t ln_mod_fp8(const float* x, long ldx, const float* shift, const float
     return launch_kernel(kernel, (unsigned)rows, threads, 0, s, x, ldx, shift, scale, cols,
                          reinterpret_cast<uint8_t*>(codes), ldc, reinterpret_cast<uint8_t*>(scales), lds);
   };
-  if (cols > 5120) return launch(ln_fp8_kernel<256, 6>, 256);
-  if (cols > 3072) return launch(ln_fp8_kernel<256, 5>, 256);
-  return launch(ln_fp8_kernel<128, 6>, 128);
+  if (cols > 5120) return launch(ln_fp8_kernel<256, 6, 5>, 256);
+  if (cols > 3072) return launch(ln_fp8_kernel<256, 5, 6>, 256);
+  if (cols > 1536) return launch(ln_fp8_kernel<128, 6, 10>, 128);
+  return launch(ln_fp8_kernel<128, 3, 14>, 128);  // 4608 x 1536: 9.3 us with the 6, 8.6 so
 }
 
 static cudaError_t cache_grid(CacheArgs* a, unsigned* grid) {

@@ -32,11 +32,10 @@ BAG_DEV uint32_t group_max(uint32_t m) {
 
 // Scale byte of a block with the largest magnitude `amax` (bits): the least b >= 0 with
 // amax <= 448 * 2^(b - 127).  448 = 1.75 * 2^8, so b is amax's exponent - 8, one more where its
-// significand is above 1.75.
+// significand is above 1.75: there the sum carries into the exponent.
 BAG_DEV uint32_t e8m0_of(uint32_t amax) {
-  if (amax >= kInfBits) return 255u;
-  const int b = (int)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return (uint32_t)max(b, 0);
+  const uint32_t b = max((amax + 0x1fffffu) >> 23, 8u) - 8u;
+  return amax >= kInfBits ? 255u : b;
 }
 
 // 1 / scale of byte b <= 247 (exact); NaN for 255, which makes every code of the block NaN.
