@@ -484,8 +484,8 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // only for this one's drain of the shared 32 columns, which the epilogue reads first.
 // The tensor core cuts what an addend has below the accumulator's last bits, towards zero, so the
 // error of a sum grows with K (1.4e-7 of the result at K = 3072, 9.3e-7 at 13824).  A unit of more
-// than F8P_PASS K blocks (LONG) is therefore computed in passes of at most that many, which the
-// epilogue adds in registers (rounded to nearest): 1.2e-6 -> 5.4e-7 at K = 13824, for 2 % more time.
+// K blocks than pass_blocks (LONG) is therefore computed in passes of at most that many, which the
+// epilogue adds in registers (rounded to nearest).
 // Tiles of a last wave that would leave half of the pairs idle are worked on as two halves of 128
 // columns (M = 256, N = 128).
 // warp 0: TMA producer; 1: MMA (even CTA); 2: scale words to shared memory; 3 (even CTA): and to
@@ -493,7 +493,14 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a
 // row a thread, with bias and gate broadcast from shared memory, and its output leaves by TMA:
 // stores, or for the residual stream an add that L2 carries out, so that the stream is not read.
-constexpr int F8P_PASS = 64;  // most K blocks of a pass
+// Most K blocks of a pass.  fp32 outputs: 32, which takes the error of a sum (2-norm, against 64
+// bits) from 1.2e-6 to 2.4e-7 at K = 13824 for 4 % of the time, and leaves K <= 4096 in one pass
+// (2.1e-7 at 3072; 40 blocks in two passes cost 6 %).  bf16 rounds to 4e-3: 64.  Codes: 20, since a
+// sum near the middle of two codes goes to the other one with its whole step: of the 12.6 million
+// codes of 1024 x 12288 x 3072 81 differ from 64 bits in one pass, 51 in two, for 5 % more time.
+__host__ __device__ constexpr int pass_blocks(int kind) {
+  return kind == BAG_FP8_CODES ? 20 : (kind == BAG_FP8_BF16 ? 64 : 32);
+}
 constexpr int F8P_STAGES = 5, F8P_STAGE = 2 * F8_TILE;
 constexpr int F8P_SHARED = 32, F8P_ACC1 = 256 - F8P_SHARED;  // TMEM columns
 constexpr int F8P_SF_COL = F8P_ACC1 + 256, F8P_SF_COLS = 12;  // A's 4 columns, W's 8
@@ -619,10 +626,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
   const int nkb = (g.K + F8_BK - 1) / F8_BK, nruns = (nkb + F8_GROUP * F8_RUN - 1) / (F8_GROUP * F8_RUN);
-  // passes of about the same length, whole runs of scale words each
-  constexpr int RUN = F8_GROUP * F8_RUN;
-  const int passes = LONG ? (nkb + F8P_PASS - 1) / F8P_PASS : 1;
-  const int pass_kb = LONG ? ((nkb + passes - 1) / passes + RUN - 1) / RUN * RUN : nkb;
+  // passes of about the same length, whole groups of scale words each
+  constexpr int most = pass_blocks(KIND);
+  static_assert(most % F8_GROUP == 0, "passes of whole groups");
+  const int least = (nkb + most - 1) / most;  // passes, but for the rounding up to groups
+  const int pass_kb = LONG ? ((nkb + least - 1) / least + F8_GROUP - 1) / F8_GROUP * F8_GROUP : nkb;
+  const int passes = LONG ? (nkb + pass_kb - 1) / pass_kb : 1;
   // units of work: `whole` tiles of 256 x 256, then every later tile as two of 256 x 128
   const long units = 2 * (long)num_m * num_n - whole;
   // first row and column of a unit, and whether it is half a tile; groups of group_rows row tiles
@@ -1086,7 +1095,7 @@ static cudaError_t launch_pair(Fp8Gemm g, cudaStream_t s) {
   auto launch = [&](auto kernel) {
     return launch_kernel(kernel, 2 * pairs, F8P_THREADS, F8P_SMEM, s, ta, tw, th, to, g, rows, whole);
   };
-  const bool l = g.K > F8P_PASS * F8_BK;
+  const bool l = g.K > pass_blocks(g.kind) * F8_BK;
   switch (g.kind) {
     case BAG_FP8_F32: return l ? launch(gemm_fp8_pair_kernel<BAG_FP8_F32, true>) : launch(gemm_fp8_pair_kernel<BAG_FP8_F32, false>);
     case BAG_FP8_BF16: return l ? launch(gemm_fp8_pair_kernel<BAG_FP8_BF16, true>) : launch(gemm_fp8_pair_kernel<BAG_FP8_BF16, false>);
@@ -1124,7 +1133,7 @@ struct Fp8Plan {
   int BN;    // 0: CTA pairs
   int logS;
 };
-static Fp8Plan plan_fp8(long M, long N, long K) {
+static Fp8Plan plan_fp8(long M, long N, long K, int kind) {
   auto cd = [](long a, long b) { return (a + b - 1) / b; };
   const double nkb = (double)cd(K, F8_BK);
   // the operands' way from HBM beside the time of the CTAs: a smooth maximum of the two, so that of
@@ -1144,7 +1153,7 @@ static Fp8Plan plan_fp8(long M, long N, long K) {
     if (t.BN < 64 && M > t.BN) continue;  // narrow tiles read W again for every tile of rows
     for (int logS = 0; logS <= 3 && nkb >= (double)(2 << logS); ++logS) {
       const double kb = (double)cd(cd(K, F8_BK), 1L << logS);
-      if (kb > F8P_PASS && logS < 3) continue;  // a longer sum on the tensor core loses precision (see LONG)
+      if (kb > pass_blocks(kind) && logS < 3) continue;  // a longer sum on the tensor core loses precision (see LONG)
       const double more = (double)(cd(cd(M, t.BN) * cd(N, 128) << logS, cluster_sms(logS)) - 1);
       us = together(t.start + 0.2 * kb + more * (t.wave + t.share * kb) + (logS ? 0.84 : 0.0) + 0.15 * (1 << logS));
       if (us < best) {
@@ -1158,7 +1167,7 @@ static Fp8Plan plan_fp8(long M, long N, long K) {
 
 cudaError_t gemm_fp8(Fp8Gemm g, cudaStream_t s) {
   if (g.M <= 0 || g.N <= 0) return cudaSuccess;
-  const Fp8Plan p = plan_fp8(g.M, g.N, g.K);
+  const Fp8Plan p = plan_fp8(g.M, g.N, g.K, g.kind);
   switch (p.BN) {
     case 16: return launch_few<16>(g, p.logS, s);
     case 32: return launch_few<32>(g, p.logS, s);
