@@ -497,7 +497,7 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // bits) from 1.2e-6 to 2.4e-7 at K = 13824 for 4 % of the time, and leaves K <= 4096 in one pass
 // (2.1e-7 at 3072; 40 blocks in two passes cost 6 %).  bf16 rounds to 4e-3: 64.  Codes: 20, since a
 // sum near the middle of two codes goes to the other one with its whole step: of the 12.6 million
-// codes of 1024 x 12288 x 3072 81 differ from 64 bits in one pass, 51 in two, for 5 % more time.
+// codes of 1024 x 12288 x 3072 81 differ from 64 bits in one pass, 51 in two, for 3 % more time.
 __host__ __device__ constexpr int pass_blocks(int kind) {
   return kind == BAG_FP8_CODES ? 20 : (kind == BAG_FP8_BF16 ? 64 : 32);
 }
@@ -999,21 +999,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
           release(tempty_even);
         }
       } else if constexpr (LONG) {
+        // the first pass's loads are in flight together (a wait for each 16 columns, added to zeros:
+        // 4608 x 12288 x 3072 codes 114 us against 110)
         float v[128];
-#pragma unroll
-        for (int j = 0; j < 128; ++j) v[j] = 0.f;
+        if (!(ok = begin())) break;
+        auto load = [&](int c) { tmem_ld32_nowait(tb + (uint32_t)c, reinterpret_cast<uint32_t*>(v) + c); };
+        if (acc) {  // the shared columns first
+          load(0);
+          tmem_ld_wait();
+          if (shares) release(free_even);
+          load(96);
+        } else {
+          load(96);
+          tmem_ld_wait();
+          if (shares) release(free_even);
+          load(0);
+        }
+        load(32);
+        load(64);
+        tmem_ld_wait();
+        release(tempty_even);
 #pragma unroll 1
-        for (int pass = 0; pass < passes && (ok = begin()); ++pass) {
+        for (int pass = 1; pass < passes && (ok = begin()); ++pass) {
           auto add = [&](int c) {
+            float t[32];
+            tmem_ld32(tb + (uint32_t)c, t);
 #pragma unroll
-            for (int h = c; h < c + 32; h += 16) {
-              float t[16];
-              tmem_ld16(tb + (uint32_t)h, t);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) v[h + j] += t[j];
+            for (int j = 0; j < 32; j += 2) {
+              const float2 w = sum2(make_float2(v[c + j], v[c + j + 1]), make_float2(t[j], t[j + 1]));
+              v[c + j] = w.x;
+              v[c + j + 1] = w.y;
             }
           };
-          if (acc) {  // the shared columns first
+          if (acc) {
             add(0);
             if (shares) release(free_even);
             add(96);
