@@ -16,6 +16,11 @@
 // parts for a cluster of C CTAs, and rank r merges 128 / C rows of the 2 C partial outputs through
 // distributed shared memory.  A launch in pairs shares (C = 1) the units of its last wave where
 // they would leave half of the slots idle.
+//
+// Bound: shared memory.  Lists differ from slot to slot, so each slot loads its own K and V^T, and a step of
+// both moves 320 KB through it (2560 cycles at 128 bytes; the products are 2048 and dense attention,
+// whose slots share the tiles, takes 2800): 3400 cycles taken.  32,760 queries x 4 heads, 64 of 256
+// blocks: 392 us (1402 TFLOP/s; floor 290), 40 heads 4.1 ms.
 #include <algorithm>
 #include <cmath>
 
@@ -478,7 +483,8 @@ __global__ void __launch_bounds__(BT_THREADS, 1)
 // fp32 products, sums and probabilities.  Sixteen lanes hold a row of K (16 bytes each), or of V^T;
 // eight rows a lane, so a warp takes 16 keys, then 16 columns of the output.  The values of a block
 // are in flight while its scores are taken, the next block's keys while the values are summed.
-// Rank 0 merges the ranks' sums in order.
+// Rank 0 merges the ranks' sums in order.  40 heads x 32 blocks of 256: 15.4 us (5.5 TB/s; floor 12.4); 24
+// heads x 8 blocks 4.5.
 constexpr int TK_TH = 256, TK_MAX_C = 8;
 
 // Element pairs of 16 bytes.

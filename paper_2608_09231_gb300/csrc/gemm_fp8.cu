@@ -119,6 +119,9 @@ __host__ __device__ __forceinline__ bool wide_scales(const uint8_t* s, long lds)
 // warp 0: TMA producer; 1: MMA; 2: scale words to shared memory; 3: and to tensor memory; 4 .. 7:
 // epilogue, thread = column n.
 // The ring is as deep as the CTAs that share an SM leave room for (`stages`, at most F8F_MAX).
+// Bound: W's way from HBM where it is large, the launch's start and end where not.  1 x 13824 x 5120
+// (BN 16, four CTAs a tile, 432 of them) takes 12 us in a chain of launches (6 TB/s of W; floor 10.5), 77 x
+// 2048 x 512 about 5.
 constexpr int F8F_MAX = 10;
 template <int BN>
 struct FewCfg {
@@ -488,6 +491,9 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // epilogue adds in registers (rounded to nearest).
 // Tiles of a last wave that would leave half of the pairs idle are worked on as two halves of 128
 // columns (M = 256, N = 128).
+// Bound: tensor cores and power.  A K block takes about 690 cycles of 512 ideal ones; 8192^3 to fp32
+// 300 to 314 us (3500 to 3660 TFLOP/s), 4608 x 12288 x 3072 with GELU to codes 110 (3160; floor 92),
+// 4608 x 3072 x 12288 into the residual stream 113.
 // warp 0: TMA producer; 1: MMA (even CTA); 2: scale words to shared memory; 3 (even CTA): and to
 // tensor memory; 4 .. 11: epilogue, two warps to each lane quarter, 128 columns (one output block) each.
 // The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a

@@ -201,6 +201,9 @@ struct CacheFmt {
   static constexpr int TOP = BITS == 8 ? 127 : 7;
   static constexpr int LANES = GROUP / 4;  // lanes of one group, four columns a lane
 };
+// A warp takes CS steps of 128 columns of a row, all loads first; 8-bit groups are its 32 lanes, 4-bit
+// ones eight lanes.  Bound: HBM, at the rate of a plain copy: 32,760 x 5120 written in 218 us and read in
+// 213 (8 bits, 9 bytes an element: 6.9 TB/s), 206 and 204 (4 bits); 6889 x 3072, 8 bits, one after the other 61.7.
 constexpr int CS = 4, C_WARPS = 8, C_SEG = CS * 128;  // steps of a warp, warps of a CTA, columns of a warp
 
 BAG_DEV float4 load_cols(const float* p, int valid, bool vec) {
@@ -330,6 +333,8 @@ __global__ void __launch_bounds__(C_WARPS * 32) cache_read_kernel(const CacheArg
 // ---------------------------------------------------------------------------
 // pooled vectors and selection of attention blocks
 // ---------------------------------------------------------------------------
+// Bound: HBM, which 128 rows' bytes of a head (32 KB a CTA) reach in one round of loads: 32,760 rows x 40
+// heads 54 us (floor 49; 125 with rows converted as they came).
 constexpr int P_TH = 256;
 
 // Eight elements of a row as 16 bytes, zeros where there is no row.
@@ -411,7 +416,10 @@ __global__ void __launch_bounds__(P_TH, 4) block_pool_kernel(const T* __restrict
 
 // One CTA pools its block of queries, scores every key block (eight lanes a block, 16 codes a
 // lane, sums of four products in integers) and keeps the `keep` largest scores.  Scores become
-// unsigned keys of the same order; four passes over 8-bit digits find the keep-th largest.
+// unsigned keys of the same order; four passes over 8-bit digits find the keep-th largest.  Bound:
+// latency (the query block's rows, the pooled keys, then some twenty barriers): 4.6 us for one query, 40
+// heads and 256 key blocks, 14.4 for 32,760 queries and 4 heads (two waves of four CTAs an SM; 4.9 of
+// reading q), 25 with the rows and keys loaded a step at a time.
 template <typename T>
 __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict__ q, long ldq, long nq, int vec,
                                                             const int8_t* __restrict__ codes,
