@@ -491,9 +491,9 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // epilogue adds in registers (rounded to nearest).
 // Tiles of a last wave that would leave half of the pairs idle are worked on as two halves of 128
 // columns (M = 256, N = 128).
-// Bound: tensor cores and power.  A K block takes about 690 cycles of 512 ideal ones; 8192^3 to fp32
-// 300 to 314 us (3500 to 3660 TFLOP/s), 4608 x 12288 x 3072 with GELU to codes 110 (3160; floor 92),
-// 4608 x 3072 x 12288 into the residual stream 113.
+// Bound: tensor cores and power.  A K block takes about 650 cycles of 512 ideal ones (a stage of the ring comes
+// round in 3300); 8192^3 to fp32 287 to 300 us, 4608 x 12288 x 3072 with GELU to codes 109 (3190 TFLOP/s;
+// floor 92), 4608 x 3072 x 12288 into the residual stream 107.
 // warp 0: TMA producer; 1: MMA (even CTA); 2: scale words to shared memory; 3 (even CTA): and to
 // tensor memory; 4 .. 11: epilogue, two warps to each lane quarter, 128 columns (one output block) each.
 // The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a
@@ -760,36 +760,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
           for (int kg = k0; kg < k1 && ok; kg += F8_GROUP, ++grp) {
             const uint32_t sa = tm + F8P_SF_COL + (grp & 1) * F8P_SF_COLS;
             if (!(ok = mbar_wait_warp(sf_ready + (grp & 1), (grp >> 1) & 1u, abort_flag))) break;
+            // a K block at a time: to wait for two holds the first one's stage longer, and the ring is what
+            // limits the rate (8192^3, operands of zeros: 297 us in pairs, 287 so; 348 with four stages)
 #pragma unroll
-            for (int b = 0; b < F8_GROUP; b += 2) {  // two K blocks at a time
+            for (int b = 0; b < F8_GROUP; ++b) {
               if (kg + b >= k1) break;
-              const bool two = kg + b + 1 < k1;
-              int s1 = s;
-              uint32_t ph1 = ph;
-              next(s1, ph1);
               if (!(ok = mbar_wait_warp(full + s, ph, abort_flag))) break;
-              if (two && !(ok = mbar_wait_warp(full + s1, ph1, abort_flag))) break;
               tc_fence_after();
-              const uint64_t a0 = sw128_desc(base + s * F8P_STAGE), a1 = sw128_desc(base + s1 * F8P_STAGE);
+              const uint64_t a0 = sw128_desc(base + s * F8P_STAGE);
               if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < F8_BK / 32; ++k)  // 32 bytes along K: two 16-byte units
                   pair_mma_mxf8(dt, a0 + 2 * k, a0 + (F8_TILE >> 4) + 2 * k, shape | scale_byte(b), sa, sa + 4,
                                 k > 0 ? 1u : add);
                 pair_commit(empty + s, 3);
-                if (two) {
-#pragma unroll
-                  for (int k = 0; k < F8_BK / 32; ++k)
-                    pair_mma_mxf8(dt, a1 + 2 * k, a1 + (F8_TILE >> 4) + 2 * k, shape | scale_byte(b + 1), sa, sa + 4, 1u);
-                  pair_commit(empty + s1, 3);
-                }
-                if (b + 2 == F8_GROUP || kg + b + 2 >= k1) pair_commit(sf_used + (grp & 1), 1);
+                if (b + 1 == F8_GROUP || kg + b + 1 >= k1) pair_commit(sf_used + (grp & 1), 1);
               }
               __syncwarp();
               add = 1;
-              s = s1;
-              ph = ph1;
-              if (two) next(s, ph);
+              next(s, ph);
             }
           }
           if (!ok) break;
