@@ -1152,7 +1152,13 @@ static Fp8Plan plan_fp8(long M, long N, long K, int kind) {
   // the operands' way from HBM beside the time of the CTAs: a smooth maximum of the two, so that of
   // splits that HBM bounds alike the one with more loads in flight is taken
   const double dram = (double)(M + N) * (double)K / 6.5e6 + 3.8;
-  auto together = [&](double us) { return std::pow(std::pow(us, 8.0) + std::pow(dram, 8.0), 1.0 / 8.0); };
+  auto pow8 = [](double x) {
+    x *= x;
+    x *= x;
+    return x * x;
+  };
+  const double dram8 = pow8(dram);
+  auto together = [&](double us) { return std::sqrt(std::sqrt(std::sqrt(pow8(us) + dram8))); };
   const long full = cd(M, 256) * cd(N, 256), pairs = std::max(1, sm_count() / 2), whole = whole_tiles(full, pairs);
   double us = 4.6 + (double)cd(whole, pairs) * (3.6 + 0.27 * nkb);
   if (whole < full) us += 1.6 + 0.19 * nkb;  // a wave of halves
