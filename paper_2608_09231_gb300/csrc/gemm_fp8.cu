@@ -1139,7 +1139,7 @@ cudaError_t gemm_fp8_init() {
 
 // Which kernel, tile and split: the least expected time.  The constants (us) fit 247 shapes of 1 to
 // 2048 rows, 512 to 13824 columns and K, each timed under every choice (3000 timings, chained
-// launches); the choice is within 1.4 % of the best one on average, 28 % at most (50 rows through
+// launches); the choice is within 1.1 % of the best one on average, 24 % at most (50 rows through
 // 5120 x 13824).  A CTA of either kernel takes about 0.2 us a K block whatever its tile (the issue
 // of its four MMAs and their waits), so few tiles want K split, and many the largest tile.
 struct Fp8Plan {
