@@ -416,32 +416,35 @@ __global__ void __launch_bounds__(P_TH, 4) block_pool_kernel(const T* __restrict
 
 // One CTA pools its block of queries, scores every key block (eight lanes a block, 16 codes a
 // lane, sums of four products in integers) and keeps the `keep` largest scores.  Scores become
-// unsigned keys of the same order; four passes over 8-bit digits find the keep-th largest.  Bound:
-// latency (the query block's rows, the pooled keys, then some twenty barriers): 4.6 us for one query, 40
-// heads and 256 key blocks, 14.4 for 32,760 queries and 4 heads (two waves of four CTAs an SM; 4.9 of
-// reading q), 25 with the rows and keys loaded a step at a time.
+// unsigned keys of the same order; passes over 8-bit digits find the keep-th largest, as many as it
+// takes until all keys with the digits found so far are kept (two, mostly).  Bound: latency (the query
+// block's rows, the pooled keys, then some ten barriers), which the CTAs of an SM hide from each other:
+// five (48 registers) with four key steps in flight take 96 us for 32,760 queries, 40 heads and 256 key
+// blocks (reading q 49), 12.5 for 4 heads, 4.2 for one query and 40 heads.  Four CTAs with eight steps in
+// flight took 107, 13.4 and 4.2, and 32 us instead of 36 for one query and 7813 key blocks; key codes
+// brought to shared memory while the queries are pooled 113, 15.0 and 4.6; always four passes 119 and 14.4.
 template <typename T>
-__global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict__ q, long ldq, long nq, int vec,
-                                                            const int8_t* __restrict__ codes,
-                                                            const float* __restrict__ scales, long ldb, int nkb,
-                                                            int group, int keep, int* __restrict__ blocks) {
+__global__ void __launch_bounds__(P_TH, 5)
+    block_select_kernel(const T* __restrict__ q, long ldq, long nq, int vec, const int8_t* __restrict__ codes,
+                        const float* __restrict__ scales, long ldb, int nkb, int group, int keep,
+                        int* __restrict__ blocks) {
   grid_dep_sync();
-  extern __shared__ uint32_t keys[];
+  extern __shared__ uint32_t key[];
   __shared__ __align__(16) float sums[16][128];
   __shared__ uint32_t red[4];
   __shared__ __align__(16) int8_t qc[128];
-  __shared__ int hist[256], warp_sum[P_TH / 32];
-  __shared__ uint32_t found[2];  // the digit, and how many keys above it
-  const long b = blockIdx.x, h = blockIdx.y;
+  __shared__ int hist[2][256], warp_sum[P_TH / 32];
+  __shared__ uint32_t found[3];  // the digit, how many keys are above it and how many have it
+  const long b = blockIdx.x, h = blockIdx.y, kh = h / group;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  hist[0][threadIdx.x] = 0;
   int code;
   pool_block<T>(q + b * 128 * ldq + h * 128, ldq, (int)min(128L, nq - b * 128), vec, sums, red, &code);
   if (threadIdx.x < 128) qc[threadIdx.x] = (int8_t)code;
   __syncthreads();
-  const long kh = h / group;
   const int4 a = reinterpret_cast<const int4*>(qc)[lane % 8];
   const int4* kc = reinterpret_cast<const int4*>(codes + kh * ldb * 128) + lane % 8;
-  constexpr int KU = 8;  // steps whose loads are in flight together
+  constexpr int KU = 4;  // steps whose loads are in flight together
   for (int j0 = warp * 4 + lane / 8; j0 - lane / 8 < nkb; j0 += KU * P_TH / 8) {
     int4 k[KU];
     float sc[KU];
@@ -459,22 +462,23 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
       for (int o = 4; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
       if (j < nkb && lane % 8 == 0) {
         const uint32_t u = __float_as_uint((float)dot * sc[i] + 0.f);  // no -0
-        keys[j] = u & 0x80000000u ? ~u : u | 0x80000000u;
+        key[j] = u & 0x80000000u ? ~u : u | 0x80000000u;
       }
     }
   }
+  __syncthreads();
   uint32_t top = 0, mask = 0;  // the digits found so far, and where they are
-  int need = keep;             // of the keys that have them
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[threadIdx.x] = 0;
-    __syncthreads();
+  int need = keep, same_all = nkb;  // of the keys that have them: how many are kept, and how many there are
+  for (int shift = 24; shift >= 0 && need < same_all; shift -= 8) {
+    int* bins = hist[shift >> 3 & 1 ^ 1];
     for (int j = threadIdx.x; j < nkb; j += P_TH)
-      if ((keys[j] & mask) == top) atomicAdd(hist + (keys[j] >> shift & 255u), 1);
+      if ((key[j] & mask) == top) atomicAdd(bins + (key[j] >> shift & 255u), 1);
+    hist[shift >> 3 & 1][threadIdx.x] = 0;  // the next pass's
     __syncthreads();
     if (warp == 0) {  // lane l: digits 255 - 8 l .. 248 - 8 l
       int n[8], mine = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mine += n[i] = hist[255 - 8 * lane - i];
+      for (int i = 0; i < 8; ++i) mine += n[i] = bins[255 - 8 * lane - i];
       int before = mine;
 #pragma unroll
       for (int o = 1; o < 32; o *= 2) {
@@ -487,6 +491,7 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
         if (before < need && before + n[i] >= need) {
           found[0] = (uint32_t)(255 - 8 * lane - i);
           found[1] = (uint32_t)before;
+          found[2] = (uint32_t)n[i];
         }
         before += n[i];
       }
@@ -495,13 +500,14 @@ __global__ void __launch_bounds__(P_TH) block_select_kernel(const T* __restrict_
     top |= found[0] << shift;
     mask |= 255u << shift;
     need -= (int)found[1];
+    same_all = (int)found[2];
   }
-  // every key above `top`, and the first `need` that equal it, in order
+  // every key whose digits are above `top`, and the first `need` that have them, in order
   int* out = blocks + (h * gridDim.x + b) * keep;
   int kept = 0, equal = 0;  // of the keys before this round's
   for (int j0 = 0; j0 < nkb; j0 += P_TH) {
     const int j = j0 + (int)threadIdx.x;
-    const uint32_t k = j < nkb ? keys[j] : 0u;
+    const uint32_t k = j < nkb ? key[j] & mask : 0u;
     const bool above = j < nkb && k > top, same = j < nkb && k == top;
     const uint32_t wa = __ballot_sync(0xffffffffu, above), ws = __ballot_sync(0xffffffffu, same);
     if (lane == 0) warp_sum[warp] = __popc(wa) << 16 | __popc(ws);
