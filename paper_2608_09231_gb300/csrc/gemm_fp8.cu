@@ -67,11 +67,13 @@ BAG_DEV void tmem_ld16(uint32_t taddr, float* v) {
 
 // The scale words of one run of groups (run r: K blocks 16 r .. 16 r + 15) for the 128 rows from
 // row0 on: rows row0 + 32 c + lane, c = 0 .. 3.  Rows past the end have scale 1 (their codes are
-// zeros).  16-byte loads where the rows allow them: a row's words of a run lie in one sector, and
-// with word loads every group would fetch it again (the ring leaves L1 too small to keep it).
+// zeros), and so have K blocks in words past the last of the nkb.  16-byte loads where the rows
+// allow them: a row's words of a run lie in one sector, and with word loads every group would fetch
+// it again (the ring leaves L1 too small to keep it).  Each load holds a byte of the row, so none
+// leaves the operand, also where the row is a part of a longer one (columns of a wider buffer).
 struct ScaleRun {
   uint4 w[4];
-  BAG_DEV void fetch(const uint8_t* __restrict__ s, long lds, bool wide, int row0, int rows, int run) {
+  BAG_DEV void fetch(const uint8_t* __restrict__ s, long lds, bool wide, int row0, int rows, int run, int nkb) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int row = row0 + 32 * c + (int)(threadIdx.x & 31);
@@ -82,7 +84,7 @@ struct ScaleRun {
         w[c] = __ldg(reinterpret_cast<const uint4*>(p));
       } else {
         const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
-        const long left = lds / 4 - run * 4;  // words of the row from here on
+        const int left = (nkb + 3) / 4 - run * 4;  // words of the row from here on
         if (left > 0) w[c].x = __ldg(q);
         if (left > 1) w[c].y = __ldg(q + 1);
         if (left > 2) w[c].z = __ldg(q + 2);
@@ -327,8 +329,8 @@ __global__ void __launch_bounds__(256)
     ScaleRun w, a;
     auto fetch = [&](int r) {
       if (r < r1) {
-        w.fetch(g.w_s, g.ldws, wide_w, n0, g.N, r);
-        a.fetch(g.a_s, g.ldas, wide_a, m0, min(g.M, m0 + BN), r);
+        w.fetch(g.w_s, g.ldws, wide_w, n0, g.N, r, nkb);
+        a.fetch(g.a_s, g.ldas, wide_a, m0, min(g.M, m0 + BN), r, nkb);
       }
     };
     fetch(r0);
@@ -837,9 +839,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
       const bool wide_a = wide_scales(g.a_s, g.ldas), wide_w = wide_scales(g.w_s, g.ldws);
       ScaleRun w[3];
       auto fetch = [&]() {
-        w[0].fetch(g.a_s, g.ldas, wide_a, m0 + (int)rank * 128, g.M, r);
-        w[1].fetch(g.w_s, g.ldws, wide_w, n0, g.N, r);
-        if (!half) w[2].fetch(g.w_s, g.ldws, wide_w, n0 + 128, g.N, r);
+        w[0].fetch(g.a_s, g.ldas, wide_a, m0 + (int)rank * 128, g.M, r, nkb);
+        w[1].fetch(g.w_s, g.ldws, wide_w, n0, g.N, r, nkb);
+        if (!half) w[2].fetch(g.w_s, g.ldws, wide_w, n0 + 128, g.N, r, nkb);
       };
       long unit = pair;
       if (unit < units) {
