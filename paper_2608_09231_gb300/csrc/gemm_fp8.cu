@@ -111,13 +111,36 @@ __host__ __device__ __forceinline__ bool wide_scales(const uint8_t* s, long lds)
 
 }  // namespace
 
+// The tensor core cuts what an addend has below the accumulator's last bits, towards zero, so the
+// error of a sum grows with K (1.4e-7 of the result at K = 3072, 9.3e-7 at 13824).  A sum of more K
+// blocks than pass_blocks (the kernels' LONG forms) is therefore computed in passes of at most that
+// many, which the epilogue adds in registers (rounded to nearest).
+// Most K blocks of a pass.  fp32 outputs: 32, which takes the error of a sum (2-norm, against 64
+// bits) from 1.2e-6 to 2.4e-7 at K = 13824 for 4 % of the time, and leaves K <= 4096 in one pass
+// (2.1e-7 at 3072; 40 blocks in two passes cost 6 %).  bf16 rounds to 4e-3: 64.  Codes: 20, since a
+// sum near the middle of two codes goes to the other one with its whole step: of the 12.6 million
+// codes of 1024 x 12288 x 3072 81 differ from 64 bits in one pass, 51 in two, for 3 % more time.
+__host__ __device__ constexpr int pass_blocks(int kind) {
+  return kind == BAG_FP8_CODES ? 20 : (kind == BAG_FP8_BF16 ? 64 : 32);
+}
+// Blocks of one of the passes that n K blocks take: about as many in each, whole groups of scale words.
+__host__ __device__ constexpr int pass_length(int n, int most) {
+  const int passes = (n + most - 1) / most;  // but for the rounding up to groups
+  return ((n + passes - 1) / passes + F8_GROUP - 1) / F8_GROUP * F8_GROUP;
+}
+static_assert(pass_blocks(BAG_FP8_F32) % F8_GROUP == 0 && pass_blocks(BAG_FP8_BF16) % F8_GROUP == 0 &&
+                  pass_blocks(BAG_FP8_CODES) % F8_GROUP == 0 && pass_blocks(BAG_FP8_RESID) % F8_GROUP == 0,
+              "passes of whole groups");
+
 // ---------------------------------------------------------------------------
 // Few rows: W is the M operand
 // ---------------------------------------------------------------------------
 // A CTA computes the transposed tile of 128 columns n and BN rows m: W's rows are the MMA's 128
 // rows, A's the N operand, which may be as narrow as 16.  Clusters of S CTAs split K and add
 // their parts through distributed shared memory in rank order (rank r finishes rows m = r, r + S,
-// ... of the tile).
+// ... of the tile).  A CTA's part of K that is longer than a pass (LONG) is summed in passes, like the
+// pair kernel's units; the sums go back to tensor memory, from where the epilogue takes them either way
+// (16 x 512 x 65536 to fp32: 22.2 us, 20.6 with parts of 64 K blocks in one sum each).
 // warp 0: TMA producer; 1: MMA; 2: scale words to shared memory; 3: and to tensor memory; 4 .. 7:
 // epilogue, thread = column n.
 // The ring is as deep as the CTAs that share an SM leave room for (`stages`, at most F8F_MAX).
@@ -144,7 +167,13 @@ struct FewCfg {
   }
 };
 
-template <int BN>
+// First K block of a rank's part (rank S: one past the last): an even one, since blocks are issued in
+// pairs.
+__host__ __device__ constexpr int few_cut(int r, int S, int nkb) {
+  return r == S ? nkb : (int)((long)r * nkb / S) & ~1;
+}
+
+template <int BN, bool LONG>
 __global__ void __launch_bounds__(256)
     gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                         const __grid_constant__ Fp8Gemm g, int logS, int stages) {
@@ -160,18 +189,20 @@ __global__ void __launch_bounds__(256)
   uint64_t* sf_ready = sf_empty + 2;  // [2]: a group's scales are in tensor memory
   uint64_t* sf_used = sf_ready + 2;   // [2]: a group's products are done, its TMEM columns free
   uint64_t* tfull = sf_used + 2;
-  uint64_t* sf_drain = tfull + 1;
+  uint64_t* tempty = tfull + 1;       // LONG: a pass's sums are read
+  uint64_t* sf_drain = tempty + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sf_drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert((2 * F8F_MAX + 11) * 8 + 8 <= 256, "the barriers, the address of tensor memory and the flag");
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int S = 1 << logS, rank = logS > 0 ? (int)cluster_ctarank() : 0;
   const int mt = (g.M + BN - 1) / BN, unit = (int)(blockIdx.x >> logS);
   const int m0 = unit % mt * BN, n0 = unit / mt * 128;
   const int nkb = (g.K + F8_BK - 1) / F8_BK;
-  // this rank's K blocks: from an even one on, since they are issued in pairs
-  auto cut = [&](int r) { return r == S ? nkb : (int)((long)r * nkb / S) & ~1; };
-  const int kb0 = cut(rank), kb1 = cut(rank + 1);
+  const int kb0 = few_cut(rank, S, nkb), kb1 = few_cut(rank + 1, S, nkb);  // this rank's K blocks
+  const int kg0 = kb0 & ~(F8_GROUP - 1);                                   // and their first group
+  const int pass_kb = LONG ? pass_length(kb1 - kg0, pass_blocks(g.kind)) : 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
@@ -185,6 +216,7 @@ __global__ void __launch_bounds__(256)
       mbar_init(sf_used + s, 1);
     }
     mbar_init(tfull, 1);
+    mbar_init(tempty, 4);  // the epilogue's warps
     mbar_init(sf_drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -248,8 +280,17 @@ __global__ void __launch_bounds__(256)
       }
     };
     bool good = true;
-    for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1 && good; kg += F8_GROUP, ++grp) {  // groups, maybe cut
+    uint32_t passes = 0;  // handed to the epilogue so far
+    for (int kg = kg0; kg < kb1 && good; kg += F8_GROUP, ++grp) {  // groups, maybe cut
       const uint32_t sw = tm + C::SF_COL + (grp & 1) * 8;
+      if constexpr (LONG) {
+        if (kg > kg0 && (kg - kg0) % pass_kb == 0) {
+          if (elect_one()) mma_commit(tfull);
+          __syncwarp();
+          if (!(good = mbar_wait_warp(tempty, passes++ & 1u, abort_flag))) break;
+          add = 0;
+        }
+      }
       if (!(good = mbar_wait_warp(sf_ready + (grp & 1), (uint32_t)(grp >> 1) & 1u, abort_flag))) break;
 #pragma unroll
       for (int b = 0; b < F8_GROUP; b += 2) {
@@ -287,9 +328,11 @@ __global__ void __launch_bounds__(256)
     // all MMAs issued so far (whatever happened above) finish before tfull completes, and
     // the bounded wait keeps tensor memory until then
     if (elect_one()) {
-      mma_commit(tfull);
       const uint64_t t0 = global_ns();
-      while (!mbar_try_wait(tfull, 0) && global_ns() - t0 < kWaitLimitNs) {
+      while (passes > 0 && !mbar_try_wait(tfull, (passes - 1) & 1u) && global_ns() - t0 < kWaitLimitNs) {
+      }
+      mma_commit(tfull);
+      while (!mbar_try_wait(tfull, passes & 1u) && global_ns() - t0 < kWaitLimitNs) {
       }
     }
     __syncwarp();
@@ -297,7 +340,7 @@ __global__ void __launch_bounds__(256)
     // ---------------- scales to tensor memory, a group ahead of the products ----------------
     const uint32_t sf = smem_u32(rest);
     int run = 0, grp = 0;
-    for (int kg = kb0 & ~(F8_GROUP - 1); kg < kb1; kg += F8_GROUP, ++grp) {
+    for (int kg = kg0; kg < kb1; kg += F8_GROUP, ++grp) {
       if (run == 0 || kg % (F8_GROUP * F8_RUN) == 0) {
         if (!mbar_wait_warp(sf_full + (run & 1), (uint32_t)(run >> 1) & 1u, abort_flag)) break;
         ++run;
@@ -352,7 +395,38 @@ __global__ void __launch_bounds__(256)
   const int cols = min(BN, g.M - m0);
   const int per = BN >> logS;                            // rows m of the tile a rank finishes
   float* part = reinterpret_cast<float*>(smem);          // [S][per][128]
-  if (epi) mbar_wait(tfull, 0, abort_flag);
+  const uint32_t tb = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  if constexpr (LONG) {
+    if (epi) {
+      float sum[BN];
+#pragma unroll
+      for (int c = 0; c < BN; ++c) sum[c] = 0.f;
+      bool good = true;
+      uint32_t pass = 0;
+#pragma unroll 1
+      for (int kg = kg0; kg < kb1; kg += pass_kb, ++pass) {
+        if (!(good = __all_sync(0xffffffffu, mbar_wait(tfull, pass & 1u, abort_flag)))) break;
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < BN; c += 16) {
+          float t[16];
+          tmem_ld16(tb + (uint32_t)c, t);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sum[c + j] += t[j];
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty);
+      }
+      if (good) {  // no product writes the accumulator any more
+#pragma unroll
+        for (int c = 0; c < BN; c += 16) tmem_st16(tb + (uint32_t)c, reinterpret_cast<const uint32_t*>(sum + c));
+        tmem_st_wait();
+      }
+    }
+  } else {
+    if (epi) mbar_wait(tfull, 0, abort_flag);
+  }
   __syncwarp();
   tc_fence_before();
   // every product is done, here and in the cluster: the rings are free.  No role waits after
@@ -363,7 +437,6 @@ __global__ void __launch_bounds__(256)
     __syncthreads();
   tc_fence_after();
   const bool ok = !*abort_flag;
-  const uint32_t tb = tmem + ((uint32_t)((warp & 3) * 32) << 16);
   if (logS > 0) {
     if (epi && ok) {
       const uint32_t here = smem_u32(part) + (uint32_t)((rank * per * 128 + row) * 4);
@@ -464,6 +537,13 @@ static long cluster_sms(int logS) {
   return logS < 2 ? sms : (logS == 2 ? sms - sms / 19 : sms - sms / 19 * 4);  // 152, 152, 144, 120 of 152
 }
 
+// K blocks of the longest of S parts.
+static int few_longest(int S, int nkb) {
+  int most = 0;
+  for (int r = 0; r < S; ++r) most = std::max(most, few_cut(r + 1, S, nkb) - few_cut(r, S, nkb));
+  return most;
+}
+
 template <int BN>
 static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
   CUtensorMap tw, ta;
@@ -474,8 +554,12 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
   if (units << logS > 0x7fffffffL) return cudaErrorInvalidConfiguration;
   const long sms = cluster_sms(logS), ctas = units << logS;
   const int stages = FewCfg<BN>::stages(ctas <= sms ? 1 : (ctas <= 2 * sms ? 2 : 3));
-  return launch_cluster(gemm_fp8_few_kernel<BN>, logS > 0 ? 1u << logS : 0u, (unsigned)ctas, 256,
-                        stages * FewCfg<BN>::STAGE + FewCfg<BN>::REST, s, tw, ta, g, logS, stages);
+  auto launch = [&](auto kernel) {
+    return launch_cluster(kernel, logS > 0 ? 1u << logS : 0u, (unsigned)ctas, 256,
+                          stages * FewCfg<BN>::STAGE + FewCfg<BN>::REST, s, tw, ta, g, logS, stages);
+  };
+  const int part = few_longest(1 << logS, (g.K + F8_BK - 1) / F8_BK);
+  return part > pass_blocks(g.kind) ? launch(gemm_fp8_few_kernel<BN, true>) : launch(gemm_fp8_few_kernel<BN, false>);
 }
 
 // ---------------------------------------------------------------------------
@@ -487,10 +571,6 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // Two accumulators of 256 columns fill tensor memory, which the scales need a little of: the second
 // one starts 32 columns inside the first (columns 224 .. 479), and the tile after this one waits
 // only for this one's drain of the shared 32 columns, which the epilogue reads first.
-// The tensor core cuts what an addend has below the accumulator's last bits, towards zero, so the
-// error of a sum grows with K (1.4e-7 of the result at K = 3072, 9.3e-7 at 13824).  A unit of more
-// K blocks than pass_blocks (LONG) is therefore computed in passes of at most that many, which the
-// epilogue adds in registers (rounded to nearest).
 // Tiles of a last wave that would leave half of the pairs idle are worked on as two halves of 128
 // columns (M = 256, N = 128).
 // Bound: tensor cores and power.  A K block takes about 650 cycles of 512 ideal ones (a stage of the ring comes
@@ -501,14 +581,6 @@ static cudaError_t launch_few(const Fp8Gemm& g, int logS, cudaStream_t s) {
 // The epilogue is the longer part of a tile with few K blocks (24 are 12,300 cycles), so it keeps a
 // row a thread, with bias and gate broadcast from shared memory, and its output leaves by TMA:
 // stores, or for the residual stream an add that L2 carries out, so that the stream is not read.
-// Most K blocks of a pass.  fp32 outputs: 32, which takes the error of a sum (2-norm, against 64
-// bits) from 1.2e-6 to 2.4e-7 at K = 13824 for 4 % of the time, and leaves K <= 4096 in one pass
-// (2.1e-7 at 3072; 40 blocks in two passes cost 6 %).  bf16 rounds to 4e-3: 64.  Codes: 20, since a
-// sum near the middle of two codes goes to the other one with its whole step: of the 12.6 million
-// codes of 1024 x 12288 x 3072 81 differ from 64 bits in one pass, 51 in two, for 3 % more time.
-__host__ __device__ constexpr int pass_blocks(int kind) {
-  return kind == BAG_FP8_CODES ? 20 : (kind == BAG_FP8_BF16 ? 64 : 32);
-}
 constexpr int F8P_STAGES = 5, F8P_STAGE = 2 * F8_TILE;
 constexpr int F8P_SHARED = 32, F8P_ACC1 = 256 - F8P_SHARED;  // TMEM columns
 constexpr int F8P_SF_COL = F8P_ACC1 + 256, F8P_SF_COLS = 12;  // A's 4 columns, W's 8
@@ -634,11 +706,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F8P_THREADS, 1)
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const int num_m = (g.M + 255) / 256, num_n = (g.N + 255) / 256;
   const int nkb = (g.K + F8_BK - 1) / F8_BK, nruns = (nkb + F8_GROUP * F8_RUN - 1) / (F8_GROUP * F8_RUN);
-  // passes of about the same length, whole groups of scale words each
-  constexpr int most = pass_blocks(KIND);
-  static_assert(most % F8_GROUP == 0, "passes of whole groups");
-  const int least = (nkb + most - 1) / most;  // passes, but for the rounding up to groups
-  const int pass_kb = LONG ? ((nkb + least - 1) / least + F8_GROUP - 1) / F8_GROUP * F8_GROUP : nkb;
+  const int pass_kb = LONG ? pass_length(nkb, pass_blocks(KIND)) : nkb;
   const int passes = LONG ? (nkb + pass_kb - 1) / pass_kb : 1;
   // units of work: `whole` tiles of 256 x 256, then every later tile as two of 256 x 128
   const long units = 2 * (long)num_m * num_n - whole;
@@ -1124,10 +1192,14 @@ cudaError_t gemm_fp8_init() {
   auto smem = [&](auto kernel, int bytes) {
     if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  smem(gemm_fp8_few_kernel<16>, FewCfg<16>::stages(1) * FewCfg<16>::STAGE + FewCfg<16>::REST);
-  smem(gemm_fp8_few_kernel<32>, FewCfg<32>::stages(1) * FewCfg<32>::STAGE + FewCfg<32>::REST);
-  smem(gemm_fp8_few_kernel<64>, FewCfg<64>::stages(1) * FewCfg<64>::STAGE + FewCfg<64>::REST);
-  smem(gemm_fp8_few_kernel<128>, FewCfg<128>::stages(1) * FewCfg<128>::STAGE + FewCfg<128>::REST);
+  smem(gemm_fp8_few_kernel<16, false>, FewCfg<16>::stages(1) * FewCfg<16>::STAGE + FewCfg<16>::REST);
+  smem(gemm_fp8_few_kernel<16, true>, FewCfg<16>::stages(1) * FewCfg<16>::STAGE + FewCfg<16>::REST);
+  smem(gemm_fp8_few_kernel<32, false>, FewCfg<32>::stages(1) * FewCfg<32>::STAGE + FewCfg<32>::REST);
+  smem(gemm_fp8_few_kernel<32, true>, FewCfg<32>::stages(1) * FewCfg<32>::STAGE + FewCfg<32>::REST);
+  smem(gemm_fp8_few_kernel<64, false>, FewCfg<64>::stages(1) * FewCfg<64>::STAGE + FewCfg<64>::REST);
+  smem(gemm_fp8_few_kernel<64, true>, FewCfg<64>::stages(1) * FewCfg<64>::STAGE + FewCfg<64>::REST);
+  smem(gemm_fp8_few_kernel<128, false>, FewCfg<128>::stages(1) * FewCfg<128>::STAGE + FewCfg<128>::REST);
+  smem(gemm_fp8_few_kernel<128, true>, FewCfg<128>::stages(1) * FewCfg<128>::STAGE + FewCfg<128>::REST);
   smem(gemm_fp8_pair_kernel<BAG_FP8_F32, false>, F8P_SMEM);
   smem(gemm_fp8_pair_kernel<BAG_FP8_F32, true>, F8P_SMEM);
   smem(gemm_fp8_pair_kernel<BAG_FP8_BF16, false>, F8P_SMEM);
@@ -1174,7 +1246,7 @@ static Fp8Plan plan_fp8(long M, long N, long K, int kind) {
     if (t.BN < 64 && M > t.BN) continue;  // narrow tiles read W again for every tile of rows
     for (int logS = 0; logS <= 3 && nkb >= (double)(2 << logS); ++logS) {
       const double kb = (double)cd(cd(K, F8_BK), 1L << logS);
-      if (kb > pass_blocks(kind) && logS < 3) continue;  // a longer sum on the tensor core loses precision (see LONG)
+      if (kb > pass_blocks(kind) && logS < 3) continue;  // passes (LONG) only where eight parts are too long still
       const double more = (double)(cd(cd(M, t.BN) * cd(N, 128) << logS, cluster_sms(logS)) - 1);
       us = together(t.start + 0.2 * kb + more * (t.wave + t.share * kb) + (logS ? 0.84 : 0.0) + 0.15 * (1 << logS));
       if (us < best) {

@@ -20,16 +20,9 @@ def part(file, head):
     return src[start:j] + (";" if src[j] == ";" else "")
 
 
-def line(file, head):
-    """The statement in csrc/`file` that starts with `head`, up to its semicolon."""
-    src = open(os.path.join(CSRC, file)).read()
-    start = src.index(head)
-    return src[start:src.index(";", start) + 1]
-
-
-def run(code, tmp_path, *args):
-    """Standard output of the C++ program `code`."""
+def run(code, tmp_path, text=""):
+    """Standard output of the C++ program `code` with `text` on its standard input."""
     source, program = tmp_path / "part.cpp", tmp_path / "part"
     source.write_text(code)
     subprocess.run(["g++", "-std=c++17", "-O1", "-o", str(program), str(source)], check=True)
-    return subprocess.run([str(program), *map(str, args)], check=True, capture_output=True, text=True).stdout
+    return subprocess.run([str(program)], input=text, check=True, capture_output=True, text=True).stdout
