@@ -5,7 +5,7 @@ import itertools
 import pytest
 
 import source_parts
-from fp8_shapes import LONG
+from fp8_shapes import FORMS, LONG
 
 KINDS = {"f32": 0, "bf16": 1, "fp8": 2, "resid": 3}
 LIMIT = {"f32": 32, "bf16": 64, "fp8": 20, "resid": 32}  # K blocks of one sum on the tensor core
@@ -68,7 +68,9 @@ def plan(tmp_path_factory):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-def test_long_sums_reach_every_tile(kind, plan):
+def test_shapes_of_the_tests_reach_every_form(kind, plan):
+    got = plan([s + (KINDS[kind],) for s in FORMS.values()])
+    assert {g[:2]: s for g, s in zip(got, FORMS.values())} == FORMS
     got = plan([s + (KINDS[kind],) for s in LONG.values()])
     assert {g[:2]: s for g, s in zip(got, LONG.values())} == LONG and all(g[2] > LIMIT[kind] for g in got)
 

@@ -1,4 +1,4 @@
-"""The 8-bit product's sums that are long enough for passes."""
+"""The 8-bit product's sums: every form of its kernels, and sums long enough for passes."""
 
 import numpy as np
 import pytest
@@ -6,7 +6,7 @@ import torch
 
 import lowbit_ref as R
 import test_gpu_lowbit as L
-from fp8_shapes import LONG
+from fp8_shapes import FORMS, LONG
 from paper_2608_09231_gb300 import bag
 
 pytestmark = pytest.mark.gpu
@@ -24,6 +24,13 @@ def ctx(lib):
 
 def ids(forms):
     return [f"{rows}-row tiles, {ctas} CTAs" if rows else "pairs" for rows, ctas in forms]
+
+
+@pytest.mark.parametrize("M,N,K", FORMS.values(), ids=ids(FORMS))
+@pytest.mark.parametrize("kind", KINDS)
+def test_every_form(M, N, K, kind, ctx):
+    """At test_gemm_fp8's bounds."""
+    L.test_gemm_fp8(M, N, K, kind, ctx)
 
 
 @pytest.mark.parametrize("M,N,K", LONG.values(), ids=ids(LONG))
