@@ -193,6 +193,7 @@ class Context:
         if st != 0:
             raise BagError(st, self.lib.bag_last_error(None).decode())
         self.h = h
+        self.stream = 0  # the caller's, as set_stream gave it
 
     def _chk(self, st):
         if st != 0:
@@ -212,6 +213,7 @@ class Context:
     # --- API mirror -----------------------------------------------------------------
     def set_stream(self, stream):
         self._chk(self.lib.bag_set_stream(self.h, ctypes.c_void_p(stream)))
+        self.stream = int(stream or 0)
 
     def load_gate(self, theta, mu=None, sd=None):
         th = np.ascontiguousarray(theta, np.float32)

@@ -15,13 +15,16 @@ shape of a Wan-type image-stream block, without its cross-attention and rotary e
 A full step runs it and keeps its change h_out - h_in in a cache of 8 or 4 bits; a reused step
 adds the kept change to its own h_in (the residual reuse of Algorithm 2, here of one block).
 
-All arithmetic runs in the CUDA library; torch supplies the device memory.  As a command it
-times both kinds of step:
+All arithmetic runs in the CUDA library, on the context's stream; torch supplies the device memory
+and copies h_in, on its current stream.  Where the two differ each waits for the other, so that a
+step follows what the caller did on the current stream and comes before what the caller does next.
+As a command it times both kinds of step:
 
   python -m paper_2608_09231_gb300.lowbit [--tokens 32760] [--hidden 5120] [--mlp 13824] [--keep 64]
 """
 
 import argparse
+import contextlib
 
 import torch
 
@@ -32,6 +35,21 @@ DEV = "cuda"
 
 def _up(n, m):
     return (n + m - 1) // m * m
+
+
+@contextlib.contextmanager
+def ordered(ctx):
+    """Calls of ctx after the work on torch's current stream, and before what follows there."""
+    here = torch.cuda.current_stream()
+    if here.cuda_stream == ctx.stream:
+        yield
+        return
+    there = torch.cuda.ExternalStream(ctx.stream) if ctx.stream else torch.cuda.default_stream()
+    there.wait_stream(here)
+    try:
+        yield
+    finally:
+        here.wait_stream(there)
 
 
 class Encoded:
@@ -45,7 +63,8 @@ class Encoded:
     @classmethod
     def of(cls, ctx, x):
         e = cls(*x.shape)
-        ctx.quant_fp8(x, e.codes, e.scales)
+        with ordered(ctx):
+            ctx.quant_fp8(x, e.codes, e.scales)
         return e
 
 
@@ -89,8 +108,12 @@ class LowBitBlock:
     def full(self, h_in, h, mod):
         """The block on h_in into h, its change kept.  mod: (shift_a, scale_a, gate_a, shift_m, scale_m,
         gate_m), fp32 [d] each."""
-        c, x, w, b = self.ctx, self.x, self.w, self.b
         h.copy_(h_in)
+        with ordered(self.ctx):
+            self._full(h_in, h, mod)
+
+    def _full(self, h_in, h, mod):
+        c, x, w, b = self.ctx, self.x, self.w, self.b
         c.ln_mod_fp8(h, mod[0], mod[1], x.codes, x.scales)
         self._project(x, w["wq"], self.q, bias=b["bq"])
         self._project(x, w["wk"], self.k, bias=b["bk"])
@@ -107,7 +130,8 @@ class LowBitBlock:
 
     def reuse(self, h_in, h):
         """h = h_in + the change kept by the last full step."""
-        self.ctx.cache_read(self.cache.codes, self.cache.scales, h, self.cache.bits, base=h_in)
+        with ordered(self.ctx):
+            self.ctx.cache_read(self.cache.codes, self.cache.scales, h, self.cache.bits, base=h_in)
 
     def run(self, streams, outs, mods, mask):
         """The steps of a sample: step t computes where mask[t] is 1 (mask[0] must be), else reuses."""
