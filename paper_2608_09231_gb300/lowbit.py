@@ -52,6 +52,13 @@ def ordered(ctx):
         here.wait_stream(there)
 
 
+def _overlap(a, b):
+    def end(t):
+        return t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+    return a.numel() > 0 and b.numel() > 0 and a.data_ptr() < end(b) and b.data_ptr() < end(a)
+
+
 class Encoded:
     """A matrix [rows, cols] as e4m3 codes with a scale for each 128 columns of a row."""
 
@@ -107,7 +114,9 @@ class LowBitBlock:
 
     def full(self, h_in, h, mod):
         """The block on h_in into h, its change kept.  mod: (shift_a, scale_a, gate_a, shift_m, scale_m,
-        gate_m), fp32 [d] each."""
+        gate_m), fp32 [d] each.  h_in is needed to the end, for the change: h may not be it."""
+        if _overlap(h_in, h):
+            raise ValueError("h_in and h share memory: the block's change would be lost")
         h.copy_(h_in)
         with ordered(self.ctx):
             self._full(h_in, h, mod)
