@@ -53,10 +53,15 @@ def ordered(ctx):
 
 
 def _overlap(a, b):
+    """Whether two matrices with dense rows share elements."""
     def end(t):
         return t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
 
-    return a.numel() > 0 and b.numel() > 0 and a.data_ptr() < end(b) and b.data_ptr() < end(a)
+    if a.numel() == 0 or b.numel() == 0 or a.data_ptr() >= end(b) or b.data_ptr() >= end(a):
+        return False
+    ld, width = a.stride(0) * a.element_size(), a.shape[1] * a.element_size()
+    apart = (b.data_ptr() - a.data_ptr()) % ld  # columns of one wider matrix, side by side
+    return not (a.stride() == b.stride() and width <= apart <= ld - b.shape[1] * b.element_size())
 
 
 class Encoded:

@@ -11,6 +11,9 @@ from paper_2608_09231_gb300 import lowbit
     (lambda x: x[:4], lambda x: x[4:], False),
     (lambda x: x[:5], lambda x: x[4:], True),
     (lambda x: x[:, :8], lambda x: x[1:], True),
+    (lambda x: x[:, :8], lambda x: x[:, 8:], False),
+    (lambda x: x[:, :8], lambda x: x[:, 7:], True),
+    (lambda x: x[:, 1:9], lambda x: x[1:, 9:], False),
     (lambda x: x[:0], lambda x: x, False),
     (lambda x: x, lambda x: x.clone(), False),
 ])
