@@ -10,7 +10,8 @@
  *   - Returns bag_status; nothing throws across the boundary.  On failure the message
  *     is available from bag_last_error(ctx).  A device-side error (a bounded wait that
  *     timed out inside a kernel) is sticky: every later call on the context returns
- *     BAG_EDEVICE_TIMEOUT until bag_reset.
+ *     BAG_EDEVICE_TIMEOUT until bag_reset.  (The operations on the caller's stream, from
+ *     bag_quant_fp8 on, have an error of their own: bag_operators_status.)
  *   - "device" pointers are CUDA global-memory pointers on the context's device; "host"
  *     pointers are ordinary CPU memory.  The library never frees caller memory and never
  *     keeps a caller pointer past the call that received it.
@@ -331,9 +332,9 @@ bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows
 /* ---- 8-bit operands with a scale for each block of 128 ----
  *
  * The operations from here to bag_attention_blocks use nothing of the context but its error text
- * and its device error word (a wait that expired in one of them is reported by bag_run, up to
- * bag_reset): they are kernels on the caller's stream itself (the one of
- * bag_set_stream), ordered like any other work that the caller puts there, never synchronise, and
+ * and a device error word of their own (a wait that expired in one of them leaves its outputs
+ * invalid, and is reported by bag_operators_status and by no other call): they are kernels on the
+ * caller's stream itself (the one of bag_set_stream), ordered like any other work that the caller puts there, never synchronise, and
  * may be captured into a CUDA graph (which then must not outlive the context).
  *
  * An encoded matrix [rows, cols] is two device buffers: codes, one float8 e4m3 byte an element
@@ -439,6 +440,16 @@ bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, lon
 bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const void* k, long ldk,
                                 const void* v, long vpad, int type, long nq, long nk, int heads,
                                 int kv_heads, const int32_t* blocks, int keep, void* o, long ldo);
+
+/* Whether the operations from bag_quant_fp8 to bag_attention_blocks have done their work: waits for
+ * the context's stream, returns BAG_EDEVICE_TIMEOUT if a bounded wait expired in one of them since
+ * the last call (which clears that), else BAG_OK.  Says nothing of bag_run and bag_step, whose own
+ * error is not touched.  BAG_ESTATE while the stream is being captured. */
+bag_status bag_operators_status(bag_ctx* ctx);
+
+/* The failure-path check below for these operations: launches the kernel on the caller's stream and
+ * returns; bag_operators_status reports what it records.  For tests of the error path only. */
+bag_status bag_check_operator_timeout(bag_ctx* ctx);
 
 /* Failure-path check: launches one kernel whose mbarrier wait can never complete (no
  * thread arrives on it), so its bounded wait gives up after the library's wait limit

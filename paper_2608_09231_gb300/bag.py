@@ -38,7 +38,7 @@ EXPORTS = ["bag_create", "bag_destroy", "bag_last_error", "bag_set_stream", "bag
            "bag_profile_run", "bag_profile_launches", "bag_rel_l1", "bag_rel_l1_noalloc",
            "bag_check_wait_timeout", "bag_quant_fp8", "bag_ln_mod_fp8", "bag_gemm_fp8",
            "bag_cache_write", "bag_cache_read", "bag_block_pool", "bag_block_select",
-           "bag_attention_blocks"]
+           "bag_attention_blocks", "bag_operators_status", "bag_check_operator_timeout"]
 
 PROF_KINDS = ["gemm", "attention", "norm", "signal", "gate", "cache"]
 
@@ -107,6 +107,8 @@ def load(path=None):
         "bag_set_policy": ([_P, _I, _P, ctypes.c_float], _I),
         "bag_set_budget": ([_P, _I], _I),
         "bag_check_wait_timeout": ([_P], _I),
+        "bag_operators_status": ([_P], _I),
+        "bag_check_operator_timeout": ([_P], _I),
         "bag_reset": ([_P], _I),
         "bag_step": ([_P, _P, _I, ctypes.POINTER(Cond), _P, _P], _I),
         "bag_run": ([_P, _P, ctypes.POINTER(Cond), ctypes.POINTER(Stats)], _I),
@@ -333,6 +335,15 @@ class Context:
         self._chk(self.lib.bag_residual_add(self.h, _ptr(out), _ptr(h_in), _ptr(R), n))
 
     # --- 8-bit operands, quantised cache, block-sparse attention (see include/bag.h) ----
+    def operators_status(self):
+        """Waits for the context's stream; raises where a wait expired in one of the operators below
+        since the last such call (their outputs are invalid then)."""
+        self._chk(self.lib.bag_operators_status(self.h))
+
+    def check_operator_timeout(self):
+        """bag_check_operator_timeout: a wait that expires, for operators_status to report."""
+        self._chk(self.lib.bag_check_operator_timeout(self.h))
+
     def quant_fp8(self, x, codes, scales):
         """Rows of x (fp32 or bf16 [rows, cols]) as e4m3 codes and power-of-two scales."""
         p, ld, rows, cols, kind = _mat(x, "x", ("float32", "bfloat16"))

@@ -151,6 +151,7 @@ struct bag_ctx {
   float *pooled_stage_u = nullptr, *vec_all_u = nullptr, *svec_u = nullptr, *mod_all_u = nullptr;
   DevState* st = nullptr;     // sampler state
   DevState* st_op = nullptr;  // state for single-operation calls
+  int* op_err = nullptr;      // error word of the operations on the caller's stream
   float* log = nullptr;
   float* tmp_f32 = nullptr;   // staging for bag_run_host text conversion
   long tmp_f32_n = 0;
@@ -674,6 +675,7 @@ static bag_status alloc_activations(bag_ctx* ctx) {
   }
   A.add((void**)&ctx->st, sizeof(DevState));
   A.add((void**)&ctx->st_op, sizeof(DevState));
+  A.add((void**)&ctx->op_err, sizeof(int));
   A.add((void**)&ctx->log, (size_t)T * kLogFloats * 4);
   A.add((void**)&ctx->d_gate, kGateFloats * 4);
   A.add((void**)&ctx->d_pmask, (size_t)T);
@@ -1880,7 +1882,7 @@ static bag_status bag_gemm_fp8_impl(bag_ctx* ctx, const void* a, long lda, const
   g.ldo = ldo;
   g.out_s = reinterpret_cast<uint8_t*>(out_s);
   g.ldos = ldos;
-  g.err = &ctx->st->err;
+  g.err = ctx->op_err;
   CK(gemm_fp8(g, ctx->user_stream));
   return BAG_OK;
 }
@@ -2003,7 +2005,7 @@ static bag_status bag_attention_blocks_impl(bag_ctx* ctx, const void* q, long ld
   a.blocks = blocks;
   a.o = o;
   a.ldo = ldo;
-  a.err = &ctx->st->err;
+  a.err = ctx->op_err;
   CK(attention_blocks(a, ctx->user_stream));
   return BAG_OK;
 }
@@ -2137,9 +2139,37 @@ bag_status bag_set_policy(bag_ctx* ctx, int policy, const uint8_t* host_mask, fl
 bag_status bag_check_wait_timeout(bag_ctx* ctx) {
   if (!ctx) return BAG_EINVAL;
   CKS(enter(ctx));
-  cudaError_t e = wait_timeout_probe(ctx->st, ctx->stream);
+  cudaError_t e = wait_timeout_probe(&ctx->st->err, ctx->stream);
   if (e != cudaSuccess) return leave(ctx, fail(ctx, BAG_ECUDA, std::string("probe: ") + cudaGetErrorString(e)));
   return leave(ctx, check_device_error(ctx));
+}
+
+static bag_status operators_status(bag_ctx* ctx) {
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  CK(cudaStreamIsCapturing(ctx->user_stream, &capturing));
+  if (capturing != cudaStreamCaptureStatusNone) return fail(ctx, BAG_ESTATE, "the context's stream is being captured");
+  int err = 0;
+  CK(cudaMemcpyAsync(&err, ctx->op_err, sizeof(err), cudaMemcpyDeviceToHost, ctx->user_stream));
+  CK(cudaStreamSynchronize(ctx->user_stream));
+  if (!err) return BAG_OK;
+  CK(cudaMemsetAsync(ctx->op_err, 0, sizeof(err), ctx->user_stream));
+  return fail(ctx, BAG_EDEVICE_TIMEOUT, "a bounded wait expired in an operation on the caller's stream");
+}
+
+bag_status bag_operators_status(bag_ctx* ctx) {
+  if (!ctx) return BAG_EINVAL;
+  return leave_op(operators_status(ctx));
+}
+
+static bag_status check_operator_timeout(bag_ctx* ctx) {
+  CK(wait_timeout_probe(ctx->op_err, ctx->user_stream));
+  return BAG_OK;
+}
+
+bag_status bag_check_operator_timeout(bag_ctx* ctx) {
+  if (!ctx) return BAG_EINVAL;
+  const OpScope scope(ctx);
+  return leave_op(check_operator_timeout(ctx));
 }
 
 bag_status bag_set_budget(bag_ctx* ctx, int B) {

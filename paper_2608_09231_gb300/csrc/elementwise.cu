@@ -758,7 +758,7 @@ cudaError_t stream_init(const DevState* st, int flag_want, float* h, const void*
 // The bounded-wait failure path on purpose: the barrier expects one arrival that never
 // comes, mbar_wait gives up after kWaitLimitNs and the error is recorded like any
 // kernel's timed-out wait.
-__global__ void wait_timeout_kernel(DevState* st) {
+__global__ void wait_timeout_kernel(int* err) {
   grid_dep_sync();
   __shared__ uint64_t bar;
   __shared__ int abort_flag;
@@ -766,11 +766,11 @@ __global__ void wait_timeout_kernel(DevState* st) {
   abort_flag = 0;
   mbar_init(&bar, 1);
   fence_mbar_init();
-  if (!mbar_wait(&bar, 0, &abort_flag)) atomicOr(&st->err, 2);
+  if (!mbar_wait(&bar, 0, &abort_flag)) atomicOr(err, 2);
 }
 
-cudaError_t wait_timeout_probe(DevState* st, cudaStream_t s) {
-  launch_kernel(wait_timeout_kernel, 1, 32, 0, s, st);
+cudaError_t wait_timeout_probe(int* err, cudaStream_t s) {
+  launch_kernel(wait_timeout_kernel, 1, 32, 0, s, err);
   return cudaGetLastError();
 }
 

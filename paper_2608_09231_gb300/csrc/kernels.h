@@ -250,8 +250,8 @@ cudaError_t gate_step(DevState* st, const float* sig_partial, int sig_rows, cons
 // block a copy of h_in.
 cudaError_t stream_init(const DevState* st, int flag_want, float* h, const void* txt0, const void* txt1,
                         int txt_bf16, const float* h_in, int nb, int nx, int ni, int d, cudaStream_t s);
-// one thread waits (bounded) on an mbarrier nothing arrives on, then sets st->err
-cudaError_t wait_timeout_probe(DevState* st, cudaStream_t s);
+// one thread waits (bounded) on an mbarrier nothing arrives on, then sets *err
+cudaError_t wait_timeout_probe(int* err, cudaStream_t s);
 cudaError_t sinusoid_all(void* out, int out_bf16, const double* sigma, int T, int dim, cudaStream_t s);
 cudaError_t expand_wan_mod(float* mod_all, const float* shared6d, const float* tables,
                            int T, int nblocks, int d, cudaStream_t s);

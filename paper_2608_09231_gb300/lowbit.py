@@ -148,7 +148,8 @@ class LowBitBlock:
             self.ctx.cache_read(self.cache.codes, self.cache.scales, h, self.cache.bits, base=h_in)
 
     def run(self, streams, outs, mods, mask):
-        """The steps of a sample: step t computes where mask[t] is 1 (mask[0] must be), else reuses."""
+        """The steps of a sample: step t computes where mask[t] is 1 (mask[0] must be), else reuses.  Waits
+        for them and raises if a kernel gave up (not while a graph is captured)."""
         if not mask[0]:
             raise ValueError("the first step has nothing to reuse")
         for t, full in enumerate(mask):
@@ -156,6 +157,9 @@ class LowBitBlock:
                 self.full(streams[t], outs[t], mods[t])
             else:
                 self.reuse(streams[t], outs[t])
+        if not torch.cuda.is_current_stream_capturing():
+            with ordered(self.ctx):
+                self.ctx.operators_status()
 
 
 def random_weights(d, F, seed=0):
