@@ -85,8 +85,10 @@ BAG_DEV float2 muladd2(float2 a, float2 b, float2 c) {
 
 // GELU (tanh form) of two values: y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3), the same
 // function as 0.5 y (1 + tanh u).  exp2 and the reciprocal of the special-function unit: relative
-// error about 2^-20, below every rounding that follows and below fp32's own at the sums this is
-// applied to.  (A power that overflows gives 1 / inf = 0.)
+// error up to 2^-20, and for negative y what the rounding of the exponent x adds, up to |x| 1.75 2^-23
+// (2^-17 at y = -6, where the value is -8e-11 and 1 + tanh u in fp32 has no bit left): below the
+// roundings to 16 and 8 bits that follow, and below fp32's own at the sums this is applied to.  (A power
+// that overflows gives 1 / inf = 0.)
 BAG_DEV float2 gelu2(float2 y) {
   const float k = -2.0f * 0.7978845608028654f * 1.4426950408889634f;  // exp(-2u) = 2^(y (k + k' y^2))
   float2 e = mul2(y, muladd2(mul2(y, y), make_float2(k * 0.044715f, k * 0.044715f), make_float2(k, k)));
