@@ -368,7 +368,9 @@ enum {
   BAG_FP8_RESID = 3  /* out fp32 [M, N] += gate * y (gate [N], null = 1); act must be 0 */
 };
 /* Product of two encoded matrices on the tensor cores: A [M, K] (codes a, scales a_s), W [N, K]
- * (codes w, scales w_s); products and their scales are summed over K in fp32.  bias: fp32
+ * (codes w, scales w_s); products and their scales are summed over K in fp32 (the tensor core cuts
+ * addends below a sum's last bit, so it sums 4096 products at most, 2560 for codes and 8192 for bf16,
+ * and such parts are added rounded to nearest).  Operands may be columns of wider matrices.  bias: fp32
  * device [N] or null.  act: 0 none, 1 GELU (tanh).  ldo: row stride of out in elements; any
  * alignment of out, bias and gate (16-byte aligned rows are stored fastest), except codes, which
  * keep an encoded matrix's rules (ldo bytes, out_s / ldos its scales; ignored otherwise).
@@ -436,7 +438,9 @@ bag_status bag_block_select(bag_ctx* ctx, const void* q, int type, long ldq, lon
  * [nq, ldo], 16-byte aligned, ldo a multiple of 8.  blocks: int32 device
  * [heads][ceil(nq / 128)][keep]; a list ends at its first entry outside [0, ceil(nk / 128)), so
  * shorter ones end in -1, and a block of queries with an empty list gets zeros (all of them where
- * nk = 0).  An index listed twice counts twice. */
+ * nk = 0).  An index listed twice counts twice.  Scores, softmax and sums are fp32; the weights are
+ * rounded to `type` before they meet v (not for one query): with BAG_F16 that is below the output's
+ * rounding, with BAG_BF16 about its size. */
 bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const void* k, long ldk,
                                 const void* v, long vpad, int type, long nq, long nk, int heads,
                                 int kv_heads, const int32_t* blocks, int keep, void* o, long ldo);

@@ -12,6 +12,11 @@
 //                from TMEM at once, P = exp2(s - m) goes back over them in 16 bits and enters the
 //                PV product from TMEM; O stays in TMEM and is rescaled only when the running
 //                maximum has grown by more than 8 (in log2 units)
+// P has 16 bits because both operands of an MMA are of one type and V's are given; the sum l is of the
+// unrounded P, in fp32.  Against 64 bits (2-norm) fp16 is off by 1.67e-3, the output's own rounding to
+// bf16 (1.66e-3); bf16 by 2.2e-3, its P adding eight-bit roundings of about the output's size.  Two
+// products of a P in two bf16 parts would take that away for half as much tensor work again; the dense
+// kernel makes the same choice, and a caller who wants the bits has fp16.
 // The slots are two (head, query block) units, or one unit is shared: its list is cut into 2 C
 // parts for a cluster of C CTAs, and rank r merges 128 / C rows of the 2 C partial outputs through
 // distributed shared memory.  A launch in pairs shares (C = 1) the units of its last wave where

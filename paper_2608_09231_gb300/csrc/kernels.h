@@ -280,7 +280,7 @@ struct Fp8Gemm {
   int act, kind;
   void* out; long ldo;
   uint8_t* out_s; long ldos;
-  int vec;   // rows of out (and bias, gate) are 16-byte aligned (set by the launcher)
+  int vec;   // CTA pairs: rows of out are 16-byte aligned (set by the launcher)
   int* err;
 };
 cudaError_t gemm_fp8(Fp8Gemm g, cudaStream_t s);

@@ -126,7 +126,7 @@ BAG_DEV float block_sum(float v, float* red) {
 // Bound: HBM behind the row's phases (load, two reductions, encode), which CTAS rows on an SM hide
 // from each other, and the issue of the encoding: packed arithmetic, one maximum of three and (at
 // 5120) CTAS held to 42 registers took 32,760 x 5120 from 155 to 132 us (floor 124: 6.4 TB/s), 4608 x
-// 3072 from 16.3 to 14.8 (10.4: three waves of rows and a start).  Two rows a CTA took 17.4 against
+// 3072 from 16.3 to 14.8 (10.4; its 4608 CTAs are 3.03 waves, whose last is 48 rows).  Two rows a CTA took 17.4 against
 // those 16.3, four 23.6; a row of 3072 on 192 threads 14.5 (7145 rows 20.8 against 20.5), on 96 16.2.
 template <int TH, int VPT, int CTAS>
 __global__ void __launch_bounds__(TH, CTAS) ln_fp8_kernel(const float* __restrict__ x, long ldx,

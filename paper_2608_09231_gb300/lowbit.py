@@ -12,6 +12,9 @@ shape of a Wan-type image-stream block, without its cross-attention and rotary e
   x  = LN-mod(h), u = GELU(x Wu^T + bu) encoded in the product's epilogue
   h += gate_m * (u Wd^T + bd)
 
+q, k and V are bf16, the 16-bit type that the products store, and so are the softmax's weights: about
+the output's own rounding, and a tenth of what 8-bit operands of the next projection lose.
+
 A full step runs it and keeps its change h_out - h_in in a cache of 8 or 4 bits; a reused step
 adds the kept change to its own h_in (the residual reuse of Algorithm 2, here of one block).
 
