@@ -331,7 +331,7 @@ bag_status bag_rel_l1_noalloc(const void* a, const void* b, int dtype, long rows
 
 /* ---- 8-bit operands with a scale for each block of 128 ----
  *
- * The operations from here to bag_attention_blocks use nothing of the context but its error text
+ * The operations from here to bag_attention_prefix use nothing of the context but its error text
  * and a device error word of their own (a wait that expired in one of them leaves its outputs
  * invalid, and is reported by bag_operators_status and by no other call): they are kernels on the
  * caller's stream itself (the one of bag_set_stream), ordered like any other work that the caller puts there, never synchronise, and
@@ -445,7 +445,92 @@ bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const voi
                                 const void* v, long vpad, int type, long nq, long nk, int heads,
                                 int kv_heads, const int32_t* blocks, int keep, void* o, long ldo);
 
-/* Whether the operations from bag_quant_fp8 to bag_attention_blocks have done their work: waits for
+/* ---- rotary positions, and attention of packed sequences ----
+ *
+ * The operations of a text's side: a prompt's tokens, or one more token of it, go through a layer
+ * whose keys and values stay in a cache.  Rows are tokens, head h of a row is columns [dh h, dh h +
+ * dh); type BAG_BF16 or BAG_F16 (rope also BAG_F32).  Like the operations above they run on the
+ * caller's stream itself, never synchronise and may be captured; what they know of the sequences is
+ * read on the device when they run. */
+enum { BAG_ROPE_INTERLEAVED = 0, BAG_ROPE_HALF = 1 };
+
+/* Rotary positions.  Pair i < pairs of each head of q and k turns by position * freqs[i] radians
+ * (backwards with inverse, which is the backward pass of q and k) and is multiplied by scale; pair i
+ * is columns (2i, 2i + 1) with BAG_ROPE_INTERLEAVED, (i, i + pairs) with BAG_ROPE_HALF; columns from
+ * 2 pairs on, and v, are copied.  Angles are exact to 2^-34 of a turn for any 32-bit position, results
+ * computed in fp32 and rounded once.  Row r of k and v goes to row slots[r] of k_out and v_out (a row
+ * outside [0, capacity) is skipped; the slots of one call have to be distinct), or to row r where
+ * slots is null (then capacity >= rows).  Each of q, k and v may be null (with its output).  q_out
+ * may be q, and without slots k_out k and v_out v; other overlaps of an output are refused. */
+typedef struct {
+  int type;               /* BAG_F32, BAG_BF16 or BAG_F16 */
+  int layout;             /* BAG_ROPE_* */
+  int heads, kv_heads;    /* of q; of k and v */
+  int dh, pairs;          /* 1 <= pairs <= dh / 2, dh <= 256 */
+  long rows;
+  const void* q; long ldq;          /* device [rows, heads * dh], row strides in elements */
+  void* q_out; long ldqo;
+  const void* k; long ldk;          /* device [rows, kv_heads * dh] */
+  void* k_out; long ldko;           /* device [capacity, kv_heads * dh] */
+  const void* v; long ldv;
+  void* v_out; long ldvo;
+  const int32_t* slots;             /* device [rows] or null */
+  long capacity;
+  const int32_t* pos;               /* device [rows], or null: position pos0 + r */
+  long pos0;
+  const double* freqs;              /* host [pairs], finite, at most 2^30; read before the call returns */
+  float scale;                      /* finite; 1 = a plain rotation */
+  int inverse;                      /* 0 or 1 */
+} bag_rope_args;
+bag_status bag_rope(bag_ctx* ctx, const bag_rope_args* a);
+
+/* Attention of packed sequences.  Sequence i's queries are rows q_start[i] .. q_start[i + 1] - 1 of q
+ * (q_start does not decrease); its keys and values are the k_len[i] rows of k and v from row
+ * k_start[i] on, or, where k_start and k_len are null, the rows of its queries.  o = softmax(scale q
+ * k^T) v; with causal, query t of lq sees keys 0 .. t + lk - lq, so queries are a sequence's last tokens.
+ * A row that sees no key gets zeros (lse -inf); rows of q outside every sequence keep what o and lse
+ * hold there.  Ranges that leave k's or q's rows are clipped to them.  heads query heads share
+ * kv_heads key heads as in bag_attention_blocks.  Rows of k and v that belong to no sequence may
+ * hold anything, NaN included; a NaN in a sequence's own values reaches all of its rows.
+ * Scores, softmax and sums are fp32; weights are rounded to `type` before they meet v.
+ *
+ * max_q and max_k: the most queries and keys of a sequence, as far as the caller knows (0: does not);
+ * a wrong number costs time, not correctness.  work: device workspace of work_bytes, 16-byte aligned,
+ * for sums over parts of the keys: bag_attention_work says how much the fastest form takes; with less
+ * (or null) fewer CTAs share a sequence.  Its contents before and after a call mean nothing, and calls
+ * that may run at the same time need one each.  The order of sums depends on the sizes, max_q,
+ * max_k and work_bytes. */
+typedef struct {
+  int type;               /* BAG_BF16 or BAG_F16 */
+  int heads, kv_heads, dh;/* dh 64 or 128 (else EUNSUPPORTED) */
+  long nq, k_rows, seqs;  /* rows of q and o; of k and v; sequences */
+  const void* q; long ldq;          /* 16-byte aligned rows (as all below), else EUNSUPPORTED */
+  const void* k; long ldk;
+  const void* v; long ldv;
+  void* o; long ldo;                /* of `type`; may overlap none of the others */
+  float* lse;                       /* device [nq, heads], or null: ln of the sum of exp(scores) of each row */
+  const int32_t* q_start;           /* device [seqs + 1] */
+  const int32_t* k_start;           /* device [seqs], or null */
+  const int32_t* k_len;
+  long max_q, max_k;
+  int causal;                       /* 0 or 1 */
+  float scale;                      /* > 0, or 0: 1 / sqrt(dh) */
+  void* work; size_t work_bytes;
+} bag_packed_args;
+bag_status bag_attention_packed(bag_ctx* ctx, const bag_packed_args* a);
+
+/* The same where every query also sees all n_prefix rows of pk and pv (strides ldpk, ldpv), as if they came
+ * before its sequence's own keys, whose mask they do not shift.  The prefix is there once, and is read
+ * for the rows of all sequences together.  k_start and k_len as above, so with k_rows = 0 and
+ * k_len = 0 the prefix is all there is.  work of at least 2 nq heads (4 dh + 8) bytes (else EINVAL). */
+bag_status bag_attention_prefix(bag_ctx* ctx, const bag_packed_args* a, const void* pk, long ldpk,
+                                const void* pv, long ldpv, long n_prefix);
+
+/* Bytes of workspace for calls of these sizes (n_prefix 0: bag_attention_packed). */
+bag_status bag_attention_work(bag_ctx* ctx, long nq, int heads, int kv_heads, int dh, long seqs, long max_q,
+                              long max_k, long n_prefix, size_t* bytes);
+
+/* Whether the operations from bag_quant_fp8 to bag_attention_prefix have done their work: waits for
  * the context's stream, returns BAG_EDEVICE_TIMEOUT if a bounded wait expired in one of them since
  * the last call (which clears that), else BAG_OK.  Says nothing of bag_run and bag_step, whose own
  * error is not touched.  BAG_ESTATE while the stream is being captured. */

@@ -28,6 +28,7 @@ FP8_F32, FP8_BF16, FP8_CODES, FP8_RESID = 0, 1, 2, 3
 SCALE_BLOCK = 128                  # columns of one scale of an encoded matrix
 CACHE_GROUP = {8: 128, 4: 32}      # columns of one scale of a quantised cache, by bits
 ATTN_BLOCK = 128                   # rows of a block of queries or keys
+ROPE_LAYOUT = {"interleaved": 0, "half": 1}
 STATUS = {0: "BAG_OK", 1: "BAG_EINVAL", 2: "BAG_ENOMEM", 3: "BAG_ECUDA", 4: "BAG_EORDER",
           5: "BAG_EDEVICE_TIMEOUT", 6: "BAG_ESTATE", 7: "BAG_EUNSUPPORTED"}
 
@@ -38,7 +39,8 @@ EXPORTS = ["bag_create", "bag_destroy", "bag_last_error", "bag_set_stream", "bag
            "bag_profile_run", "bag_profile_launches", "bag_rel_l1", "bag_rel_l1_noalloc",
            "bag_check_wait_timeout", "bag_quant_fp8", "bag_ln_mod_fp8", "bag_gemm_fp8",
            "bag_cache_write", "bag_cache_read", "bag_block_pool", "bag_block_select",
-           "bag_attention_blocks", "bag_operators_status", "bag_check_operator_timeout"]
+           "bag_attention_blocks", "bag_rope", "bag_attention_packed", "bag_attention_prefix",
+           "bag_attention_work", "bag_operators_status", "bag_check_operator_timeout"]
 
 PROF_KINDS = ["gemm", "attention", "norm", "signal", "gate", "cache"]
 
@@ -87,6 +89,22 @@ _lib = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _L = ctypes.c_long
+_Z = ctypes.c_size_t
+_F = ctypes.c_float
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("type", _I), ("layout", _I), ("heads", _I), ("kv_heads", _I), ("dh", _I), ("pairs", _I), ("rows", _L),
+                ("q", _P), ("ldq", _L), ("q_out", _P), ("ldqo", _L), ("k", _P), ("ldk", _L), ("k_out", _P), ("ldko", _L),
+                ("v", _P), ("ldv", _L), ("v_out", _P), ("ldvo", _L), ("slots", _P), ("capacity", _L), ("pos", _P),
+                ("pos0", _L), ("freqs", _P), ("scale", _F), ("inverse", _I)]
+
+
+class PackedArgs(ctypes.Structure):
+    _fields_ = [("type", _I), ("heads", _I), ("kv_heads", _I), ("dh", _I), ("nq", _L), ("k_rows", _L), ("seqs", _L),
+                ("q", _P), ("ldq", _L), ("k", _P), ("ldk", _L), ("v", _P), ("ldv", _L), ("o", _P), ("ldo", _L),
+                ("lse", _P), ("q_start", _P), ("k_start", _P), ("k_len", _P), ("max_q", _L), ("max_k", _L),
+                ("causal", _I), ("scale", _F), ("work", _P), ("work_bytes", _Z)]
 
 
 def load(path=None):
@@ -131,6 +149,10 @@ def load(path=None):
         "bag_block_pool": ([_P, _P, _I, _L, _L, _I, _P, _P, _L], _I),
         "bag_block_select": ([_P, _P, _I, _L, _L, _I, _P, _P, _L, _L, _I, _I, _P], _I),
         "bag_attention_blocks": ([_P, _P, _L, _P, _L, _P, _L, _I, _L, _L, _I, _I, _P, _I, _P, _L], _I),
+        "bag_rope": ([_P, ctypes.POINTER(RopeArgs)], _I),
+        "bag_attention_packed": ([_P, ctypes.POINTER(PackedArgs)], _I),
+        "bag_attention_prefix": ([_P, ctypes.POINTER(PackedArgs), _P, _L, _P, _L, _L], _I),
+        "bag_attention_work": ([_P, _L, _I, _I, _I, _L, _L, _L, _L, ctypes.POINTER(_Z)], _I),
         "bag_rel_l1": ([_P, _P, _P, _I, _L, _L, _P, _P], _I),
         "bag_rel_l1_noalloc": ([_P, _P, _I, _L, _L, _P, _P], _I),
         "bag_profile_run": ([_P, _P, ctypes.POINTER(Cond), ctypes.POINTER(Stats),
@@ -458,6 +480,97 @@ class Context:
         self._chk(self.lib.bag_attention_blocks(self.h, qp, ldq, kp, ldk, vt.data_ptr(), vt.shape[2], _T16[kind], nq, nk,
                                                 heads, kv_heads, at, keep, op, ldo))
 
+    # --- rotary positions, attention of packed sequences (see include/bag.h) ------------
+    def rope(self, q, q_out, freqs, dh, pos=None, pos0=0, k=None, k_out=None, v=None, v_out=None, slots=None,
+             layout="half", scale=1.0, inverse=False):
+        """Rotary positions of q [rows, heads * dh] into q_out and of k into k_out, whose rows are `slots`
+        (default: the same); v is copied into v_out's.  freqs: host array of radians a position, one for
+        each rotated pair of a head; pos: int32 [rows], default pos0 + row.  Any of q, k, v may be None."""
+        f = np.ascontiguousarray(freqs, np.float64)
+        if f.ndim != 1 or layout not in ROPE_LAYOUT:
+            raise ValueError(f"freqs {f.shape} is not a vector, or layout {layout!r} none of {list(ROPE_LAYOUT)}")
+        first = next((x for x in (q, k, v) if x is not None), None)
+        if first is None or dh < 1:
+            raise ValueError("rope needs q, k or v, and a head's width")
+        kind, (rows, _) = _type(first)[0], first.shape if first.dim() == 2 else (-1, 0)
+        if kind not in _T32:
+            _want(first, "q, k and v", f"one of {list(_T32)}")
+        a = [None, 0, None, 0] * 3
+        heads, kv_heads, capacity = 0, 0, rows
+        for i, (x, y, name) in enumerate(((q, q_out, "q"), (k, k_out, "k"), (v, v_out, "v"))):
+            if (x is None) != (y is None):
+                raise ValueError(f"{name} and {name}_out go together")
+            if x is None:
+                continue
+            p, ld, n, cols, _ = _mat(x, name, (kind,))
+            po, ldo, no, co, _ = _mat(y, name + "_out", (kind,))
+            if n != rows or co != cols or cols % dh or (no != rows if i == 0 or slots is None else False):
+                _want(y, name + "_out", f"rows of {cols} columns for {rows} of {name}, in heads of {dh}")
+            a[4 * i:4 * i + 4] = p, ld, po, ldo
+            if i == 0:
+                heads = cols // dh
+            else:
+                if kv_heads and (kv_heads != cols // dh or capacity != no):
+                    raise ValueError(f"k_out and v_out differ: {tuple(k_out.shape)} and {tuple(v_out.shape)}")
+                kv_heads, capacity = cols // dh, no
+        args = RopeArgs(_T32[kind], ROPE_LAYOUT[layout], heads, kv_heads, dh, f.size, rows, *a,
+                        _vec(slots, "slots", rows, "int32"), capacity, _vec(pos, "pos", rows, "int32"), pos0,
+                        f.ctypes.data, scale, int(inverse))
+        self._chk(self.lib.bag_rope(self.h, ctypes.byref(args)))
+
+    @staticmethod
+    def _packed(q, k, v, o, q_start, heads, kv_heads, k_start, k_len, max_q, max_k, causal, scale, lse, work):
+        qp, ldq, nq, wq, kind = _mat(q, "q", ("float16", "bfloat16"))
+        op, ldo, no, wo, _ = _mat(o, "o", (kind,))
+        kp, ldk, nk, wk, _ = _mat(k, "k", (kind,))
+        vp, ldv, nv, wv, _ = _mat(v, "v", (kind,))
+        dh = wq // heads
+        if wq != heads * dh or wk != kv_heads * dh or wv != wk or nv != nk or no != nq or wo != wq:
+            raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)} and o {tuple(o.shape)} do not "
+                             f"fit {heads} and {kv_heads} heads")
+        if q_start.dim() != 1 or q_start.shape[0] < 1:
+            _want(q_start, "q_start", "a device vector of one more than the sequences")
+        seqs = q_start.shape[0] - 1
+        if lse is not None and (lse.shape != (nq, heads) or not lse.is_cuda or not lse.is_contiguous() or
+                                _type(lse)[0] != "float32"):
+            _want(lse, "lse", f"dense float32 [{nq}, {heads}] on the device")
+        if work is not None and not (work.is_cuda and work.is_contiguous()):
+            _want(work, "work", "dense memory on the device")
+        return PackedArgs(_T16[kind], heads, kv_heads, dh, nq, nk, seqs, qp, ldq, kp, ldk, vp, ldv, op, ldo, _dp(lse),
+                          _vec(q_start, "q_start", seqs + 1, "int32"), _vec(k_start, "k_start", seqs, "int32"),
+                          _vec(k_len, "k_len", seqs, "int32"), max_q or 0, max_k or 0, int(causal), scale or 0.0,
+                          _dp(work), 0 if work is None else work.numel() * work.element_size()), kind, wk
+
+    def attention_packed(self, q, k, v, o, q_start, heads, kv_heads=None, k_start=None, k_len=None, max_q=None,
+                         max_k=None, causal=True, scale=None, lse=None, work=None):
+        """Attention of packed sequences: sequence i's queries are rows q_start[i] to q_start[i + 1] of q [nq,
+        heads * dh], its keys the k_len[i] rows of k and v [rows, kv_heads * dh] from k_start[i] on (default:
+        the rows of its queries); o like q.  max_q, max_k: the longest, as far as known; lse: fp32 [nq,
+        heads]; work: memory of attention_work bytes, without which a sequence's keys are not shared among
+        CTAs."""
+        a, _, _ = self._packed(q, k, v, o, q_start, heads, heads if kv_heads is None else kv_heads, k_start, k_len,
+                               max_q, max_k, causal, scale, lse, work)
+        self._chk(self.lib.bag_attention_packed(self.h, ctypes.byref(a)))
+
+    def attention_prefix(self, q, k, v, o, q_start, prefix_k, prefix_v, heads, kv_heads=None, k_start=None,
+                         k_len=None, max_q=None, max_k=None, causal=True, scale=None, lse=None, work=None):
+        """attention_packed where every query also sees all rows of prefix_k and prefix_v [rows, kv_heads * dh]
+        first; needs work."""
+        a, kind, wk = self._packed(q, k, v, o, q_start, heads, heads if kv_heads is None else kv_heads, k_start, k_len,
+                                   max_q, max_k, causal, scale, lse, work)
+        kp, ldk, n, ck, _ = _mat(prefix_k, "prefix_k", (kind,))
+        vp, ldv, nv, cv, _ = _mat(prefix_v, "prefix_v", (kind,))
+        if ck != wk or cv != wk or n != nv:
+            raise ValueError(f"prefix_k {tuple(prefix_k.shape)} and prefix_v {tuple(prefix_v.shape)} do not fit rows of {wk}")
+        self._chk(self.lib.bag_attention_prefix(self.h, ctypes.byref(a), kp, ldk, vp, ldv, n))
+
+    def attention_work(self, nq, heads, dh, kv_heads, seqs, max_q, max_k, n_prefix=0):
+        """Bytes of workspace for attention_packed, or with n_prefix for attention_prefix, of these sizes."""
+        n = _Z()
+        self._chk(self.lib.bag_attention_work(self.h, nq, heads, kv_heads, dh, seqs, max_q or 0, max_k or 0, n_prefix,
+                                              ctypes.byref(n)))
+        return n.value
+
 
 # --- tensors handed to the low-precision operators ---------------------------------------
 # A wrong element type or a row whose elements are not dense would reach the kernels as a
@@ -510,6 +623,7 @@ def _encoded(codes, scales, name, rows, cols):
 
 
 _T16 = {"float16": 2, "bfloat16": 1}  # BAG_F16, BAG_BF16
+_T32 = {"float32": 0, **_T16}
 
 
 def rel_l1_noalloc(a, b, rows, cols, out, stream=0, bf16=None):

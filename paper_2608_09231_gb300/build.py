@@ -20,7 +20,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libbag.so")
 
 SOURCES = ["bag_api.cu", "gemm.cu", "attn.cu", "attn_tc.cu", "elementwise.cu", "noalloc.cu",
-           "lowbit.cu", "gemm_fp8.cu", "attn_blocks.cu"]
+           "lowbit.cu", "gemm_fp8.cu", "attn_blocks.cu", "rope.cu", "attn_packed.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -2010,6 +2010,170 @@ static bag_status bag_attention_blocks_impl(bag_ctx* ctx, const void* q, long ld
   return BAG_OK;
 }
 
+// Whether two matrices of rows `width` bytes wide, ld bytes apart, share memory.  Columns of one wider
+// matrix, side by side, do not.
+static bool share(const void* a, long lda, long rows_a, long width_a, const void* b, long ldb, long rows_b, long width_b) {
+  if (!a || !b || rows_a <= 0 || rows_b <= 0 || width_a <= 0 || width_b <= 0) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t ea = pa + (uintptr_t)(rows_a - 1) * lda + width_a, eb = pb + (uintptr_t)(rows_b - 1) * ldb + width_b;
+  if (pa >= eb || pb >= ea) return false;
+  if (lda != ldb) return true;
+  const long apart = (long)((pb >= pa ? pb - pa : lda - (pa - pb) % lda) % (uintptr_t)lda);
+  return !(width_a <= apart && apart <= lda - width_b);
+}
+
+// f radians as a fraction of a turn, times 2^64 (modulo 2^64).  1 / 2 pi in two parts, so that the
+// fraction is good to its last bits.
+static uint64_t turn_fraction(double f) {
+  const double hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;
+  const double g = std::fabs(f), t = g * hi, rest = std::fma(g, hi, -t) + g * lo;
+  const double upper = (t - std::floor(t)) * 0x1p32, whole = std::floor(upper);
+  const uint64_t turns = ((uint64_t)whole << 32) + (uint64_t)std::llround((upper - whole) * 0x1p32 + rest * 0x1p64);
+  return f < 0 ? 0 - turns : turns;
+}
+
+static bag_status bag_rope_impl(bag_ctx* ctx, const bag_rope_args* a) {
+  if (!a) return fail(ctx, BAG_EINVAL, "null arguments");
+  const bool kv = a->k || a->v;
+  if ((a->type != BAG_F32 && a->type != BAG_BF16 && a->type != BAG_F16) ||
+      (a->layout != BAG_ROPE_INTERLEAVED && a->layout != BAG_ROPE_HALF) || (a->inverse != 0 && a->inverse != 1))
+    return fail(ctx, BAG_EINVAL, "bad rope type, layout or direction");
+  if (a->dh < 2 || a->dh > 2 * kRopePairs || a->pairs < 1 || 2 * a->pairs > a->dh)
+    return fail(ctx, BAG_EINVAL, "rope needs heads of 2 to 256 columns and 1 to dh / 2 pairs");
+  if (a->rows < 0 || a->rows > kMaxRows || (a->q && (a->heads < 1 || a->heads > kMaxHeads)) ||
+      (kv && (a->kv_heads < 1 || a->kv_heads > kMaxHeads || a->capacity < 0 || a->capacity > kMaxRows ||
+              (!a->slots && a->capacity < a->rows))))
+    return fail(ctx, BAG_EINVAL, "bad rope shape");
+  if (a->rows == 0) return BAG_OK;
+  if (!a->q != !a->q_out || !a->k != !a->k_out || !a->v != !a->v_out || !(a->q || kv))
+    return fail(ctx, BAG_EINVAL, "rope takes q, k or v, each with its output");
+  const long size = a->type == BAG_F32 ? 4 : 2, wq = (long)a->heads * a->dh, wk = (long)a->kv_heads * a->dh;
+  struct Mat {
+    const void* p;
+    long ld, width, rows;
+  };
+  const Mat in[3] = {{a->q, a->ldq, wq, a->rows}, {a->k, a->ldk, wk, a->rows}, {a->v, a->ldv, wk, a->rows}};
+  const long cap = a->slots ? a->capacity : a->rows;
+  const Mat out[3] = {{a->q_out, a->ldqo, wq, a->rows}, {a->k_out, a->ldko, wk, cap}, {a->v_out, a->ldvo, wk, cap}};
+  for (const Mat* m : {in, out})
+    for (int i = 0; i < 3; ++i)
+      if (m[i].p && (m[i].ld < m[i].width || !aligned(m[i].p, size)))
+        return fail(ctx, BAG_EINVAL, "a row stride is less than a row, or a tensor is not aligned to its type");
+  if (!aligned(a->slots, 4) || !aligned(a->pos, 4)) return fail(ctx, BAG_EINVAL, "slots or positions are not aligned");
+  auto common = [&](const Mat& x, const Mat& y) {
+    return share(x.p, x.ld * size, x.rows, x.width * size, y.p, y.ld * size, y.rows, y.width * size);
+  };
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 3; ++i) {
+      const bool same = i == o && in[i].p == out[o].p && in[i].ld == out[o].ld && (o == 0 || !a->slots);
+      if (!same && common(in[i], out[o])) return fail(ctx, BAG_EINVAL, "an output of rope overlaps an input");
+      if (i < o && common(out[i], out[o])) return fail(ctx, BAG_EINVAL, "outputs of rope overlap");
+    }
+  }
+  if (!a->freqs || !std::isfinite(a->scale)) return fail(ctx, BAG_EINVAL, "freqs is null or scale not finite");
+  RopeArgs r{};
+  for (int i = 0; i < a->pairs; ++i) {
+    if (!(std::fabs(a->freqs[i]) <= 0x1p30)) return fail(ctx, BAG_EINVAL, "a frequency is not finite or above 2^30");
+    r.turns[i] = turn_fraction(a->freqs[i]);
+  }
+  r.q = a->q, r.ldq = a->ldq, r.q_out = a->q_out, r.ldqo = a->ldqo;
+  r.k = a->k, r.ldk = a->ldk, r.k_out = a->k_out, r.ldko = a->ldko;
+  r.v = a->v, r.ldv = a->ldv, r.v_out = a->v_out, r.ldvo = a->ldvo;
+  r.slots = a->slots, r.capacity = a->capacity;
+  r.pos = a->pos, r.pos0 = a->pos0;
+  r.rows = a->rows;
+  r.heads = a->heads, r.kv_heads = a->kv_heads, r.dh = a->dh, r.pairs = a->pairs;
+  r.half = a->layout == BAG_ROPE_HALF, r.inverse = a->inverse;
+  r.scale = a->scale;
+  CK(rope(r, (int)size, a->type == BAG_F16, ctx->user_stream));
+  return BAG_OK;
+}
+
+// Sizes that bag_attention_work and the attention of packed sequences have in common.
+static bag_status check_packed(bag_ctx* ctx, long nq, int heads, int kv_heads, int dh, long seqs, long max_q,
+                               long max_k, long n_prefix) {
+  if (nq < 0 || nq > kMaxRows || heads <= 0 || heads > kMaxHeads || kv_heads <= 0 || heads % kv_heads || seqs < 0 ||
+      seqs > kMaxRows || max_q < 0 || max_k < 0 || n_prefix < 0 || n_prefix > kMaxRows)
+    return fail(ctx, BAG_EINVAL, "bad shape of packed sequences");
+  if (dh != 64 && dh != 128) return fail(ctx, BAG_EUNSUPPORTED, "attention of packed sequences takes heads of 64 or 128");
+  return BAG_OK;
+}
+
+static bag_status bag_attention_packed_impl(bag_ctx* ctx, const bag_packed_args* a, const void* pk, long ldpk,
+                                            const void* pv, long ldpv, long n_prefix) {
+  if (!a) return fail(ctx, BAG_EINVAL, "null arguments");
+  CKS(check_packed(ctx, a->nq, a->heads, a->kv_heads, a->dh, a->seqs, a->max_q, a->max_k, n_prefix));
+  if ((a->type != BAG_BF16 && a->type != BAG_F16) || (a->causal != 0 && a->causal != 1) ||
+      !(a->scale >= 0.f && std::isfinite(a->scale)))
+    return fail(ctx, BAG_EINVAL, "bad type, mask or scale of attention");
+  if (a->k_rows < 0 || a->k_rows > kMaxRows || !a->k_start != !a->k_len || (!a->k_start && a->k_rows < a->nq))
+    return fail(ctx, BAG_EINVAL, "k_start and k_len go together; without them k has a row for each query");
+  if (a->nq == 0 || a->seqs == 0) return BAG_OK;
+  const long wq = (long)a->heads * a->dh, wk = (long)a->kv_heads * a->dh;
+  if (!a->q || !a->o || !a->q_start || (a->k_rows && (!a->k || !a->v)) || (n_prefix && (!pk || !pv)))
+    return fail(ctx, BAG_EINVAL, "null pointer");
+  if (a->ldq < wq || a->ldo < wq || (a->k_rows && (a->ldk < wk || a->ldv < wk)) ||
+      (n_prefix && (ldpk < wk || ldpv < wk)))
+    return fail(ctx, BAG_EINVAL, "a row stride is less than a row");
+  auto rows16 = [](const void* p, long ld, long rows) { return !rows || (aligned(p, 16) && ld % 8 == 0); };
+  if (!rows16(a->q, a->ldq, 1) || !rows16(a->o, a->ldo, 1) || !rows16(a->k, a->ldk, a->k_rows) ||
+      !rows16(a->v, a->ldv, a->k_rows) || !rows16(pk, ldpk, n_prefix) || !rows16(pv, ldpv, n_prefix))
+    return fail(ctx, BAG_EUNSUPPORTED, "attention of packed sequences needs 16-byte aligned rows");
+  if (!aligned(a->lse, 4) || !aligned(a->q_start, 4) || !aligned(a->k_start, 4) || !aligned(a->k_len, 4) ||
+      (a->work_bytes && !a->work) || !aligned(a->work, 16))
+    return fail(ctx, BAG_EINVAL, "lse, starts, lengths or work is null or not aligned");
+  struct Mat {
+    const void* p;
+    long ld, rows, width;
+  };
+  const Mat in[] = {{a->q, a->ldq * 2, a->nq, wq * 2}, {a->k, a->ldk * 2, a->k_rows, wk * 2},
+                    {a->v, a->ldv * 2, a->k_rows, wk * 2}, {pk, ldpk * 2, n_prefix, wk * 2},
+                    {pv, ldpv * 2, n_prefix, wk * 2}};
+  const long nl = a->nq * a->heads * 4;
+  const Mat out[] = {{a->o, a->ldo * 2, a->nq, wq * 2}, {a->lse, nl, 1, nl},
+                     {a->work, (long)a->work_bytes, 1, (long)a->work_bytes}};
+  auto common = [](const Mat& x, const Mat& y) { return share(x.p, x.ld, x.rows, x.width, y.p, y.ld, y.rows, y.width); };
+  for (int o = 0; o < 3; ++o) {
+    for (const Mat& m : in)
+      if (common(out[o], m)) return fail(ctx, BAG_EINVAL, "o, lse or work overlaps an input");
+    for (int i = 0; i < o; ++i)
+      if (common(out[o], out[i])) return fail(ctx, BAG_EINVAL, "o, lse and work overlap");
+  }
+  PackedArgs g{};
+  g.q = a->q, g.ldq = a->ldq, g.k = a->k, g.ldk = a->ldk, g.v = a->v, g.ldv = a->ldv;
+  g.pk = pk, g.ldpk = ldpk, g.pv = pv, g.ldpv = ldpv;
+  g.o = a->o, g.ldo = a->ldo, g.lse = a->lse;
+  g.q_start = a->q_start, g.k_start = a->k_start, g.k_len = a->k_len;
+  g.nq = a->nq, g.k_rows = a->k_rows, g.n_prefix = n_prefix, g.seqs = a->seqs;
+  g.max_q = a->max_q ? std::min(a->max_q, a->nq) : a->nq;
+  const long most_k = a->k_start ? a->k_rows : a->nq;
+  g.max_k = a->max_k ? std::min(a->max_k, most_k) : most_k;
+  g.heads = a->heads, g.kv_heads = a->kv_heads, g.dh = a->dh, g.f16 = a->type == BAG_F16, g.causal = a->causal;
+  g.scale_log2 = (float)(1.4426950408889634 * (a->scale > 0.f ? (double)a->scale : 1.0 / std::sqrt((double)a->dh)));
+  g.work = a->work, g.work_bytes = a->work_bytes;
+  g.err = ctx->op_err;
+  size_t least;
+  attention_packed_work(g, &least);
+  if (a->work_bytes < least)
+    return fail(ctx, BAG_EINVAL, "attention behind a prefix needs a workspace of " + std::to_string(least) + " bytes");
+  CK(attention_packed(g, ctx->user_stream));
+  return BAG_OK;
+}
+
+static bag_status bag_attention_work_impl(bag_ctx* ctx, long nq, int heads, int kv_heads, int dh, long seqs, long max_q,
+                                          long max_k, long n_prefix, size_t* bytes) {
+  if (!bytes) return fail(ctx, BAG_EINVAL, "bytes is null");
+  CKS(check_packed(ctx, nq, heads, kv_heads, dh, seqs, max_q, max_k, n_prefix));
+  PackedArgs g{};
+  g.nq = nq, g.heads = heads, g.kv_heads = kv_heads, g.dh = dh, g.seqs = seqs;
+  g.k_rows = kMaxRows, g.n_prefix = n_prefix;
+  g.max_q = max_q ? std::min(max_q, nq) : nq;
+  g.max_k = max_k ? max_k : nq;
+  size_t least;
+  *bytes = nq && seqs ? std::max(attention_packed_work(g, &least), least) : 0;
+  return BAG_OK;
+}
+
 static bag_status bag_residual_add_impl(bag_ctx* ctx, float* out, const float* h_in, const float* R, long n) {
   if (!ctx || !out || !h_in || !R) return BAG_EINVAL;
   if (n < 0 || n % 4) return fail(ctx, BAG_EINVAL, "n must be a multiple of 4");
@@ -2378,6 +2542,31 @@ bag_status bag_attention_blocks(bag_ctx* ctx, const void* q, long ldq, const voi
   const OpScope scope(ctx);
   return leave_op(bag_attention_blocks_impl(ctx, q, ldq, k, ldk, v, vpad, type, nq, nk, heads, kv_heads, blocks,
                                             keep, o, ldo));
+}
+
+bag_status bag_rope(bag_ctx* ctx, const bag_rope_args* a) {
+  if (!ctx) return BAG_EINVAL;
+  const OpScope scope(ctx);
+  return leave_op(bag_rope_impl(ctx, a));
+}
+
+bag_status bag_attention_packed(bag_ctx* ctx, const bag_packed_args* a) {
+  if (!ctx) return BAG_EINVAL;
+  const OpScope scope(ctx);
+  return leave_op(bag_attention_packed_impl(ctx, a, nullptr, 0, nullptr, 0, 0));
+}
+
+bag_status bag_attention_prefix(bag_ctx* ctx, const bag_packed_args* a, const void* pk, long ldpk, const void* pv,
+                                long ldpv, long n_prefix) {
+  if (!ctx) return BAG_EINVAL;
+  const OpScope scope(ctx);
+  return leave_op(bag_attention_packed_impl(ctx, a, pk, ldpk, pv, ldpv, n_prefix));
+}
+
+bag_status bag_attention_work(bag_ctx* ctx, long nq, int heads, int kv_heads, int dh, long seqs, long max_q,
+                              long max_k, long n_prefix, size_t* bytes) {
+  if (!ctx) return BAG_EINVAL;
+  return bag_attention_work_impl(ctx, nq, heads, kv_heads, dh, seqs, max_q, max_k, n_prefix, bytes);
 }
 
 }  // extern "C"

@@ -1382,6 +1382,7 @@ cudaError_t kernels_init() {
   if (r == cudaSuccess) r = attention_tc_init();
   if (r == cudaSuccess) r = gemm_fp8_init();
   if (r == cudaSuccess) r = attention_blocks_init();
+  if (r == cudaSuccess) r = attention_packed_init();
   num_sms();
   return r;
 }

@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
 #include <utility>
 
 namespace bag {
@@ -316,6 +317,45 @@ struct BlockAttnArgs {
 };
 cudaError_t attention_blocks(const BlockAttnArgs& a, cudaStream_t s);
 cudaError_t attention_blocks_init();
+
+// ---- rotary positions and attention of packed sequences (see bag.h) ----
+constexpr int kRopePairs = 128;    // most pairs of a head
+struct RopeArgs {
+  const void* q; long ldq; void* q_out; long ldqo;     // null: no queries
+  const void* k; long ldk; void* k_out; long ldko;
+  const void* v; long ldv; void* v_out; long ldvo;
+  const int32_t* slots; long capacity;                 // null = row r of k, v to row r
+  const int32_t* pos; long pos0;                       // null = pos0 + r
+  long rows;
+  int heads, kv_heads, dh, pairs;
+  int half, inverse;
+  float scale;
+  int rows_cta;                                        // set by the launcher
+  uint64_t turns[kRopePairs];                          // turns a position of each pair, times 2^64
+};
+cudaError_t rope(RopeArgs a, int size, int f16, cudaStream_t s);
+
+struct PackedArgs {
+  const void* q; long ldq;
+  const void* k; long ldk;
+  const void* v; long ldv;
+  const void* pk; long ldpk;       // the shared prefix (n_prefix = 0: none)
+  const void* pv; long ldpv;
+  void* o; long ldo;
+  float* lse;                      // [nq][heads] or null
+  const int32_t* q_start;          // [seqs + 1]
+  const int32_t* k_start;          // [seqs], null = as the queries
+  const int32_t* k_len;            // [seqs]
+  long nq, k_rows, n_prefix, seqs, max_q, max_k;
+  int heads, kv_heads, dh, f16, causal;
+  float scale_log2;
+  void* work; size_t work_bytes;
+  int* err;
+};
+cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s);
+// bytes of workspace with which a call takes its fastest form, and without which it is refused
+size_t attention_packed_work(const PackedArgs& a, size_t* least);
+cudaError_t attention_packed_init();  // part of kernels_init
 
 // message returned by bag_last_error(NULL) (entry points without a context)
 }  // namespace bag
