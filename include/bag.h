@@ -520,9 +520,8 @@ typedef struct {
 bag_status bag_attention_packed(bag_ctx* ctx, const bag_packed_args* a);
 
 /* The same where every query also sees all n_prefix rows of pk and pv (strides ldpk, ldpv), as if they came
- * before its sequence's own keys, whose mask they do not shift.  The prefix is there once, and is read
- * for the rows of all sequences together.  k_start and k_len as above, so with k_rows = 0 and
- * k_len = 0 the prefix is all there is.  work of at least 2 nq heads (4 dh + 8) bytes (else EINVAL). */
+ * before its sequence's own keys, whose mask they do not shift.  The prefix is there once; where
+ * sequences are short it is read for the rows of all of them together, which takes a workspace. */
 bag_status bag_attention_prefix(bag_ctx* ctx, const bag_packed_args* a, const void* pk, long ldpk,
                                 const void* pv, long ldpv, long n_prefix);
 

@@ -555,7 +555,7 @@ class Context:
     def attention_prefix(self, q, k, v, o, q_start, prefix_k, prefix_v, heads, kv_heads=None, k_start=None,
                          k_len=None, max_q=None, max_k=None, causal=True, scale=None, lse=None, work=None):
         """attention_packed where every query also sees all rows of prefix_k and prefix_v [rows, kv_heads * dh]
-        first; needs work."""
+        first."""
         a, kind, wk = self._packed(q, k, v, o, q_start, heads, heads if kv_heads is None else kv_heads, k_start, k_len,
                                    max_q, max_k, causal, scale, lse, work)
         kp, ldk, n, ck, _ = _mat(prefix_k, "prefix_k", (kind,))

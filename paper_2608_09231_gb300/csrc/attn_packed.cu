@@ -23,11 +23,18 @@ struct PackedParams {
   int nq, k_rows, n_prefix, seqs;
   int heads, kv_heads, group, causal;
   float scale_log2;
-  // parts of the keys: parts1 of the prefix, chunk1 keys each, then own_parts() of a sequence, chunk2 keys each.
+  // The prefix is met by the rows of all sequences together (parts1 parts of chunk1 keys, whose sums are joined
+  // with those over own keys), or comes before each sequence's own keys (fused key tiles; then parts1 = 0).
+  // own_parts() parts of a sequence, chunk2 keys (those of the fused tiles among them) each.
   // Part i of row t and head h: part_o[((i * nq + t) * heads + h) * dh ...], part_ml likewise.
   int parts1, parts2, chunk1, chunk2;
+  int fused;
   float* part_o;
   float2* part_ml;
+  // tensor-core kernel: rows of a unit (128 or 256), units over the rows of all sequences and of each, and
+  // whether own keys are its part too
+  int unit_rows, slots1, slots2;
+  int* err;
 };
 
 // A sequence's rows of q and of k and v, clipped to the tensors' own.
@@ -54,7 +61,7 @@ BAG_DEV Span span_all(const PackedParams& p) {
 // Parts that hold a sequence's own keys; the last of parts2 takes all that the others leave (their sizes
 // come from the caller's estimate of the longest sequence).
 BAG_DEV int own_parts(const PackedParams& p, int lk) {
-  return (int)min(((long)lk + p.chunk2 - 1) / p.chunk2, (long)p.parts2);
+  return (int)min(((long)p.fused * 128 + lk + p.chunk2 - 1) / p.chunk2, (long)p.parts2);
 }
 
 template <bool F16>
@@ -112,37 +119,20 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
   long unit = blockIdx.x;
   const int head = (int)(unit % p.kv_heads);
   unit /= p.kv_heads;
-  const bool prefix = unit < p.parts1;
-  int part;       // index of the part
-  int k_lo, k_hi; // its keys
-  bool direct = false;
-  Span s;
-  const uint16_t *kb, *vb;
-  long ldk, ldv;
-  if (prefix) {
-    s = span_all(p);
-    part = (int)unit;
-    k_lo = min((long)part * p.chunk1, (long)s.lk);
-    k_hi = min((long)k_lo + p.chunk1, (long)s.lk);
-    kb = p.pk, vb = p.pv, ldk = p.ldpk, ldv = p.ldpv;
-  } else {
-    unit -= p.parts1;
-    s = span_of(p, (int)(unit / p.parts2));
-    const int own = (int)(unit % p.parts2), parts = own_parts(p, s.lk);
-    if (own >= (p.parts1 ? parts : max(parts, 1))) return;
-    direct = p.parts1 == 0 && parts <= 1;
-    part = p.parts1 + own;
-    k_lo = (int)min((long)own * p.chunk2, (long)s.lk);
-    k_hi = own == p.parts2 - 1 ? s.lk : (int)min((long)k_lo + p.chunk2, (long)s.lk);
-    kb = p.k + s.k0 * p.ldk, vb = p.v + s.k0 * p.ldv, ldk = p.ldk, ldv = p.ldv;
-  }
-  kb += head * DH;
-  vb += head * DH;
+  const Span s = span_of(p, (int)(unit / p.parts2));
+  const int own = (int)(unit % p.parts2), parts = own_parts(p, s.lk);
+  if (own >= (p.parts1 ? parts : max(parts, 1))) return;
+  const bool direct = p.parts1 == 0 && parts <= 1;
+  const int part = p.parts1 + own;
+  const int k_lo = (int)min((long)own * p.chunk2, (long)s.lk);
+  const int k_hi = own == p.parts2 - 1 ? s.lk : (int)min((long)k_lo + p.chunk2, (long)s.lk);
+  const uint16_t *kb = p.k + s.k0 * p.ldk + head * DH, *vb = p.v + s.k0 * p.ldv + head * DH;
+  const long ldk = p.ldk, ldv = p.ldv;
   const long R = (long)s.lq * G;
   // keys that row r of this part sees end before
   auto limit = [&](long r) {
     if (r >= R) return k_lo;
-    if (prefix || !p.causal) return k_hi;
+    if (!p.causal) return k_hi;
     return (int)min(max(r / G + 1 + s.lk - s.lq, (long)k_lo), (long)k_hi);
   };
   for (long r0 = 0; r0 < R; r0 += 16) {
@@ -289,7 +279,7 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
 #pragma unroll
       for (int w = 0; w < F_WARPS; ++w) {
         const float2 f = sml[w * 16 + lr];
-        den += f.x == -INFINITY ? 0.f : ex2(f.x - top) * f.y;
+        den += f.y == 0.f ? 0.f : ex2(f.x - top) * f.y;
         const float* row = so + (w * 16 + lr) * LD + col;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += row[e];
@@ -297,7 +287,7 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
       const long tok = s.q0 + r / G;
       const int h = head * G + (int)(r % G);
       if (direct) {
-        const float inv = top == -INFINITY ? 0.f : 1.f / den;
+        const float inv = den == 0.f ? 0.f : 1.f / den;
         uint4 w;
         w.x = pack16<F16>(v[0] * inv, v[1] * inv);
         w.y = pack16<F16>(v[2] * inv, v[3] * inv);
@@ -314,6 +304,453 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
       }
     }
     __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// many rows: tensor cores
+// ---------------------------------------------------------------------------
+namespace {
+constexpr int PT = 128;                    // rows and keys of a tile
+constexpr int PT_CHUNK = PT * 64 * 2;      // 128 rows x 64 columns: one 128-byte swizzle column
+constexpr int PT_STAGES = 2;               // of the K ring and of the V ring
+constexpr int PT_THREADS = 384;
+constexpr int PT_TMEM_COLS = 512;          // S_A [0,128) S_B [128,256) O_A [256,384) O_B [384,512)
+// registers a thread: 168 at launch; 128 * 72 + 256 * 216 = 384 * 168
+constexpr int PT_REGS_ISSUE = 72, PT_REGS_SOFTMAX = 216;
+constexpr int PT_OLD = 36;                 // floats a row in the output transpose
+constexpr int PT_OUT = 4 * 32 * PT_OLD * 4;  // bytes of a tile's
+template <int DH>
+struct PtSmem {
+  static constexpr int TILE = DH / 64 * PT_CHUNK;
+  static constexpr int Q = 0, K = 2 * TILE, V = K + PT_STAGES * TILE, OUT = DH == 128 ? Q : V + PT_STAGES * TILE;
+  static constexpr int BAR = DH == 128 ? V + PT_STAGES * TILE : OUT + 2 * PT_OUT;
+  static constexpr int BYTES = BAR + 256 + 1024;
+};
+static_assert(PT_OUT <= PtSmem<128>::TILE, "a tile's output transpose fits its queries");
+
+// Shared-memory descriptor of a tile whose rows run along the contraction (V: a row a key), 128-byte
+// swizzle: 64-column chunks PT_CHUNK apart, groups of eight rows 1024 bytes apart.
+BAG_DEV uint64_t sw128_desc_mn(uint32_t saddr) {
+  return sw128_desc(saddr) & ~((uint64_t)0x3fff << 16) | (uint64_t)(PT_CHUNK >> 4) << 16;
+}
+
+// The sequence whose units hold slot `slot`: sequence i's slots are q_start[i] * group / unit_rows + i and on,
+// so that each has as many as its rows need and at most one more.  Called by a whole warp.
+BAG_DEV int sequence_of_slot(const PackedParams& p, long slot, long* first) {
+  const int lane = threadIdx.x % 32;
+  auto start = [&](int i) { return (long)__ldg(p.q_start + i) * p.group / p.unit_rows + i; };
+  int lo = 0, n = p.seqs;
+  while (n > 1) {
+    const int step = (n + 31) / 32, i = lane * step;
+    const uint32_t at = __ballot_sync(0xffffffffu, i < n && start(lo + i) <= slot);
+    const int skip = max(__popc(at) - 1, 0) * step;
+    lo += skip;
+    n = min(step, n - skip);
+  }
+  *first = start(lo);
+  return lo;
+}
+}  // namespace
+
+// One CTA takes one or two tiles of 128 rows (query token, head of the group: row r is token r / group) and
+// walks the tiles of 128 keys that the last of them sees:
+//   warp 0        TMA producer of K and V tiles into 2-stage rings of their own
+//   warp 1        MMA issuer, in turn between the tiles: S_A,0 S_B,0 | PV_A,j S_A,j+1 | PV_B,j S_B,j+1 | ...
+//                 It zeros the rows of V past a sequence's (or the prefix's) last key, up to the next 16,
+//                 where the products end: whatever lies there would meet weights of zero, and may be NaN
+//   warps 4..11   load the queries, then the softmax of tile A (4..7) and B (8..11), a row a thread, as in
+//                 the dense kernel: P goes back over the scores in 16 bits and enters the second product
+//                 from TMEM; O stays in TMEM and is rescaled only when the maximum has grown by more than 8
+// V is read as it lies, a row a key: as an operand whose rows run along the contraction.
+template <bool F16, int DH>
+__global__ void __launch_bounds__(PT_THREADS, 1)
+    attn_packed_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                       const __grid_constant__ CUtensorMap tmPK, const __grid_constant__ CUtensorMap tmPV,
+                       const PackedParams p) {
+  using M = PtSmem<DH>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint8_t *sQ = smem + M::Q, *sK = smem + M::K, *sV = smem + M::V;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::BAR);
+  uint64_t* q_full = bars + 0;
+  uint64_t* k_full = bars + 1;    // [2]
+  uint64_t* k_empty = bars + 3;   // [2]
+  uint64_t* v_full = bars + 5;    // [2]
+  uint64_t* v_empty = bars + 7;   // [2]
+  uint64_t* s_full = bars + 9;    // [2] per query tile
+  uint64_t* p_full = bars + 11;   // [2]
+  uint64_t* o_done = bars + 13;   // [2]
+  uint64_t* drain = bars + 15;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+  grid_dep_sync();
+  // the unit: its rows, its part of the keys
+  const int G = p.group;
+  long unit = blockIdx.x;
+  const int head = (int)(unit % p.kv_heads);
+  unit /= p.kv_heads;
+  const long units1 = (long)p.slots1 * p.parts1;
+  const bool all_rows = unit < units1;  // the prefix with the rows of all sequences
+  Span s;
+  long r0;
+  int part, j0, most;  // index of the part; its first key tile, and how many it may have
+  int fused;           // key tiles of the prefix, before the sequence's own
+  if (all_rows) {
+    s = span_all(p);
+    part = (int)(unit % p.parts1);
+    r0 = unit / p.parts1 * p.unit_rows;
+    most = p.chunk1 / PT;
+    j0 = part * most;
+    fused = (p.n_prefix + PT - 1) / PT;
+    s.lk = 0;
+  } else {
+    unit -= units1;
+    part = (int)(unit % p.parts2);
+    const long slot = p.slots2 - 1 - unit / p.parts2;  // later rows see more keys: they go first
+    long first;
+    s = span_of(p, sequence_of_slot(p, slot, &first));
+    r0 = (slot - first) * p.unit_rows;
+    j0 = (int)((long)part * (p.chunk2 / PT));
+    most = part == p.parts2 - 1 ? 0x7fffffff : p.chunk2 / PT;
+    fused = p.fused;
+  }
+  const long R = (long)s.lq * G;
+  if (r0 < 0 || r0 >= R) return;
+  bool direct = false;
+  if (!all_rows) {
+    const int parts = own_parts(p, s.lk);
+    if (part >= (p.parts1 ? parts : max(parts, 1))) return;
+    direct = p.parts1 == 0 && parts <= 1;
+    part += p.parts1;
+  }
+  // own keys that row r sees
+  auto sees = [&](long r) {
+    return p.causal ? (int)min(max(r / G + 1 + s.lk - s.lq, 0L), (long)s.lk) : s.lk;
+  };
+  int n[2];  // key tiles of each tile of rows
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const long end = min(r0 + (x + 1) * PT, R);
+    n[x] = x * PT < p.unit_rows && end > r0 + x * PT
+               ? min(max(fused + (sees(end - 1) + PT - 1) / PT - j0, 0), most)
+               : 0;
+  }
+  const int nkb = max(n[0], n[1]);
+  // keys of tile j (of this part) that exist, and the tile's place
+  auto keys_of = [&](int j) {
+    const int t = j0 + j;
+    return t < fused ? p.n_prefix - t * PT : s.lk - (t - fused) * PT;
+  };
+  auto last_user = [&](int j) { return j < n[1] ? 1 : 0; };
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 8);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(k_full + i, 1);
+      mbar_init(k_empty + i, 1);
+      mbar_init(v_full + i, 1);
+      mbar_init(v_empty + i, 1);
+      mbar_init(s_full + i, 1);
+      mbar_init(p_full + i, 4);  // one arrival per softmax warp of the tile
+      mbar_init(o_done + i, 1);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(fused ? &tmPK : &tmK);
+    tma_prefetch_desc(fused ? &tmPV : &tmV);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, PT_TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(*tmem_slot);
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PT_REGS_ISSUE));
+    if (warp == 0 && lane == 0) {
+      // ---------------- TMA producer ----------------
+      int kj = 0, vj = 0;  // tiles issued
+      for (int j = 0; j < nkb; ++j) {
+        const int st = j % PT_STAGES, t = j0 + j;
+        const uint32_t ph = ((j / PT_STAGES) & 1) ^ 1;
+        const bool pre = t < fused;
+        const int row = pre ? t * PT : s.k0 + (t - fused) * PT;
+        const CUtensorMap *mk = pre ? &tmPK : &tmK, *mv = pre ? &tmPV : &tmV;
+        if (!mbar_wait(k_empty + st, ph, abort_flag)) break;
+        uint8_t* k = sK + st * M::TILE;
+        mbar_arrive_expect_tx(k_full + st, M::TILE);
+        for (int c = 0; c < DH / 64; ++c) tma_load_2d(k + c * PT_CHUNK, mk, head * DH + c * 64, row, k_full + st);
+        ++kj;
+        if (!mbar_wait(v_empty + st, ph, abort_flag)) break;
+        uint8_t* v = sV + st * M::TILE;
+        mbar_arrive_expect_tx(v_full + st, M::TILE);
+        for (int c = 0; c < DH / 64; ++c) tma_load_2d(v + c * PT_CHUNK, mv, head * DH + c * 64, row, v_full + st);
+        ++vj;
+      }
+      if (vj < nkb) {
+        // wait (bounded) for copies still in flight before the CTA may exit
+        const uint64_t t0 = global_ns();
+        auto landed = [&](uint64_t* bar, uint32_t ph) {
+          while (!mbar_try_wait(bar, ph) && global_ns() - t0 < kWaitLimitNs) {
+          }
+        };
+        for (int j = max(0, kj - PT_STAGES); j < kj; ++j) landed(k_full + j % PT_STAGES, (j / PT_STAGES) & 1);
+        for (int j = max(0, vj - PT_STAGES); j < vj; ++j) landed(v_full + j % PT_STAGES, (j / PT_STAGES) & 1);
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
+      constexpr uint32_t idesc_s = F16 ? idesc_f16_f32(PT, PT) : idesc_bf16_f32(PT, PT);
+      constexpr uint32_t idesc_o = (F16 ? idesc_f16_f32(PT, DH) : idesc_bf16_f32(PT, DH)) | 1u << 16;  // B along its rows
+      const uint32_t q_addr = smem_u32(sQ), k_addr = smem_u32(sK), v_addr = smem_u32(sV);
+      // K step kk of a tile: 64-column chunk kk / 4, 32 bytes per step inside it (16-byte units)
+      auto koff = [](int kk) { return (uint64_t)(((kk >> 2) * PT_CHUNK + (kk & 3) * 32) >> 4); };
+      auto issue_s = [&](int x, int j) {
+        const uint64_t qd = sw128_desc(q_addr + x * M::TILE);
+        const uint64_t kd = sw128_desc(k_addr + (j % PT_STAGES) * M::TILE);
+        const bool release = x == last_user(j);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < DH / 16; ++kk)
+            mma_bf16(tmem + x * 128, qd + koff(kk), kd + koff(kk), idesc_s, kk > 0 ? 1u : 0u);
+          mma_commit(s_full + x);
+          if (release) mma_commit(k_empty + j % PT_STAGES);
+        }
+        __syncwarp();
+      };
+      auto issue_pv = [&](int x, int j) {
+        const uint64_t vd = sw128_desc_mn(v_addr + (j % PT_STAGES) * M::TILE);
+        const int steps = min(PT, keys_of(j) + 15) / 16;
+        const bool release = x == last_user(j), done = j == n[x] - 1;
+        if (elect_one()) {
+          if (steps == PT / 16) {
+#pragma unroll
+            for (int kk = 0; kk < PT / 16; ++kk)
+              mma_bf16_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                          (j > 0 || kk > 0) ? 1u : 0u);
+          } else {
+            for (int kk = 0; kk < steps; ++kk)
+              mma_bf16_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                          (j > 0 || kk > 0) ? 1u : 0u);
+          }
+          if (release) mma_commit(v_empty + j % PT_STAGES);
+          if (done) mma_commit(o_done + x);
+        }
+        __syncwarp();
+      };
+      auto wait = [&](uint64_t* bar, uint32_t ph) {
+        const bool w = mbar_wait_warp(bar, ph, abort_flag);
+        tc_fence_after();
+        return w;
+      };
+      bool ok = nkb > 0 && wait(q_full, 0) && wait(k_full, 0);
+      if (ok) {
+        if (n[0] > 0) issue_s(0, 0);
+        if (n[1] > 0) issue_s(1, 0);
+      }
+      for (int j = 0; j < nkb && ok; ++j) {
+        const int s1 = (j + 1) % PT_STAGES;
+        ok = wait(v_full + j % PT_STAGES, (j / PT_STAGES) & 1);
+        const int from = keys_of(j), to = (from + 15) / 16 * 16;
+        if (ok && from < PT) {  // the rows past the last key, up to where the products end
+          for (int i = lane; i < (to - from) * (DH / 8); i += 32) {
+            const int row = from + i / (DH / 8), piece = i % (DH / 8);
+            *reinterpret_cast<uint4*>(sV + (j % PT_STAGES) * M::TILE + piece / 8 * PT_CHUNK + row * 128 + piece % 8 * 16) =
+                make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        bool next = false;  // the next K tile is there
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (!ok || j >= n[x]) continue;
+          // PV_j of this tile, then its S_{j+1} into the columns P_j came from (in issue order)
+          if (!(ok = wait(p_full + x, j & 1))) break;
+          issue_pv(x, j);
+          if (j + 1 < n[x]) {
+            if (!next && !(ok = wait(k_full + s1, ((j + 1) / PT_STAGES) & 1))) break;
+            next = true;
+            issue_s(x, j + 1);
+          }
+        }
+      }
+      if (elect_one()) {
+        mma_commit(drain);
+        const uint64_t t0 = global_ns();
+        while (!mbar_try_wait(drain, 0) && global_ns() - t0 < kWaitLimitNs) {
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PT_REGS_SOFTMAX));
+    // ---------------- softmax warpgroups (warps 4..7: tile A, 8..11: tile B) ----------------
+    const int x = (warp - 4) >> 2;
+    const int quad = warp & 3;
+    if (n[x] > 0) {  // the tile's queries, rows past the last as zeros
+      constexpr int LR = DH / 8;  // lanes of a row
+      const int t = threadIdx.x - 128 - x * 128, piece = t % LR;
+      uint8_t* q = sQ + x * M::TILE + piece / 8 * PT_CHUNK;
+      const uint16_t* src = p.q + (long)head * G * DH + piece * 8;
+#pragma unroll 8
+      for (int i = 0; i < LR; ++i) {
+        const int row = i * (128 / LR) + t / LR;
+        const long r = r0 + x * PT + row;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (r < R) v = __ldg(reinterpret_cast<const uint4*>(src + (s.q0 + r / G) * p.ldq + r % G * DH));
+        *reinterpret_cast<uint4*>(q + row * 128 + ((piece % 8) ^ (row & 7)) * 16) = v;
+      }
+      fence_proxy_async_smem();
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(q_full);
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    const uint32_t s_addr = tmem + lane_base + x * 128;
+    const uint32_t o_addr = tmem + lane_base + 256 + x * 128;
+    const int own = sees(min(r0 + x * PT + quad * 32 + lane, R - 1));
+    float m_use = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n[x]; ++j) {
+      const bool w = mbar_wait(s_full + x, j & 1, abort_flag);
+      if (!__all_sync(0xffffffffu, w)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const int t = j0 + j;
+      const int kvalid = t < fused ? p.n_prefix - t * PT : own - (t - fused) * PT;  // keys of the tile that the row sees
+      // the whole S row in registers: four loads, one wait
+      uint32_t r[PT];
+#pragma unroll
+      for (int c = 0; c < PT / 32; ++c) tmem_ld32_nowait(s_addr + c * 32, r + c * 32);
+      tmem_ld_wait();
+      if (__any_sync(0xffffffffu, kvalid < PT)) {
+#pragma unroll
+        for (int i = 0; i < PT; ++i)
+          if (i >= kvalid) r[i] = __float_as_uint(-INFINITY);
+      }
+      // row maximum: four independent chains of three-input maxima
+      float mq[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) mq[u] = fmaxf(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
+#pragma unroll
+      for (int i = 8; i < PT; i += 8)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          mq[u] = max3(mq[u], __uint_as_float(r[i + 2 * u]), __uint_as_float(r[i + 2 * u + 1]));
+      const float mx2 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * p.scale_log2;
+      float alpha = 1.f;
+      if (mx2 > m_use + 8.f) {
+        alpha = ex2(m_use - mx2);
+        m_use = mx2;
+        l *= alpha;
+      }
+      const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
+      float ls0 = 0.f, ls1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < PT / 32; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          float x0, x1;
+          fma2(x0, x1, __uint_as_float(r[c * 32 + i]), __uint_as_float(r[c * 32 + i + 1]), p.scale_log2, neg_m);
+          const float a0 = ex2(x0), a1 = ex2(x1);
+          add2(ls0, ls1, a0, a1);
+          pk[i / 2] = pack16<F16>(a0, a1);
+        }
+        tmem_st16(s_addr + c * 16, pk);
+      }
+      l += ls0 + ls1;
+      // O_x holds PV of every earlier key tile (the S of this tile was issued after it);
+      // rescale it before this tile's PV is issued
+      if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+        for (int c = 0; c < DH / 32; ++c) {
+          float o[32];
+          tmem_ld32(o_addr + c * 32, o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] *= alpha;
+          tmem_st32(o_addr + c * 32, o);
+        }
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + x);
+    }
+    if (ok && n[x] > 0) ok = __all_sync(0xffffffffu, mbar_wait(o_done + x, 0, abort_flag));
+    tc_fence_after();
+    if (ok && r0 + x * PT < R && x * PT < p.unit_rows) {
+      const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
+      const float f = direct ? (any ? 1.f / l : 0.f) : 1.f;
+      {  // the row's maximum and sum
+        const long r = r0 + x * PT + quad * 32 + lane;
+        if (r < R) {
+          const long tok = s.q0 + r / G, h = (long)head * G + r % G;
+          if (!direct)
+            p.part_ml[((long)part * p.nq + tok) * p.heads + h] = make_float2(any ? m_use : -INFINITY, l);
+          else if (p.lse)
+            p.lse[tok * p.heads + h] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        }
+      }
+      // through shared memory (where a tile's queries were, which no product reads any more): four lanes
+      // hold 32 consecutive columns of a row, so a store covers eight rows' runs
+      float* buf = reinterpret_cast<float*>(smem + M::OUT + x * (DH == 128 ? M::TILE : PT_OUT)) + quad * 32 * PT_OLD;
+      const int lr = lane >> 2, c8 = (lane & 3) * 8;
+      long at[4];  // of rows lr + 8 u: element of o or of part_o
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const long r = r0 + x * PT + quad * 32 + lr + 8 * u;
+        const long tok = s.q0 + r / G, h = (long)head * G + r % G;
+        at[u] = r >= R ? -1 : (direct ? tok * p.ldo + h * DH : (((long)part * p.nq + tok) * p.heads + h) * DH) + c8;
+      }
+#pragma unroll 1
+      for (int c = 0; c < DH; c += 32) {
+        float o[32];
+        if (n[x] > 0) tmem_ld32(o_addr + c, o);
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          *reinterpret_cast<float4*>(buf + lane * PT_OLD + i) =
+              any && n[x] > 0 ? make_float4(o[i] * f, o[i + 1] * f, o[i + 2] * f, o[i + 3] * f)
+                              : make_float4(0.f, 0.f, 0.f, 0.f);
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float4* v = reinterpret_cast<const float4*>(buf + (8 * u + lr) * PT_OLD + c8);
+          const float4 a = v[0], b = v[1];
+          if (at[u] < 0) continue;
+          if (direct) {
+            uint4 w;
+            w.x = pack16<F16>(a.x, a.y);
+            w.y = pack16<F16>(a.z, a.w);
+            w.z = pack16<F16>(b.x, b.y);
+            w.w = pack16<F16>(b.z, b.w);
+            *reinterpret_cast<uint4*>(p.o + at[u] + c) = w;
+          } else {
+            float4* d = reinterpret_cast<float4*>(p.part_o + at[u] + c);
+            d[0] = a;
+            d[1] = b;
+          }
+        }
+        __syncwarp();
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag && p.err) atomicOr(p.err, 1);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, PT_TMEM_COLS);
   }
 }
 
@@ -354,8 +791,8 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
     const long at = ((long)i * p.nq + tok) * p.heads + h;
     const float2 f = p.part_ml[at];
     const float4 v = *reinterpret_cast<const float4*>(p.part_o + at * DH + 4 * x);
-    if (f.x == -INFINITY) continue;
-    const float top = fmaxf(m, f.x), a = m == -INFINITY ? 0.f : ex2(m - top), b = ex2(f.x - top);
+    if (f.y == 0.f) continue;  // no key of the part is seen
+    const float top = fmaxf(m, f.x), a = l == 0.f ? 0.f : ex2(m - top), b = ex2(f.x - top);
     m = top;
     l = l * a + f.y * b;
     acc.x = acc.x * a + v.x * b;
@@ -373,7 +810,7 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
-    const float w = sml[i].x == -INFINITY ? 0.f : ex2(sml[i].x - top);
+    const float w = sml[i].y == 0.f ? 0.f : ex2(sml[i].x - top);
     const float4 v = so[i][x];
     den += w * sml[i].y;
     acc.x += w * v.x;
@@ -381,7 +818,7 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
     acc.z += w * v.z;
     acc.w += w * v.w;
   }
-  const float inv = top == -INFINITY ? 0.f : 1.f / den;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
   uint2 u;
   u.x = pack16<F16>(acc.x * inv, acc.y * inv);
   u.y = pack16<F16>(acc.z * inv, acc.w * inv);
@@ -390,45 +827,58 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
 }
 
 namespace {
+// The form of a call.  few: own keys by attn_few_kernel; rows: of a unit of the tensor-core kernel.
 struct Plan {
   int parts1, parts2, chunk1, chunk2;
+  int few, fused, rows;
 };
 
 size_t part_bytes(const PackedArgs& a) { return (size_t)a.nq * (size_t)a.heads * ((size_t)a.dh * 4 + 8); }
 
-// How the keys are cut, with at most `most` parts in all.
+long cdiv(long a, long b) { return (a + b - 1) / b; }
+
+// How the rows and keys are cut, with at most `most` parts in all.
 Plan plan_of(const PackedArgs& a, long most) {
   Plan t{};
-  auto chunk = [](long keys, long parts) { return (int)((keys + parts * F_KEYS - 1) / (parts * F_KEYS) * F_KEYS); };
+  const long G = a.heads / a.kv_heads, sms = sm_count();
   const long max_k = std::min(std::max(a.max_k, 1L), std::max(a.k_rows, 1L));
-  auto want = [&](long keys, long units) {
-    return std::max(1L, std::min((keys + 255) / 256, 4L * sm_count() / std::max(1L, units)));
-  };
-  long p1 = a.n_prefix ? want(a.n_prefix, a.kv_heads) : 0;
-  long p2 = want(max_k, a.seqs * a.kv_heads);
+  const long max_q = std::max(1L, std::min(a.max_q, a.nq)), rows = a.nq * G;
+  t.few = max_q * G <= 16;
+  // units of 256 rows where there are enough of them
+  auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
+  t.rows = units(256) * 2 > sms ? 256 : 128;
+  const bool together = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
+  const long per = t.few ? F_KEYS : PT;  // keys that a part has a multiple of
+  auto chunk = [](long keys, long parts, long n) { return (int)(cdiv(cdiv(keys, parts), n) * n); };
+  long p1 = 0, p2 = 1;
+  if (together) p1 = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, t.rows) * a.kv_heads)));
+  const long keys = max_k + (together ? 0 : cdiv(a.n_prefix, PT) * PT);
+  if (t.few)
+    p2 = std::max(1L, std::min(cdiv(max_k, 256), 4 * sms / std::max(1L, a.seqs * a.kv_heads)));
+  else if (units(t.rows) * 2 <= sms)
+    p2 = std::max(1L, std::min(keys / 1024, sms / std::max(1L, units(t.rows))));
   if (p1 + p2 > most) {
     if (p1) p1 = std::max(1L, std::min(p1, most - 1));
     p2 = std::max(1L, most - p1);
   }
-  t.chunk1 = p1 ? chunk(a.n_prefix, p1) : F_KEYS;
-  t.parts1 = p1 ? (int)((a.n_prefix + t.chunk1 - 1) / t.chunk1) : 0;
-  t.chunk2 = chunk(max_k, p2);
+  t.fused = together ? 0 : (int)cdiv(a.n_prefix, PT);
+  if (t.fused) t.few = 0;
+  t.chunk1 = p1 ? chunk(a.n_prefix, p1, PT) : PT;
+  t.parts1 = p1 ? (int)cdiv(a.n_prefix, t.chunk1) : 0;
+  t.chunk2 = chunk(keys, p2, t.few ? per : PT);
   t.parts2 = (int)p2;
   return t;
 }
 }  // namespace
 
-size_t attention_packed_work(const PackedArgs& a, size_t* least) {
+size_t attention_packed_work(const PackedArgs& a) {
   const Plan t = plan_of(a, 1L << 30);
-  const size_t one = part_bytes(a);
-  *least = t.parts1 ? 2 * one : 0;
-  return t.parts1 + t.parts2 > 1 ? (size_t)(t.parts1 + t.parts2) * one : 0;
+  return t.parts1 + t.parts2 > 1 ? (size_t)(t.parts1 + t.parts2) * part_bytes(a) : 0;
 }
 
 cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   if (a.nq <= 0 || a.seqs <= 0) return cudaSuccess;
-  const size_t one = part_bytes(a);
-  const long most = (long)std::min<size_t>(a.work_bytes / one, 1u << 30);
+  const long most = (long)std::min<size_t>(a.work_bytes / part_bytes(a), 1u << 30);
   const Plan t = plan_of(a, most);
   PackedParams p{};
   auto u16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
@@ -440,21 +890,50 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   p.nq = (int)a.nq, p.k_rows = (int)a.k_rows, p.n_prefix = (int)a.n_prefix, p.seqs = (int)a.seqs;
   p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = a.heads / a.kv_heads, p.causal = a.causal;
   p.scale_log2 = a.scale_log2;
-  p.parts1 = t.parts1, p.parts2 = t.parts2, p.chunk1 = t.chunk1, p.chunk2 = t.chunk2;
+  p.parts1 = t.parts1, p.parts2 = t.parts2, p.chunk1 = t.chunk1, p.chunk2 = t.chunk2, p.fused = t.fused;
   p.part_o = reinterpret_cast<float*>(a.work);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)(t.parts1 + t.parts2) * a.nq * a.heads * a.dh);
-  const long units = (t.parts1 + a.seqs * t.parts2) * a.kv_heads, joins = a.nq * a.heads;
-  if (units > 0x7fffffffL || joins > 0x7fffffffL) return cudaErrorInvalidConfiguration;
-  auto launch = [&](auto few, auto join, int smem) {
-    cudaError_t e = launch_kernel(few, (unsigned)units, F_TH, smem, s, p);
+  const long rows = a.nq * p.group;
+  p.unit_rows = t.rows;
+  const long slots1 = t.parts1 ? cdiv(rows, t.rows) : 0, slots2 = t.few ? 0 : rows / t.rows + a.seqs;
+  p.err = a.err;
+  const long tiles = (slots1 * t.parts1 + slots2 * t.parts2) * a.kv_heads;
+  const long few = t.few ? a.seqs * t.parts2 * a.kv_heads : 0, joins = a.nq * a.heads;
+  if (tiles > 0x7fffffffL || few > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
+    return cudaErrorInvalidConfiguration;
+  p.slots1 = (int)slots1, p.slots2 = (int)slots2;
+  CUtensorMap tk, tv, tpk, tpv;
+  if (tiles) {
+    const uint64_t width = (uint64_t)a.kv_heads * a.dh;
+    // a tensor without rows is never read: another one stands for its map
+    auto map = [&](CUtensorMap* m, const void* x, long ld, long n) {
+      return encode_tmap_2d_bf16(m, x, width, (uint64_t)n, (uint64_t)ld * 2, 64, PT) != 0;
+    };
+    if (a.k_rows && slots2 && (map(&tk, a.k, a.ldk, a.k_rows) || map(&tv, a.v, a.ldv, a.k_rows))) return cudaErrorInvalidValue;
+    if (a.n_prefix) {
+      if (map(&tpk, a.pk, a.ldpk, a.n_prefix) || map(&tpv, a.pv, a.ldpv, a.n_prefix)) return cudaErrorInvalidValue;
+      if (!a.k_rows || !slots2) tk = tpk, tv = tpv;
+    } else {
+      if (!a.k_rows && (map(&tk, a.q, a.ldq, a.nq) || map(&tv, a.q, a.ldq, a.nq))) return cudaErrorInvalidValue;
+      tpk = tk, tpv = tv;
+    }
+  }
+  auto launch = [&](auto few_kernel, auto kernel, auto join, int few_bytes, int bytes) {
+    cudaError_t e = cudaSuccess;
+    if (few) e = launch_kernel(few_kernel, (unsigned)few, F_TH, few_bytes, s, p);
+    if (tiles && e == cudaSuccess) e = launch_kernel(kernel, (unsigned)tiles, PT_THREADS, bytes, s, tk, tv, tpk, tpv, p);
     if (e == cudaSuccess && t.parts1 + t.parts2 > 1) e = launch_kernel(join, (unsigned)joins, JN_TH, 0, s, p);
     return e;
   };
   if (a.dh == 128)
-    return a.f16 ? launch(attn_few_kernel<true, 128>, attn_join_kernel<true, 128>, few_smem<128>())
-                 : launch(attn_few_kernel<false, 128>, attn_join_kernel<false, 128>, few_smem<128>());
-  return a.f16 ? launch(attn_few_kernel<true, 64>, attn_join_kernel<true, 64>, few_smem<64>())
-               : launch(attn_few_kernel<false, 64>, attn_join_kernel<false, 64>, few_smem<64>());
+    return a.f16 ? launch(attn_few_kernel<true, 128>, attn_packed_kernel<true, 128>, attn_join_kernel<true, 128>,
+                          few_smem<128>(), PtSmem<128>::BYTES)
+                 : launch(attn_few_kernel<false, 128>, attn_packed_kernel<false, 128>, attn_join_kernel<false, 128>,
+                          few_smem<128>(), PtSmem<128>::BYTES);
+  return a.f16 ? launch(attn_few_kernel<true, 64>, attn_packed_kernel<true, 64>, attn_join_kernel<true, 64>,
+                        few_smem<64>(), PtSmem<64>::BYTES)
+               : launch(attn_few_kernel<false, 64>, attn_packed_kernel<false, 64>, attn_join_kernel<false, 64>,
+                        few_smem<64>(), PtSmem<64>::BYTES);
 }
 
 cudaError_t attention_packed_init() {
@@ -466,6 +945,10 @@ cudaError_t attention_packed_init() {
   smem(attn_few_kernel<false, 128>, few_smem<128>());
   smem(attn_few_kernel<true, 64>, few_smem<64>());
   smem(attn_few_kernel<false, 64>, few_smem<64>());
+  smem(attn_packed_kernel<true, 128>, PtSmem<128>::BYTES);
+  smem(attn_packed_kernel<false, 128>, PtSmem<128>::BYTES);
+  smem(attn_packed_kernel<true, 64>, PtSmem<64>::BYTES);
+  smem(attn_packed_kernel<false, 64>, PtSmem<64>::BYTES);
   return r;
 }
 

@@ -2152,10 +2152,6 @@ static bag_status bag_attention_packed_impl(bag_ctx* ctx, const bag_packed_args*
   g.scale_log2 = (float)(1.4426950408889634 * (a->scale > 0.f ? (double)a->scale : 1.0 / std::sqrt((double)a->dh)));
   g.work = a->work, g.work_bytes = a->work_bytes;
   g.err = ctx->op_err;
-  size_t least;
-  attention_packed_work(g, &least);
-  if (a->work_bytes < least)
-    return fail(ctx, BAG_EINVAL, "attention behind a prefix needs a workspace of " + std::to_string(least) + " bytes");
   CK(attention_packed(g, ctx->user_stream));
   return BAG_OK;
 }
@@ -2169,8 +2165,7 @@ static bag_status bag_attention_work_impl(bag_ctx* ctx, long nq, int heads, int 
   g.k_rows = kMaxRows, g.n_prefix = n_prefix;
   g.max_q = max_q ? std::min(max_q, nq) : nq;
   g.max_k = max_k ? max_k : nq;
-  size_t least;
-  *bytes = nq && seqs ? std::max(attention_packed_work(g, &least), least) : 0;
+  *bytes = nq && seqs ? attention_packed_work(g) : 0;
   return BAG_OK;
 }
 

@@ -353,8 +353,8 @@ struct PackedArgs {
   int* err;
 };
 cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s);
-// bytes of workspace with which a call takes its fastest form, and without which it is refused
-size_t attention_packed_work(const PackedArgs& a, size_t* least);
+// bytes of workspace with which a call takes its fastest form
+size_t attention_packed_work(const PackedArgs& a);
 cudaError_t attention_packed_init();  // part of kernels_init
 
 // message returned by bag_last_error(NULL) (entry points without a context)

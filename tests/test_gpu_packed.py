@@ -227,6 +227,20 @@ def test_values_that_are_not_finite(ctx):
     assert torch.equal(bad, want)
 
 
+@pytest.mark.parametrize("lens", [[(1, 6000), (1, 6000)], [(40, 6000), (3, 6000)]])
+@pytest.mark.parametrize("prefix", [None, 700])
+def test_nan_queries_with_keys_in_parts(lens, prefix, ctx):
+    """No part of a row's keys may lose that its scores are NaN."""
+    b = Batch(lens, 4, 2, 128, "f16", prefix=prefix)
+    b.q[0, :128] = math.nan
+    b.run(ctx)
+    n = b.starts[-1]
+    bad = ~torch.isfinite(b.o.reshape(-1, 4, 128)[:n]).all(2)
+    want = torch.zeros_like(bad)
+    want[0, 0] = True
+    assert torch.equal(bad, want) and torch.equal(torch.isnan(b.lse[:n]), want)
+
+
 def test_a_prefix_equals_its_keys_in_front(ctx):
     """The same attention written in two ways, both within their bound of 64 bits and of each other."""
     b = Batch([(1, 200), (60, 60), (3, 9)], 14, 2, 128, "f16", prefix=260)
@@ -387,8 +401,11 @@ def test_refusals(ctx):
     ):
         with pytest.raises(ValueError):
             f()
-    with pytest.raises(bag.BagError, match="workspace"):
-        ctx.attention_prefix(q, k, v, o, st, k, v, 4, 2, **b.dev)
+    with pytest.raises(ValueError):
+        ctx.attention_prefix(q, k, v, o, st, k[:, :128], v, 4, 2, **b.dev)
+    with pytest.raises(bag.BagError) as e:
+        ctx.attention_prefix(q, k, v, o, st, o[:, :256], v[:7], 4, 2, **b.dev)  # o over the prefix
+    assert e.value.status == 1
     with pytest.raises(bag.BagError) as e:
         ctx.attention_work(4, 5, 128, 2, 1, 4, 9)
     assert e.value.status == 1
