@@ -7,6 +7,7 @@
 // (m, l, O) with l = sum 2^(s - m), O = sum 2^(s - m) v, s in log2 units; parts are joined by
 // m = max m_i, l = sum 2^(m_i - m) l_i, O likewise.
 #include <algorithm>
+#include <cstdlib>
 
 #include "attn_common.cuh"
 #include "kernels.h"
@@ -31,9 +32,9 @@ struct PackedParams {
   int fused;
   float* part_o;
   float2* part_ml;
-  // tensor-core kernel: rows of a unit (128 or 256), units over the rows of all sequences and of each, and
-  // whether own keys are its part too
-  int unit_rows, slots1, slots2;
+  // tensor-core kernel: a tile's rows are `tokens` query tokens x `together` heads of a group; units over the
+  // tokens of all sequences and of each
+  int together, tokens, slots1, slots2;
   int* err;
 };
 
@@ -128,19 +129,19 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
   const int k_hi = own == p.parts2 - 1 ? s.lk : (int)min((long)k_lo + p.chunk2, (long)s.lk);
   const uint16_t *kb = p.k + s.k0 * p.ldk + head * DH, *vb = p.v + s.k0 * p.ldv + head * DH;
   const long ldk = p.ldk, ldv = p.ldv;
-  const long R = (long)s.lq * G;
+  const int R = s.lq * G;  // below 2^31
   // keys that row r of this part sees end before
-  auto limit = [&](long r) {
+  auto limit = [&](int r) {
     if (r >= R) return k_lo;
     if (!p.causal) return k_hi;
-    return (int)min(max(r / G + 1 + s.lk - s.lq, (long)k_lo), (long)k_hi);
+    return min(max(r / G + 1 + s.lk - s.lq, k_lo), k_hi);
   };
-  for (long r0 = 0; r0 < R; r0 += 16) {
+  for (int r0 = 0; r0 < R; r0 += 16) {
     uint4 qa[2][J];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const long r = r0 + n + 8 * i;
-      const uint16_t* at = p.q + (s.q0 + r / G) * p.ldq + (head * G + r % G) * DH;
+      const int r = r0 + n + 8 * i;
+      const uint16_t* at = p.q + (long)(s.q0 + r / G) * p.ldq + (long)(head * G + r % G) * DH;
 #pragma unroll
       for (int j = 0; j < J; ++j) qa[i][j] = r < R ? __ldg(reinterpret_cast<const uint4*>(at + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
     }
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
     __syncthreads();
     for (int it = threadIdx.x; it < 16 * (DH / 8); it += F_TH) {
       const int lr = it / (DH / 8), col = it % (DH / 8) * 8;
-      const long r = r0 + lr;
+      const int r = r0 + lr;
       if (r >= R) continue;
       float top = -INFINITY, den = 0.f, v[8];
 #pragma unroll
@@ -313,21 +314,22 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
 namespace {
 constexpr int PT = 128;                    // rows and keys of a tile
 constexpr int PT_CHUNK = PT * 64 * 2;      // 128 rows x 64 columns: one 128-byte swizzle column
-constexpr int PT_STAGES = 2;               // of the K ring and of the V ring
-constexpr int PT_THREADS = 384;
-constexpr int PT_TMEM_COLS = 512;          // S_A [0,128) S_B [128,256) O_A [256,384) O_B [384,512)
-// registers a thread: 168 at launch; 128 * 72 + 256 * 216 = 384 * 168
-constexpr int PT_REGS_ISSUE = 72, PT_REGS_SOFTMAX = 216;
 constexpr int PT_OLD = 36;                 // floats a row in the output transpose
 constexpr int PT_OUT = 4 * 32 * PT_OLD * 4;  // bytes of a tile's
-template <int DH>
-struct PtSmem {
+// A CTA of NT tiles: threads, tensor memory (the scores' NT * 128 columns, then the outputs'), registers (168
+// a thread at launch with two tiles, 128 with one: 128 * 88 + 256 * 208 and 128 * 72 + 128 * 184 of them)
+// and shared memory (two CTAs on an SM with one tile).
+template <int DH, int NT>
+struct Pt {
+  static constexpr int THREADS = 128 + NT * 128, TMEM_COLS = NT * 256;
+  static constexpr int REGS_ISSUE = NT == 2 ? 88 : 72, REGS_SOFTMAX = NT == 2 ? 208 : 184;
+  static constexpr int STAGES = NT == 1 && DH == 128 ? 1 : 2;  // of the K ring and of the V ring
   static constexpr int TILE = DH / 64 * PT_CHUNK;
-  static constexpr int Q = 0, K = 2 * TILE, V = K + PT_STAGES * TILE, OUT = DH == 128 ? Q : V + PT_STAGES * TILE;
-  static constexpr int BAR = DH == 128 ? V + PT_STAGES * TILE : OUT + 2 * PT_OUT;
+  static constexpr int Q = 0, K = NT * TILE, V = K + STAGES * TILE, OUT = DH == 128 ? Q : V + STAGES * TILE;
+  static constexpr int BAR = DH == 128 ? V + STAGES * TILE : OUT + NT * PT_OUT;
   static constexpr int BYTES = BAR + 256 + 1024;
 };
-static_assert(PT_OUT <= PtSmem<128>::TILE, "a tile's output transpose fits its queries");
+static_assert(PT_OUT <= Pt<128, 1>::TILE, "a tile's output transpose fits its queries");
 
 // Shared-memory descriptor of a tile whose rows run along the contraction (V: a row a key), 128-byte
 // swizzle: 64-column chunks PT_CHUNK apart, groups of eight rows 1024 bytes apart.
@@ -335,11 +337,11 @@ BAG_DEV uint64_t sw128_desc_mn(uint32_t saddr) {
   return sw128_desc(saddr) & ~((uint64_t)0x3fff << 16) | (uint64_t)(PT_CHUNK >> 4) << 16;
 }
 
-// The sequence whose units hold slot `slot`: sequence i's slots are q_start[i] * group / unit_rows + i and on,
-// so that each has as many as its rows need and at most one more.  Called by a whole warp.
-BAG_DEV int sequence_of_slot(const PackedParams& p, long slot, long* first) {
+// The sequence whose units (of `per` tokens) hold slot `slot`: sequence i's slots are q_start[i] / per + i and
+// on, so that each has as many as its tokens need and at most one more.  Called by a whole warp.
+BAG_DEV int sequence_of_slot(const PackedParams& p, int per, int slot, int* first) {
   const int lane = threadIdx.x % 32;
-  auto start = [&](int i) { return (long)__ldg(p.q_start + i) * p.group / p.unit_rows + i; };
+  auto start = [&](int i) { return (int)((unsigned)max(__ldg(p.q_start + i), 0) / (unsigned)per) + i; };
   int lo = 0, n = p.seqs;
   while (n > 1) {
     const int step = (n + 31) / 32, i = lane * step;
@@ -351,24 +353,69 @@ BAG_DEV int sequence_of_slot(const PackedParams& p, long slot, long* first) {
   *first = start(lo);
   return lo;
 }
+
+// What a CTA works on.
+struct Unit {
+  int q0, tokens;        // its first query row, and how many (none: nothing to do)
+  int sees;              // own keys that its first token sees (below zero: none; of all with no mask)
+  int k0, lk;            // the sequence's keys
+  int fused;             // key tiles of the prefix, before them
+  int part, j0, most;    // the part of the keys, its first tile, and how many it may have
+  int direct;            // it is the only one: the output is final
+};
+BAG_DEV Unit unit_of(const PackedParams& p, int per, int at) {
+  Unit u{};
+  const int units1 = p.slots1 * p.parts1;
+  if (at < units1) {  // the prefix with the tokens of all sequences
+    const Span s = span_all(p);
+    const int slot = at / p.parts1;
+    u.part = at - slot * p.parts1;
+    u.q0 = s.q0 + slot * per;
+    u.tokens = max(min(s.lq - slot * per, per), 0);
+    u.most = p.chunk1 / PT;
+    u.j0 = u.part * u.most;
+    u.fused = (p.n_prefix + PT - 1) / PT;
+    return u;
+  }
+  at -= units1;
+  const int back = at / p.parts2, own = at - back * p.parts2;
+  const int slot = p.slots2 - 1 - back;  // later tokens see more keys: they go first
+  int first;
+  const Span s = span_of(p, sequence_of_slot(p, per, slot, &first));
+  if (slot < first || slot - first >= (s.lq + per - 1) / per) return u;
+  const int parts = own_parts(p, s.lk), t0 = (slot - first) * per;
+  if (own >= (p.parts1 ? parts : max(parts, 1))) return u;
+  u.q0 = s.q0 + t0;
+  u.tokens = min(s.lq - t0, per);
+  u.sees = p.causal ? t0 + 1 + s.lk - s.lq : s.lk;
+  u.k0 = s.k0, u.lk = s.lk;
+  u.fused = p.fused;
+  u.part = p.parts1 + own;
+  u.j0 = own * (p.chunk2 / PT);
+  u.most = own == p.parts2 - 1 ? 0x7fffffff : p.chunk2 / PT;
+  u.direct = p.parts1 == 0 && parts <= 1;
+  return u;
+}
 }  // namespace
 
-// One CTA takes one or two tiles of 128 rows (query token, head of the group: row r is token r / group) and
-// walks the tiles of 128 keys that the last of them sees:
-//   warp 0        TMA producer of K and V tiles into 2-stage rings of their own
+// One CTA takes NT tiles of up to 128 rows (row r: query token r / together, head r % together of those that share
+// the key head) and walks the tiles of 128 keys that the last of them sees:
+//   warp 0        TMA producer: the queries, then K and V tiles into rings of their own
 //   warp 1        MMA issuer, in turn between the tiles: S_A,0 S_B,0 | PV_A,j S_A,j+1 | PV_B,j S_B,j+1 | ...
-//                 It zeros the rows of V past a sequence's (or the prefix's) last key, up to the next 16,
-//                 where the products end: whatever lies there would meet weights of zero, and may be NaN
-//   warps 4..11   load the queries, then the softmax of tile A (4..7) and B (8..11), a row a thread, as in
-//                 the dense kernel: P goes back over the scores in 16 bits and enters the second product
-//                 from TMEM; O stays in TMEM and is rescaled only when the maximum has grown by more than 8
+//                 It zeros the rows of V past a sequence's (or the prefix's) last key: whatever lies there would
+//                 meet weights of zero, and may be NaN
+//   warp 2        finds the unit while warp 1 allocates tensor memory
+//   warps 4..     the softmax of tile A (4..7) and B (8..11), a row a thread, as in the dense kernel: P goes
+//                 back over the scores in 16 bits and enters the second product from TMEM; O stays in
+//                 TMEM and is rescaled only when the maximum has grown by more than 8
 // V is read as it lies, a row a key: as an operand whose rows run along the contraction.
-template <bool F16, int DH>
-__global__ void __launch_bounds__(PT_THREADS, 1)
-    attn_packed_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                       const __grid_constant__ CUtensorMap tmPK, const __grid_constant__ CUtensorMap tmPV,
-                       const PackedParams p) {
-  using M = PtSmem<DH>;
+template <bool F16, int DH, int NT>
+__global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
+    attn_packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                       const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmPK,
+                       const __grid_constant__ CUtensorMap tmPV, const PackedParams p) {
+  using M = Pt<DH, NT>;
+  constexpr int PT_STAGES = M::STAGES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -385,70 +432,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
   uint64_t* drain = bars + 15;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  Unit* found = reinterpret_cast<Unit*>(tmem_slot + 2);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-
-  grid_dep_sync();
-  // the unit: its rows, its part of the keys
-  const int G = p.group;
-  long unit = blockIdx.x;
-  const int head = (int)(unit % p.kv_heads);
-  unit /= p.kv_heads;
-  const long units1 = (long)p.slots1 * p.parts1;
-  const bool all_rows = unit < units1;  // the prefix with the rows of all sequences
-  Span s;
-  long r0;
-  int part, j0, most;  // index of the part; its first key tile, and how many it may have
-  int fused;           // key tiles of the prefix, before the sequence's own
-  if (all_rows) {
-    s = span_all(p);
-    part = (int)(unit % p.parts1);
-    r0 = unit / p.parts1 * p.unit_rows;
-    most = p.chunk1 / PT;
-    j0 = part * most;
-    fused = (p.n_prefix + PT - 1) / PT;
-    s.lk = 0;
-  } else {
-    unit -= units1;
-    part = (int)(unit % p.parts2);
-    const long slot = p.slots2 - 1 - unit / p.parts2;  // later rows see more keys: they go first
-    long first;
-    s = span_of(p, sequence_of_slot(p, slot, &first));
-    r0 = (slot - first) * p.unit_rows;
-    j0 = (int)((long)part * (p.chunk2 / PT));
-    most = part == p.parts2 - 1 ? 0x7fffffff : p.chunk2 / PT;
-    fused = p.fused;
-  }
-  const long R = (long)s.lq * G;
-  if (r0 < 0 || r0 >= R) return;
-  bool direct = false;
-  if (!all_rows) {
-    const int parts = own_parts(p, s.lk);
-    if (part >= (p.parts1 ? parts : max(parts, 1))) return;
-    direct = p.parts1 == 0 && parts <= 1;
-    part += p.parts1;
-  }
-  // own keys that row r sees
-  auto sees = [&](long r) {
-    return p.causal ? (int)min(max(r / G + 1 + s.lk - s.lq, 0L), (long)s.lk) : s.lk;
-  };
-  int n[2];  // key tiles of each tile of rows
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const long end = min(r0 + (x + 1) * PT, R);
-    n[x] = x * PT < p.unit_rows && end > r0 + x * PT
-               ? min(max(fused + (sees(end - 1) + PT - 1) / PT - j0, 0), most)
-               : 0;
-  }
-  const int nkb = max(n[0], n[1]);
-  // keys of tile j (of this part) that exist, and the tile's place
-  auto keys_of = [&](int j) {
-    const int t = j0 + j;
-    return t < fused ? p.n_prefix - t * PT : s.lk - (t - fused) * PT;
-  };
-  auto last_user = [&](int j) { return j < n[1] ? 1 : 0; };
+  const int per_head = p.slots1 * p.parts1 + p.slots2 * p.parts2;
+  const int hu = blockIdx.x / per_head;             // a head at a time, so that its keys stay in L2
+  const int head0 = hu * p.together, head = head0 / p.group;  // first query head, key head
 
   if (threadIdx.x == 0) {
-    mbar_init(q_full, 8);
+    mbar_init(q_full, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i, 1);
       mbar_init(k_empty + i, 1);
@@ -461,29 +452,59 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
-    tma_prefetch_desc(fused ? &tmPK : &tmK);
-    tma_prefetch_desc(fused ? &tmPV : &tmV);
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
   }
   __syncwarp();
   if (warp == 1) {
-    tmem_alloc(tmem_slot, PT_TMEM_COLS);
+    tmem_alloc(tmem_slot, M::TMEM_COLS);
     tmem_relinquish();
+  }
+  grid_dep_sync();
+  if (warp == 2) {
+    const Unit u = unit_of(p, NT * p.tokens, blockIdx.x - hu * per_head);
+    if (lane == 0) *found = u;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
+  const Unit& u = *found;
+  const int fused = u.fused, j0 = u.j0, lk = u.lk;
+  // own keys that the unit's token i sees
+  auto sees = [&](int i) { return p.causal ? min(max(u.sees + i, 0), lk) : lk; };
+  int n[2] = {0, 0};  // key tiles of each tile of rows
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    const int end = min((x + 1) * p.tokens, u.tokens);
+    if (end > x * p.tokens) n[x] = min(max(fused + (sees(end - 1) + PT - 1) / PT - j0, 0), u.most);
+  }
+  const int nkb = max(n[0], n[1]);
+  // keys of tile j (of this part) that exist
+  auto keys_of = [&](int j) {
+    const int t = j0 + j;
+    return t < fused ? p.n_prefix - t * PT : lk - (t - fused) * PT;
+  };
+  auto last_user = [&](int j) { return j < n[1] ? 1 : 0; };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PT_REGS_ISSUE));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(M::REGS_ISSUE));
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer ----------------
+      if (nkb > 0) {
+        const int rows = p.tokens * p.together, tiles = (n[0] > 0) + (n[1] > 0);
+        mbar_arrive_expect_tx(q_full, tiles * (DH / 64) * rows * 128);
+        for (int x = 0; x < NT; ++x)
+          for (int c = 0; c < DH / 64 && n[x] > 0; ++c)
+            tma_load_3d(sQ + x * M::TILE + c * PT_CHUNK, &tmQ, c * 64, head0, u.q0 + x * p.tokens, q_full);
+      }
       int kj = 0, vj = 0;  // tiles issued
       for (int j = 0; j < nkb; ++j) {
         const int st = j % PT_STAGES, t = j0 + j;
         const uint32_t ph = ((j / PT_STAGES) & 1) ^ 1;
         const bool pre = t < fused;
-        const int row = pre ? t * PT : s.k0 + (t - fused) * PT;
+        const int row = pre ? t * PT : u.k0 + (t - fused) * PT;
         const CUtensorMap *mk = pre ? &tmPK : &tmK, *mv = pre ? &tmPV : &tmV;
         if (!mbar_wait(k_empty + st, ph, abort_flag)) break;
         uint8_t* k = sK + st * M::TILE;
@@ -503,6 +524,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
           while (!mbar_try_wait(bar, ph) && global_ns() - t0 < kWaitLimitNs) {
           }
         };
+        landed(q_full, 0);
         for (int j = max(0, kj - PT_STAGES); j < kj; ++j) landed(k_full + j % PT_STAGES, (j / PT_STAGES) & 1);
         for (int j = max(0, vj - PT_STAGES); j < vj; ++j) landed(v_full + j % PT_STAGES, (j / PT_STAGES) & 1);
       }
@@ -513,10 +535,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
       const uint32_t q_addr = smem_u32(sQ), k_addr = smem_u32(sK), v_addr = smem_u32(sV);
       // K step kk of a tile: 64-column chunk kk / 4, 32 bytes per step inside it (16-byte units)
       auto koff = [](int kk) { return (uint64_t)(((kk >> 2) * PT_CHUNK + (kk & 3) * 32) >> 4); };
-      auto issue_s = [&](int x, int j) {
+      // S of tile x and key tile j; release: the tile's K is no longer needed
+      auto issue_s = [&](int x, int j, bool release) {
         const uint64_t qd = sw128_desc(q_addr + x * M::TILE);
         const uint64_t kd = sw128_desc(k_addr + (j % PT_STAGES) * M::TILE);
-        const bool release = x == last_user(j);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < DH / 16; ++kk)
@@ -526,21 +548,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
         }
         __syncwarp();
       };
-      auto issue_pv = [&](int x, int j) {
+      // release: the tile's V is no longer needed; done: no other product follows for tile x
+      auto issue_pv = [&](int x, int j, bool release, bool done) {
         const uint64_t vd = sw128_desc_mn(v_addr + (j % PT_STAGES) * M::TILE);
-        const int steps = min(PT, keys_of(j) + 15) / 16;
-        const bool release = x == last_user(j), done = j == n[x] - 1;
         if (elect_one()) {
-          if (steps == PT / 16) {
 #pragma unroll
-            for (int kk = 0; kk < PT / 16; ++kk)
-              mma_bf16_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
-                          (j > 0 || kk > 0) ? 1u : 0u);
-          } else {
-            for (int kk = 0; kk < steps; ++kk)
-              mma_bf16_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
-                          (j > 0 || kk > 0) ? 1u : 0u);
-          }
+          for (int kk = 0; kk < PT / 16; ++kk)
+            mma_bf16_ts(tmem + NT * 128 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                        (j > 0 || kk > 0) ? 1u : 0u);
           if (release) mma_commit(v_empty + j % PT_STAGES);
           if (done) mma_commit(o_done + x);
         }
@@ -551,35 +566,53 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
         tc_fence_after();
         return w;
       };
-      bool ok = nkb > 0 && wait(q_full, 0) && wait(k_full, 0);
-      if (ok) {
-        if (n[0] > 0) issue_s(0, 0);
-        if (n[1] > 0) issue_s(1, 0);
-      }
-      for (int j = 0; j < nkb && ok; ++j) {
-        const int s1 = (j + 1) % PT_STAGES;
-        ok = wait(v_full + j % PT_STAGES, (j / PT_STAGES) & 1);
-        const int from = keys_of(j), to = (from + 15) / 16 * 16;
-        if (ok && from < PT) {  // the rows past the last key, up to where the products end
-          for (int i = lane; i < (to - from) * (DH / 8); i += 32) {
-            const int row = from + i / (DH / 8), piece = i % (DH / 8);
+      auto k_there = [&](int j) { return wait(k_full + j % PT_STAGES, (j / PT_STAGES) & 1); };
+      // V of tile j, zeros past its last key: only the prefix's last tile and the sequence's can end early
+      const int ends0 = fused - 1 - j0, ends1 = fused + (lk + PT - 1) / PT - 1 - j0;
+      auto v_there = [&](int j) {
+        if (!wait(v_full + j % PT_STAGES, (j / PT_STAGES) & 1)) return false;
+        if (j == ends0 || j == ends1) {
+          for (int i = keys_of(j) * (DH / 8) + lane; i < PT * (DH / 8); i += 32) {
+            const int row = i / (DH / 8), piece = i % (DH / 8);
             *reinterpret_cast<uint4*>(sV + (j % PT_STAGES) * M::TILE + piece / 8 * PT_CHUNK + row * 128 + piece % 8 * 16) =
                 make_uint4(0u, 0u, 0u, 0u);
           }
           fence_proxy_async_smem();
           __syncwarp();
         }
+        return true;
+      };
+      const int both = (NT == 2 ? min(n[0], n[1]) : n[0]) - 1;  // steps after which all tiles go on
+      bool ok = nkb > 0 && wait(q_full, 0) && k_there(0);
+      if (ok) {
+        if (n[0] > 0) issue_s(0, 0, n[1] == 0);
+        if (NT == 2 && n[1] > 0) issue_s(1, 0, true);
+      }
+      int j = 0;
+      for (; j < both && ok; ++j) {
+        // PV_j of a tile, then its S_{j+1} into the columns P_j came from (in issue order)
+        if (!(ok = v_there(j) && wait(p_full, j & 1))) break;
+        issue_pv(0, j, NT == 1, false);
+        if (!(ok = k_there(j + 1))) break;
+        issue_s(0, j + 1, NT == 1);
+        if constexpr (NT == 2) {
+          if (!(ok = wait(p_full + 1, j & 1))) break;
+          issue_pv(1, j, true, false);
+          issue_s(1, j + 1, true);
+        }
+      }
+      for (; j < nkb && ok; ++j) {  // a tile ends
+        if (!(ok = v_there(j))) break;
         bool next = false;  // the next K tile is there
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < NT; ++x) {
           if (!ok || j >= n[x]) continue;
-          // PV_j of this tile, then its S_{j+1} into the columns P_j came from (in issue order)
           if (!(ok = wait(p_full + x, j & 1))) break;
-          issue_pv(x, j);
+          issue_pv(x, j, x == last_user(j), j == n[x] - 1);
           if (j + 1 < n[x]) {
-            if (!next && !(ok = wait(k_full + s1, ((j + 1) / PT_STAGES) & 1))) break;
+            if (!next && !(ok = k_there(j + 1))) break;
             next = true;
-            issue_s(x, j + 1);
+            issue_s(x, j + 1, x == last_user(j + 1));
           }
         }
       }
@@ -592,34 +625,25 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
     }
     __syncwarp();
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PT_REGS_SOFTMAX));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(M::REGS_SOFTMAX));
     // ---------------- softmax warpgroups (warps 4..7: tile A, 8..11: tile B) ----------------
-    const int x = (warp - 4) >> 2;
-    const int quad = warp & 3;
-    if (n[x] > 0) {  // the tile's queries, rows past the last as zeros
-      constexpr int LR = DH / 8;  // lanes of a row
-      const int t = threadIdx.x - 128 - x * 128, piece = t % LR;
-      uint8_t* q = sQ + x * M::TILE + piece / 8 * PT_CHUNK;
-      const uint16_t* src = p.q + (long)head * G * DH + piece * 8;
-#pragma unroll 8
-      for (int i = 0; i < LR; ++i) {
-        const int row = i * (128 / LR) + t / LR;
-        const long r = r0 + x * PT + row;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (r < R) v = __ldg(reinterpret_cast<const uint4*>(src + (s.q0 + r / G) * p.ldq + r % G * DH));
-        *reinterpret_cast<uint4*>(q + row * 128 + ((piece % 8) ^ (row & 7)) * 16) = v;
-      }
-      fence_proxy_async_smem();
-    }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(q_full);
+    const int x = NT == 2 ? (warp - 4) >> 2 : 0;
+    const int quad = warp & 3, tiles = x ? n[1] : n[0];
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t s_addr = tmem + lane_base + x * 128;
-    const uint32_t o_addr = tmem + lane_base + 256 + x * 128;
-    const int own = sees(min(r0 + x * PT + quad * 32 + lane, R - 1));
+    const uint32_t o_addr = tmem + lane_base + NT * 128 + x * 128;
+    // the token (of the unit) and head of row i of the tile; none: past the last
+    auto token = [&](int i, int* g) {
+      const int t = (unsigned)i / (unsigned)p.together;
+      *g = head0 + i - t * p.together;
+      return t < p.tokens && x * p.tokens + t < u.tokens ? x * p.tokens + t : -1;
+    };
+    int h;
+    const int mine = token(quad * 32 + lane, &h);  // the thread's row
+    const int own = sees(mine < 0 ? u.tokens - 1 : mine);
     float m_use = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int j = 0; j < n[x]; ++j) {
+    for (int j = 0; j < tiles; ++j) {
       const bool w = mbar_wait(s_full + x, j & 1, abort_flag);
       if (!__all_sync(0xffffffffu, w)) {
         ok = false;
@@ -687,20 +711,17 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(p_full + x);
     }
-    if (ok && n[x] > 0) ok = __all_sync(0xffffffffu, mbar_wait(o_done + x, 0, abort_flag));
+    if (ok && tiles > 0) ok = __all_sync(0xffffffffu, mbar_wait(o_done + x, 0, abort_flag));
     tc_fence_after();
-    if (ok && r0 + x * PT < R && x * PT < p.unit_rows) {
+    if (ok && x * p.tokens < u.tokens) {
       const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
-      const float f = direct ? (any ? 1.f / l : 0.f) : 1.f;
-      {  // the row's maximum and sum
-        const long r = r0 + x * PT + quad * 32 + lane;
-        if (r < R) {
-          const long tok = s.q0 + r / G, h = (long)head * G + r % G;
-          if (!direct)
-            p.part_ml[((long)part * p.nq + tok) * p.heads + h] = make_float2(any ? m_use : -INFINITY, l);
-          else if (p.lse)
-            p.lse[tok * p.heads + h] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
-        }
+      const float f = u.direct ? (any ? 1.f / l : 0.f) : 1.f;
+      if (mine >= 0) {  // the row's maximum and sum
+        const long at = (long)(u.q0 + mine) * p.heads + h;
+        if (!u.direct)
+          p.part_ml[(long)u.part * p.nq * p.heads + at] = make_float2(any ? m_use : -INFINITY, l);
+        else if (p.lse)
+          p.lse[at] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
       // through shared memory (where a tile's queries were, which no product reads any more): four lanes
       // hold 32 consecutive columns of a row, so a store covers eight rows' runs
@@ -708,35 +729,35 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
       const int lr = lane >> 2, c8 = (lane & 3) * 8;
       long at[4];  // of rows lr + 8 u: element of o or of part_o
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const long r = r0 + x * PT + quad * 32 + lr + 8 * u;
-        const long tok = s.q0 + r / G, h = (long)head * G + r % G;
-        at[u] = r >= R ? -1 : (direct ? tok * p.ldo + h * DH : (((long)part * p.nq + tok) * p.heads + h) * DH) + c8;
+      for (int i = 0; i < 4; ++i) {
+        const int t = token(quad * 32 + lr + 8 * i, &h);
+        const long row = u.q0 + t;
+        at[i] = t < 0 ? -1 : (u.direct ? row * p.ldo + h * DH : (((long)u.part * p.nq + row) * p.heads + h) * DH) + c8;
       }
 #pragma unroll 1
       for (int c = 0; c < DH; c += 32) {
         float o[32];
-        if (n[x] > 0) tmem_ld32(o_addr + c, o);
+        if (tiles > 0) tmem_ld32(o_addr + c, o);
 #pragma unroll
         for (int i = 0; i < 32; i += 4)
           *reinterpret_cast<float4*>(buf + lane * PT_OLD + i) =
-              any && n[x] > 0 ? make_float4(o[i] * f, o[i + 1] * f, o[i + 2] * f, o[i + 3] * f)
+              any && tiles > 0 ? make_float4(o[i] * f, o[i + 1] * f, o[i + 2] * f, o[i + 3] * f)
                               : make_float4(0.f, 0.f, 0.f, 0.f);
         __syncwarp();
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float4* v = reinterpret_cast<const float4*>(buf + (8 * u + lr) * PT_OLD + c8);
+        for (int i = 0; i < 4; ++i) {
+          const float4* v = reinterpret_cast<const float4*>(buf + (8 * i + lr) * PT_OLD + c8);
           const float4 a = v[0], b = v[1];
-          if (at[u] < 0) continue;
-          if (direct) {
+          if (at[i] < 0) continue;
+          if (u.direct) {
             uint4 w;
             w.x = pack16<F16>(a.x, a.y);
             w.y = pack16<F16>(a.z, a.w);
             w.z = pack16<F16>(b.x, b.y);
             w.w = pack16<F16>(b.z, b.w);
-            *reinterpret_cast<uint4*>(p.o + at[u] + c) = w;
+            *reinterpret_cast<uint4*>(p.o + at[i] + c) = w;
           } else {
-            float4* d = reinterpret_cast<float4*>(p.part_o + at[u] + c);
+            float4* d = reinterpret_cast<float4*>(p.part_o + at[i] + c);
             d[0] = a;
             d[1] = b;
           }
@@ -750,7 +771,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1)
   if (threadIdx.x == 0 && *abort_flag && p.err) atomicOr(p.err, 1);
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, PT_TMEM_COLS);
+    tmem_dealloc(tmem, M::TMEM_COLS);
   }
 }
 
@@ -830,7 +851,7 @@ namespace {
 // The form of a call.  few: own keys by attn_few_kernel; rows: of a unit of the tensor-core kernel.
 struct Plan {
   int parts1, parts2, chunk1, chunk2;
-  int few, fused, rows;
+  int few, fused, rows, together;
 };
 
 size_t part_bytes(const PackedArgs& a) { return (size_t)a.nq * (size_t)a.heads * ((size_t)a.dh * 4 + 8); }
@@ -844,6 +865,11 @@ Plan plan_of(const PackedArgs& a, long most) {
   const long max_k = std::min(std::max(a.max_k, 1L), std::max(a.k_rows, 1L));
   const long max_q = std::max(1L, std::min(a.max_q, a.nq)), rows = a.nq * G;
   t.few = max_q * G <= 16;
+  // heads of a group that share a tile: as many as leave few of its rows empty, or whose rows of a
+  // sequence fit one (more units of a key head would read its keys again)
+  t.together = 1;
+  for (int g = 2; g <= G && g <= PT; ++g)
+    if (G % g == 0 && (PT / g * g >= PT - PT / 10 || max_q * g <= PT)) t.together = g;
   // units of 256 rows where there are enough of them
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
   t.rows = units(256) * 2 > sms ? 256 : 128;
@@ -893,17 +919,20 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   p.parts1 = t.parts1, p.parts2 = t.parts2, p.chunk1 = t.chunk1, p.chunk2 = t.chunk2, p.fused = t.fused;
   p.part_o = reinterpret_cast<float*>(a.work);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)(t.parts1 + t.parts2) * a.nq * a.heads * a.dh);
-  const long rows = a.nq * p.group;
-  p.unit_rows = t.rows;
-  const long slots1 = t.parts1 ? cdiv(rows, t.rows) : 0, slots2 = t.few ? 0 : rows / t.rows + a.seqs;
+  p.together = t.together, p.tokens = PT / t.together;
+  const long per = p.tokens * (t.rows / PT), groups = a.heads / t.together;
+  const long slots1 = t.parts1 ? cdiv(a.nq, per) : 0, slots2 = t.few ? 0 : a.nq / per + a.seqs;
   p.err = a.err;
-  const long tiles = (slots1 * t.parts1 + slots2 * t.parts2) * a.kv_heads;
+  const long tiles = (slots1 * t.parts1 + slots2 * t.parts2) * groups;
   const long few = t.few ? a.seqs * t.parts2 * a.kv_heads : 0, joins = a.nq * a.heads;
   if (tiles > 0x7fffffffL || few > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
     return cudaErrorInvalidConfiguration;
   p.slots1 = (int)slots1, p.slots2 = (int)slots2;
-  CUtensorMap tk, tv, tpk, tpv;
+  CUtensorMap tq, tk, tv, tpk, tpv;
   if (tiles) {
+    if (encode_tmap_3d_16(&tq, a.q, (uint64_t)a.dh, (uint64_t)a.heads, (uint64_t)a.nq, (uint64_t)a.dh * 2, (uint64_t)a.ldq * 2,
+                          (uint32_t)t.together, (uint32_t)p.tokens))
+      return cudaErrorInvalidValue;
     const uint64_t width = (uint64_t)a.kv_heads * a.dh;
     // a tensor without rows is never read: another one stands for its map
     auto map = [&](CUtensorMap* m, const void* x, long ld, long n) {
@@ -918,22 +947,24 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
       tpk = tk, tpv = tv;
     }
   }
-  auto launch = [&](auto few_kernel, auto kernel, auto join, int few_bytes, int bytes) {
+  auto launch = [&](auto f16, auto width) {
+    constexpr bool F16 = decltype(f16)::value;
+    constexpr int DH = decltype(width)::value;
     cudaError_t e = cudaSuccess;
-    if (few) e = launch_kernel(few_kernel, (unsigned)few, F_TH, few_bytes, s, p);
-    if (tiles && e == cudaSuccess) e = launch_kernel(kernel, (unsigned)tiles, PT_THREADS, bytes, s, tk, tv, tpk, tpv, p);
-    if (e == cudaSuccess && t.parts1 + t.parts2 > 1) e = launch_kernel(join, (unsigned)joins, JN_TH, 0, s, p);
+    if (few) e = launch_kernel(attn_few_kernel<F16, DH>, (unsigned)few, F_TH, few_smem<DH>(), s, p);
+    if (tiles && e == cudaSuccess)
+      e = t.rows == 256 ? launch_kernel(attn_packed_kernel<F16, DH, 2>, (unsigned)tiles, Pt<DH, 2>::THREADS,
+                                        Pt<DH, 2>::BYTES, s, tq, tk, tv, tpk, tpv, p)
+                        : launch_kernel(attn_packed_kernel<F16, DH, 1>, (unsigned)tiles, Pt<DH, 1>::THREADS,
+                                        Pt<DH, 1>::BYTES, s, tq, tk, tv, tpk, tpv, p);
+    if (e == cudaSuccess && t.parts1 + t.parts2 > 1)
+      e = launch_kernel(attn_join_kernel<F16, DH>, (unsigned)joins, JN_TH, 0, s, p);
     return e;
   };
-  if (a.dh == 128)
-    return a.f16 ? launch(attn_few_kernel<true, 128>, attn_packed_kernel<true, 128>, attn_join_kernel<true, 128>,
-                          few_smem<128>(), PtSmem<128>::BYTES)
-                 : launch(attn_few_kernel<false, 128>, attn_packed_kernel<false, 128>, attn_join_kernel<false, 128>,
-                          few_smem<128>(), PtSmem<128>::BYTES);
-  return a.f16 ? launch(attn_few_kernel<true, 64>, attn_packed_kernel<true, 64>, attn_join_kernel<true, 64>,
-                        few_smem<64>(), PtSmem<64>::BYTES)
-               : launch(attn_few_kernel<false, 64>, attn_packed_kernel<false, 64>, attn_join_kernel<false, 64>,
-                        few_smem<64>(), PtSmem<64>::BYTES);
+  using Wide = std::integral_constant<int, 128>;
+  using Narrow = std::integral_constant<int, 64>;
+  if (a.dh == 128) return a.f16 ? launch(std::true_type{}, Wide{}) : launch(std::false_type{}, Wide{});
+  return a.f16 ? launch(std::true_type{}, Narrow{}) : launch(std::false_type{}, Narrow{});
 }
 
 cudaError_t attention_packed_init() {
@@ -945,10 +976,14 @@ cudaError_t attention_packed_init() {
   smem(attn_few_kernel<false, 128>, few_smem<128>());
   smem(attn_few_kernel<true, 64>, few_smem<64>());
   smem(attn_few_kernel<false, 64>, few_smem<64>());
-  smem(attn_packed_kernel<true, 128>, PtSmem<128>::BYTES);
-  smem(attn_packed_kernel<false, 128>, PtSmem<128>::BYTES);
-  smem(attn_packed_kernel<true, 64>, PtSmem<64>::BYTES);
-  smem(attn_packed_kernel<false, 64>, PtSmem<64>::BYTES);
+  smem(attn_packed_kernel<true, 128, 1>, Pt<128, 1>::BYTES);
+  smem(attn_packed_kernel<false, 128, 1>, Pt<128, 1>::BYTES);
+  smem(attn_packed_kernel<true, 64, 1>, Pt<64, 1>::BYTES);
+  smem(attn_packed_kernel<false, 64, 1>, Pt<64, 1>::BYTES);
+  smem(attn_packed_kernel<true, 128, 2>, Pt<128, 2>::BYTES);
+  smem(attn_packed_kernel<false, 128, 2>, Pt<128, 2>::BYTES);
+  smem(attn_packed_kernel<true, 64, 2>, Pt<64, 2>::BYTES);
+  smem(attn_packed_kernel<false, 64, 2>, Pt<64, 2>::BYTES);
   return r;
 }
 

@@ -2095,6 +2095,8 @@ static bag_status check_packed(bag_ctx* ctx, long nq, int heads, int kv_heads, i
   if (nq < 0 || nq > kMaxRows || heads <= 0 || heads > kMaxHeads || kv_heads <= 0 || heads % kv_heads || seqs < 0 ||
       seqs > kMaxRows || max_q < 0 || max_k < 0 || n_prefix < 0 || n_prefix > kMaxRows)
     return fail(ctx, BAG_EINVAL, "bad shape of packed sequences");
+  if (nq > kMaxRows / (heads / kv_heads))
+    return fail(ctx, BAG_EUNSUPPORTED, "queries times the heads that share a key head must fit 31 bits");
   if (dh != 64 && dh != 128) return fail(ctx, BAG_EUNSUPPORTED, "attention of packed sequences takes heads of 64 or 128");
   return BAG_OK;
 }

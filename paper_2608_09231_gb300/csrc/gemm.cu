@@ -66,6 +66,19 @@ int encode_tmap_2d_bytes(CUtensorMap* map, int size, const void* base, uint64_t 
   return encode_tmap_2d(map, type, base, inner, outer, row_stride_bytes, box_inner, box_outer);
 }
 
+int encode_tmap_3d_16(CUtensorMap* map, const void* base, uint64_t cols, uint64_t mid, uint64_t outer,
+                      uint64_t mid_stride_bytes, uint64_t outer_stride_bytes, uint32_t box_mid, uint32_t box_outer) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return -1;
+  cuuint64_t dims[3] = {cols, mid, outer}, strides[2] = {mid_stride_bytes, outer_stride_bytes};
+  cuuint32_t box[3] = {64, box_mid, box_outer}, estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? 0
+             : -1;
+}
+
 static int num_sms() {
   static int n = 0;
   if (n == 0) {

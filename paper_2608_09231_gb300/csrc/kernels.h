@@ -373,4 +373,8 @@ int encode_tmap_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner, uint
 int encode_tmap_2d_bytes(CUtensorMap* map, int size, const void* base, uint64_t inner, uint64_t outer,
                          uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer);
 
+// 16-bit elements of a [outer][mid][cols] tensor, boxes of 64 columns x box_mid x box_outer, 128-byte swizzle
+int encode_tmap_3d_16(CUtensorMap* map, const void* base, uint64_t cols, uint64_t mid, uint64_t outer,
+                      uint64_t mid_stride_bytes, uint64_t outer_stride_bytes, uint32_t box_mid, uint32_t box_outer);
+
 }  // namespace bag
