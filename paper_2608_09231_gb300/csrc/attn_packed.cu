@@ -314,8 +314,8 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
 namespace {
 constexpr int PT = 128;                    // rows and keys of a tile
 constexpr int PT_CHUNK = PT * 64 * 2;      // 128 rows x 64 columns: one 128-byte swizzle column
-constexpr int PT_OLD = 36;                 // floats a row in the output transpose
-constexpr int PT_OUT = 4 * 32 * PT_OLD * 4;  // bytes of a tile's
+constexpr int PT_LD = 144;                 // bytes a row in the output transpose (16 against bank conflicts)
+constexpr int PT_OUT = 4 * 32 * PT_LD;     // bytes of a tile's
 // A CTA of NT tiles: threads, tensor memory (the scores' NT * 128 columns, then the outputs'), registers (168
 // a thread at launch with two tiles, 128 with one: 128 * 88 + 256 * 208 and 128 * 72 + 128 * 184 of them)
 // and shared memory (two CTAs on an SM with one tile).
@@ -326,7 +326,8 @@ struct Pt {
   static constexpr int STAGES = NT == 1 && DH == 128 ? 1 : 2;  // of the K ring and of the V ring
   static constexpr int TILE = DH / 64 * PT_CHUNK;
   static constexpr int Q = 0, K = NT * TILE, V = K + STAGES * TILE, OUT = DH == 128 ? Q : V + STAGES * TILE;
-  static constexpr int BAR = DH == 128 ? V + STAGES * TILE : OUT + NT * PT_OUT;
+  static constexpr int ROWS = DH == 128 ? V + STAGES * TILE : OUT + NT * PT_OUT;  // where a row's output goes
+  static constexpr int BAR = ROWS + NT * PT * 8;
   static constexpr int BYTES = BAR + 256 + 1024;
 };
 static_assert(PT_OUT <= Pt<128, 1>::TILE, "a tile's output transpose fits its queries");
@@ -337,21 +338,30 @@ BAG_DEV uint64_t sw128_desc_mn(uint32_t saddr) {
   return sw128_desc(saddr) & ~((uint64_t)0x3fff << 16) | (uint64_t)(PT_CHUNK >> 4) << 16;
 }
 
-// The sequence whose units (of `per` tokens) hold slot `slot`: sequence i's slots are q_start[i] / per + i and
-// on, so that each has as many as its tokens need and at most one more.  Called by a whole warp.
-BAG_DEV int sequence_of_slot(const PackedParams& p, int per, int slot, int* first) {
+// The sequence whose units (of `per` tokens) hold slot `slot`, and its first slot: sequence i's slots are
+// q_start[i] / per + i and on, so that each has as many as its tokens need and at most one more.  Called by a
+// whole warp; up to 32 sequences take one round of loads.
+BAG_DEV Span span_of_slot(const PackedParams& p, int per, int slot, int* first) {
   const int lane = threadIdx.x % 32;
   auto start = [&](int i) { return (int)((unsigned)max(__ldg(p.q_start + i), 0) / (unsigned)per) + i; };
   int lo = 0, n = p.seqs;
-  while (n > 1) {
+  while (n > 32) {
     const int step = (n + 31) / 32, i = lane * step;
     const uint32_t at = __ballot_sync(0xffffffffu, i < n && start(lo + i) <= slot);
     const int skip = max(__popc(at) - 1, 0) * step;
     lo += skip;
     n = min(step, n - skip);
   }
-  *first = start(lo);
-  return lo;
+  Span s = span_of(p, lo + min(lane, n - 1));
+  const int mine = start(lo + min(lane, n - 1));
+  const uint32_t at = __ballot_sync(0xffffffffu, lane < n && mine <= slot);
+  const int src = max(__popc(at) - 1, 0);
+  *first = __shfl_sync(0xffffffffu, mine, src);
+  s.q0 = __shfl_sync(0xffffffffu, s.q0, src);
+  s.lq = __shfl_sync(0xffffffffu, s.lq, src);
+  s.k0 = __shfl_sync(0xffffffffu, s.k0, src);
+  s.lk = __shfl_sync(0xffffffffu, s.lk, src);
+  return s;
 }
 
 // What a CTA works on.
@@ -381,7 +391,7 @@ BAG_DEV Unit unit_of(const PackedParams& p, int per, int at) {
   const int back = at / p.parts2, own = at - back * p.parts2;
   const int slot = p.slots2 - 1 - back;  // later tokens see more keys: they go first
   int first;
-  const Span s = span_of(p, sequence_of_slot(p, per, slot, &first));
+  const Span s = span_of_slot(p, per, slot, &first);
   if (slot < first || slot - first >= (s.lq + per - 1) / per) return u;
   const int parts = own_parts(p, s.lk), t0 = (slot - first) * per;
   if (own >= (p.parts1 ? parts : max(parts, 1))) return u;
@@ -632,15 +642,20 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t s_addr = tmem + lane_base + x * 128;
     const uint32_t o_addr = tmem + lane_base + NT * 128 + x * 128;
-    // the token (of the unit) and head of row i of the tile; none: past the last
-    auto token = [&](int i, int* g) {
-      const int t = (unsigned)i / (unsigned)p.together;
-      *g = head0 + i - t * p.together;
-      return t < p.tokens && x * p.tokens + t < u.tokens ? x * p.tokens + t : -1;
-    };
-    int h;
-    const int mine = token(quad * 32 + lane, &h);  // the thread's row
+    // the thread's row: its token of the unit (none: -1), and where its output goes, for the warp's lanes that
+    // store it (worked out here, beside the loads of the first tiles)
+    const int row = quad * 32 + lane, of = (unsigned)row / (unsigned)p.together;
+    const int mine = of < p.tokens && x * p.tokens + of < u.tokens ? x * p.tokens + of : -1;
     const int own = sees(mine < 0 ? u.tokens - 1 : mine);
+    const int h = head0 + row - of * p.together;
+    long* at = reinterpret_cast<long*>(smem + M::ROWS) + x * PT + quad * 32;
+    at[lane] = mine < 0 ? -1
+                        : (u.direct ? (u.q0 + mine) * p.ldo + h * DH
+                                    : (((long)u.part * p.nq + u.q0 + mine) * p.heads + h) * DH);
+    // tiles with keys that a row of the warp does not see: the prefix's last one, where it is not full, and from
+    // the first one on that ends behind the warp's first row's keys
+    const int cut0 = p.n_prefix % PT ? fused - 1 : -1;
+    const int cut1 = fused + (int)__reduce_min_sync(0xffffffffu, (unsigned)own) / PT;
     float m_use = -INFINITY, l = 0.f;
     bool ok = true;
     for (int j = 0; j < tiles; ++j) {
@@ -651,13 +666,13 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
       }
       tc_fence_after();
       const int t = j0 + j;
-      const int kvalid = t < fused ? p.n_prefix - t * PT : own - (t - fused) * PT;  // keys of the tile that the row sees
       // the whole S row in registers: four loads, one wait
       uint32_t r[PT];
 #pragma unroll
       for (int c = 0; c < PT / 32; ++c) tmem_ld32_nowait(s_addr + c * 32, r + c * 32);
       tmem_ld_wait();
-      if (__any_sync(0xffffffffu, kvalid < PT)) {
+      if (t == cut0 || t >= cut1) {
+        const int kvalid = t < fused ? p.n_prefix - t * PT : own - (t - fused) * PT;  // keys that the row sees
 #pragma unroll
         for (int i = 0; i < PT; ++i)
           if (i >= kvalid) r[i] = __float_as_uint(-INFINITY);
@@ -715,54 +730,66 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     tc_fence_after();
     if (ok && x * p.tokens < u.tokens) {
       const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
-      const float f = u.direct ? (any ? 1.f / l : 0.f) : 1.f;
+      const float f = 1.f / l;
       if (mine >= 0) {  // the row's maximum and sum
-        const long at = (long)(u.q0 + mine) * p.heads + h;
+        const long r = (long)(u.q0 + mine) * p.heads + h;
         if (!u.direct)
-          p.part_ml[(long)u.part * p.nq * p.heads + at] = make_float2(any ? m_use : -INFINITY, l);
+          p.part_ml[(long)u.part * p.nq * p.heads + r] = make_float2(any ? m_use : -INFINITY, l);
         else if (p.lse)
-          p.lse[at] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
+          p.lse[r] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
-      // through shared memory (where a tile's queries were, which no product reads any more): four lanes
-      // hold 32 consecutive columns of a row, so a store covers eight rows' runs
-      float* buf = reinterpret_cast<float*>(smem + M::OUT + x * (DH == 128 ? M::TILE : PT_OUT)) + quad * 32 * PT_OLD;
-      const int lr = lane >> 2, c8 = (lane & 3) * 8;
-      long at[4];  // of rows lr + 8 u: element of o or of part_o
+      // through shared memory (where a tile's queries were, which no product reads any more), so that a store
+      // covers whole runs of a few rows: 64 columns in 16 bits, or 32 of a part in fp32, at a time
+      uint8_t* buf = smem + M::OUT + x * (DH == 128 ? M::TILE : PT_OUT) + quad * 32 * PT_LD;
+      long to[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = token(quad * 32 + lr + 8 * i, &h);
-        const long row = u.q0 + t;
-        at[i] = t < 0 ? -1 : (u.direct ? row * p.ldo + h * DH : (((long)u.part * p.nq + row) * p.heads + h) * DH) + c8;
-      }
+      for (int i = 0; i < 8; ++i) to[i] = at[4 * i + (lane >> 3)];
+      const bool seen = any && tiles > 0;
+      if (u.direct) {
 #pragma unroll 1
-      for (int c = 0; c < DH; c += 32) {
-        float o[32];
-        if (tiles > 0) tmem_ld32(o_addr + c, o);
-#pragma unroll
-        for (int i = 0; i < 32; i += 4)
-          *reinterpret_cast<float4*>(buf + lane * PT_OLD + i) =
-              any && tiles > 0 ? make_float4(o[i] * f, o[i + 1] * f, o[i + 2] * f, o[i + 3] * f)
-                              : make_float4(0.f, 0.f, 0.f, 0.f);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4* v = reinterpret_cast<const float4*>(buf + (8 * i + lr) * PT_OLD + c8);
-          const float4 a = v[0], b = v[1];
-          if (at[i] < 0) continue;
-          if (u.direct) {
-            uint4 w;
-            w.x = pack16<F16>(a.x, a.y);
-            w.y = pack16<F16>(a.z, a.w);
-            w.z = pack16<F16>(b.x, b.y);
-            w.w = pack16<F16>(b.z, b.w);
-            *reinterpret_cast<uint4*>(p.o + at[i] + c) = w;
-          } else {
-            float4* d = reinterpret_cast<float4*>(p.part_o + at[i] + c);
-            d[0] = a;
-            d[1] = b;
+        for (int c = 0; c < DH; c += 64) {
+          uint32_t o[64];
+          if (tiles > 0) {
+            tmem_ld32_nowait(o_addr + c, o);
+            tmem_ld32_nowait(o_addr + c + 32, o + 32);
+            tmem_ld_wait();
           }
+#pragma unroll
+          for (int i = 0; i < 64; i += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = seen ? pack16<F16>(__uint_as_float(o[i + 2 * e]) * f, __uint_as_float(o[i + 2 * e + 1]) * f) : 0u;
+            *reinterpret_cast<uint4*>(buf + lane * PT_LD + i * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(buf + (4 * i + (lane >> 3)) * PT_LD + (lane & 7) * 16);
+            if (to[i] >= 0) *reinterpret_cast<uint4*>(p.o + to[i] + c + (lane & 7) * 8) = v;
+          }
+          __syncwarp();
         }
-        __syncwarp();
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < DH; c += 32) {
+          uint32_t o[32];
+          if (tiles > 0) {
+            tmem_ld32_nowait(o_addr + c, o);
+            tmem_ld_wait();
+          }
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            *reinterpret_cast<uint4*>(buf + lane * PT_LD + i * 4) =
+                seen ? make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_uint4(0u, 0u, 0u, 0u);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(buf + (4 * i + (lane >> 3)) * PT_LD + (lane & 7) * 16);
+            if (to[i] >= 0) *reinterpret_cast<uint4*>(p.part_o + to[i] + c + (lane & 7) * 4) = v;
+          }
+          __syncwarp();
+        }
       }
     }
   }
@@ -873,6 +900,7 @@ Plan plan_of(const PackedArgs& a, long most) {
   // units of 256 rows where there are enough of them
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
   t.rows = units(256) * 2 > sms ? 256 : 128;
+  if (const char* e = std::getenv("X_ROWS")) t.rows = std::atoi(e);
   const bool together = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
   const long per = t.few ? F_KEYS : PT;  // keys that a part has a multiple of
   auto chunk = [](long keys, long parts, long n) { return (int)(cdiv(cdiv(keys, parts), n) * n); };
