@@ -36,6 +36,11 @@ struct PackedParams {
   // tokens of all sequences and of each
   int together, tokens, slots1, slots2;
   int* err;
+  // few-row kernel: whether a unit's keys may be shared among CTAs, their sums (see attn_few_kernel)
+  int few, split;
+  float* piece_o;      // [CTA][2][16][dh]
+  float2* piece_ml;    // [CTA][2][16]
+  long* place;         // [0]: tiles of a CTA, [1 + sequence]: its first tile
 };
 
 // A sequence's rows of q and of k and v, clipped to the tensors' own.
@@ -94,90 +99,170 @@ BAG_DEV uint4 ld_stream(const uint16_t* p) {
 }
 
 constexpr int F_WARPS = 8, F_TH = 32 * F_WARPS;
-constexpr int F_KEYS = 16;  // of a warp's step
+constexpr int F_KEYS = 16;               // of a warp's step
+constexpr int F_TILE = F_WARPS * F_KEYS;  // of the CTA's
+constexpr int F_ROWS = 16;               // query rows of a unit
 template <int DH>
 constexpr int few_smem() {
-  return F_WARPS * 16 * (DH + 4) * 4 + F_WARPS * 16 * 8;
+  return F_WARPS * F_ROWS * (DH + 4) * 4 + F_WARPS * F_ROWS * 8;
 }
+
+// Units of a sequence (16 rows, a key head), and key tiles of one (at least one: it writes the rows' output).
+BAG_DEV long few_units(const PackedParams& p, int lq) { return (long)((lq * p.group + F_ROWS - 1) / F_ROWS) * p.kv_heads; }
+BAG_DEV int few_tiles(int lk) { return max((lk + F_TILE - 1) / F_TILE, 1); }
 }  // namespace
 
-// Up to 16 rows (query token, head of the group) at a time against keys in registers: a warp takes 16
-// keys a step.  A key's 16-byte pieces go from global memory straight into the B operands of
+// Up to 16 rows (query token, head of the group) of a sequence and key head, a unit, against keys in registers: a
+// warp takes 16 keys a step.  A key's 16-byte pieces go from global memory straight into the B operands of
 // mma.m16n8k16: the order of a contraction is free, so lane (n, c) holds head columns 32 j + 8 c .. + 7 of
 // key n for Q K^T (the rows of Q are loaded in the same order), and columns 64 u + 8 n .. + 7 of keys 2 c,
 // 2 c + 1, 2 c + 8 and 2 c + 9 for P V, whose pairs of keys a byte permutation makes; its column n of
 // product t is then head column 64 u + 8 n + t, and a lane ends with runs of 8 columns of the output.
 // Keys past the last are loaded as zeros (whatever lies there, NaN included).
+// Split: the key tiles of all units lie in a row, and each CTA takes an equal share of them, so that lengths need
+// not be alike and one wave of CTAs does it all; every CTA adds the lengths up for itself.  A unit that lies in
+// one CTA's share is finished there; of the others a CTA holds at most two pieces, one that starts its
+// unit (piece 1) and one that does not (piece 0), which attn_join_kernel adds up.  The next unit's first
+// loads are in flight while the warps' sums are joined.
 template <bool F16, int DH>
-__global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p) {
+__global__ void __launch_bounds__(F_TH, DH == 64 ? 2 : 1) attn_few_kernel(const PackedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ long before[F_TH], warp_sum[F_WARPS];
   constexpr int LD = DH + 4, U = DH / 64, J = DH / 32;
   float* so = reinterpret_cast<float*>(smem);                                      // [F_WARPS][16][LD]
-  float2* sml = reinterpret_cast<float2*>(smem + F_WARPS * 16 * LD * 4);           // [F_WARPS][16]
+  float2* sml = reinterpret_cast<float2*>(smem + F_WARPS * F_ROWS * LD * 4);       // [F_WARPS][16]
   grid_dep_sync();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, n = lane >> 2, c = lane & 3;
   const int G = p.group;
-  long unit = blockIdx.x;
-  const int head = (int)(unit % p.kv_heads);
-  unit /= p.kv_heads;
-  const Span s = span_of(p, (int)(unit / p.parts2));
-  const int own = (int)(unit % p.parts2), parts = own_parts(p, s.lk);
-  if (own >= (p.parts1 ? parts : max(parts, 1))) return;
-  const bool direct = p.parts1 == 0 && parts <= 1;
-  const int part = p.parts1 + own;
-  const int k_lo = (int)min((long)own * p.chunk2, (long)s.lk);
-  const int k_hi = own == p.parts2 - 1 ? s.lk : (int)min((long)k_lo + p.chunk2, (long)s.lk);
-  const uint16_t *kb = p.k + s.k0 * p.ldk + head * DH, *vb = p.v + s.k0 * p.ldv + head * DH;
-  const long ldk = p.ldk, ldv = p.ldv;
-  const int R = s.lq * G;  // below 2^31
-  // keys that row r of this part sees end before
-  auto limit = [&](int r) {
-    if (r >= R) return k_lo;
-    if (!p.causal) return k_hi;
-    return min(max(r / G + 1 + s.lk - s.lq, k_lo), k_hi);
+
+  // sequences [first, first + F_TH): what lies before each of them (of these), and their sum
+  auto add_up = [&](int first) {
+    long w = 0;
+    const int i = first + (int)threadIdx.x;
+    if (i < p.seqs) {
+      const Span s = span_of(p, i);
+      w = few_units(p, s.lq) * (p.split ? few_tiles(s.lk) : 1);
+    }
+    long sum = w;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const long y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    __syncthreads();  // the last call's values have been read
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    long all = 0, mine = 0;
+#pragma unroll
+    for (int v = 0; v < F_WARPS; ++v) {
+      if (v < warp) mine += warp_sum[v];
+      all += warp_sum[v];
+    }
+    before[threadIdx.x] = mine + sum - w;
+    __syncthreads();
+    return all;
   };
-  for (int r0 = 0; r0 < R; r0 += 16) {
-    uint4 qa[2][J];
+  int first = 0;          // of the sequences in `before`
+  long base = 0;          // what lies before them
+  long here = add_up(0), total = here;
+  for (int i = F_TH; i < p.seqs; i += F_TH) total += add_up(i);
+  if (p.seqs > F_TH) add_up(0);
+  const long share = p.split ? (total + gridDim.x - 1) / gridDim.x : 1;
+  long pos = (long)blockIdx.x * share;
+  const long stop = p.split ? min(pos + share, total) : total;
+  if (p.split && blockIdx.x == 0 && threadIdx.x == 0) p.place[0] = share;
+
+  // what is done next: a unit, or some tiles of one
+  struct Work {
+    int q0, rows, head, r0;      // the sequence's first query row and rows, the key head, the unit's first row
+    int k_lo, k_hi;              // keys
+    int shift;                   // row r sees keys up to r / G + shift
+    int k0;
+    int tiles;                   // of all (split)
+    bool starts, ends;           // the unit's keys do
+  };
+  auto find = [&]() {
+    while (pos >= base + here) {
+      base += here;
+      first += F_TH;
+      here = add_up(first);
+    }
+    int lo = 0;
+#pragma unroll
+    for (int o = F_TH / 2; o > 0; o /= 2)
+      if (first + lo + o < p.seqs && before[lo + o] <= pos - base) lo += o;
+    const Span s = span_of(p, first + lo);
+    const int all = p.split ? few_tiles(s.lk) : 1, blocks = (s.lq * G + F_ROWS - 1) / F_ROWS;
+    const long off = pos - base - before[lo], unit = off / all;
+    const int t0 = (int)(off - unit * all);
+    if (p.split && off == 0 && threadIdx.x == 0) p.place[1 + first + lo] = pos;
+    Work w;
+    w.q0 = s.q0;
+    w.rows = s.lq * G;
+    w.head = (int)(unit / blocks);
+    w.r0 = (int)(unit - (long)w.head * blocks) * F_ROWS;
+    w.tiles = p.split ? (int)min((long)(all - t0), stop - pos) : 1;
+    w.starts = t0 == 0;
+    w.ends = !p.split || t0 + w.tiles == all;
+    w.k_lo = t0 * F_TILE;
+    w.k_hi = w.ends ? s.lk : w.k_lo + w.tiles * F_TILE;
+    w.shift = p.causal ? 1 + s.lk - s.lq : 0x40000000;
+    w.k0 = s.k0;
+    return w;
+  };
+  // keys that row r of the unit sees end before
+  auto limit = [&](const Work& w, int r) {
+    if (r >= w.rows) return w.k_lo;
+    return min(max(p.causal ? r / G + w.shift : w.k_hi, w.k_lo), w.k_hi);
+  };
+  uint4 qa[2][J], kf[2][J], vf[4][U];
+  const uint16_t *kb = nullptr, *vb = nullptr;
+  int end = 0;  // of the keys that the unit's last row sees
+  auto load_k = [&](int k0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = k0 + 8 * t + n;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        kf[t][j] = key < end ? ld_stream(kb + key * p.ldk + 32 * j + 8 * c) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto load_v = [&](int k0) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int key = k0 + 2 * c + (t & 1) + 8 * (t >> 1);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        vf[t][u] = key < end ? ld_stream(vb + key * p.ldv + 64 * u + 8 * n) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto begin = [&](const Work& w) {
+    kb = p.k + w.k0 * p.ldk + w.head * DH;
+    vb = p.v + w.k0 * p.ldv + w.head * DH;
+    end = limit(w, min(w.r0 + F_ROWS, w.rows) - 1);
+    const int k0 = w.k_lo + warp * F_KEYS;
+    if (k0 < end) load_k(k0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int r = r0 + n + 8 * i;
-      const uint16_t* at = p.q + (long)(s.q0 + r / G) * p.ldq + (long)(head * G + r % G) * DH;
+      const int r = w.r0 + n + 8 * i;
+      const uint16_t* at = p.q + (long)(w.q0 + r / G) * p.ldq + (long)(w.head * G + r % G) * DH;
 #pragma unroll
-      for (int j = 0; j < J; ++j) qa[i][j] = r < R ? __ldg(reinterpret_cast<const uint4*>(at + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < J; ++j)
+        qa[i][j] = r < w.rows ? __ldg(reinterpret_cast<const uint4*>(at + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
     }
-    const int lim[2] = {limit(r0 + n), limit(r0 + n + 8)};
-    const int end = limit(min(r0 + 15, R - 1));  // the last row sees most
+    if (k0 < end) load_v(k0);
+  };
+  if (pos >= stop) return;
+  Work w = find();
+  begin(w);
+  while (true) {
+    const int lim[2] = {limit(w, w.r0 + n), limit(w, w.r0 + n + 8)};
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[U * 8][4];
 #pragma unroll
     for (int i = 0; i < U * 8; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-    uint4 kf[2][J], vf[4][U];
-    auto load_k = [&](int k0) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int key = k0 + 8 * t + n;
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-          kf[t][j] = key < end ? ld_stream(kb + key * ldk + 32 * j + 8 * c) : make_uint4(0, 0, 0, 0);
-      }
-    };
-    auto load_v = [&](int k0) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int key = k0 + 2 * c + (t & 1) + 8 * (t >> 1);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          vf[t][u] = key < end ? ld_stream(vb + key * ldv + 64 * u + 8 * n) : make_uint4(0, 0, 0, 0);
-      }
-    };
-    constexpr int STEP = F_WARPS * F_KEYS;
-    int k0 = k_lo + warp * F_KEYS;
-    if (k0 < end) {
-      load_k(k0);
-      load_v(k0);
-    }
-    for (; k0 < end; k0 += STEP) {
+    for (int k0 = w.k_lo + warp * F_KEYS; k0 < end; k0 += F_TILE) {
       float sc[2][4];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -189,7 +274,7 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
           mma16816<F16>(sc[t], qa[0][j].z, qa[1][j].z, qa[0][j].w, qa[1][j].w, kf[t][j].z, kf[t][j].w);
         }
       }
-      if (k0 + STEP < end) load_k(k0 + STEP);
+      if (k0 + F_TILE < end) load_k(k0 + F_TILE);
       bool moved = false;
       float alpha[2];
 #pragma unroll
@@ -214,9 +299,9 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float w = ex2(fmaf(sc[t][2 * i + e], p.scale_log2, neg));
-            l[i] += w;
-            sc[t][2 * i + e] = w;
+            const float x = ex2(fmaf(sc[t][2 * i + e], p.scale_log2, neg));
+            l[i] += x;
+            sc[t][2 * i + e] = x;
           }
       }
       if (__any_sync(0xffffffffu, moved)) {
@@ -240,23 +325,31 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
                         __byte_perm(word(vf[2][u]), word(vf[3][u]), sel));
         }
       }
-      if (k0 + STEP < end) load_v(k0 + STEP);
+      if (k0 + F_TILE < end) load_v(k0 + F_TILE);
+    }
+    // where the sums go, then the next unit's loads
+    const Work done = w;
+    pos += p.split ? w.tiles : gridDim.x;
+    const bool more = pos < stop;
+    if (more) {
+      w = find();
+      begin(w);
     }
     // the warps' parts
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-      if (c == 0) sml[warp * 16 + n + 8 * i] = make_float2(m[i], l[i]);
+      if (c == 0) sml[warp * F_ROWS + n + 8 * i] = make_float2(m[i], l[i]);
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < F_WARPS; ++w) top = fmaxf(top, sml[w * 16 + n + 8 * i].x);
+      for (int v = 0; v < F_WARPS; ++v) top = fmaxf(top, sml[v * F_ROWS + n + 8 * i].x);
       const float f = m[i] == -INFINITY ? 0.f : ex2(m[i] - top);
-      float* row = so + (warp * 16 + n + 8 * i) * LD;
+      float* row = so + (warp * F_ROWS + n + 8 * i) * LD;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -268,42 +361,46 @@ __global__ void __launch_bounds__(F_TH, 1) attn_few_kernel(const PackedParams p)
                             o[u * 8 + t + 2][2 * i + e] * f, o[u * 8 + t + 3][2 * i + e] * f);
     }
     __syncthreads();
-    for (int it = threadIdx.x; it < 16 * (DH / 8); it += F_TH) {
+    for (int it = threadIdx.x; it < F_ROWS * (DH / 8); it += F_TH) {
       const int lr = it / (DH / 8), col = it % (DH / 8) * 8;
-      const int r = r0 + lr;
-      if (r >= R) continue;
+      const int r = done.r0 + lr;
+      if (r >= done.rows) continue;
       float top = -INFINITY, den = 0.f, v[8];
 #pragma unroll
-      for (int w = 0; w < F_WARPS; ++w) top = fmaxf(top, sml[w * 16 + lr].x);
+      for (int i = 0; i < F_WARPS; ++i) top = fmaxf(top, sml[i * F_ROWS + lr].x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = 0.f;
 #pragma unroll
-      for (int w = 0; w < F_WARPS; ++w) {
-        const float2 f = sml[w * 16 + lr];
+      for (int i = 0; i < F_WARPS; ++i) {
+        const float2 f = sml[i * F_ROWS + lr];
         den += f.y == 0.f ? 0.f : ex2(f.x - top) * f.y;
-        const float* row = so + (w * 16 + lr) * LD + col;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += row[e];
+        const float4* row = reinterpret_cast<const float4*>(so + (i * F_ROWS + lr) * LD + col);
+        const float4 a = row[0], b = row[1];
+        v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+        v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
       }
-      const long tok = s.q0 + r / G;
-      const int h = head * G + (int)(r % G);
-      if (direct) {
+      const long tok = done.q0 + r / G;
+      const int h = done.head * G + r % G;
+      const bool whole = done.starts && done.ends;
+      if (whole && p.parts1 == 0) {
         const float inv = den == 0.f ? 0.f : 1.f / den;
-        uint4 w;
-        w.x = pack16<F16>(v[0] * inv, v[1] * inv);
-        w.y = pack16<F16>(v[2] * inv, v[3] * inv);
-        w.z = pack16<F16>(v[4] * inv, v[5] * inv);
-        w.w = pack16<F16>(v[6] * inv, v[7] * inv);
-        *reinterpret_cast<uint4*>(p.o + tok * p.ldo + (long)h * DH + col) = w;
+        uint4 x;
+        x.x = pack16<F16>(v[0] * inv, v[1] * inv);
+        x.y = pack16<F16>(v[2] * inv, v[3] * inv);
+        x.z = pack16<F16>(v[4] * inv, v[5] * inv);
+        x.w = pack16<F16>(v[6] * inv, v[7] * inv);
+        *reinterpret_cast<uint4*>(p.o + tok * p.ldo + (long)h * DH + col) = x;
         if (p.lse && col == 0) p.lse[tok * p.heads + h] = (top + log2f(den)) * 0.6931471805599453f;
       } else {
-        const long at = ((long)part * p.nq + tok) * p.heads + h;
-        float4* d = reinterpret_cast<float4*>(p.part_o + at * DH + col);
+        const long at = whole ? ((long)p.parts1 * p.nq + tok) * p.heads + h
+                              : (long)(blockIdx.x * 2 + (done.starts ? 1 : 0)) * F_ROWS + lr;
+        float4* d = reinterpret_cast<float4*>((whole ? p.part_o : p.piece_o) + at * DH + col);
         d[0] = make_float4(v[0], v[1], v[2], v[3]);
         d[1] = make_float4(v[4], v[5], v[6], v[7]);
-        if (col == 0) p.part_ml[at] = make_float2(top, den);
+        if (col == 0) (whole ? p.part_ml : p.piece_ml)[at] = make_float2(top, den);
       }
     }
+    if (!more) break;
     __syncthreads();
   }
 }
@@ -828,17 +925,34 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   __shared__ float2 sml[GROUPS];
   grid_dep_sync();
   const int tok = (int)(blockIdx.x / p.heads), h = (int)(blockIdx.x % p.heads);
-  const Span s = span_of(p, sequence_of(p, tok));
+  const int seq = sequence_of(p, tok);
+  const Span s = span_of(p, seq);
   if (tok < s.q0 || tok >= s.q0 + s.lq) return;
-  const int own = own_parts(p, s.lk), parts = p.parts1 + own;
+  int own = 1;
+  long piece = -1;  // the first of the few-row kernel's
+  if (!p.few) {
+    own = own_parts(p, s.lk);
+  } else if (p.split) {
+    const int r = (tok - s.q0) * p.group + h % p.group, blocks = (s.lq * p.group + F_ROWS - 1) / F_ROWS;
+    const long tiles = few_tiles(s.lk), share = p.place[0];
+    const long t0 = p.place[1 + seq] + ((long)(h / p.group) * blocks + r / F_ROWS) * tiles;
+    const long c0 = t0 / share, c1 = (t0 + tiles - 1) / share;
+    if (c1 > c0) {
+      own = (int)(c1 - c0) + 1;
+      piece = c0 * 2 * F_ROWS + r % F_ROWS;
+    }
+  }
+  const int parts = p.parts1 + own;
   if (p.parts1 == 0 && own <= 1) return;  // written by its only part
   const int g = threadIdx.x / L, x = threadIdx.x % L;
   float m = -INFINITY, l = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = g; i < parts; i += GROUPS) {
-    const long at = ((long)i * p.nq + tok) * p.heads + h;
-    const float2 f = p.part_ml[at];
-    const float4 v = *reinterpret_cast<const float4*>(p.part_o + at * DH + 4 * x);
+    const int k = i - p.parts1;
+    const bool whole = k < 0 || piece < 0;  // pieces: the first CTA's starts the unit (1), the others' do not
+    const long at = whole ? ((long)i * p.nq + tok) * p.heads + h : piece + (long)k * 2 * F_ROWS + (k == 0 ? F_ROWS : 0);
+    const float2 f = (whole ? p.part_ml : p.piece_ml)[at];
+    const float4 v = *reinterpret_cast<const float4*>((whole ? p.part_o : p.piece_o) + at * DH + 4 * x);
     if (f.y == 0.f) continue;  // no key of the part is seen
     const float top = fmaxf(m, f.x), a = l == 0.f ? 0.f : ex2(m - top), b = ex2(f.x - top);
     m = top;
@@ -875,23 +989,30 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
 }
 
 namespace {
-// The form of a call.  few: own keys by attn_few_kernel; rows: of a unit of the tensor-core kernel.
+// The form of a call: own keys by attn_few_kernel or the tensor cores, the prefix with all rows together (parts1)
+// or before each sequence's own keys (fused key tiles).
 struct Plan {
   int parts1, parts2, chunk1, chunk2;
-  int few, fused, rows, together;
+  int few, split, ctas;       // ctas: of the few-row kernel
+  int fused, rows, together;  // rows: of a unit of the tensor-core kernel
 };
 
-size_t part_bytes(const PackedArgs& a) { return (size_t)a.nq * (size_t)a.heads * ((size_t)a.dh * 4 + 8); }
-
 long cdiv(long a, long b) { return (a + b - 1) / b; }
+size_t part_bytes(const PackedArgs& a) { return (size_t)a.nq * (size_t)a.heads * ((size_t)a.dh * 4 + 8); }
+size_t piece_bytes(const PackedArgs& a, const Plan& t) {
+  return t.split ? (size_t)t.ctas * 2 * F_ROWS * ((size_t)a.dh * 4 + 8) + ((size_t)a.seqs + 1) * 8 : 0;
+}
+// parts that are kept (with one in all it is the output)
+long parts_of(const Plan& t) { return t.parts1 + t.parts2 > 1 ? t.parts1 + t.parts2 : 0; }
 
-// How the rows and keys are cut, with at most `most` parts in all.
-Plan plan_of(const PackedArgs& a, long most) {
+// How the rows and keys are cut, with a workspace of at most `bytes`.
+Plan plan_of(const PackedArgs& a, size_t bytes) {
   Plan t{};
   const long G = a.heads / a.kv_heads, sms = sm_count();
   const long max_k = std::min(std::max(a.max_k, 1L), std::max(a.k_rows, 1L));
   const long max_q = std::max(1L, std::min(a.max_q, a.nq)), rows = a.nq * G;
-  t.few = max_q * G <= 16;
+  const long most = (long)std::min<size_t>(bytes / part_bytes(a), 1u << 30);  // parts
+  t.few = max_q * G <= F_ROWS;
   // heads of a group that share a tile: as many as leave few of its rows empty, or whose rows of a
   // sequence fit one (more units of a key head would read its keys again)
   t.together = 1;
@@ -901,39 +1022,44 @@ Plan plan_of(const PackedArgs& a, long most) {
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
   t.rows = units(256) * 2 > sms ? 256 : 128;
   if (const char* e = std::getenv("X_ROWS")) t.rows = std::atoi(e);
-  const bool together = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
-  const long per = t.few ? F_KEYS : PT;  // keys that a part has a multiple of
-  auto chunk = [](long keys, long parts, long n) { return (int)(cdiv(cdiv(keys, parts), n) * n); };
+  const bool all_rows = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
+  if (a.n_prefix && !all_rows) t.few = 0;
+  auto chunk = [](long keys, long parts) { return (int)(cdiv(cdiv(keys, parts), PT) * PT); };
   long p1 = 0, p2 = 1;
-  if (together) p1 = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, t.rows) * a.kv_heads)));
-  const long keys = max_k + (together ? 0 : cdiv(a.n_prefix, PT) * PT);
-  if (t.few)
-    p2 = std::max(1L, std::min(cdiv(max_k, 256), 4 * sms / std::max(1L, a.seqs * a.kv_heads)));
-  else if (units(t.rows) * 2 <= sms)
+  if (all_rows) p1 = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, t.rows) * a.kv_heads)));
+  t.fused = all_rows ? 0 : (int)cdiv(a.n_prefix, PT);
+  const long keys = max_k + (long)t.fused * PT;
+  if (!t.few && units(t.rows) * 2 <= sms)
     p2 = std::max(1L, std::min(keys / 1024, sms / std::max(1L, units(t.rows))));
   if (p1 + p2 > most) {
     if (p1) p1 = std::max(1L, std::min(p1, most - 1));
     p2 = std::max(1L, most - p1);
   }
-  t.fused = together ? 0 : (int)cdiv(a.n_prefix, PT);
-  if (t.fused) t.few = 0;
-  t.chunk1 = p1 ? chunk(a.n_prefix, p1, PT) : PT;
+  t.chunk1 = p1 ? chunk(a.n_prefix, p1) : PT;
   t.parts1 = p1 ? (int)cdiv(a.n_prefix, t.chunk1) : 0;
-  t.chunk2 = chunk(keys, p2, t.few ? per : PT);
+  t.chunk2 = chunk(keys, p2);
   t.parts2 = (int)p2;
+  if (t.few) {
+    const long units16 = a.seqs * a.kv_heads * cdiv(max_q * G, F_ROWS), slots = sms * (a.dh == 64 ? 2 : 1);
+    t.split = max_k > 2 * F_TILE;
+    t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * cdiv(max_k, F_TILE) : units16));
+    if (t.split && bytes < parts_of(t) * part_bytes(a) + piece_bytes(a, t)) {
+      t.split = 0;
+      t.ctas = (int)std::min(slots, units16);
+    }
+  }
   return t;
 }
 }  // namespace
 
 size_t attention_packed_work(const PackedArgs& a) {
-  const Plan t = plan_of(a, 1L << 30);
-  return t.parts1 + t.parts2 > 1 ? (size_t)(t.parts1 + t.parts2) * part_bytes(a) : 0;
+  const Plan t = plan_of(a, ~(size_t)0 >> 1);
+  return parts_of(t) * part_bytes(a) + piece_bytes(a, t);
 }
 
 cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   if (a.nq <= 0 || a.seqs <= 0) return cudaSuccess;
-  const long most = (long)std::min<size_t>(a.work_bytes / part_bytes(a), 1u << 30);
-  const Plan t = plan_of(a, most);
+  const Plan t = plan_of(a, a.work_bytes);
   PackedParams p{};
   auto u16 = [](const void* x) { return reinterpret_cast<const uint16_t*>(x); };
   p.q = u16(a.q), p.k = u16(a.k), p.v = u16(a.v), p.pk = u16(a.pk), p.pv = u16(a.pv);
@@ -945,15 +1071,21 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = a.heads / a.kv_heads, p.causal = a.causal;
   p.scale_log2 = a.scale_log2;
   p.parts1 = t.parts1, p.parts2 = t.parts2, p.chunk1 = t.chunk1, p.chunk2 = t.chunk2, p.fused = t.fused;
+  // the workspace: sums of parts, of pieces, then what is 8 bytes wide
+  const size_t kept = (size_t)parts_of(t) * a.nq * a.heads, pieces = t.split ? (size_t)t.ctas * 2 * F_ROWS : 0;
   p.part_o = reinterpret_cast<float*>(a.work);
-  p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)(t.parts1 + t.parts2) * a.nq * a.heads * a.dh);
+  p.piece_o = p.part_o + kept * a.dh;
+  p.part_ml = reinterpret_cast<float2*>(p.piece_o + pieces * a.dh);
+  p.piece_ml = p.part_ml + kept;
+  p.place = reinterpret_cast<long*>(p.piece_ml + pieces);
+  p.few = t.few, p.split = t.split;
   p.together = t.together, p.tokens = PT / t.together;
   const long per = p.tokens * (t.rows / PT), groups = a.heads / t.together;
   const long slots1 = t.parts1 ? cdiv(a.nq, per) : 0, slots2 = t.few ? 0 : a.nq / per + a.seqs;
   p.err = a.err;
   const long tiles = (slots1 * t.parts1 + slots2 * t.parts2) * groups;
-  const long few = t.few ? a.seqs * t.parts2 * a.kv_heads : 0, joins = a.nq * a.heads;
-  if (tiles > 0x7fffffffL || few > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
+  const long few = t.few ? t.ctas : 0, joins = a.nq * a.heads;
+  if (tiles > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
     return cudaErrorInvalidConfiguration;
   p.slots1 = (int)slots1, p.slots2 = (int)slots2;
   CUtensorMap tq, tk, tv, tpk, tpv;
@@ -985,7 +1117,7 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
                                         Pt<DH, 2>::BYTES, s, tq, tk, tv, tpk, tpv, p)
                         : launch_kernel(attn_packed_kernel<F16, DH, 1>, (unsigned)tiles, Pt<DH, 1>::THREADS,
                                         Pt<DH, 1>::BYTES, s, tq, tk, tv, tpk, tpv, p);
-    if (e == cudaSuccess && t.parts1 + t.parts2 > 1)
+    if (e == cudaSuccess && (parts_of(t) || t.split))
       e = launch_kernel(attn_join_kernel<F16, DH>, (unsigned)joins, JN_TH, 0, s, p);
     return e;
   };
