@@ -98,7 +98,9 @@ BAG_DEV uint4 ld_stream(const uint16_t* p) {
   return v;
 }
 
-constexpr int F_WARPS = 8, F_TH = 32 * F_WARPS;
+constexpr int F_WARPS = 4, F_TH = 32 * F_WARPS;
+template <int DH>
+constexpr int few_ctas() { return (DH == 64 ? 16 : 8) / F_WARPS; }  // on an SM
 constexpr int F_KEYS = 16;               // of a warp's step
 constexpr int F_TILE = F_WARPS * F_KEYS;  // of the CTA's
 constexpr int F_ROWS = 16;               // query rows of a unit
@@ -107,9 +109,11 @@ constexpr int few_smem() {
   return F_WARPS * F_ROWS * (DH + 4) * 4 + F_WARPS * F_ROWS * 8;
 }
 
-// Units of a sequence (16 rows, a key head), and key tiles of one (at least one: it writes the rows' output).
+// Units of a sequence (16 rows, a key head), and the length of one where they lie in a row: its key tiles, and
+// F_COST for what a unit costs besides them.
 BAG_DEV long few_units(const PackedParams& p, int lq) { return (long)((lq * p.group + F_ROWS - 1) / F_ROWS) * p.kv_heads; }
-BAG_DEV int few_tiles(int lk) { return max((lk + F_TILE - 1) / F_TILE, 1); }
+constexpr int F_COST = 1;
+BAG_DEV int few_length(int lk) { return (lk + F_TILE - 1) / F_TILE + F_COST; }
 }  // namespace
 
 // Up to 16 rows (query token, head of the group) of a sequence and key head, a unit, against keys in registers: a
@@ -125,7 +129,7 @@ BAG_DEV int few_tiles(int lk) { return max((lk + F_TILE - 1) / F_TILE, 1); }
 // unit (piece 1) and one that does not (piece 0), which attn_join_kernel adds up.  The next unit's first
 // loads are in flight while the warps' sums are joined.
 template <bool F16, int DH>
-__global__ void __launch_bounds__(F_TH, DH == 64 ? 2 : 1) attn_few_kernel(const PackedParams p) {
+__global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const PackedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ long before[F_TH], warp_sum[F_WARPS];
   constexpr int LD = DH + 4, U = DH / 64, J = DH / 32;
@@ -141,7 +145,7 @@ __global__ void __launch_bounds__(F_TH, DH == 64 ? 2 : 1) attn_few_kernel(const 
     const int i = first + (int)threadIdx.x;
     if (i < p.seqs) {
       const Span s = span_of(p, i);
-      w = few_units(p, s.lq) * (p.split ? few_tiles(s.lk) : 1);
+      w = few_units(p, s.lq) * (p.split ? few_length(s.lk) : 1);
     }
     long sum = w;
 #pragma unroll
@@ -178,7 +182,7 @@ __global__ void __launch_bounds__(F_TH, DH == 64 ? 2 : 1) attn_few_kernel(const 
     int k_lo, k_hi;              // keys
     int shift;                   // row r sees keys up to r / G + shift
     int k0;
-    int tiles;                   // of all (split)
+    int length;                  // of it (split)
     bool starts, ends;           // the unit's keys do
   };
   auto find = [&]() {
@@ -192,20 +196,20 @@ __global__ void __launch_bounds__(F_TH, DH == 64 ? 2 : 1) attn_few_kernel(const 
     for (int o = F_TH / 2; o > 0; o /= 2)
       if (first + lo + o < p.seqs && before[lo + o] <= pos - base) lo += o;
     const Span s = span_of(p, first + lo);
-    const int all = p.split ? few_tiles(s.lk) : 1, blocks = (s.lq * G + F_ROWS - 1) / F_ROWS;
+    const int all = p.split ? few_length(s.lk) : 1, blocks = (s.lq * G + F_ROWS - 1) / F_ROWS;
     const long off = pos - base - before[lo], unit = off / all;
-    const int t0 = (int)(off - unit * all);
+    const int at = (int)(off - unit * all);
     if (p.split && off == 0 && threadIdx.x == 0) p.place[1 + first + lo] = pos;
     Work w;
     w.q0 = s.q0;
     w.rows = s.lq * G;
     w.head = (int)(unit / blocks);
     w.r0 = (int)(unit - (long)w.head * blocks) * F_ROWS;
-    w.tiles = p.split ? (int)min((long)(all - t0), stop - pos) : 1;
-    w.starts = t0 == 0;
-    w.ends = !p.split || t0 + w.tiles == all;
-    w.k_lo = t0 * F_TILE;
-    w.k_hi = w.ends ? s.lk : w.k_lo + w.tiles * F_TILE;
+    w.length = p.split ? (int)min((long)(all - at), stop - pos) : 1;
+    w.starts = at == 0;
+    w.ends = at + w.length == all;
+    w.k_lo = max(at - F_COST, 0) * F_TILE;
+    w.k_hi = w.ends ? s.lk : max(at + w.length - F_COST, 0) * F_TILE;
     w.shift = p.causal ? 1 + s.lk - s.lq : 0x40000000;
     w.k0 = s.k0;
     return w;
@@ -329,7 +333,7 @@ __global__ void __launch_bounds__(F_TH, DH == 64 ? 2 : 1) attn_few_kernel(const 
     }
     // where the sums go, then the next unit's loads
     const Work done = w;
-    pos += p.split ? w.tiles : gridDim.x;
+    pos += p.split ? w.length : gridDim.x;
     const bool more = pos < stop;
     if (more) {
       w = find();
@@ -917,12 +921,14 @@ BAG_DEV int sequence_of(const PackedParams& p, int t) {
 }
 }  // namespace
 
-// Joins the parts of a row and head: DH / 4 lanes a part, in turn over the parts, in a fixed order.
+// Joins the parts of a row and head: their weights first, then DH / 4 lanes a part, in a fixed order.
 template <bool F16, int DH>
 __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) {
   constexpr int L = DH / 4, GROUPS = JN_TH / L;
   __shared__ float4 so[GROUPS][L];
-  __shared__ float2 sml[GROUPS];
+  __shared__ float dens[GROUPS], red[JN_TH / 32];
+  __shared__ float2 weight[JN_TH];
+  __shared__ const float* from[JN_TH];
   grid_dep_sync();
   const int tok = (int)(blockIdx.x / p.heads), h = (int)(blockIdx.x % p.heads);
   const int seq = sequence_of(p, tok);
@@ -934,9 +940,9 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
     own = own_parts(p, s.lk);
   } else if (p.split) {
     const int r = (tok - s.q0) * p.group + h % p.group, blocks = (s.lq * p.group + F_ROWS - 1) / F_ROWS;
-    const long tiles = few_tiles(s.lk), share = p.place[0];
-    const long t0 = p.place[1 + seq] + ((long)(h / p.group) * blocks + r / F_ROWS) * tiles;
-    const long c0 = t0 / share, c1 = (t0 + tiles - 1) / share;
+    const long length = few_length(s.lk), share = p.place[0];
+    const long start = p.place[1 + seq] + ((long)(h / p.group) * blocks + r / F_ROWS) * length;
+    const long c0 = start / share, c1 = (start + length - 1) / share;
     if (c1 > c0) {
       own = (int)(c1 - c0) + 1;
       piece = c0 * 2 * F_ROWS + r % F_ROWS;
@@ -944,41 +950,65 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   }
   const int parts = p.parts1 + own;
   if (p.parts1 == 0 && own <= 1) return;  // written by its only part
-  const int g = threadIdx.x / L, x = threadIdx.x % L;
-  float m = -INFINITY, l = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = g; i < parts; i += GROUPS) {
+  // where part i's sums lie; of pieces, the first CTA's starts the unit (1), the others' do not
+  auto place = [&](int i, const float2*& ml) {
     const int k = i - p.parts1;
-    const bool whole = k < 0 || piece < 0;  // pieces: the first CTA's starts the unit (1), the others' do not
+    const bool whole = k < 0 || piece < 0;
     const long at = whole ? ((long)i * p.nq + tok) * p.heads + h : piece + (long)k * 2 * F_ROWS + (k == 0 ? F_ROWS : 0);
-    const float2 f = (whole ? p.part_ml : p.piece_ml)[at];
-    const float4 v = *reinterpret_cast<const float4*>((whole ? p.part_o : p.piece_o) + at * DH + 4 * x);
-    if (f.y == 0.f) continue;  // no key of the part is seen
-    const float top = fmaxf(m, f.x), a = l == 0.f ? 0.f : ex2(m - top), b = ex2(f.x - top);
-    m = top;
-    l = l * a + f.y * b;
-    acc.x = acc.x * a + v.x * b;
-    acc.y = acc.y * a + v.y * b;
-    acc.z = acc.z * a + v.z * b;
-    acc.w = acc.w * a + v.w * b;
+    ml = (whole ? p.part_ml : p.piece_ml) + at;
+    return (whole ? p.part_o : p.piece_o) + at * DH;
+  };
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = threadIdx.x / L, x = threadIdx.x % L;
+  float top = -INFINITY;
+  for (int i = threadIdx.x; i < parts; i += JN_TH) {
+    const float2* ml;
+    place(i, ml);
+    top = fmaxf(top, ml->x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) red[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < JN_TH / 32; ++i) top = fmaxf(top, red[i]);
+  float den = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < parts; i0 += JN_TH) {
+    if (i0) __syncthreads();
+    if (i0 + (int)threadIdx.x < parts) {  // weights of the next parts (0: no key of the part is seen)
+      const float2* ml;
+      from[threadIdx.x] = place(i0 + threadIdx.x, ml);
+      const float2 f = *ml;
+      weight[threadIdx.x] = make_float2(f.y == 0.f ? 0.f : ex2(f.x - top), f.y);
+    }
+    __syncthreads();
+    const int n = min(JN_TH, parts - i0);
+#pragma unroll 8
+    for (int i = g; i < n; i += GROUPS) {
+      const float2 f = weight[i];
+      const float4 v = *reinterpret_cast<const float4*>(from[i] + 4 * x);
+      const bool none = f.y == 0.f;  // then v may be the product of no weight and NaN
+      den += f.x * f.y;
+      acc.x += none ? 0.f : f.x * v.x;
+      acc.y += none ? 0.f : f.x * v.y;
+      acc.z += none ? 0.f : f.x * v.z;
+      acc.w += none ? 0.f : f.x * v.w;
+    }
   }
   so[g][x] = acc;
-  if (x == 0) sml[g] = make_float2(m, l);
+  if (x == 0) dens[g] = den;
   __syncthreads();
   if (threadIdx.x >= L) return;
-  float top = -INFINITY, den = 0.f;
+  acc = so[0][x];
+  den = dens[0];
 #pragma unroll
-  for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, sml[i].x);
-  acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int i = 0; i < GROUPS; ++i) {
-    const float w = sml[i].y == 0.f ? 0.f : ex2(sml[i].x - top);
+  for (int i = 1; i < GROUPS; ++i) {
     const float4 v = so[i][x];
-    den += w * sml[i].y;
-    acc.x += w * v.x;
-    acc.y += w * v.y;
-    acc.z += w * v.z;
-    acc.w += w * v.w;
+    den += dens[i];
+    acc.x += v.x;
+    acc.y += v.y;
+    acc.z += v.z;
+    acc.w += v.w;
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;
   uint2 u;
@@ -1040,9 +1070,9 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   t.chunk2 = chunk(keys, p2);
   t.parts2 = (int)p2;
   if (t.few) {
-    const long units16 = a.seqs * a.kv_heads * cdiv(max_q * G, F_ROWS), slots = sms * (a.dh == 64 ? 2 : 1);
-    t.split = max_k > 2 * F_TILE;
-    t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * cdiv(max_k, F_TILE) : units16));
+    const long units16 = a.seqs * a.kv_heads * cdiv(max_q * G, F_ROWS), slots = sms * (a.dh == 64 ? few_ctas<64>() : few_ctas<128>());
+    t.split = max_k > 256;
+    t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * cdiv(max_k, 2 * F_TILE) : units16));
     if (t.split && bytes < parts_of(t) * part_bytes(a) + piece_bytes(a, t)) {
       t.split = 0;
       t.ctas = (int)std::min(slots, units16);
