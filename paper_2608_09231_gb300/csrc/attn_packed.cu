@@ -7,7 +7,6 @@
 // (m, l, O) with l = sum 2^(s - m), O = sum 2^(s - m) v, s in log2 units; parts are joined by
 // m = max m_i, l = sum 2^(m_i - m) l_i, O likewise.
 #include <algorithm>
-#include <cstdlib>
 
 #include "attn_common.cuh"
 #include "kernels.h"
@@ -415,28 +414,73 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
 namespace {
 constexpr int PT = 128;                    // rows and keys of a tile
 constexpr int PT_CHUNK = PT * 64 * 2;      // 128 rows x 64 columns: one 128-byte swizzle column
-constexpr int PT_LD = 144;                 // bytes a row in the output transpose (16 against bank conflicts)
+constexpr int PT_LD = 80;                  // bytes a row in the output transpose (16 against bank conflicts)
 constexpr int PT_OUT = 4 * 32 * PT_LD;     // bytes of a tile's
 // A CTA of NT tiles: threads, tensor memory (the scores' NT * 128 columns, then the outputs'), registers (168
-// a thread at launch with two tiles, 128 with one: 128 * 88 + 256 * 208 and 128 * 72 + 128 * 184 of them)
+// a thread at launch with two tiles, 128 with one: 128 * 88 + 256 * 208 and 128 * 64 + 128 * 192 of them)
 // and shared memory (two CTAs on an SM with one tile).
 template <int DH, int NT>
 struct Pt {
   static constexpr int THREADS = 128 + NT * 128, TMEM_COLS = NT * 256;
-  static constexpr int REGS_ISSUE = NT == 2 ? 88 : 72, REGS_SOFTMAX = NT == 2 ? 208 : 184;
+  static constexpr int REGS_ISSUE = NT == 2 ? 88 : 64, REGS_SOFTMAX = NT == 2 ? 208 : 192;
   static constexpr int STAGES = NT == 1 && DH == 128 ? 1 : 2;  // of the K ring and of the V ring
   static constexpr int TILE = DH / 64 * PT_CHUNK;
-  static constexpr int Q = 0, K = NT * TILE, V = K + STAGES * TILE, OUT = DH == 128 ? Q : V + STAGES * TILE;
-  static constexpr int ROWS = DH == 128 ? V + STAGES * TILE : OUT + NT * PT_OUT;  // where a row's output goes
+  static constexpr int Q = 0, K = NT * TILE, V = K + STAGES * TILE, OUT = V + STAGES * TILE;
+  static constexpr int ROWS = OUT + NT * PT_OUT;  // where a row's output goes
   static constexpr int BAR = ROWS + NT * PT * 8;
-  static constexpr int BYTES = BAR + 256 + 1024;
+  static constexpr int BYTES = BAR + 384 + 1024;
 };
-static_assert(PT_OUT <= Pt<128, 1>::TILE, "a tile's output transpose fits its queries");
+static_assert(2 * (Pt<128, 1>::BYTES + 1024) <= 228 * 1024 && 2 * (Pt<64, 1>::BYTES + 1024) <= 228 * 1024, "two CTAs on an SM");
+static_assert(Pt<128, 2>::BYTES <= 227 * 1024, "shared memory of a CTA");
 
-// Shared-memory descriptor of a tile whose rows run along the contraction (V: a row a key), 128-byte
-// swizzle: 64-column chunks PT_CHUNK apart, groups of eight rows 1024 bytes apart.
-BAG_DEV uint64_t sw128_desc_mn(uint32_t saddr) {
-  return sw128_desc(saddr) & ~((uint64_t)0x3fff << 16) | (uint64_t)(PT_CHUNK >> 4) << 16;
+// Another CTA's work: the launch hands over the index of one that has not started, which then never does
+// (16 bytes to `response`, signalled on bar), until none is left.
+BAG_DEV void next_cta_request(void* response, uint64_t* bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   smem_u32(response)),
+               "r"(smem_u32(bar))
+               : "memory");
+}
+BAG_DEV bool next_cta(const void* response, int* x) {
+  uint32_t there, at;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+      : "=r"(there), "=r"(at)
+      : "r"(smem_u32(response))
+      : "memory");
+  *x = (int)at;
+  return there != 0;
+}
+
+// Shared-memory descriptors (as sw128_desc) by their lower words: the upper one (1024 bytes from eight rows to
+// the next, version, 128-byte swizzle) is the same for all, and a register less for each.  _mn: of a tile whose
+// rows run along the contraction (V: a row a key), 64-column chunks PT_CHUNK apart.
+constexpr uint32_t PT_DESC_HI = (1024 >> 4) | 1u << 14 | 2u << 29;
+BAG_DEV uint32_t desc_k(uint32_t saddr) { return (saddr & 0x3ffffu) >> 4 | 1u << 16; }
+BAG_DEV uint32_t desc_mn(uint32_t saddr) { return (saddr & 0x3ffffu) >> 4 | (uint32_t)(PT_CHUNK >> 4) << 16; }
+// D (TMEM) (+)= A (shared memory) * B (shared memory), and with A in TMEM
+BAG_DEV void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(PT_DESC_HI)
+      : "memory");
+}
+BAG_DEV void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+      "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "n"(PT_DESC_HI)
+      : "memory");
 }
 
 // The sequence whose units (of `per` tokens) hold slot `slot`, and its first slot: sequence i's slots are
@@ -465,60 +509,77 @@ BAG_DEV Span span_of_slot(const PackedParams& p, int per, int slot, int* first) 
   return s;
 }
 
-// What a CTA works on.
+// What a CTA works on at a time.
 struct Unit {
-  int q0, tokens;        // its first query row, and how many (none: nothing to do)
+  int q0, tokens;        // its first query row, and how many (0: nothing to do, -1: no unit is left)
+  int head0;             // first query head of its rows
   int sees;              // own keys that its first token sees (below zero: none; of all with no mask)
   int k0, lk;            // the sequence's keys
   int fused;             // key tiles of the prefix, before them
-  int part, j0, most;    // the part of the keys, its first tile, and how many it may have
-  int direct;            // it is the only one: the output is final
+  int part, j0;          // the part of the keys, and its first tile
+  int n[2];              // key tiles of each tile of rows
+  int direct;            // the part is the only one: the output is final
 };
-BAG_DEV Unit unit_of(const PackedParams& p, int per, int at) {
+// own keys that the unit's token i sees
+BAG_DEV int sees_of(const PackedParams& p, const Unit& u, int i) {
+  return p.causal ? min(max(u.sees + i, 0), u.lk) : u.lk;
+}
+BAG_DEV Unit unit_of(const PackedParams& p, int nt, int at) {
   Unit u{};
-  const int units1 = p.slots1 * p.parts1;
+  const int per_head = p.slots1 * p.parts1 + p.slots2 * p.parts2, units1 = p.slots1 * p.parts1, per = nt * p.tokens;
+  const int hu = at / per_head;  // a head at a time, so that its keys stay in L2
+  at -= hu * per_head;
+  u.head0 = hu * p.together;
+  int most;  // tiles that the part may have
   if (at < units1) {  // the prefix with the tokens of all sequences
     const Span s = span_all(p);
     const int slot = at / p.parts1;
     u.part = at - slot * p.parts1;
     u.q0 = s.q0 + slot * per;
     u.tokens = max(min(s.lq - slot * per, per), 0);
-    u.most = p.chunk1 / PT;
-    u.j0 = u.part * u.most;
+    most = p.chunk1 / PT;
+    u.j0 = u.part * most;
     u.fused = (p.n_prefix + PT - 1) / PT;
-    return u;
+  } else {
+    at -= units1;
+    const int back = at / p.parts2, own = at - back * p.parts2;
+    const int slot = p.slots2 - 1 - back;  // later tokens see more keys: they go first
+    int first;
+    const Span s = span_of_slot(p, per, slot, &first);
+    if (slot < first || slot - first >= (s.lq + per - 1) / per) return u;
+    const int parts = own_parts(p, s.lk), t0 = (slot - first) * per;
+    if (own >= (p.parts1 ? parts : max(parts, 1))) return u;
+    u.q0 = s.q0 + t0;
+    u.tokens = min(s.lq - t0, per);
+    u.sees = p.causal ? t0 + 1 + s.lk - s.lq : s.lk;
+    u.k0 = s.k0, u.lk = s.lk;
+    u.fused = p.fused;
+    u.part = p.parts1 + own;
+    u.j0 = own * (p.chunk2 / PT);
+    most = own == p.parts2 - 1 ? 0x7fffffff : p.chunk2 / PT;
+    u.direct = p.parts1 == 0 && parts <= 1;
   }
-  at -= units1;
-  const int back = at / p.parts2, own = at - back * p.parts2;
-  const int slot = p.slots2 - 1 - back;  // later tokens see more keys: they go first
-  int first;
-  const Span s = span_of_slot(p, per, slot, &first);
-  if (slot < first || slot - first >= (s.lq + per - 1) / per) return u;
-  const int parts = own_parts(p, s.lk), t0 = (slot - first) * per;
-  if (own >= (p.parts1 ? parts : max(parts, 1))) return u;
-  u.q0 = s.q0 + t0;
-  u.tokens = min(s.lq - t0, per);
-  u.sees = p.causal ? t0 + 1 + s.lk - s.lq : s.lk;
-  u.k0 = s.k0, u.lk = s.lk;
-  u.fused = p.fused;
-  u.part = p.parts1 + own;
-  u.j0 = own * (p.chunk2 / PT);
-  u.most = own == p.parts2 - 1 ? 0x7fffffff : p.chunk2 / PT;
-  u.direct = p.parts1 == 0 && parts <= 1;
+  for (int x = 0; x < nt; ++x) {
+    const int end = min((x + 1) * p.tokens, u.tokens);
+    if (end > x * p.tokens) u.n[x] = min(max(u.fused + (sees_of(p, u, end - 1) + PT - 1) / PT - u.j0, 0), most);
+  }
   return u;
 }
 }  // namespace
 
-// One CTA takes NT tiles of up to 128 rows (row r: query token r / together, head r % together of those that share
-// the key head) and walks the tiles of 128 keys that the last of them sees:
-//   warp 0        TMA producer: the queries, then K and V tiles into rings of their own
+// A CTA takes units of NT tiles of up to 128 rows (row r: query token r / together, head r % together of those that
+// share the key head), one after the other, and walks the tiles of 128 keys that the last of their rows sees:
+//   warp 0        finds the units (its own, then those of CTAs that have not started, each asked for when the
+//                 last loads of the one before are due) and loads by TMA: the queries, then K and V tiles
+//                 into rings of their own
 //   warp 1        MMA issuer, in turn between the tiles: S_A,0 S_B,0 | PV_A,j S_A,j+1 | PV_B,j S_B,j+1 | ...
 //                 It zeros the rows of V past a sequence's (or the prefix's) last key: whatever lies there would
 //                 meet weights of zero, and may be NaN
-//   warp 2        finds the unit while warp 1 allocates tensor memory
 //   warps 4..     the softmax of tile A (4..7) and B (8..11), a row a thread, as in the dense kernel: P goes
 //                 back over the scores in 16 bits and enters the second product from TMEM; O stays in
 //                 TMEM and is rescaled only when the maximum has grown by more than 8
+// So the loads and scores of a unit run beside the output of the one before, and what a CTA costs to launch
+// (tensor memory, barriers, the launch itself, some 5,000 cycles) comes once for each that is resident.
 // V is read as it lies, a row a key: as an operand whose rows run along the contraction.
 template <bool F16, int DH, int NT>
 __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
@@ -533,24 +594,28 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
   uint8_t *sQ = smem + M::Q, *sK = smem + M::K, *sV = smem + M::V;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::BAR);
   uint64_t* q_full = bars + 0;
-  uint64_t* k_full = bars + 1;    // [2]
-  uint64_t* k_empty = bars + 3;   // [2]
-  uint64_t* v_full = bars + 5;    // [2]
-  uint64_t* v_empty = bars + 7;   // [2]
-  uint64_t* s_full = bars + 9;    // [2] per query tile
-  uint64_t* p_full = bars + 11;   // [2]
-  uint64_t* o_done = bars + 13;   // [2]
-  uint64_t* drain = bars + 15;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16);
+  uint64_t* q_empty = bars + 1;
+  uint64_t* k_full = bars + 2;    // [2]
+  uint64_t* k_empty = bars + 4;   // [2]
+  uint64_t* v_full = bars + 6;    // [2]
+  uint64_t* v_empty = bars + 8;   // [2]
+  uint64_t* s_full = bars + 10;   // [2] per query tile
+  uint64_t* p_full = bars + 12;   // [2]
+  uint64_t* o_done = bars + 14;   // [2]
+  uint64_t* u_full = bars + 16;   // [2] of the ring of units
+  uint64_t* u_empty = bars + 18;  // [2]
+  uint64_t* asked = bars + 20;
+  uint64_t* drain = bars + 21;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 22);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  Unit* found = reinterpret_cast<Unit*>(tmem_slot + 2);
+  uint8_t* response = reinterpret_cast<uint8_t*>(bars + 24);  // 16 bytes
+  Unit* units = reinterpret_cast<Unit*>(bars + 26);           // [2]
+  static_assert(26 * 8 + 2 * sizeof(Unit) <= 384 && M::BAR % 16 == 0, "barriers and units");
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int per_head = p.slots1 * p.parts1 + p.slots2 * p.parts2;
-  const int hu = blockIdx.x / per_head;             // a head at a time, so that its keys stay in L2
-  const int head0 = hu * p.together, head = head0 / p.group;  // first query head, key head
 
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i, 1);
       mbar_init(k_empty + i, 1);
@@ -559,7 +624,10 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
       mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 4);  // one arrival per softmax warp of the tile
       mbar_init(o_done + i, 1);
+      mbar_init(u_full + i, 1);
+      mbar_init(u_empty + i, 1 + 4 * NT);  // the issuer and the softmax warps
     }
+    mbar_init(asked, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -573,71 +641,107 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     tmem_relinquish();
   }
   grid_dep_sync();
-  if (warp == 2) {
-    const Unit u = unit_of(p, NT * p.tokens, blockIdx.x - hu * per_head);
-    if (lane == 0) *found = u;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
-  const Unit& u = *found;
-  const int fused = u.fused, j0 = u.j0, lk = u.lk;
-  // own keys that the unit's token i sees
-  auto sees = [&](int i) { return p.causal ? min(max(u.sees + i, 0), lk) : lk; };
-  int n[2] = {0, 0};  // key tiles of each tile of rows
-#pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    const int end = min((x + 1) * p.tokens, u.tokens);
-    if (end > x * p.tokens) n[x] = min(max(fused + (sees(end - 1) + PT - 1) / PT - j0, 0), u.most);
-  }
-  const int nkb = max(n[0], n[1]);
-  // keys of tile j (of this part) that exist
-  auto keys_of = [&](int j) {
-    const int t = j0 + j;
-    return t < fused ? p.n_prefix - t * PT : lk - (t - fused) * PT;
+  auto wait = [&](uint64_t* bar, uint32_t ph) {
+    const bool w = mbar_wait_warp(bar, ph, abort_flag);
+    tc_fence_after();
+    return w;
   };
-  auto last_user = [&](int j) { return j < n[1] ? 1 : 0; };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(M::REGS_ISSUE));
-    if (warp == 0 && lane == 0) {
-      // ---------------- TMA producer ----------------
-      if (nkb > 0) {
-        const int rows = p.tokens * p.together, tiles = (n[0] > 0) + (n[1] > 0);
-        mbar_arrive_expect_tx(q_full, tiles * (DH / 64) * rows * 128);
-        for (int x = 0; x < NT; ++x)
-          for (int c = 0; c < DH / 64 && n[x] > 0; ++c)
-            tma_load_3d(sQ + x * M::TILE + c * PT_CHUNK, &tmQ, c * 64, head0, u.q0 + x * p.tokens, q_full);
+    if (warp == 0) {
+      // ---------------- units and TMA ----------------
+      int at = blockIdx.x, c = 0, qn = 0, kn = 0, vn = 0, asks = 0;  // unit; units, Q, K and V tiles, requests so far
+      bool ok = true, left = true;
+      while (ok && left) {
+        bool ask = true;  // for the next unit, once
+        auto request = [&]() {
+          if (lane == 0) {
+            fence_proxy_async_smem();  // the last answer has been read
+            mbar_arrive_expect_tx(asked, 16);
+            next_cta_request(response, asked);
+          }
+          ask = false;
+        };
+        if (!(ok = wait(u_empty + (c & 1), ((c >> 1) & 1) ^ 1))) break;
+        const Unit& u = units[c & 1];
+        {
+          const Unit found = unit_of(p, NT, at);
+          if (lane == 0) units[c & 1] = found;
+        }
+        __syncwarp();
+        if (u.tokens > 0) {
+          if (lane == 0) mbar_arrive(u_full + (c & 1));
+          ++c;
+          const int nkb = max(u.n[0], u.n[1]), head = u.head0 / p.group;
+          if (nkb > 0) {
+            if (!(ok = wait(q_empty, (qn & 1) ^ 1))) break;
+            if (lane == 0) {
+              const int tiles = (u.n[0] > 0) + (u.n[1] > 0);
+              mbar_arrive_expect_tx(q_full, tiles * (DH / 64) * p.tokens * p.together * 128);
+              for (int x = 0; x < NT; ++x)
+                for (int d = 0; d < DH / 64 && u.n[x] > 0; ++d)
+                  tma_load_3d(sQ + x * M::TILE + d * PT_CHUNK, &tmQ, d * 64, u.head0, u.q0 + x * p.tokens, q_full);
+            }
+            ++qn;
+          }
+          for (int j = 0; j < nkb; ++j) {
+            const int t = u.j0 + j;
+            const bool pre = t < u.fused;
+            const int row = pre ? t * PT : u.k0 + (t - u.fused) * PT;
+            const CUtensorMap *mk = pre ? &tmPK : &tmK, *mv = pre ? &tmPV : &tmV;
+            if (ask && j >= nkb - 3) request();
+            const int ks = kn % PT_STAGES, vs = vn % PT_STAGES;
+            if (!(ok = wait(k_empty + ks, ((kn / PT_STAGES) & 1) ^ 1))) break;
+            if (lane == 0) {
+              mbar_arrive_expect_tx(k_full + ks, M::TILE);
+              for (int d = 0; d < DH / 64; ++d)
+                tma_load_2d(sK + ks * M::TILE + d * PT_CHUNK, mk, head * DH + d * 64, row, k_full + ks);
+            }
+            ++kn;
+            if (!(ok = wait(v_empty + vs, ((vn / PT_STAGES) & 1) ^ 1))) break;
+            if (lane == 0) {
+              mbar_arrive_expect_tx(v_full + vs, M::TILE);
+              for (int d = 0; d < DH / 64; ++d)
+                tma_load_2d(sV + vs * M::TILE + d * PT_CHUNK, mv, head * DH + d * 64, row, v_full + vs);
+            }
+            ++vn;
+          }
+        }
+        if (ok && ask) request();
+        if (!ask) {
+          // also after an abort: the answer may not come when the CTA has gone
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(asked, asks & 1) && global_ns() - t0 < kWaitLimitNs) {
+          }
+          if (!__all_sync(0xffffffffu, mbar_try_wait(asked, asks & 1))) {
+            *abort_flag = 1;
+            ok = false;
+          }
+          ++asks;
+          __syncwarp();
+          left = ok && next_cta(response, &at);
+          __syncwarp();
+        }
       }
-      int kj = 0, vj = 0;  // tiles issued
-      for (int j = 0; j < nkb; ++j) {
-        const int st = j % PT_STAGES, t = j0 + j;
-        const uint32_t ph = ((j / PT_STAGES) & 1) ^ 1;
-        const bool pre = t < fused;
-        const int row = pre ? t * PT : u.k0 + (t - fused) * PT;
-        const CUtensorMap *mk = pre ? &tmPK : &tmK, *mv = pre ? &tmPV : &tmV;
-        if (!mbar_wait(k_empty + st, ph, abort_flag)) break;
-        uint8_t* k = sK + st * M::TILE;
-        mbar_arrive_expect_tx(k_full + st, M::TILE);
-        for (int c = 0; c < DH / 64; ++c) tma_load_2d(k + c * PT_CHUNK, mk, head * DH + c * 64, row, k_full + st);
-        ++kj;
-        if (!mbar_wait(v_empty + st, ph, abort_flag)) break;
-        uint8_t* v = sV + st * M::TILE;
-        mbar_arrive_expect_tx(v_full + st, M::TILE);
-        for (int c = 0; c < DH / 64; ++c) tma_load_2d(v + c * PT_CHUNK, mv, head * DH + c * 64, row, v_full + st);
-        ++vj;
+      if (ok && (ok = wait(u_empty + (c & 1), ((c >> 1) & 1) ^ 1)) && lane == 0) {
+        units[c & 1].tokens = -1;
+        mbar_arrive(u_full + (c & 1));
       }
-      if (vj < nkb) {
+      if (!ok) {
         // wait (bounded) for copies still in flight before the CTA may exit
         const uint64_t t0 = global_ns();
         auto landed = [&](uint64_t* bar, uint32_t ph) {
           while (!mbar_try_wait(bar, ph) && global_ns() - t0 < kWaitLimitNs) {
           }
         };
-        landed(q_full, 0);
-        for (int j = max(0, kj - PT_STAGES); j < kj; ++j) landed(k_full + j % PT_STAGES, (j / PT_STAGES) & 1);
-        for (int j = max(0, vj - PT_STAGES); j < vj; ++j) landed(v_full + j % PT_STAGES, (j / PT_STAGES) & 1);
+        if (qn > 0) landed(q_full, (qn - 1) & 1);
+        for (int j = max(0, kn - PT_STAGES); j < kn; ++j) landed(k_full + j % PT_STAGES, (j / PT_STAGES) & 1);
+        for (int j = max(0, vn - PT_STAGES); j < vn; ++j) landed(v_full + j % PT_STAGES, (j / PT_STAGES) & 1);
       }
     } else if (warp == 1) {
       // ---------------- MMA issuer (converged warp, one elected lane issues) ----------------
@@ -645,87 +749,113 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
       constexpr uint32_t idesc_o = (F16 ? idesc_f16_f32(PT, DH) : idesc_bf16_f32(PT, DH)) | 1u << 16;  // B along its rows
       const uint32_t q_addr = smem_u32(sQ), k_addr = smem_u32(sK), v_addr = smem_u32(sV);
       // K step kk of a tile: 64-column chunk kk / 4, 32 bytes per step inside it (16-byte units)
-      auto koff = [](int kk) { return (uint64_t)(((kk >> 2) * PT_CHUNK + (kk & 3) * 32) >> 4); };
-      // S of tile x and key tile j; release: the tile's K is no longer needed
-      auto issue_s = [&](int x, int j, bool release) {
-        const uint64_t qd = sw128_desc(q_addr + x * M::TILE);
-        const uint64_t kd = sw128_desc(k_addr + (j % PT_STAGES) * M::TILE);
-        if (elect_one()) {
+      auto koff = [](int kk) { return (uint32_t)(((kk >> 2) * PT_CHUNK + (kk & 3) * 32) >> 4); };
+      int base = 0, qn = 0;  // key tiles of the units before; units with any
+      int done0 = 0, done1 = 0;  // those of each tile of rows
+      bool ok = true;
+      for (int c = 0; ok; ++c) {
+        if (!(ok = wait(u_full + (c & 1), (c >> 1) & 1))) break;
+        const Unit& u = units[c & 1];
+        const int n0 = u.n[0], n1 = NT == 2 ? u.n[1] : 0, nkb = max(n0, n1), fused = u.fused, j0 = u.j0, lk = u.lk;
+        if (u.tokens < 0) break;
+        int scores = n0 + n1;  // products that still need the queries
+        // S of tile x and key tile j; release: the tile's K is no longer needed
+        auto issue_s = [&](int x, int j, bool release) {
+          const int st = (base + j) % PT_STAGES;
+          const uint32_t qd = desc_k(q_addr + x * M::TILE);
+          const uint32_t kd = desc_k(k_addr + st * M::TILE);
+          const bool last = --scores == 0;
+          if (elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < DH / 16; ++kk)
-            mma_bf16(tmem + x * 128, qd + koff(kk), kd + koff(kk), idesc_s, kk > 0 ? 1u : 0u);
-          mma_commit(s_full + x);
-          if (release) mma_commit(k_empty + j % PT_STAGES);
-        }
-        __syncwarp();
-      };
-      // release: the tile's V is no longer needed; done: no other product follows for tile x
-      auto issue_pv = [&](int x, int j, bool release, bool done) {
-        const uint64_t vd = sw128_desc_mn(v_addr + (j % PT_STAGES) * M::TILE);
-        if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < PT / 16; ++kk)
-            mma_bf16_ts(tmem + NT * 128 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
-                        (j > 0 || kk > 0) ? 1u : 0u);
-          if (release) mma_commit(v_empty + j % PT_STAGES);
-          if (done) mma_commit(o_done + x);
-        }
-        __syncwarp();
-      };
-      auto wait = [&](uint64_t* bar, uint32_t ph) {
-        const bool w = mbar_wait_warp(bar, ph, abort_flag);
-        tc_fence_after();
-        return w;
-      };
-      auto k_there = [&](int j) { return wait(k_full + j % PT_STAGES, (j / PT_STAGES) & 1); };
-      // V of tile j, zeros past its last key: only the prefix's last tile and the sequence's can end early
-      const int ends0 = fused - 1 - j0, ends1 = fused + (lk + PT - 1) / PT - 1 - j0;
-      auto v_there = [&](int j) {
-        if (!wait(v_full + j % PT_STAGES, (j / PT_STAGES) & 1)) return false;
-        if (j == ends0 || j == ends1) {
-          for (int i = keys_of(j) * (DH / 8) + lane; i < PT * (DH / 8); i += 32) {
-            const int row = i / (DH / 8), piece = i % (DH / 8);
-            *reinterpret_cast<uint4*>(sV + (j % PT_STAGES) * M::TILE + piece / 8 * PT_CHUNK + row * 128 + piece % 8 * 16) =
-                make_uint4(0u, 0u, 0u, 0u);
+            for (int kk = 0; kk < DH / 16; ++kk)
+              mma_ss(tmem + x * 128, qd + koff(kk), kd + koff(kk), idesc_s, kk > 0 ? 1u : 0u);
+            mma_commit(s_full + x);
+            if (release) mma_commit(k_empty + st);
+            if (last) mma_commit(q_empty);
           }
-          fence_proxy_async_smem();
           __syncwarp();
-        }
-        return true;
-      };
-      const int both = (NT == 2 ? min(n[0], n[1]) : n[0]) - 1;  // steps after which all tiles go on
-      bool ok = nkb > 0 && wait(q_full, 0) && k_there(0);
-      if (ok) {
-        if (n[0] > 0) issue_s(0, 0, n[1] == 0);
-        if (NT == 2 && n[1] > 0) issue_s(1, 0, true);
-      }
-      int j = 0;
-      for (; j < both && ok; ++j) {
-        // PV_j of a tile, then its S_{j+1} into the columns P_j came from (in issue order)
-        if (!(ok = v_there(j) && wait(p_full, j & 1))) break;
-        issue_pv(0, j, NT == 1, false);
-        if (!(ok = k_there(j + 1))) break;
-        issue_s(0, j + 1, NT == 1);
-        if constexpr (NT == 2) {
-          if (!(ok = wait(p_full + 1, j & 1))) break;
-          issue_pv(1, j, true, false);
-          issue_s(1, j + 1, true);
-        }
-      }
-      for (; j < nkb && ok; ++j) {  // a tile ends
-        if (!(ok = v_there(j))) break;
-        bool next = false;  // the next K tile is there
+        };
+        // release: the tile's V is no longer needed; last: no other product follows for tile x
+        auto issue_pv = [&](int x, int j, bool release, bool last) {
+          const int st = (base + j) % PT_STAGES;
+          const uint32_t vd = desc_mn(v_addr + st * M::TILE);
+          if (elect_one()) {
 #pragma unroll
-        for (int x = 0; x < NT; ++x) {
-          if (!ok || j >= n[x]) continue;
-          if (!(ok = wait(p_full + x, j & 1))) break;
-          issue_pv(x, j, x == last_user(j), j == n[x] - 1);
-          if (j + 1 < n[x]) {
-            if (!next && !(ok = k_there(j + 1))) break;
-            next = true;
-            issue_s(x, j + 1, x == last_user(j + 1));
+            for (int kk = 0; kk < PT / 16; ++kk)
+              mma_ts(tmem + NT * 128 + x * 128, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), idesc_o,
+                     (j > 0 || kk > 0) ? 1u : 0u);
+            if (release) mma_commit(v_empty + st);
+            if (last) mma_commit(o_done + x);
           }
+          __syncwarp();
+        };
+        auto k_there = [&](int j) { return wait(k_full + (base + j) % PT_STAGES, ((base + j) / PT_STAGES) & 1); };
+        auto p_there = [&](int x, int j) { return wait(p_full + x, ((x ? done1 : done0) + j) & 1); };
+        // V of tile j, zeros past its last key: only the prefix's last tile and the sequence's can end early
+        const int ends0 = fused - 1 - j0, ends1 = fused + (lk + PT - 1) / PT - 1 - j0;
+        auto v_there = [&](int j) {
+          const int st = (base + j) % PT_STAGES;
+          if (!wait(v_full + st, ((base + j) / PT_STAGES) & 1)) return false;
+          if (j == ends0 || j == ends1) {
+            const int t = j0 + j, keys = t < fused ? p.n_prefix - t * PT : lk - (t - fused) * PT;
+            for (int i = keys * 128 + lane * 16; i < PT_CHUNK; i += 512)  // a chunk's rows lie together
+#pragma unroll
+              for (int d = 0; d < DH / 64; ++d)
+                *reinterpret_cast<uint4*>(sV + st * M::TILE + d * PT_CHUNK + i) = make_uint4(0u, 0u, 0u, 0u);
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          return true;
+        };
+        auto last_user = [&](int j) { return j < n1 ? 1 : 0; };
+        if (nkb > 0) {
+          if (!(ok = wait(q_full, qn & 1))) break;
+          ++qn;
+          // PV_j of a tile, then its S_{j+1} into the columns P_j came from (in issue order): first the S_0 alone,
+          // then steps after which all tiles go on, then those where one ends
+          const int both = max((NT == 2 ? min(n0, n1) : n0) - 1, 0);
+          int j = -1;
+#pragma unroll 1
+          for (int end = 0; ok; end = nkb) {
+#pragma unroll 1
+            for (; j < end && ok; ++j) {
+              if (j >= 0 && !(ok = v_there(j))) break;
+              bool next = false;  // the next K tile is there
+#pragma unroll 1
+              for (int x = 0; x < NT; ++x) {
+                const int nx = x ? n1 : n0;
+                if (j >= nx) continue;
+                if (j >= 0) {
+                  if (!(ok = p_there(x, j))) break;
+                  issue_pv(x, j, x == last_user(j), j == nx - 1);
+                }
+                if (j + 1 < nx) {
+                  if (!next && !(ok = k_there(j + 1))) break;
+                  next = true;
+                  issue_s(x, j + 1, x == last_user(j + 1));
+                }
+              }
+            }
+            if (end == nkb) break;
+            for (; j < both && ok; ++j) {
+              if (!(ok = v_there(j) && p_there(0, j))) break;
+              issue_pv(0, j, NT == 1, false);
+              if (!(ok = k_there(j + 1))) break;
+              issue_s(0, j + 1, NT == 1);
+              if constexpr (NT == 2) {
+                if (!(ok = p_there(1, j))) break;
+                issue_pv(1, j, true, false);
+                issue_s(1, j + 1, true);
+              }
+            }
+          }
+          if (!ok) break;
+          base += nkb;
+          done0 += n0;
+          done1 += n1;
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(u_empty + (c & 1));
       }
       if (elect_one()) {
         mma_commit(drain);
@@ -739,159 +869,163 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(M::REGS_SOFTMAX));
     // ---------------- softmax warpgroups (warps 4..7: tile A, 8..11: tile B) ----------------
     const int x = NT == 2 ? (warp - 4) >> 2 : 0;
-    const int quad = warp & 3, tiles = x ? n[1] : n[0];
+    const int quad = warp & 3;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t s_addr = tmem + lane_base + x * 128;
     const uint32_t o_addr = tmem + lane_base + NT * 128 + x * 128;
-    // the thread's row: its token of the unit (none: -1), and where its output goes, for the warp's lanes that
-    // store it (worked out here, beside the loads of the first tiles)
     const int row = quad * 32 + lane, of = (unsigned)row / (unsigned)p.together;
-    const int mine = of < p.tokens && x * p.tokens + of < u.tokens ? x * p.tokens + of : -1;
-    const int own = sees(mine < 0 ? u.tokens - 1 : mine);
-    const int h = head0 + row - of * p.together;
     long* at = reinterpret_cast<long*>(smem + M::ROWS) + x * PT + quad * 32;
-    at[lane] = mine < 0 ? -1
-                        : (u.direct ? (u.q0 + mine) * p.ldo + h * DH
-                                    : (((long)u.part * p.nq + u.q0 + mine) * p.heads + h) * DH);
-    // tiles with keys that a row of the warp does not see: the prefix's last one, where it is not full, and from
-    // the first one on that ends behind the warp's first row's keys
-    const int cut0 = p.n_prefix % PT ? fused - 1 : -1;
-    const int cut1 = fused + (int)__reduce_min_sync(0xffffffffu, (unsigned)own) / PT;
-    float m_use = -INFINITY, l = 0.f;
+    uint8_t* buf = smem + M::OUT + x * PT_OUT + quad * 32 * PT_LD;
+    int steps = 0, outputs = 0;  // key tiles, and units with any, so far
     bool ok = true;
-    for (int j = 0; j < tiles; ++j) {
-      const bool w = mbar_wait(s_full + x, j & 1, abort_flag);
-      if (!__all_sync(0xffffffffu, w)) {
-        ok = false;
-        break;
-      }
-      tc_fence_after();
-      const int t = j0 + j;
-      // the whole S row in registers: four loads, one wait
-      uint32_t r[PT];
-#pragma unroll
-      for (int c = 0; c < PT / 32; ++c) tmem_ld32_nowait(s_addr + c * 32, r + c * 32);
-      tmem_ld_wait();
-      if (t == cut0 || t >= cut1) {
-        const int kvalid = t < fused ? p.n_prefix - t * PT : own - (t - fused) * PT;  // keys that the row sees
-#pragma unroll
-        for (int i = 0; i < PT; ++i)
-          if (i >= kvalid) r[i] = __float_as_uint(-INFINITY);
-      }
-      // row maximum: four independent chains of three-input maxima
-      float mq[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) mq[u] = fmaxf(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
-#pragma unroll
-      for (int i = 8; i < PT; i += 8)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          mq[u] = max3(mq[u], __uint_as_float(r[i + 2 * u]), __uint_as_float(r[i + 2 * u + 1]));
-      const float mx2 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * p.scale_log2;
-      float alpha = 1.f;
-      if (mx2 > m_use + 8.f) {
-        alpha = ex2(m_use - mx2);
-        m_use = mx2;
-        l *= alpha;
-      }
-      const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
-      float ls0 = 0.f, ls1 = 0.f;
-#pragma unroll
-      for (int c = 0; c < PT / 32; ++c) {
-        uint32_t pk[16];
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          float x0, x1;
-          fma2(x0, x1, __uint_as_float(r[c * 32 + i]), __uint_as_float(r[c * 32 + i + 1]), p.scale_log2, neg_m);
-          const float a0 = ex2(x0), a1 = ex2(x1);
-          add2(ls0, ls1, a0, a1);
-          pk[i / 2] = pack16<F16>(a0, a1);
+    for (int c = 0; ok; ++c) {
+      if (!(ok = wait(u_full + (c & 1), (c >> 1) & 1))) break;
+      const Unit& u = units[c & 1];
+      if (u.tokens < 0) break;
+      const int tiles = u.n[x];
+      // the thread's row: its token of the unit, and how many keys from the part's first tile on it sees (those
+      // of a last prefix tile that is not full counted as 128)
+      auto token = [&]() { return of < p.tokens && x * p.tokens + of < u.tokens ? x * p.tokens + of : -1; };
+      const int own = sees_of(p, u, token() < 0 ? u.tokens - 1 : token());
+      const int limit = own + (u.fused - u.j0) * PT;
+      // tiles with keys that a row of the warp does not see: that last one of the prefix, and all from the first
+      // on that ends behind the keys of the warp's first row
+      const int cut0 = p.n_prefix % PT ? u.fused - 1 - u.j0 : -1;
+      const int cut1 = u.fused - u.j0 + (int)__reduce_min_sync(0xffffffffu, (unsigned)own) / PT;
+      float m_use = -INFINITY, l = 0.f;
+      for (int j = 0; j < tiles; ++j) {
+        const bool w = mbar_wait(s_full + x, (steps + j) & 1, abort_flag);
+        if (!__all_sync(0xffffffffu, w)) {
+          ok = false;
+          break;
         }
-        tmem_st16(s_addr + c * 16, pk);
-      }
-      l += ls0 + ls1;
-      // O_x holds PV of every earlier key tile (the S of this tile was issued after it);
-      // rescale it before this tile's PV is issued
-      if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-#pragma unroll 1
-        for (int c = 0; c < DH / 32; ++c) {
-          float o[32];
-          tmem_ld32(o_addr + c * 32, o);
+        tc_fence_after();
+        // the whole S row in registers: four loads, one wait
+        uint32_t r[PT];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] *= alpha;
-          tmem_st32(o_addr + c * 32, o);
+        for (int i = 0; i < PT / 32; ++i) tmem_ld32_nowait(s_addr + i * 32, r + i * 32);
+        tmem_ld_wait();
+        if (j == cut0 || j >= cut1) {
+          const int kvalid = j == cut0 ? p.n_prefix % PT : limit - j * PT;  // keys that the row sees
+#pragma unroll
+          for (int i = 0; i < PT; ++i)
+            if (i >= kvalid) r[i] = __float_as_uint(-INFINITY);
         }
-      }
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_full + x);
-    }
-    if (ok && tiles > 0) ok = __all_sync(0xffffffffu, mbar_wait(o_done + x, 0, abort_flag));
-    tc_fence_after();
-    if (ok && x * p.tokens < u.tokens) {
-      const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
-      const float f = 1.f / l;
-      if (mine >= 0) {  // the row's maximum and sum
-        const long r = (long)(u.q0 + mine) * p.heads + h;
-        if (!u.direct)
-          p.part_ml[(long)u.part * p.nq * p.heads + r] = make_float2(any ? m_use : -INFINITY, l);
-        else if (p.lse)
-          p.lse[r] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
-      }
-      // through shared memory (where a tile's queries were, which no product reads any more), so that a store
-      // covers whole runs of a few rows: 64 columns in 16 bits, or 32 of a part in fp32, at a time
-      uint8_t* buf = smem + M::OUT + x * (DH == 128 ? M::TILE : PT_OUT) + quad * 32 * PT_LD;
-      long to[8];
+        // row maximum: four independent chains of three-input maxima
+        float mq[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) to[i] = at[4 * i + (lane >> 3)];
-      const bool seen = any && tiles > 0;
-      if (u.direct) {
+        for (int i = 0; i < 4; ++i) mq[i] = fmaxf(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+#pragma unroll
+        for (int i = 8; i < PT; i += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            mq[k] = max3(mq[k], __uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+        const float mx2 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * p.scale_log2;
+        float alpha = 1.f;
+        if (mx2 > m_use + 8.f) {
+          alpha = ex2(m_use - mx2);
+          m_use = mx2;
+          l *= alpha;
+        }
+        const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
+        float ls0 = 0.f, ls1 = 0.f;
+#pragma unroll
+        for (int b = 0; b < PT / 32; ++b) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            float x0, x1;
+            fma2(x0, x1, __uint_as_float(r[b * 32 + i]), __uint_as_float(r[b * 32 + i + 1]), p.scale_log2, neg_m);
+            const float a0 = ex2(x0), a1 = ex2(x1);
+            add2(ls0, ls1, a0, a1);
+            pk[i / 2] = pack16<F16>(a0, a1);
+          }
+          tmem_st16(s_addr + b * 16, pk);
+        }
+        l += ls0 + ls1;
+        // O_x holds PV of every earlier key tile (the S of this tile was issued after it);
+        // rescale it before this tile's PV is issued
+        if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
 #pragma unroll 1
-        for (int c = 0; c < DH; c += 64) {
-          uint32_t o[64];
-          if (tiles > 0) {
-            tmem_ld32_nowait(o_addr + c, o);
-            tmem_ld32_nowait(o_addr + c + 32, o + 32);
-            tmem_ld_wait();
-          }
+          for (int b = 0; b < DH / 32; ++b) {
+            float o[32];
+            tmem_ld32(o_addr + b * 32, o);
 #pragma unroll
-          for (int i = 0; i < 64; i += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = seen ? pack16<F16>(__uint_as_float(o[i + 2 * e]) * f, __uint_as_float(o[i + 2 * e + 1]) * f) : 0u;
-            *reinterpret_cast<uint4*>(buf + lane * PT_LD + i * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < 32; ++i) o[i] *= alpha;
+            tmem_st32(o_addr + b * 32, o);
           }
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + x);
+      }
+      if (!ok) break;
+      steps += tiles;
+      if (tiles > 0 && !(ok = wait(o_done + x, outputs++ & 1))) break;
+      if (x * p.tokens < u.tokens) {
+        const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
+        const float f = 1.f / l;
+        const int mine = token(), h = u.head0 + row - of * p.together;
+        // where the row's output goes, for the lanes that store it
+        at[lane] = mine < 0 ? -1
+                            : (u.direct ? (u.q0 + mine) * p.ldo + h * DH
+                                        : (((long)u.part * p.nq + u.q0 + mine) * p.heads + h) * DH);
+        if (mine >= 0) {  // the row's maximum and sum
+          const long i = (long)(u.q0 + mine) * p.heads + h;
+          if (!u.direct)
+            p.part_ml[(long)u.part * p.nq * p.heads + i] = make_float2(any ? m_use : -INFINITY, l);
+          else if (p.lse)
+            p.lse[i] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        }
+        // through shared memory, so that a store covers whole runs of a few rows: 64 bytes a row at a time, 32
+        // columns in 16 bits or 16 of a part in fp32
+        __syncwarp();
+        long to[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = at[8 * i + (lane >> 2)];
+        const bool seen = any && tiles > 0, direct = u.direct;
+        auto turn = [&](const uint32_t* w, int col) {  // 16 words a row, to column col of the output
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<uint4*>(buf + lane * PT_LD + i * 4) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint4 v = *reinterpret_cast<const uint4*>(buf + (4 * i + (lane >> 3)) * PT_LD + (lane & 7) * 16);
-            if (to[i] >= 0) *reinterpret_cast<uint4*>(p.o + to[i] + c + (lane & 7) * 8) = v;
+          for (int i = 0; i < 4; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(buf + (8 * i + (lane >> 2)) * PT_LD + (lane & 3) * 16);
+            if (to[i] >= 0) {
+              if (direct)
+                *reinterpret_cast<uint4*>(p.o + to[i] + col + (lane & 3) * 8) = v;
+              else
+                *reinterpret_cast<uint4*>(p.part_o + to[i] + col + (lane & 3) * 4) = v;
+            }
           }
           __syncwarp();
-        }
-      } else {
+        };
 #pragma unroll 1
-        for (int c = 0; c < DH; c += 32) {
+        for (int b = 0; b < DH; b += 32) {
           uint32_t o[32];
           if (tiles > 0) {
-            tmem_ld32_nowait(o_addr + c, o);
+            tmem_ld32_nowait(o_addr + b, o);
             tmem_ld_wait();
           }
+          if (direct) {
+            uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            *reinterpret_cast<uint4*>(buf + lane * PT_LD + i * 4) =
-                seen ? make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_uint4(0u, 0u, 0u, 0u);
-          __syncwarp();
+            for (int i = 0; i < 16; ++i)
+              w[i] = seen ? pack16<F16>(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f) : 0u;
+            turn(w, b);
+          } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint4 v = *reinterpret_cast<const uint4*>(buf + (4 * i + (lane >> 3)) * PT_LD + (lane & 7) * 16);
-            if (to[i] >= 0) *reinterpret_cast<uint4*>(p.part_o + to[i] + c + (lane & 7) * 4) = v;
+            for (int i = 0; i < 32; ++i) o[i] = seen ? o[i] : 0u;
+            turn(o, b);
+            turn(o + 16, b + 16);
           }
-          __syncwarp();
         }
+        tc_fence_before();  // the next unit's products into O come after these loads
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(u_empty + (c & 1));
     }
   }
   tc_fence_before();
@@ -1051,7 +1185,6 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   // units of 256 rows where there are enough of them
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
   t.rows = units(256) * 2 > sms ? 256 : 128;
-  if (const char* e = std::getenv("X_ROWS")) t.rows = std::atoi(e);
   const bool all_rows = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
   if (a.n_prefix && !all_rows) t.few = 0;
   auto chunk = [](long keys, long parts) { return (int)(cdiv(cdiv(keys, parts), PT) * PT); };
