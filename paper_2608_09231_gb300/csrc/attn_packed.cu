@@ -131,6 +131,7 @@ template <bool F16, int DH>
 __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const PackedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ long before[F_TH], warp_sum[F_WARPS];
+  __shared__ Span spans[F_TH];  // of the sequences in `before`
   constexpr int LD = DH + 4, U = DH / 64, J = DH / 32;
   float* so = reinterpret_cast<float*>(smem);                                      // [F_WARPS][16][LD]
   float2* sml = reinterpret_cast<float2*>(smem + F_WARPS * F_ROWS * LD * 4);       // [F_WARPS][16]
@@ -142,8 +143,9 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
   auto add_up = [&](int first) {
     long w = 0;
     const int i = first + (int)threadIdx.x;
+    Span s{};
     if (i < p.seqs) {
-      const Span s = span_of(p, i);
+      s = span_of(p, i);
       w = few_units(p, s.lq) * (p.split ? few_length(s.lk) : 1);
     }
     long sum = w;
@@ -162,6 +164,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
       all += warp_sum[v];
     }
     before[threadIdx.x] = mine + sum - w;
+    spans[threadIdx.x] = s;
     __syncthreads();
     return all;
   };
@@ -194,7 +197,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
 #pragma unroll
     for (int o = F_TH / 2; o > 0; o /= 2)
       if (first + lo + o < p.seqs && before[lo + o] <= pos - base) lo += o;
-    const Span s = span_of(p, first + lo);
+    const Span s = spans[lo];
     const int all = p.split ? few_length(s.lk) : 1, blocks = (s.lq * G + F_ROWS - 1) / F_ROWS;
     const long off = pos - base - before[lo], unit = off / all;
     const int at = (int)(off - unit * all);
@@ -1038,7 +1041,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
 }
 
 namespace {
-constexpr int JN_TH = 128;
+constexpr int JN_TH = 128, JR_TH = 256;
 
 // The sequence of query row t: the last one that starts at or before it.  Called by a whole warp.
 BAG_DEV int sequence_of(const PackedParams& p, int t) {
@@ -1055,7 +1058,45 @@ BAG_DEV int sequence_of(const PackedParams& p, int t) {
 }
 }  // namespace
 
-// Joins the parts of a row and head: their weights first, then DH / 4 lanes a part, in a fixed order.
+namespace {
+// Where the sums of a row's and head's parts lie.
+struct Parts {
+  long regular;    // of part 0 among part_ml (times dh: among part_o)
+  long piece;      // of the few-row kernel's first piece among piece_ml, -1: none
+  int parts1, n;   // parts of the prefix; of all (none: the output is there already)
+  long step;       // from part to part
+  BAG_DEV long at(int i, bool* whole) const {
+    const int k = i - parts1;
+    *whole = k < 0 || piece < 0;  // of pieces, the first CTA's starts the unit (1), the others' do not
+    return *whole ? regular + i * step : piece + (long)k * 2 * F_ROWS + (k == 0 ? F_ROWS : 0);
+  }
+};
+BAG_DEV Parts parts_of(const PackedParams& p, int seq, const Span& s, int tok, int h) {
+  Parts a;
+  a.regular = (long)tok * p.heads + h;
+  a.step = (long)p.nq * p.heads;
+  a.piece = -1;
+  a.parts1 = p.parts1;
+  int own = 1;
+  if (!p.few) {
+    own = own_parts(p, s.lk);
+  } else if (p.split) {
+    const int r = (tok - s.q0) * p.group + h % p.group, blocks = (s.lq * p.group + F_ROWS - 1) / F_ROWS;
+    const long length = few_length(s.lk), share = p.place[0];
+    const long start = p.place[1 + seq] + ((long)(h / p.group) * blocks + r / F_ROWS) * length;
+    const long c0 = start / share, c1 = (start + length - 1) / share;
+    if (c1 > c0) {
+      own = (int)(c1 - c0) + 1;
+      a.piece = c0 * 2 * F_ROWS + r % F_ROWS;
+    }
+  }
+  a.n = p.parts1 == 0 && own <= 1 ? 0 : p.parts1 + own;
+  return a;
+}
+}  // namespace
+
+// Joins the parts of a row and head: their weights first, then DH / 4 lanes a part, in a fixed order.  For few rows
+// with many parts.
 template <bool F16, int DH>
 __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) {
   constexpr int L = DH / 4, GROUPS = JN_TH / L;
@@ -1068,36 +1109,14 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   const int seq = sequence_of(p, tok);
   const Span s = span_of(p, seq);
   if (tok < s.q0 || tok >= s.q0 + s.lq) return;
-  int own = 1;
-  long piece = -1;  // the first of the few-row kernel's
-  if (!p.few) {
-    own = own_parts(p, s.lk);
-  } else if (p.split) {
-    const int r = (tok - s.q0) * p.group + h % p.group, blocks = (s.lq * p.group + F_ROWS - 1) / F_ROWS;
-    const long length = few_length(s.lk), share = p.place[0];
-    const long start = p.place[1 + seq] + ((long)(h / p.group) * blocks + r / F_ROWS) * length;
-    const long c0 = start / share, c1 = (start + length - 1) / share;
-    if (c1 > c0) {
-      own = (int)(c1 - c0) + 1;
-      piece = c0 * 2 * F_ROWS + r % F_ROWS;
-    }
-  }
-  const int parts = p.parts1 + own;
-  if (p.parts1 == 0 && own <= 1) return;  // written by its only part
-  // where part i's sums lie; of pieces, the first CTA's starts the unit (1), the others' do not
-  auto place = [&](int i, const float2*& ml) {
-    const int k = i - p.parts1;
-    const bool whole = k < 0 || piece < 0;
-    const long at = whole ? ((long)i * p.nq + tok) * p.heads + h : piece + (long)k * 2 * F_ROWS + (k == 0 ? F_ROWS : 0);
-    ml = (whole ? p.part_ml : p.piece_ml) + at;
-    return (whole ? p.part_o : p.piece_o) + at * DH;
-  };
+  const Parts a = parts_of(p, seq, s, tok, h);
+  if (a.n == 0) return;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = threadIdx.x / L, x = threadIdx.x % L;
   float top = -INFINITY;
-  for (int i = threadIdx.x; i < parts; i += JN_TH) {
-    const float2* ml;
-    place(i, ml);
-    top = fmaxf(top, ml->x);
+  for (int i = threadIdx.x; i < a.n; i += JN_TH) {
+    bool whole;
+    const long at = a.at(i, &whole);
+    top = fmaxf(top, (whole ? p.part_ml : p.piece_ml)[at].x);
   }
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -1107,16 +1126,17 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   for (int i = 0; i < JN_TH / 32; ++i) top = fmaxf(top, red[i]);
   float den = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = 0; i0 < parts; i0 += JN_TH) {
+  for (int i0 = 0; i0 < a.n; i0 += JN_TH) {
     if (i0) __syncthreads();
-    if (i0 + (int)threadIdx.x < parts) {  // weights of the next parts (0: no key of the part is seen)
-      const float2* ml;
-      from[threadIdx.x] = place(i0 + threadIdx.x, ml);
-      const float2 f = *ml;
+    if (i0 + (int)threadIdx.x < a.n) {  // weights of the next parts (0: no key of the part is seen)
+      bool whole;
+      const long at = a.at(i0 + threadIdx.x, &whole);
+      const float2 f = (whole ? p.part_ml : p.piece_ml)[at];
+      from[threadIdx.x] = (whole ? p.part_o : p.piece_o) + at * DH;
       weight[threadIdx.x] = make_float2(f.y == 0.f ? 0.f : ex2(f.x - top), f.y);
     }
     __syncthreads();
-    const int n = min(JN_TH, parts - i0);
+    const int n = min(JN_TH, a.n - i0);
 #pragma unroll 8
     for (int i = g; i < n; i += GROUPS) {
       const float2 f = weight[i];
@@ -1152,6 +1172,66 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   if (p.lse && x == 0) p.lse[(long)tok * p.heads + h] = (top + log2f(den)) * 0.6931471805599453f;
 }
 
+// The same for many rows with few parts: a CTA a row and some of its heads, a warp a head at a time, DH / 32 columns
+// a lane.  Bound: HBM or L2, which the loads of a CTA's heads reach together (a CTA for each head took 80 us
+// of the 130 for 2048 rows x 32 heads in two parts).
+template <bool F16, int DH>
+__global__ void __launch_bounds__(JR_TH) attn_join_rows_kernel(const PackedParams p) {
+  constexpr int C = DH / 32;
+  grid_dep_sync();
+  const int tok = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int seq = sequence_of(p, tok);
+  const Span s = span_of(p, seq);
+  if (tok < s.q0 || tok >= s.q0 + s.lq) return;
+#pragma unroll 2
+  for (int h = blockIdx.y * (JR_TH / 32) + warp; h < p.heads; h += gridDim.y * (JR_TH / 32)) {
+    const Parts a = parts_of(p, seq, s, tok, h);
+    if (a.n == 0) continue;
+    float top = -INFINITY, den = 0.f, acc[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    for (int i0 = 0; i0 < a.n; i0 += 32) {
+      const int n = min(32, a.n - i0);
+      bool whole = true;
+      const long at = a.at(i0 + min(lane, n - 1), &whole);
+      const float2 f = (whole ? p.part_ml : p.piece_ml)[at];
+      float m = f.x;  // of 32 parts, then of those before too
+#pragma unroll
+      for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      m = fmaxf(m, top);
+      const float before = den == 0.f ? 0.f : ex2(top - m), w = f.y == 0.f ? 0.f : ex2(f.x - m);
+      top = m;
+      den *= before;
+#pragma unroll
+      for (int i = 0; i < C; ++i) acc[i] *= before;
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) {
+        const float wi = __shfl_sync(0xffffffffu, w, i), li = __shfl_sync(0xffffffffu, f.y, i);
+        const bool wh = __shfl_sync(0xffffffffu, (int)whole, i);
+        const float* v = (wh ? p.part_o : p.piece_o) + __shfl_sync(0xffffffffu, at, i) * DH + lane * C;
+        float x[C];
+        if constexpr (C == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(v);
+          x[0] = t.x, x[1] = t.y, x[2] = t.z, x[3] = t.w;
+        } else {
+          const float2 t = *reinterpret_cast<const float2*>(v);
+          x[0] = t.x, x[1] = t.y;
+        }
+        den += wi * li;
+#pragma unroll
+        for (int e = 0; e < C; ++e) acc[e] += li == 0.f ? 0.f : wi * x[e];  // no weight: x may be NaN
+      }
+    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    uint16_t* o = p.o + tok * p.ldo + (long)h * DH + lane * C;
+    if constexpr (C == 4)
+      *reinterpret_cast<uint2*>(o) = make_uint2(pack16<F16>(acc[0] * inv, acc[1] * inv), pack16<F16>(acc[2] * inv, acc[3] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(o) = pack16<F16>(acc[0] * inv, acc[1] * inv);
+    if (p.lse && lane == 0) p.lse[(long)tok * p.heads + h] = (top + log2f(den)) * 0.6931471805599453f;
+  }
+}
+
 namespace {
 // The form of a call: own keys by attn_few_kernel or the tensor cores, the prefix with all rows together (parts1)
 // or before each sequence's own keys (fused key tiles).
@@ -1184,7 +1264,7 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
     if (G % g == 0 && (PT / g * g >= PT - PT / 10 || max_q * g <= PT)) t.together = g;
   // units of 256 rows where there are enough of them
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
-  t.rows = units(256) * 2 > sms ? 256 : 128;
+  t.rows = units(256) * 2 > sms || units(256) * cdiv(max_k + a.n_prefix, PT) >= 8 * sms ? 256 : 128;
   const bool all_rows = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
   if (a.n_prefix && !all_rows) t.few = 0;
   auto chunk = [](long keys, long parts) { return (int)(cdiv(cdiv(keys, parts), PT) * PT); };
@@ -1192,8 +1272,11 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   if (all_rows) p1 = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, t.rows) * a.kv_heads)));
   t.fused = all_rows ? 0 : (int)cdiv(a.n_prefix, PT);
   const long keys = max_k + (long)t.fused * PT;
-  if (!t.few && units(t.rows) * 2 <= sms)
-    p2 = std::max(1L, std::min(keys / 1024, sms / std::max(1L, units(t.rows))));
+  // keys in parts where the longest unit would take longer than the others on one SM (half as many keys each, where
+  // lengths differ or the mask is causal), four for each SM
+  const long tiles = cdiv(keys, PT);
+  if (!t.few && units(t.rows) < 2 * sms)
+    p2 = std::max(1L, tiles / std::max(12L, tiles * units(t.rows) / (4 * sms)));
   if (p1 + p2 > most) {
     if (p1) p1 = std::max(1L, std::min(p1, most - 1));
     p2 = std::max(1L, most - p1);
@@ -1281,7 +1364,11 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
                         : launch_kernel(attn_packed_kernel<F16, DH, 1>, (unsigned)tiles, Pt<DH, 1>::THREADS,
                                         Pt<DH, 1>::BYTES, s, tq, tk, tv, tpk, tpv, p);
     if (e == cudaSuccess && (parts_of(t) || t.split))
-      e = launch_kernel(attn_join_kernel<F16, DH>, (unsigned)joins, JN_TH, 0, s, p);
+      e = joins >= 4L * sm_count()
+              ? launch_kernel(attn_join_rows_kernel<F16, DH>,
+                              dim3((unsigned)a.nq, (unsigned)std::max(1L, std::min(cdiv(a.heads, 8), 8L * sm_count() / a.nq))),
+                              JR_TH, 0, s, p)
+              : launch_kernel(attn_join_kernel<F16, DH>, (unsigned)joins, JN_TH, 0, s, p);
     return e;
   };
   using Wide = std::integral_constant<int, 128>;
