@@ -466,7 +466,7 @@ typedef struct {
   int type;               /* BAG_F32, BAG_BF16 or BAG_F16 */
   int layout;             /* BAG_ROPE_* */
   int heads, kv_heads;    /* of q; of k and v */
-  int dh, pairs;          /* 1 <= pairs <= dh / 2, dh <= 256 */
+  int dh, pairs;          /* 1 <= pairs <= dh / 2, dh even, at most 256 */
   long rows;
   const void* q; long ldq;          /* device [rows, heads * dh], row strides in elements */
   void* q_out; long ldqo;

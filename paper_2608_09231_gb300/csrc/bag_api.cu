@@ -2038,8 +2038,8 @@ static bag_status bag_rope_impl(bag_ctx* ctx, const bag_rope_args* a) {
   if ((a->type != BAG_F32 && a->type != BAG_BF16 && a->type != BAG_F16) ||
       (a->layout != BAG_ROPE_INTERLEAVED && a->layout != BAG_ROPE_HALF) || (a->inverse != 0 && a->inverse != 1))
     return fail(ctx, BAG_EINVAL, "bad rope type, layout or direction");
-  if (a->dh < 2 || a->dh > 2 * kRopePairs || a->pairs < 1 || 2 * a->pairs > a->dh)
-    return fail(ctx, BAG_EINVAL, "rope needs heads of 2 to 256 columns and 1 to dh / 2 pairs");
+  if (a->dh < 2 || a->dh > 2 * kRopePairs || a->dh % 2 || a->pairs < 1 || 2 * a->pairs > a->dh)
+    return fail(ctx, BAG_EINVAL, "rope needs heads of 2 to 256 columns, an even number, and 1 to dh / 2 pairs");
   if (a->rows < 0 || a->rows > kMaxRows || (a->q && (a->heads < 1 || a->heads > kMaxHeads)) ||
       (kv && (a->kv_heads < 1 || a->kv_heads > kMaxHeads || a->capacity < 0 || a->capacity > kMaxRows ||
               (!a->slots && a->capacity < a->rows))))

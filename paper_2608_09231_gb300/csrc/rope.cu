@@ -7,13 +7,16 @@
 // and cosine (sincospif).  A CTA computes a row's table once, in shared memory, for all heads; then a
 // thread keeps the entries of its V pairs in registers and walks the heads.
 // Bound: HBM (each element read and written once).
+#include <algorithm>
+#include <type_traits>
+
 #include "common.cuh"
 #include "kernels.h"
 
 namespace bag {
 
 namespace {
-constexpr int R_TH = 256;
+constexpr int R_TH = 256, R_HEADS = 2;
 
 template <typename T>
 BAG_DEV float r_in(T x);
@@ -32,107 +35,145 @@ BAG_DEV __half r_out(float x) { return __float2half_rn(x); }
 template <>
 BAG_DEV __nv_bfloat16 r_out(float x) { return __float2bfloat16_rn(x); }
 
-// V elements that are loaded and stored at once
+// V elements that are loaded and stored at once: 16 bytes, kept as words, or one.
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Elems {
-  T e[V];
+struct Elems {
+  uint4 w;
+  BAG_DEV void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
+  BAG_DEV void store(T* p) const { *reinterpret_cast<uint4*>(p) = w; }
+  BAG_DEV void get(float* e) const {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        e[i] = __uint_as_float(v[i]);
+      } else if constexpr (std::is_same_v<T, __half>) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+        e[2 * i] = f.x;
+        e[2 * i + 1] = f.y;
+      } else {  // bf16: the upper half of an fp32 word
+        e[2 * i] = __uint_as_float(v[i] << 16);
+        e[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+      }
+    }
+  }
+  BAG_DEV void set(const float* e) {
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4)
+        v[i] = __float_as_uint(e[i]);
+      else if constexpr (std::is_same_v<T, __half>)
+        v[i] = pack_f16x2(e[2 * i], e[2 * i + 1]);
+      else
+        v[i] = pack_bf16x2(e[2 * i], e[2 * i + 1]);
+    }
+    w = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+};
+template <typename T>
+struct Elems<T, 1> {
+  T w;
+  BAG_DEV void load(const T* p) { w = *p; }
+  BAG_DEV void store(T* p) const { *p = w; }
+  BAG_DEV void get(float* e) const { e[0] = r_in(w); }
+  BAG_DEV void set(const float* e) { w = r_out<T>(e[0]); }
 };
 }  // namespace
 
-// V: pairs of a thread's chunk (16 bytes of elements, or 1).  rows_cta rows a CTA, each by R_TH / rows_cta
-// threads.
+// A head is taken in chunks of 2 V elements, V pairs (their first and second elements, or the elements in turn)
+// or V and V columns past the rotated ones; a thread has one chunk of a row, and some of its heads.  rows_cta
+// rows a CTA, each by R_TH / rows_cta threads.  The first heads are on their way while the table is made.
+// Output elements may be the input's own (in place), so the loads of R_HEADS heads go ahead of their stores by hand.
 template <typename T, int V, bool HALF>
-__global__ void __launch_bounds__(R_TH) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(R_TH, 4) rope_kernel(const __grid_constant__ RopeArgs a) {
   __shared__ __align__(16) float2 table[R_TH];  // [rows_cta][pairs]
   grid_dep_sync();
+  using E = Elems<T, V>;
   const long row0 = (long)blockIdx.x * a.rows_cta;
+  const int per_row = R_TH / a.rows_cta, chunks = a.dh / (2 * V), lanes = per_row / chunks;
+  const int lr = threadIdx.x / per_row, at = threadIdx.x - lr * per_row;
+  const int hl = at / chunks, chunk = at - hl * chunks;
+  const long row = row0 + lr;
+  const bool works = row < a.rows && hl < lanes, turns = chunk * V < a.pairs;
+  // heads in turn: those of q, of k, of v
+  const int nq = a.q ? a.heads : 0, nk = a.k ? a.kv_heads : 0, nh = nq + nk + (a.v ? a.kv_heads : 0);
+  // a thread's two vectors of a head
+  const int o0 = turns ? (HALF ? chunk * V : 2 * chunk * V) : 2 * chunk * V;
+  const int o1 = turns && HALF ? a.pairs + chunk * V : (2 * chunk + 1) * V;
+  auto source = [&](int h) {
+    if (h < nq) return reinterpret_cast<const T*>(a.q) + row * a.ldq + (long)h * a.dh;
+    if (h < nq + nk) return reinterpret_cast<const T*>(a.k) + row * a.ldk + (long)(h - nq) * a.dh;
+    return reinterpret_cast<const T*>(a.v) + row * a.ldv + (long)(h - nq - nk) * a.dh;
+  };
+  E u[R_HEADS], w[R_HEADS];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < R_HEADS; ++i) {
+      const int h = h0 + i * lanes;
+      if (h < nh) {
+        const T* x = source(h);
+        u[i].load(x + o0);
+        w[i].load(x + o1);
+      }
+    }
+  };
+  if (works) load(hl);
+  long kv_row = row;
+  if (works && a.slots) kv_row = __ldg(a.slots + row);
   for (int i = threadIdx.x; i < a.rows_cta * a.pairs; i += R_TH) {
-    const int lr = i / a.pairs, pair = i - lr * a.pairs;
-    const long row = row0 + lr;
-    if (row < a.rows) {
-      const uint64_t pos = (uint64_t)(a.pos ? (long)__ldg(a.pos + row) : a.pos0 + row);
+    const int r = i / a.pairs, pair = i - r * a.pairs;
+    if (row0 + r < a.rows) {
+      const uint64_t pos = (uint64_t)(a.pos ? (long)__ldg(a.pos + row0 + r) : a.pos0 + row0 + r);
       const uint64_t angle = pos * a.turns[pair];
-      const float u = (float)(int)((angle + 0x80000000ull) >> 32) * 0x1p-31f;  // half turns, [-1, 1]
+      const float half_turns = (float)(int)((angle + 0x80000000ull) >> 32) * 0x1p-31f;  // [-1, 1]
       float s, c;
-      sincospif(u, &s, &c);
+      sincospif(half_turns, &s, &c);
       table[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
     }
   }
   __syncthreads();
-  const int per_row = R_TH / a.rows_cta, chunks = a.pairs / V, lanes = per_row / chunks;
-  const int lr = threadIdx.x / per_row, at = threadIdx.x - lr * per_row;
-  const long row = row0 + lr;
-  if (row >= a.rows) return;
-  long kv_row = row;
-  bool kept = true;  // the row has a place in the cache
-  if (a.slots) {
-    kv_row = __ldg(a.slots + row);
-    kept = kv_row >= 0 && kv_row < a.capacity;
-  }
-  // heads in turn: those of q, of k, of v
-  const int nq = a.q ? a.heads : 0, nk = a.k && kept ? a.kv_heads : 0, nv = a.v && kept ? a.kv_heads : 0;
-  auto place = [&](int h, const T*& x, T*& y) {
-    if (h < nq) {
-      x = reinterpret_cast<const T*>(a.q) + row * a.ldq + (long)h * a.dh;
-      y = reinterpret_cast<T*>(a.q_out) + row * a.ldqo + (long)h * a.dh;
-    } else if (h < nq + nk) {
-      x = reinterpret_cast<const T*>(a.k) + row * a.ldk + (long)(h - nq) * a.dh;
-      y = reinterpret_cast<T*>(a.k_out) + kv_row * a.ldko + (long)(h - nq) * a.dh;
-    } else {
-      x = reinterpret_cast<const T*>(a.v) + row * a.ldv + (long)(h - nq - nk) * a.dh;
-      y = reinterpret_cast<T*>(a.v_out) + kv_row * a.ldvo + (long)(h - nq - nk) * a.dh;
-    }
-  };
-  using E = Elems<T, V>;
-  const int hl = at / chunks, chunk = at - hl * chunks;
-  if (hl < lanes) {
-    float c[V], s[V];
+  if (!works) return;
+  const bool kept = kv_row >= 0 && kv_row < a.capacity;  // the row has a place in the cache
+  float c[V], s[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float2 t = table[lr * a.pairs + chunk * V + i];
-      c[i] = t.x;
-      s[i] = t.y;
-    }
-    // a thread's two vectors of a head: the pairs' first and second elements, or their elements in turn
-    const int o0 = HALF ? chunk * V : 2 * chunk * V, o1 = HALF ? a.pairs + chunk * V : (2 * chunk + 1) * V;
-#pragma unroll 4
-    for (int h = hl; h < nq + nk + nv; h += lanes) {
-      const T* x;
+  for (int i = 0; i < V; ++i) {
+    const float2 t = turns ? table[lr * a.pairs + chunk * V + i] : make_float2(1.f, 0.f);
+    c[i] = t.x;
+    s[i] = t.y;
+  }
+  for (int h0 = hl; h0 < nh; h0 += R_HEADS * lanes) {
+#pragma unroll
+    for (int i = 0; i < R_HEADS; ++i) {
+      const int h = h0 + i * lanes;
+      if (h >= nh) continue;
       T* y;
-      place(h, x, y);
-      E u = *reinterpret_cast<const E*>(x + o0), w = *reinterpret_cast<const E*>(x + o1);
-      if (h < nq + nk) {
+      if (h < nq)
+        y = reinterpret_cast<T*>(a.q_out) + row * a.ldqo + (long)h * a.dh;
+      else if (!kept)
+        continue;
+      else if (h < nq + nk)
+        y = reinterpret_cast<T*>(a.k_out) + kv_row * a.ldko + (long)(h - nq) * a.dh;
+      else
+        y = reinterpret_cast<T*>(a.v_out) + kv_row * a.ldvo + (long)(h - nq - nk) * a.dh;
+      if (turns && h < nq + nk) {
         float e[2 * V];
+        u[i].get(e);
+        w[i].get(e + V);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          e[i] = r_in(u.e[i]);
-          e[V + i] = r_in(w.e[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int i0 = HALF ? i : 2 * i, i1 = HALF ? V + i : 2 * i + 1;
+        for (int k = 0; k < V; ++k) {
+          const int i0 = HALF ? k : 2 * k, i1 = HALF ? V + k : 2 * k + 1;
           const float p = e[i0], q = e[i1];
-          e[i0] = p * c[i] - q * s[i];
-          e[i1] = p * s[i] + q * c[i];
+          e[i0] = p * c[k] - q * s[k];
+          e[i1] = p * s[k] + q * c[k];
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          u.e[i] = r_out<T>(e[i]);
-          w.e[i] = r_out<T>(e[V + i]);
-        }
+        u[i].set(e);
+        w[i].set(e + V);
       }
-      *reinterpret_cast<E*>(y + o0) = u;
-      *reinterpret_cast<E*>(y + o1) = w;
+      u[i].store(y + o0);
+      w[i].store(y + o1);
     }
-  }
-  // columns past the rotated ones
-  const int rest = (a.dh - 2 * a.pairs) / V;
-  for (int i = at; i < rest * (nq + nk + nv); i += per_row) {
-    const int h = i / rest, col = 2 * a.pairs + (i - h * rest) * V;
-    const T* x;
-    T* y;
-    place(h, x, y);
-    if (x != y) *reinterpret_cast<E*>(y + col) = *reinterpret_cast<const E*>(x + col);
+    if (h0 + R_HEADS * lanes < nh) load(h0 + R_HEADS * lanes);
   }
 }
 
@@ -142,12 +183,13 @@ cudaError_t rope(RopeArgs a, int size, int f16, cudaStream_t s) {
   auto fits = [&](const void* p, long ld) {
     return !p || ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0;
   };
-  const bool vec = a.pairs % v == 0 && a.dh % v == 0 && fits(a.q, a.ldq) && fits(a.q_out, a.ldqo) && fits(a.k, a.ldk) &&
+  const bool vec = a.pairs % v == 0 && a.dh % (2 * v) == 0 && fits(a.q, a.ldq) && fits(a.q_out, a.ldqo) && fits(a.k, a.ldk) &&
                    fits(a.k_out, a.ldko) && fits(a.v, a.ldv) && fits(a.v_out, a.ldvo);
   // few rows: one a CTA, so that they spread over the SMs
   a.rows_cta = 1;
+  const int chunks = vec ? a.dh / (2 * v) : (a.dh + 1) / 2;
   if (a.rows >= 4L * sm_count())
-    while (a.rows_cta < 4 && 2 * a.rows_cta * a.pairs <= R_TH) a.rows_cta *= 2;
+    while (a.rows_cta < 4 && 2 * a.rows_cta * std::max(a.pairs, chunks) <= R_TH) a.rows_cta *= 2;
   const long ctas = (a.rows + a.rows_cta - 1) / a.rows_cta;
   if (ctas > 0x7fffffffL) return cudaErrorInvalidConfiguration;
   auto launch = [&](auto kernel) { return launch_kernel(kernel, (unsigned)ctas, R_TH, 0, s, a); };

@@ -205,6 +205,7 @@ def test_refusals(ctx):
     for call in (
         lambda: ctx.rope(x, y, freqs(65), 128),                                # more pairs than a head has
         lambda: ctx.rope(x, y, [], 128),
+        lambda: ctx.rope(x[:, :255], y[:, :255], [1.0], 85),                   # an odd width
         lambda: ctx.rope(x, y, [math.nan], 128),
         lambda: ctx.rope(x, y, [math.inf], 128),
         lambda: ctx.rope(x, y, f, 128, scale=math.inf),
