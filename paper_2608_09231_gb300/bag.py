@@ -487,33 +487,21 @@ class Context:
         (default: the same); v is copied into v_out's.  freqs: host array of radians a position, one for
         each rotated pair of a head; pos: int32 [rows], default pos0 + row.  Any of q, k, v may be None."""
         f = np.ascontiguousarray(freqs, np.float64)
-        if f.ndim != 1 or layout not in ROPE_LAYOUT:
+        kind = ROPE_LAYOUT.get(layout)
+        if f.ndim != 1 or kind is None:
             raise ValueError(f"freqs {f.shape} is not a vector, or layout {layout!r} none of {list(ROPE_LAYOUT)}")
-        first = next((x for x in (q, k, v) if x is not None), None)
-        if first is None or dh < 1:
+        if dh < 1 or (q is None and k is None and v is None):
             raise ValueError("rope needs q, k or v, and a head's width")
-        kind, (rows, _) = _type(first)[0], first.shape if first.dim() == 2 else (-1, 0)
-        if kind not in _T32:
-            _want(first, "q, k and v", f"one of {list(_T32)}")
-        a = [None, 0, None, 0] * 3
-        heads, kv_heads, capacity = 0, 0, rows
-        for i, (x, y, name) in enumerate(((q, q_out, "q"), (k, k_out, "k"), (v, v_out, "v"))):
-            if (x is None) != (y is None):
-                raise ValueError(f"{name} and {name}_out go together")
-            if x is None:
-                continue
-            p, ld, n, cols, _ = _mat(x, name, (kind,))
-            po, ldo, no, co, _ = _mat(y, name + "_out", (kind,))
-            if n != rows or co != cols or cols % dh or (no != rows if i == 0 or slots is None else False):
-                _want(y, name + "_out", f"rows of {cols} columns for {rows} of {name}, in heads of {dh}")
-            a[4 * i:4 * i + 4] = p, ld, po, ldo
-            if i == 0:
-                heads = cols // dh
-            else:
-                if kv_heads and (kv_heads != cols // dh or capacity != no):
-                    raise ValueError(f"k_out and v_out differ: {tuple(k_out.shape)} and {tuple(v_out.shape)}")
-                kv_heads, capacity = cols // dh, no
-        args = RopeArgs(_T32[kind], ROPE_LAYOUT[layout], heads, kv_heads, dh, f.size, rows, *a,
+        q_a, rows, heads, _, dt = _in_out(q, q_out, "q", dh, None, None, slots is None)
+        k_a, rows, kv_heads, capacity, dt = _in_out(k, k_out, "k", dh, rows, dt, slots is None)
+        v_a, rows, v_heads, v_cap, dt = _in_out(v, v_out, "v", dh, rows, dt, slots is None)
+        if q is not None and q_out.shape[0] != rows:
+            _want(q_out, "q_out", f"{rows} rows")
+        if k is None:
+            kv_heads, capacity = v_heads, v_cap
+        elif v is not None and (v_heads != kv_heads or v_cap != capacity):
+            raise ValueError(f"v {tuple(v.shape)} and v_out {tuple(v_out.shape)} differ from k and k_out")
+        args = RopeArgs(_T32[dt], kind, heads, kv_heads, dh, f.size, rows, *q_a, *k_a, *v_a,
                         _vec(slots, "slots", rows, "int32"), capacity, _vec(pos, "pos", rows, "int32"), pos0,
                         f.ctypes.data, scale, int(inverse))
         self._chk(self.lib.bag_rope(self.h, ctypes.byref(args)))
@@ -596,12 +584,31 @@ def _mat(t, name, types=None):
     of `types` (None: of one-byte elements)."""
     shape, (kind, size) = t.shape, _type(t)
     if len(shape) != 2 or not t.is_cuda or (size != 1 if types is None else kind not in types):
-        _want(t, name, f"a device matrix of {types or 'one-byte elements'}")
+        _want(t, name, f"a device matrix of {tuple(types) if types else 'one-byte elements'}")
     rows, cols = shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         _want(t, name, "a matrix with dense rows")
     return t.data_ptr(), ld if rows > 1 else max(ld, cols), rows, cols, kind
+
+
+_NO_ROWS = (None, 0, None, 0)
+
+
+def _in_out(x, y, name, dh, rows, kind, same_rows):
+    """((pointer, row stride) of x and of y, rows, heads, rows of y, type) of rows x of heads of dh columns and
+    their output y, of `rows` rows and type `kind` where those are given."""
+    if x is None or y is None:
+        if x is not y:
+            raise ValueError(f"{name} and {name}_out go together")
+        return _NO_ROWS, rows, 0, rows or 0, kind
+    p, ld, n, cols, kx = _mat(x, name, _T32)
+    po, ldo, no, co, ky = _mat(y, name + "_out", _T32)
+    if (rows is not None and n != rows) or (kind or kx) != kx or cols % dh:
+        _want(x, name, f"{n if rows is None else rows} rows of {kind or kx}, in heads of {dh}")
+    if ky != kx or co != cols or (same_rows and no != n):
+        _want(y, name + "_out", f"{kx} rows of {cols} columns" + (f", {n} of them" if same_rows else ""))
+    return (p, ld, po, ldo), n, cols // dh, no, kx
 
 
 def _vec(t, name, n, kind="float32"):
