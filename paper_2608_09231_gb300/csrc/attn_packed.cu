@@ -34,6 +34,7 @@ struct PackedParams {
   // tensor-core kernel: a tile's rows are `tokens` query tokens x `together` heads of a group; units over the
   // tokens of all sequences and of each
   int together, tokens, slots1, slots2;
+  int by_head;  // order of the units: a head after the other, or all heads of a slot
   int* err;
   // few-row kernel: whether a unit's keys may be shared among CTAs, their sums (see attn_few_kernel)
   int few, split;
@@ -486,29 +487,50 @@ BAG_DEV void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uin
       : "memory");
 }
 
-// The sequence whose units (of `per` tokens) hold slot `slot`, and its first slot: sequence i's slots are
-// q_start[i] / per + i and on, so that each has as many as its tokens need and at most one more.  Called by a
-// whole warp; up to 32 sequences take one round of loads.
-BAG_DEV Span span_of_slot(const PackedParams& p, int per, int slot, int* first) {
+// The sequence of the units' slot `slot` (units of `per` tokens, a key head), and the unit's index in it (-1: none).
+// Up to 32 sequences: in order of their keys, most first (units that take long go first), each with as many
+// slots as it has units.  More: as they come, the last first, sequence i's slots from q_start[i] / per + i on
+// (as many as its units, or one more).  A sequence's last unit sees most keys, and goes first.  Called by a
+// whole warp.
+BAG_DEV Span span_of_slot(const PackedParams& p, int per, int slot, int* index) {
   const int lane = threadIdx.x % 32;
-  auto start = [&](int i) { return (int)((unsigned)max(__ldg(p.q_start + i), 0) / (unsigned)per) + i; };
-  int lo = 0, n = p.seqs;
-  while (n > 32) {
-    const int step = (n + 31) / 32, i = lane * step;
-    const uint32_t at = __ballot_sync(0xffffffffu, i < n && start(lo + i) <= slot);
-    const int skip = max(__popc(at) - 1, 0) * step;
-    lo += skip;
-    n = min(step, n - skip);
+  Span s;
+  int first, units, src;
+  if (p.seqs <= 32) {
+    s = span_of(p, min(lane, p.seqs - 1));
+    units = lane < p.seqs ? (s.lq + per - 1) / per : 0;
+    first = 0;
+    for (int i = 0; i < p.seqs; ++i) {
+      const int lk = __shfl_sync(0xffffffffu, s.lk, i), n = __shfl_sync(0xffffffffu, units, i);
+      if (lk > s.lk || (lk == s.lk && i < lane)) first += n;
+    }
+    const uint32_t at = __ballot_sync(0xffffffffu, slot >= first && slot < first + units);
+    src = at ? __ffs(at) - 1 : 0;
+  } else {
+    auto start = [&](int i) { return (int)((unsigned)max(__ldg(p.q_start + i), 0) / (unsigned)per) + i; };
+    slot = p.slots2 - 1 - slot;
+    int lo = 0, n = p.seqs;
+    while (n > 32) {
+      const int step = (n + 31) / 32, i = lane * step;
+      const uint32_t at = __ballot_sync(0xffffffffu, i < n && start(lo + i) <= slot);
+      const int skip = max(__popc(at) - 1, 0) * step;
+      lo += skip;
+      n = min(step, n - skip);
+    }
+    s = span_of(p, lo + min(lane, n - 1));
+    units = (s.lq + per - 1) / per;
+    first = start(lo + min(lane, n - 1));
+    src = max(__popc(__ballot_sync(0xffffffffu, lane < n && first <= slot)) - 1, 0);
+    // the same order as above: the highest slot is the last unit
+    slot = first + units - 1 - (slot - first);
   }
-  Span s = span_of(p, lo + min(lane, n - 1));
-  const int mine = start(lo + min(lane, n - 1));
-  const uint32_t at = __ballot_sync(0xffffffffu, lane < n && mine <= slot);
-  const int src = max(__popc(at) - 1, 0);
-  *first = __shfl_sync(0xffffffffu, mine, src);
   s.q0 = __shfl_sync(0xffffffffu, s.q0, src);
   s.lq = __shfl_sync(0xffffffffu, s.lq, src);
   s.k0 = __shfl_sync(0xffffffffu, s.k0, src);
   s.lk = __shfl_sync(0xffffffffu, s.lk, src);
+  units = __shfl_sync(0xffffffffu, units, src);
+  const int i = units - 1 - (__shfl_sync(0xffffffffu, slot, src) - __shfl_sync(0xffffffffu, first, src));
+  *index = i >= 0 && i < units ? i : -1;
   return s;
 }
 
@@ -530,8 +552,15 @@ BAG_DEV int sees_of(const PackedParams& p, const Unit& u, int i) {
 BAG_DEV Unit unit_of(const PackedParams& p, int nt, int at) {
   Unit u{};
   const int per_head = p.slots1 * p.parts1 + p.slots2 * p.parts2, units1 = p.slots1 * p.parts1, per = nt * p.tokens;
-  const int hu = at / per_head;  // a head at a time, so that its keys stay in L2
-  at -= hu * per_head;
+  int hu;
+  if (p.by_head) {  // a head at a time, so that its keys stay in L2
+    hu = at / per_head;
+    at -= hu * per_head;
+  } else {  // all heads of a slot
+    const int groups = p.heads / p.together, i = at / groups;
+    hu = at - i * groups;
+    at = i;
+  }
   u.head0 = hu * p.together;
   int most;  // tiles that the part may have
   if (at < units1) {  // the prefix with the tokens of all sequences
@@ -546,11 +575,10 @@ BAG_DEV Unit unit_of(const PackedParams& p, int nt, int at) {
   } else {
     at -= units1;
     const int back = at / p.parts2, own = at - back * p.parts2;
-    const int slot = p.slots2 - 1 - back;  // later tokens see more keys: they go first
-    int first;
-    const Span s = span_of_slot(p, per, slot, &first);
-    if (slot < first || slot - first >= (s.lq + per - 1) / per) return u;
-    const int parts = own_parts(p, s.lk), t0 = (slot - first) * per;
+    int index;
+    const Span s = span_of_slot(p, per, back, &index);
+    if (index < 0) return u;
+    const int parts = own_parts(p, s.lk), t0 = index * per;
     if (own >= (p.parts1 ? parts : max(parts, 1))) return u;
     u.q0 = s.q0 + t0;
     u.tokens = min(s.lq - t0, per);
@@ -1041,7 +1069,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
 }
 
 namespace {
-constexpr int JN_TH = 128, JR_TH = 256;
+constexpr int JN_TH = 256, JR_TH = 256;
 
 // The sequence of query row t: the last one that starts at or before it.  Called by a whole warp.
 BAG_DEV int sequence_of(const PackedParams& p, int t) {
@@ -1334,6 +1362,7 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   if (tiles > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
     return cudaErrorInvalidConfiguration;
   p.slots1 = (int)slots1, p.slots2 = (int)slots2;
+  p.by_head = (a.k_rows + a.n_prefix) * a.kv_heads * a.dh * 4 > (128L << 20);
   CUtensorMap tq, tk, tv, tpk, tpv;
   if (tiles) {
     if (encode_tmap_3d_16(&tq, a.q, (uint64_t)a.dh, (uint64_t)a.heads, (uint64_t)a.nq, (uint64_t)a.dh * 2, (uint64_t)a.ldq * 2,
