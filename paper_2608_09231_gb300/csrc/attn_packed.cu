@@ -322,14 +322,25 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
       }
       const uint32_t a0 = pack16<F16>(sc[0][0], sc[0][1]), a1 = pack16<F16>(sc[0][2], sc[0][3]),
                      a2 = pack16<F16>(sc[1][0], sc[1][1]), a3 = pack16<F16>(sc[1][2], sc[1][3]);
+      // bf16: what its eight bits leave of a weight, as a second operand
+      auto rest = [](uint32_t w, float a, float b) {
+        return pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+      };
+      uint32_t r0, r1, r2, r3;
+      if constexpr (!F16) {
+        r0 = rest(a0, sc[0][0], sc[0][1]), r1 = rest(a1, sc[0][2], sc[0][3]);
+        r2 = rest(a2, sc[1][0], sc[1][1]), r3 = rest(a3, sc[1][2], sc[1][3]);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           auto word = [&](const uint4& v) { return t < 2 ? v.x : (t < 4 ? v.y : (t < 6 ? v.z : v.w)); };
           const uint32_t sel = t & 1 ? 0x7632u : 0x5410u;
-          mma16816<F16>(o[u * 8 + t], a0, a1, a2, a3, __byte_perm(word(vf[0][u]), word(vf[1][u]), sel),
-                        __byte_perm(word(vf[2][u]), word(vf[3][u]), sel));
+          const uint32_t b0 = __byte_perm(word(vf[0][u]), word(vf[1][u]), sel),
+                         b1 = __byte_perm(word(vf[2][u]), word(vf[3][u]), sel);
+          mma16816<F16>(o[u * 8 + t], a0, a1, a2, a3, b0, b1);
+          if constexpr (!F16) mma16816<F16>(o[u * 8 + t], r0, r1, r2, r3, b0, b1);
         }
       }
       if (k0 + F_TILE < end) load_v(k0 + F_TILE);
@@ -1281,7 +1292,7 @@ long parts_of(const Plan& t) { return t.parts1 + t.parts2 > 1 ? t.parts1 + t.par
 Plan plan_of(const PackedArgs& a, size_t bytes) {
   Plan t{};
   const long G = a.heads / a.kv_heads, sms = sm_count();
-  const long max_k = std::min(std::max(a.max_k, 1L), std::max(a.k_rows, 1L));
+  const long max_k = std::max(a.max_k, 1L);  // as the caller says, so that the size told for a call is the call's
   const long max_q = std::max(1L, std::min(a.max_q, a.nq)), rows = a.nq * G;
   const long most = (long)std::min<size_t>(bytes / part_bytes(a), 1u << 30);  // parts
   t.few = max_q * G <= F_ROWS;
@@ -1362,7 +1373,7 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   if (tiles > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
     return cudaErrorInvalidConfiguration;
   p.slots1 = (int)slots1, p.slots2 = (int)slots2;
-  p.by_head = (a.k_rows + a.n_prefix) * a.kv_heads * a.dh * 4 > (128L << 20);
+  p.by_head = (std::min(a.max_k, a.k_rows) + a.n_prefix) * a.kv_heads * a.dh * 4 > (128L << 20);
   CUtensorMap tq, tk, tv, tpk, tpv;
   if (tiles) {
     if (encode_tmap_3d_16(&tq, a.q, (uint64_t)a.dh, (uint64_t)a.heads, (uint64_t)a.nq, (uint64_t)a.dh * 2, (uint64_t)a.ldq * 2,

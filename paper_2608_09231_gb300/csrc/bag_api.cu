@@ -2148,8 +2148,7 @@ static bag_status bag_attention_packed_impl(bag_ctx* ctx, const bag_packed_args*
   g.q_start = a->q_start, g.k_start = a->k_start, g.k_len = a->k_len;
   g.nq = a->nq, g.k_rows = a->k_rows, g.n_prefix = n_prefix, g.seqs = a->seqs;
   g.max_q = a->max_q ? std::min(a->max_q, a->nq) : a->nq;
-  const long most_k = a->k_start ? a->k_rows : a->nq;
-  g.max_k = a->max_k ? std::min(a->max_k, most_k) : most_k;
+  g.max_k = a->max_k ? std::min(a->max_k, kMaxRows) : (a->k_start ? a->k_rows : a->nq);
   g.heads = a->heads, g.kv_heads = a->kv_heads, g.dh = a->dh, g.f16 = a->type == BAG_F16, g.causal = a->causal;
   g.scale_log2 = (float)(1.4426950408889634 * (a->scale > 0.f ? (double)a->scale : 1.0 / std::sqrt((double)a->dh)));
   g.work = a->work, g.work_bytes = a->work_bytes;
@@ -2166,7 +2165,7 @@ static bag_status bag_attention_work_impl(bag_ctx* ctx, long nq, int heads, int 
   g.nq = nq, g.heads = heads, g.kv_heads = kv_heads, g.dh = dh, g.seqs = seqs;
   g.k_rows = kMaxRows, g.n_prefix = n_prefix;
   g.max_q = max_q ? std::min(max_q, nq) : nq;
-  g.max_k = max_k ? max_k : nq;
+  g.max_k = max_k ? std::min(max_k, kMaxRows) : nq;
   *bytes = nq && seqs ? attention_packed_work(g) : 0;
   return BAG_OK;
 }

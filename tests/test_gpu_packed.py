@@ -2,6 +2,7 @@
 bounds)."""
 
 import math
+import random
 
 import pytest
 import torch
@@ -136,6 +137,50 @@ def test_packed(lens, heads, kv_heads, dh, dtype, causal, ctx):
 @pytest.mark.parametrize("heads,kv_heads,dh,dtype", [(7, 1, 128, "bf16"), (12, 4, 64, "f16"), (8, 8, 128, "f16"), (40, 2, 64, "bf16")])
 def test_prefix(lens, prefix, heads, kv_heads, dh, dtype, ctx):
     b = Batch(LENS[lens], heads, kv_heads, dh, dtype, key=prefix, prefix=prefix)
+    b.run(ctx).check()
+
+
+def many(n, seed, lq, lk):
+    """n sequences of random lengths up to lq new and lk more keys, some of them empty."""
+    g = random.Random(seed)
+    out = []
+    for _ in range(n):
+        m = 0 if g.random() < 0.1 else g.randint(1, lq)
+        out.append((m, max(0, m + g.randint(-2, lk))))
+    return out
+
+
+@pytest.mark.parametrize("n", [31, 32, 33, 127, 128, 129, 300, 700])
+@pytest.mark.parametrize("lq,lk", [(1, 60), (1, 700), (3, 40), (60, 100)])
+@pytest.mark.parametrize("prefix", [None, 200])
+def test_many_sequences(n, lq, lk, prefix, ctx):
+    """More sequences than a warp finds at once, or a CTA adds up at once; queries that start behind others' rows."""
+    if n * lq > 12000:
+        n = 12000 // lq
+    b = Batch(many(n, n + lq, lq, lk), 4, 2, 64, "f16", key=n, prefix=prefix, before=2)
+    b.run(ctx).check()
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(28, 1), (40, 1), (48, 1), (13, 1), (130, 1), (131, 1), (256, 2), (10, 2), (33, 3)])
+@pytest.mark.parametrize("lens", ["prompt", "mixed", "tokens", "extend"])
+def test_groups_of_heads(heads, kv_heads, lens, ctx):
+    """Groups that do not divide a tile's rows, or do not fit them."""
+    b = Batch(LENS[lens], heads, kv_heads, 64, "bf16", key=heads)
+    b.run(ctx).check()
+
+
+@pytest.mark.parametrize("lens", ["mixed", "tokens"])
+def test_strides_of_their_own(lens, ctx):
+    """q, k, v and o as columns of wider tensors of four different widths, and a prefix likewise."""
+    b = Batch(LENS[lens], 6, 2, 128, "f16", prefix=140)
+
+    def inside(x, width, at):
+        y = torch.full((x.shape[0], width), math.nan, device=DEV, dtype=x.dtype)
+        y[:, at:at + x.shape[1]] = x
+        return y[:, at:at + x.shape[1]]
+
+    b.q, b.k, b.v = inside(b.q, 1000, 64), inside(b.k, 264, 8), inside(b.v, 600, 320)
+    b.pk, b.pv = inside(b.pk, 272, 0), inside(b.pv, 1024, 512)
     b.run(ctx).check()
 
 
