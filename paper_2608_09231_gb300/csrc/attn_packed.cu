@@ -6,6 +6,11 @@
 // over the prefix's keys and the own keys j <= t + lk - lq.  Sums over parts of the keys are kept as
 // (m, l, O) with l = sum 2^(s - m), O = sum 2^(s - m) v, s in log2 units; parts are joined by
 // m = max m_i, l = sum 2^(m_i - m) l_i, O likewise.
+//
+// A sequence's rows of a key head are its query tokens times the heads that share it.  At most 16 of them: the
+// keys are what there is to read, and attn_few_kernel streams them.  More: attn_packed_kernel, on the tensor
+// cores.  A prefix that all sequences share is met by the rows of all of them together, where they have few each,
+// or goes ahead of each sequence's own keys.  attn_join_* add up where keys were cut.
 #include <algorithm>
 
 #include "attn_common.cuh"
@@ -128,6 +133,12 @@ BAG_DEV int few_length(int lk) { return (lk + F_TILE - 1) / F_TILE + F_COST; }
 // one CTA's share is finished there; of the others a CTA holds at most two pieces, one that starts its
 // unit (piece 1) and one that does not (piece 0), which attn_join_kernel adds up.  The next unit's first
 // loads are in flight while the warps' sums are joined.
+// Bound: HBM.  64 tokens over 512 to 32,767 keys each (32 heads, 8 key heads, 2.3 GB) 360 us, 6.4 TB/s or 95 % of the
+// copy rate (a grid of sequences, heads and parts of up to 8192 keys: 392 to 546); one token over 131,071
+// keys 51 us (floor 40, the rest a launch's start and the join).  Four warps a CTA and two CTAs on an SM
+// instead of eight and one: 376 -> 363 us, 128 tokens over short own keys 85 -> 65.  bf16 weights enter P V in
+// two parts, whose rounding would otherwise be the largest error (2-norm 1.9e-3 against 1.7e-3, the
+// output's own): 4 % of the time, as the products are not what bounds it.
 template <bool F16, int DH>
 __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const PackedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -545,6 +556,24 @@ BAG_DEV Span span_of_slot(const PackedParams& p, int per, int slot, int* index) 
   return s;
 }
 
+// mbar_wait_warp for the hand-over of units: a role without work in a unit waits as long as the others take for it,
+// which for very many keys in one part may pass a wait's usual limit.  A failure elsewhere still ends it at once.
+BAG_DEV bool wait_unit(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  bool there = mbar_try_wait(bar, parity);
+  const uint64_t t0 = global_ns();
+  for (uint32_t i = 1; !there; ++i) {
+    there = mbar_try_wait(bar, parity);
+    if (!there && (i & 63) == 0) {
+      if (*abort) break;
+      if (global_ns() - t0 > 30 * kWaitLimitNs) {
+        *abort = 1;
+        break;
+      }
+    }
+  }
+  return __all_sync(0xffffffffu, there);
+}
+
 // What a CTA works on at a time.
 struct Unit {
   int q0, tokens;        // its first query row, and how many (0: nothing to do, -1: no unit is left)
@@ -622,7 +651,18 @@ BAG_DEV Unit unit_of(const PackedParams& p, int nt, int at) {
 //                 TMEM and is rescaled only when the maximum has grown by more than 8
 // So the loads and scores of a unit run beside the output of the one before, and what a CTA costs to launch
 // (tensor memory, barriers, the launch itself, some 5,000 cycles) comes once for each that is resident.
-// V is read as it lies, a row a key: as an operand whose rows run along the contraction.
+// V is read as it lies, a row a key: as an operand whose rows run along the contraction (as fast as the other way).
+// P is rounded to the operands' type, as in the dense kernel: both operands of an MMA are of one type.
+// Two tiles and one CTA on an SM, or one tile and two CTAs: the first reads each K and V tile once for 256 rows
+// (16,384 tokens, 32 heads 1300 against 1480 us, 16 x 512 tokens 62 against 72), the second has more CTAs for
+// few rows (77 tokens, 32 heads 7.1 against 8.3, 512 tokens 11.9 against 12.9).
+// Bound: a step of both tiles takes some 2,600 cycles for 2,048 of products: a tile's scores, softmax and P V
+// follow each other, and the hand-overs between the warps (about 1,200 cycles a step) are only partly hidden
+// by the other tile.  A unit costs some 6,000 cycles besides, mostly its output.  16,384 causal tokens, 32 heads 1300 us
+// (1690 TFLOP/s), 4608 x 24 heads 103, 4 x 2048 x 32 115, 16 x 512 x 32 61 (query and output bytes 25); heads of
+// 64: 16,384 x 32 1150, where the softmax has twice the work for each product.
+// Not kept: two threads a row (4 x 2048 124 -> 188 us: the issuing warp loses its slots), an MMA warp whose issue branches on
+// the last tile (16,384 tokens 1380 -> 1480), 64-bit descriptors in registers (spills in the issuing warp).
 template <bool F16, int DH, int NT>
 __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     attn_packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -709,7 +749,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
           }
           ask = false;
         };
-        if (!(ok = wait(u_empty + (c & 1), ((c >> 1) & 1) ^ 1))) break;
+        if (!(ok = wait_unit(u_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag))) break;
         const Unit& u = units[c & 1];
         {
           const Unit found = unit_of(p, NT, at);
@@ -770,7 +810,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
           __syncwarp();
         }
       }
-      if (ok && (ok = wait(u_empty + (c & 1), ((c >> 1) & 1) ^ 1)) && lane == 0) {
+      if (ok && (ok = wait_unit(u_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) && lane == 0) {
         units[c & 1].tokens = -1;
         mbar_arrive(u_full + (c & 1));
       }
@@ -796,7 +836,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
       int done0 = 0, done1 = 0;  // those of each tile of rows
       bool ok = true;
       for (int c = 0; ok; ++c) {
-        if (!(ok = wait(u_full + (c & 1), (c >> 1) & 1))) break;
+        if (!(ok = wait_unit(u_full + (c & 1), (c >> 1) & 1, abort_flag))) break;
         const Unit& u = units[c & 1];
         const int n0 = u.n[0], n1 = NT == 2 ? u.n[1] : 0, nkb = max(n0, n1), fused = u.fused, j0 = u.j0, lk = u.lk;
         if (u.tokens < 0) break;
@@ -921,7 +961,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     int steps = 0, outputs = 0;  // key tiles, and units with any, so far
     bool ok = true;
     for (int c = 0; ok; ++c) {
-      if (!(ok = wait(u_full + (c & 1), (c >> 1) & 1))) break;
+      if (!(ok = wait_unit(u_full + (c & 1), (c >> 1) & 1, abort_flag))) break;
       const Unit& u = units[c & 1];
       if (u.tokens < 0) break;
       const int tiles = u.n[x];
@@ -1135,7 +1175,7 @@ BAG_DEV Parts parts_of(const PackedParams& p, int seq, const Span& s, int tok, i
 }  // namespace
 
 // Joins the parts of a row and head: their weights first, then DH / 4 lanes a part, in a fixed order.  For few rows
-// with many parts.
+// with many parts.  Bound: latency (28 heads of one token in 76 pieces: 4 to 5 us behind the kernel before).
 template <bool F16, int DH>
 __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) {
   constexpr int L = DH / 4, GROUPS = JN_TH / L;
@@ -1306,7 +1346,7 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   t.rows = units(256) * 2 > sms || units(256) * cdiv(max_k + a.n_prefix, PT) >= 8 * sms ? 256 : 128;
   const bool all_rows = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
   if (a.n_prefix && !all_rows) t.few = 0;
-  auto chunk = [](long keys, long parts) { return (int)(cdiv(cdiv(keys, parts), PT) * PT); };
+  auto chunk = [](long keys, long parts) { return (int)std::min(cdiv(cdiv(keys, parts), PT) * PT, 0x7fffff80L); };
   long p1 = 0, p2 = 1;
   if (all_rows) p1 = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, t.rows) * a.kv_heads)));
   t.fused = all_rows ? 0 : (int)cdiv(a.n_prefix, PT);
@@ -1327,7 +1367,7 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   if (t.few) {
     const long units16 = a.seqs * a.kv_heads * cdiv(max_q * G, F_ROWS), slots = sms * (a.dh == 64 ? few_ctas<64>() : few_ctas<128>());
     t.split = max_k > 256;
-    t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * cdiv(max_k, 2 * F_TILE) : units16));
+    t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * std::min(cdiv(max_k, 2 * F_TILE), slots) : units16));
     if (t.split && bytes < parts_of(t) * part_bytes(a) + piece_bytes(a, t)) {
       t.split = 0;
       t.ctas = (int)std::min(slots, units16);

@@ -2063,7 +2063,9 @@ static bag_status bag_rope_impl(bag_ctx* ctx, const bag_rope_args* a) {
   auto common = [&](const Mat& x, const Mat& y) {
     return share(x.p, x.ld * size, x.rows, x.width * size, y.p, y.ld * size, y.rows, y.width * size);
   };
+  const Mat index[2] = {{a->slots, 4 * a->rows / size, 4 * a->rows / size, 1}, {a->pos, 4 * a->rows / size, 4 * a->rows / size, 1}};
   for (int o = 0; o < 3; ++o) {
+    if (common(index[0], out[o]) || common(index[1], out[o])) return fail(ctx, BAG_EINVAL, "an output of rope overlaps slots or positions");
     for (int i = 0; i < 3; ++i) {
       const bool same = i == o && in[i].p == out[o].p && in[i].ld == out[o].ld && (o == 0 || !a->slots);
       if (!same && common(in[i], out[o])) return fail(ctx, BAG_EINVAL, "an output of rope overlaps an input");
@@ -2110,6 +2112,7 @@ static bag_status bag_attention_packed_impl(bag_ctx* ctx, const bag_packed_args*
     return fail(ctx, BAG_EINVAL, "bad type, mask or scale of attention");
   if (a->k_rows < 0 || a->k_rows > kMaxRows || !a->k_start != !a->k_len || (!a->k_start && a->k_rows < a->nq))
     return fail(ctx, BAG_EINVAL, "k_start and k_len go together; without them k has a row for each query");
+  if (a->k_rows > kMaxRows - n_prefix) return fail(ctx, BAG_EUNSUPPORTED, "prefix and cache rows together must fit 31 bits");
   if (a->nq == 0 || a->seqs == 0) return BAG_OK;
   const long wq = (long)a->heads * a->dh, wk = (long)a->kv_heads * a->dh;
   if (!a->q || !a->o || !a->q_start || (a->k_rows && (!a->k || !a->v)) || (n_prefix && (!pk || !pv)))
@@ -2130,7 +2133,8 @@ static bag_status bag_attention_packed_impl(bag_ctx* ctx, const bag_packed_args*
   };
   const Mat in[] = {{a->q, a->ldq * 2, a->nq, wq * 2}, {a->k, a->ldk * 2, a->k_rows, wk * 2},
                     {a->v, a->ldv * 2, a->k_rows, wk * 2}, {pk, ldpk * 2, n_prefix, wk * 2},
-                    {pv, ldpv * 2, n_prefix, wk * 2}};
+                    {pv, ldpv * 2, n_prefix, wk * 2}, {a->q_start, (a->seqs + 1) * 4, 1, (a->seqs + 1) * 4},
+                    {a->k_start, a->seqs * 4, 1, a->seqs * 4}, {a->k_len, a->seqs * 4, 1, a->seqs * 4}};
   const long nl = a->nq * a->heads * 4;
   const Mat out[] = {{a->o, a->ldo * 2, a->nq, wq * 2}, {a->lse, nl, 1, nl},
                      {a->work, (long)a->work_bytes, 1, (long)a->work_bytes}};

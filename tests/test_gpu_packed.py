@@ -197,9 +197,10 @@ def test_prefix_alone(dh, ctx):
 
 @pytest.mark.parametrize("share", [0.0, 0.2, 0.55, 1.0])
 @pytest.mark.parametrize("lens", [[(1, 9000)], [(1, 3000), (1, 10), (1, 2999), (2, 40)], [(40, 5000)], [(300, 4000), (5, 4000)]])
-def test_less_workspace(share, lens, ctx):
+@pytest.mark.parametrize("prefix", [None, 900])
+def test_less_workspace(share, lens, prefix, ctx):
     for dtype in ("f16", "bf16"):
-        b = Batch(lens, 8, 2, 128, dtype)
+        b = Batch(lens, 8, 2, 128, dtype, prefix=prefix)
         work = b.work(ctx, share)
         b.run(ctx, work=work).check()
 
@@ -423,6 +424,8 @@ def test_refusals(ctx):
     wide = torch.zeros(7, 520, device=DEV, dtype=b.dt)
     for f, status in (
         (call(q, k, v, q, st), 1),                                           # o over q
+        (call(q, k, v, o, o.view(torch.int32)[0, :2]), 1),                   # and over the starts
+        (call(q, k, v, o, st, work=o), 1),
         (call(q, k, v, o, st, scale=-1.0), 1),
         (call(q, k, v, o, st, scale=math.inf), 1),
         (call(q, k, v, o, st, k_len=None), 1),

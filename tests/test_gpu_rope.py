@@ -214,6 +214,7 @@ def test_refusals(ctx):
         lambda: ctx.rope(x[:4], x[2:6], f, 128),                               # moved by two rows
         lambda: ctx.rope(x[:, :128], x[:, 64:192], f, 128),                    # and by half a head
         lambda: ctx.rope(x, y, f, 128, k=x, k_out=y),                          # one output for both
+        lambda: ctx.rope(x, y, f, 128, pos=y.view(torch.int32)[1, :8]),        # positions in an output
         lambda: ctx.rope(None, None, f, 128, k=x, k_out=x, slots=torch.arange(8, device=DEV, dtype=torch.int32)),
     ):
         with pytest.raises(bag.BagError) as e:
