@@ -1044,30 +1044,38 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
       }
       if (!ok) break;
       steps += tiles;
-      if (tiles > 0 && !(ok = wait(o_done + x, outputs++ & 1))) break;
-      if (x * p.tokens < u.tokens) {
-        const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
-        const float f = 1.f / l;
+      // while the last product is on its way: the row's maximum and sum, and where its output goes, for the lanes
+      // that store it
+      const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
+      const float f = 1.f / l;
+      const bool direct = u.direct;
+      {
         const int mine = token(), h = u.head0 + row - of * p.together;
-        // where the row's output goes, for the lanes that store it
-        at[lane] = mine < 0 ? -1
-                            : (u.direct ? (u.q0 + mine) * p.ldo + h * DH
-                                        : (((long)u.part * p.nq + u.q0 + mine) * p.heads + h) * DH);
-        if (mine >= 0) {  // the row's maximum and sum
-          const long i = (long)(u.q0 + mine) * p.heads + h;
-          if (!u.direct)
+        const long i = (long)(u.q0 + mine) * p.heads + h;
+        at[lane] = mine < 0 ? -1 : (direct ? (u.q0 + mine) * p.ldo + h * DH : ((long)u.part * p.nq * p.heads + i) * DH);
+        if (mine >= 0) {
+          if (!direct)
             p.part_ml[(long)u.part * p.nq * p.heads + i] = make_float2(any ? m_use : -INFINITY, l);
           else if (p.lse)
             p.lse[i] = any ? (m_use + log2f(l)) * 0.6931471805599453f : -INFINITY;
         }
+      }
+      __syncwarp();
+      long to[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] = at[8 * i + (lane >> 2)];
+      if (tiles > 0 && !(ok = wait(o_done + x, outputs++ & 1))) break;
+      if (x * p.tokens < u.tokens) {
+        const bool seen = any && tiles > 0;
+        uint32_t o[32];
+        auto load = [&](int b) {
+          if (tiles > 0) tmem_ld32_nowait(o_addr + b, o);
+        };
+        load(0);
+        tmem_ld_wait();
         // through shared memory, so that a store covers whole runs of a few rows: 64 bytes a row at a time, 32
         // columns in 16 bits or 16 of a part in fp32
-        __syncwarp();
-        long to[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = at[8 * i + (lane >> 2)];
-        const bool seen = any && tiles > 0, direct = u.direct;
-        auto turn = [&](const uint32_t* w, int col) {  // 16 words a row, to column col of the output
+        auto turn = [&](const uint32_t* w, auto* out, int col) {
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
             *reinterpret_cast<uint4*>(buf + lane * PT_LD + i * 4) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
@@ -1075,33 +1083,30 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint4 v = *reinterpret_cast<const uint4*>(buf + (8 * i + (lane >> 2)) * PT_LD + (lane & 3) * 16);
-            if (to[i] >= 0) {
-              if (direct)
-                *reinterpret_cast<uint4*>(p.o + to[i] + col + (lane & 3) * 8) = v;
-              else
-                *reinterpret_cast<uint4*>(p.part_o + to[i] + col + (lane & 3) * 4) = v;
-            }
+            if (to[i] >= 0) *reinterpret_cast<uint4*>(out + to[i] + col + (lane & 3) * (16 / sizeof(*out))) = v;
           }
           __syncwarp();
         };
+        if (direct) {
 #pragma unroll 1
-        for (int b = 0; b < DH; b += 32) {
-          uint32_t o[32];
-          if (tiles > 0) {
-            tmem_ld32_nowait(o_addr + b, o);
-            tmem_ld_wait();
-          }
-          if (direct) {
+          for (int b = 0; b < DH; b += 32) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               w[i] = seen ? pack16<F16>(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f) : 0u;
-            turn(w, b);
-          } else {
+            if (b + 32 < DH) load(b + 32);
+            turn(w, p.o, b);
+            tmem_ld_wait();
+          }
+        } else {
+#pragma unroll 1
+          for (int b = 0; b < DH; b += 32) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = seen ? o[i] : 0u;
-            turn(o, b);
-            turn(o + 16, b + 16);
+            turn(o, p.part_o, b);
+            turn(o + 16, p.part_o, b + 16);
+            if (b + 32 < DH) load(b + 32);
+            tmem_ld_wait();
           }
         }
         tc_fence_before();  // the next unit's products into O come after these loads
