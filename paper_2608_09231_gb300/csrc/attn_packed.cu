@@ -1342,22 +1342,41 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   const long most = (long)std::min<size_t>(bytes / part_bytes(a), 1u << 30);  // parts
   t.few = max_q * G <= F_ROWS;
   // heads of a group that share a tile: as many as leave few of its rows empty, or whose rows of a
-  // sequence fit one (more units of a key head would read its keys again)
+  // sequence fit one.  More units of a key head read its keys again, and a sequence's last tile is less full: with
+  // one of seven heads, 24 prompts behind a prefix take 74 us, with all seven (126 of 128 rows) 46.
   t.together = 1;
   for (int g = 2; g <= G && g <= PT; ++g)
     if (G % g == 0 && (PT / g * g >= PT - PT / 10 || max_q * g <= PT)) t.together = g;
-  // units of 256 rows where there are enough of them
+  // The prefix with the rows of all sequences together, or ahead of each one's own keys, by the expected time (ns; a
+  // tile of rows against a tile of keys takes 5.4, or 7.8 where a sequence fills one tile only; a unit 25; sums of
+  // parts are written and read at 5 TB/s).  64 sequences behind 2048 tokens, 32 / 8 heads: 5, 8, 16, 24 and 32
+  // queries each 37, 43, 59, 86 and 102 us together, 71 to 74 apart; 16 of 32 behind 16,384: 112 and 165;
+  // 24 of 16 to 300 behind 1003, 28 / 4 heads: 63 and 39.
+  bool all_rows = a.n_prefix > 0 && most >= 2;
+  const long all_parts = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, 2 * PT) * a.kv_heads)));
+  if (all_rows && !t.few) {
+    const double each = (double)cdiv(cdiv(rows, a.seqs), PT), own = (double)a.kv_heads * a.seqs * each;
+    const double pre = (double)cdiv(a.n_prefix, PT), keys = (double)cdiv(max_k, PT);
+    const double apart = own * (pre + keys) * (each > 1 ? 5.4 : 7.8);
+    const double together = (double)a.kv_heads * cdiv(rows, PT) * pre * 5.4 + own * (25.0 + keys * 7.8) +
+                            (double)a.nq * a.heads * (8.0 * a.dh + 16.0) * (all_parts + 1) / 5000.0 + 8000.0;
+    all_rows = together < apart;
+  }
+  // units of 256 rows where there are enough of them, or enough keys, and sequences (or the rows of all) fill
+  // them: 16 x 512 tokens, 32 / 8 heads 62 us (72 with 128), 512 tokens over 33,000 keys 233 (244); but one prompt
+  // of 77 tokens 6.9 (8.3), 512 x 28 / 4 heads 11.7 (12.9), 32 x 8 tokens over up to 8192 keys 49 (65)
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
-  t.rows = units(256) * 2 > sms || units(256) * cdiv(max_k + a.n_prefix, PT) >= 8 * sms ? 256 : 128;
-  const bool all_rows = a.n_prefix > 0 && most >= 2 && (t.few || rows / a.seqs < 96);
+  t.rows = (all_rows || max_q * G > PT) &&
+                   (units(256) * 2 > sms || units(256) * cdiv(max_k + a.n_prefix, PT) >= 8 * sms) ? 256 : 128;
   if (a.n_prefix && !all_rows) t.few = 0;
   auto chunk = [](long keys, long parts) { return (int)std::min(cdiv(cdiv(keys, parts), PT) * PT, 0x7fffff80L); };
   long p1 = 0, p2 = 1;
-  if (all_rows) p1 = std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, t.rows) * a.kv_heads)));
+  if (all_rows) p1 = t.rows == 2 * PT ? all_parts : std::max(1L, std::min(cdiv(a.n_prefix, 512), sms / std::max(1L, cdiv(rows, PT) * a.kv_heads)));
   t.fused = all_rows ? 0 : (int)cdiv(a.n_prefix, PT);
   const long keys = max_k + (long)t.fused * PT;
-  // keys in parts where the longest unit would take longer than the others on one SM (half as many keys each, where
-  // lengths differ or the mask is causal), four for each SM
+  // keys in parts where units are few, four for each SM: 8 texts with 16 to 512 new tokens of up to 16,896 162 -> 106 us
+  // (2, 3, 4, 6 and 8 for each SM: 126, 105, 108, 122 and 120), at least 12 key tiles each (2048 tokens in two parts
+  // of 8 took 78 us, whole 46: the sums of many rows)
   const long tiles = cdiv(keys, PT);
   if (!t.few && units(t.rows) < 2 * sms)
     p2 = std::max(1L, tiles / std::max(12L, tiles * units(t.rows) / (4 * sms)));
@@ -1371,6 +1390,7 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   t.parts2 = (int)p2;
   if (t.few) {
     const long units16 = a.seqs * a.kv_heads * cdiv(max_q * G, F_ROWS), slots = sms * (a.dh == 64 ? few_ctas<64>() : few_ctas<128>());
+    // equal shares, but for keys too few to be worth a join (128 tokens over 10 to 400 keys: 24 us, in whole units 25)
     t.split = max_k > 256;
     t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * std::min(cdiv(max_k, 2 * F_TILE), slots) : units16));
     if (t.split && bytes < parts_of(t) * part_bytes(a) + piece_bytes(a, t)) {
@@ -1418,6 +1438,8 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   if (tiles > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
     return cudaErrorInvalidConfiguration;
   p.slots1 = (int)slots1, p.slots2 = (int)slots2;
+  // all heads of a slot together while the keys of a sequence fit L2: 4608 tokens x 24 heads 123 -> 103 us, 8192 x 24
+  // 318 -> 282; not beyond: 16,384 x 24 1099 -> 1140, 32,760 x 40 6390 -> 6530
   p.by_head = (std::min(a.max_k, a.k_rows) + a.n_prefix) * a.kv_heads * a.dh * 4 > (128L << 20);
   CUtensorMap tq, tk, tv, tpk, tpv;
   if (tiles) {
