@@ -194,44 +194,66 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
   struct Work {
     int q0, rows, head, r0;      // the sequence's first query row and rows, the key head, the unit's first row
     int k_lo, k_hi;              // keys
-    int shift;                   // row r sees keys up to r / G + shift
+    int shift, last;             // token t sees keys before t + shift; the sequence's last token
     int k0;
     int length;                  // of it (split)
     bool starts, ends;           // the unit's keys do
   };
+  int lo = -1;  // the sequence that holds pos, among those of `before` (-1: not known)
   auto find = [&]() {
     while (pos >= base + here) {
       base += here;
       first += F_TH;
       here = add_up(first);
+      lo = -1;
     }
-    int lo = 0;
+    if (lo < 0) {
+      lo = 0;
 #pragma unroll
-    for (int o = F_TH / 2; o > 0; o /= 2)
-      if (first + lo + o < p.seqs && before[lo + o] <= pos - base) lo += o;
+      for (int o = F_TH / 2; o > 0; o /= 2)
+        if (first + lo + o < p.seqs && before[lo + o] <= pos - base) lo += o;
+    } else {  // the same one mostly, or the next
+      while (lo + 1 < F_TH && first + lo + 1 < p.seqs && before[lo + 1] <= pos - base) ++lo;
+    }
     const Span s = spans[lo];
     const int all = p.split ? few_length(s.lk) : 1, blocks = (s.lq * G + F_ROWS - 1) / F_ROWS;
-    const long off = pos - base - before[lo], unit = off / all;
+    const long off = pos - base - before[lo];
+    const long unit = off <= 0x7fffffffL ? (long)((unsigned)off / (unsigned)all) : off / all;
     const int at = (int)(off - unit * all);
     if (p.split && off == 0 && threadIdx.x == 0) p.place[1 + first + lo] = pos;
     Work w;
     w.q0 = s.q0;
     w.rows = s.lq * G;
-    w.head = (int)(unit / blocks);
-    w.r0 = (int)(unit - (long)w.head * blocks) * F_ROWS;
+    w.head = blocks == 1 ? (int)unit : (int)(unit / blocks);
+    w.r0 = blocks == 1 ? 0 : (int)(unit - (long)w.head * blocks) * F_ROWS;
     w.length = p.split ? (int)min((long)(all - at), stop - pos) : 1;
     w.starts = at == 0;
     w.ends = at + w.length == all;
     w.k_lo = max(at - F_COST, 0) * F_TILE;
     w.k_hi = w.ends ? s.lk : max(at + w.length - F_COST, 0) * F_TILE;
-    w.shift = p.causal ? 1 + s.lk - s.lq : 0x40000000;
+    w.shift = 1 + s.lk - s.lq;
+    w.last = s.lq - 1;
     w.k0 = s.k0;
     return w;
   };
-  // keys that row r of the unit sees end before
-  auto limit = [&](const Work& w, int r) {
+  // token and head (of the group) of row r = r0 + i; of the rows that a thread has to do with in a sequence's first
+  // unit (mostly the only one) worked out once
+  struct Row {
+    int tok, g;
+  };
+  auto row_of = [&](int r) {
+    const int t = (unsigned)r / (unsigned)G;
+    return Row{t, r - t * G};
+  };
+  constexpr int ITEMS = F_ROWS * (DH / 8) / F_TH;  // of a thread where the sums are stored: rows F_TH / (DH / 8) apart
+  const Row first_rows[2] = {row_of(n), row_of(n + 8)};
+  const Row last_rows[2] = {row_of(threadIdx.x / (DH / 8)), row_of(threadIdx.x / (DH / 8) + F_TH / (DH / 8))};
+  static_assert(ITEMS <= 2 && F_ROWS * (DH / 8) == ITEMS * F_TH, "a thread's items");
+  const Row end_row = row_of(F_ROWS - 1);
+  // keys that row r (token tok of the sequence) of the unit sees end before
+  auto limit = [&](const Work& w, int r, int tok) {
     if (r >= w.rows) return w.k_lo;
-    return min(max(p.causal ? r / G + w.shift : w.k_hi, w.k_lo), w.k_hi);
+    return min(max(p.causal ? tok + w.shift : w.k_hi, w.k_lo), w.k_hi);
   };
   uint4 qa[2][J], kf[2][J], vf[4][U];
   const uint16_t *kb = nullptr, *vb = nullptr;
@@ -257,13 +279,16 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
   auto begin = [&](const Work& w) {
     kb = p.k + w.k0 * p.ldk + w.head * DH;
     vb = p.v + w.k0 * p.ldv + w.head * DH;
-    end = limit(w, min(w.r0 + F_ROWS, w.rows) - 1);
+    // the last row sees most
+    end = w.r0 + F_ROWS <= w.rows ? limit(w, 0, w.r0 == 0 ? end_row.tok : row_of(w.r0 + F_ROWS - 1).tok)
+                                  : limit(w, 0, w.last);
     const int k0 = w.k_lo + warp * F_KEYS;
     if (k0 < end) load_k(k0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = w.r0 + n + 8 * i;
-      const uint16_t* at = p.q + (long)(w.q0 + r / G) * p.ldq + (long)(w.head * G + r % G) * DH;
+      const Row t = w.r0 == 0 ? first_rows[i] : row_of(r);
+      const uint16_t* at = p.q + (w.q0 + t.tok) * p.ldq + (w.head * G + t.g) * DH;
 #pragma unroll
       for (int j = 0; j < J; ++j)
         qa[i][j] = r < w.rows ? __ldg(reinterpret_cast<const uint4*>(at + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
@@ -274,7 +299,12 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
   Work w = find();
   begin(w);
   while (true) {
-    const int lim[2] = {limit(w, w.r0 + n), limit(w, w.r0 + n + 8)};
+    int lim[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = w.r0 + n + 8 * i;
+      lim[i] = limit(w, r, w.r0 == 0 ? first_rows[i].tok : row_of(r).tok);
+    }
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[U * 8][4];
 #pragma unroll
     for (int i = 0; i < U * 8; ++i)
@@ -390,26 +420,28 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
                             o[u * 8 + t + 2][2 * i + e] * f, o[u * 8 + t + 3][2 * i + e] * f);
     }
     __syncthreads();
-    for (int it = threadIdx.x; it < F_ROWS * (DH / 8); it += F_TH) {
-      const int lr = it / (DH / 8), col = it % (DH / 8) * 8;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int lr = threadIdx.x / (DH / 8) + i * (F_TH / (DH / 8)), col = threadIdx.x % (DH / 8) * 8;
       const int r = done.r0 + lr;
       if (r >= done.rows) continue;
       float top = -INFINITY, den = 0.f, v[8];
 #pragma unroll
-      for (int i = 0; i < F_WARPS; ++i) top = fmaxf(top, sml[i * F_ROWS + lr].x);
+      for (int k = 0; k < F_WARPS; ++k) top = fmaxf(top, sml[k * F_ROWS + lr].x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = 0.f;
 #pragma unroll
-      for (int i = 0; i < F_WARPS; ++i) {
-        const float2 f = sml[i * F_ROWS + lr];
+      for (int k = 0; k < F_WARPS; ++k) {
+        const float2 f = sml[k * F_ROWS + lr];
         den += f.y == 0.f ? 0.f : ex2(f.x - top) * f.y;
-        const float4* row = reinterpret_cast<const float4*>(so + (i * F_ROWS + lr) * LD + col);
+        const float4* row = reinterpret_cast<const float4*>(so + (k * F_ROWS + lr) * LD + col);
         const float4 a = row[0], b = row[1];
         v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
         v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
       }
-      const long tok = done.q0 + r / G;
-      const int h = done.head * G + r % G;
+      const Row t = done.r0 == 0 ? last_rows[i] : row_of(r);
+      const long tok = done.q0 + t.tok;
+      const int h = done.head * G + t.g;
       const bool whole = done.starts && done.ends;
       if (whole && p.parts1 == 0) {
         const float inv = den == 0.f ? 0.f : 1.f / den;
