@@ -1159,8 +1159,12 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
 namespace {
 constexpr int JN_TH = 256, JR_TH = 256;
 
-// The sequence of query row t: the last one that starts at or before it.  Called by a whole warp.
-BAG_DEV int sequence_of(const PackedParams& p, int t) {
+// The sequence of query row t, the last one that starts at or before it, and its span.  Called by a whole warp.
+BAG_DEV int sequence_of(const PackedParams& p, int t, Span* s) {
+  if (p.seqs == p.nq) {  // a token each, mostly
+    *s = span_of(p, t);
+    if (t >= s->q0 && t < s->q0 + s->lq) return t;
+  }
   const int lane = threadIdx.x % 32;
   int lo = 0, n = p.seqs;
   while (n > 1) {
@@ -1170,6 +1174,7 @@ BAG_DEV int sequence_of(const PackedParams& p, int t) {
     lo += skip;
     n = min(step, n - skip);
   }
+  *s = span_of(p, lo);
   return lo;
 }
 }  // namespace
@@ -1222,8 +1227,8 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
   __shared__ const float* from[JN_TH];
   grid_dep_sync();
   const int tok = (int)(blockIdx.x / p.heads), h = (int)(blockIdx.x % p.heads);
-  const int seq = sequence_of(p, tok);
-  const Span s = span_of(p, seq);
+  Span s;
+  const int seq = sequence_of(p, tok, &s);
   if (tok < s.q0 || tok >= s.q0 + s.lq) return;
   const Parts a = parts_of(p, seq, s, tok, h);
   if (a.n == 0) return;
@@ -1296,8 +1301,8 @@ __global__ void __launch_bounds__(JR_TH) attn_join_rows_kernel(const PackedParam
   constexpr int C = DH / 32;
   grid_dep_sync();
   const int tok = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int seq = sequence_of(p, tok);
-  const Span s = span_of(p, seq);
+  Span s;
+  const int seq = sequence_of(p, tok, &s);
   if (tok < s.q0 || tok >= s.q0 + s.lq) return;
 #pragma unroll 2
   for (int h = blockIdx.y * (JR_TH / 32) + warp; h < p.heads; h += gridDim.y * (JR_TH / 32)) {
@@ -1311,6 +1316,21 @@ __global__ void __launch_bounds__(JR_TH) attn_join_rows_kernel(const PackedParam
       bool whole = true;
       const long at = a.at(i0 + min(lane, n - 1), &whole);
       const float2 f = (whole ? p.part_ml : p.piece_ml)[at];
+      const float* from = (whole ? p.part_o : p.piece_o) + at * DH;
+      // four parts' columns at a time, the first ones on their way beside the weights
+      float x[4][C];
+      auto load = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float* v = reinterpret_cast<const float*>(
+                               __shfl_sync(0xffffffffu, reinterpret_cast<uintptr_t>(from), min(i + k, n - 1))) + lane * C;
+          if constexpr (C == 4)
+            *reinterpret_cast<float4*>(x[k]) = *reinterpret_cast<const float4*>(v);
+          else
+            *reinterpret_cast<float2*>(x[k]) = *reinterpret_cast<const float2*>(v);
+        }
+      };
+      load(0);
       float m = f.x;  // of 32 parts, then of those before too
 #pragma unroll
       for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -1320,22 +1340,17 @@ __global__ void __launch_bounds__(JR_TH) attn_join_rows_kernel(const PackedParam
       den *= before;
 #pragma unroll
       for (int i = 0; i < C; ++i) acc[i] *= before;
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float wi = __shfl_sync(0xffffffffu, w, i), li = __shfl_sync(0xffffffffu, f.y, i);
-        const bool wh = __shfl_sync(0xffffffffu, (int)whole, i);
-        const float* v = (wh ? p.part_o : p.piece_o) + __shfl_sync(0xffffffffu, at, i) * DH + lane * C;
-        float x[C];
-        if constexpr (C == 4) {
-          const float4 t = *reinterpret_cast<const float4*>(v);
-          x[0] = t.x, x[1] = t.y, x[2] = t.z, x[3] = t.w;
-        } else {
-          const float2 t = *reinterpret_cast<const float2*>(v);
-          x[0] = t.x, x[1] = t.y;
-        }
-        den += wi * li;
+      for (int i = 0; i < n; i += 4) {
 #pragma unroll
-        for (int e = 0; e < C; ++e) acc[e] += li == 0.f ? 0.f : wi * x[e];  // no weight: x may be NaN
+        for (int k = 0; k < 4; ++k) {
+          const float wi = __shfl_sync(0xffffffffu, w, min(i + k, n - 1)), li = __shfl_sync(0xffffffffu, f.y, min(i + k, n - 1));
+          if (i + k < n) {
+            den += wi * li;
+#pragma unroll
+            for (int e = 0; e < C; ++e) acc[e] += li == 0.f ? 0.f : wi * x[k][e];  // no weight: x may be NaN
+          }
+        }
+        if (i + 4 < n) load(i + 4);
       }
     }
     const float inv = den == 0.f ? 0.f : 1.f / den;
