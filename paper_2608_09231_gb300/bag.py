@@ -8,6 +8,7 @@ missing or fails to load, load() raises.
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -93,6 +94,17 @@ _Z = ctypes.c_size_t
 _F = ctypes.c_float
 
 
+_CODES = {_I: "i", _L: "l", _P: "P", _F: "f", _Z: "N"}
+
+
+def _packer(cls):
+    """A C structure's bytes from its fields (addresses as integers, 0 for none). Filling a ctypes structure instead
+    takes 1.3 us more of a call (9.8 -> 11.1 us for rope, 6.8 -> 8.1 for attention_packed, on the host alone)."""
+    layout = struct.Struct("@" + "".join(_CODES[t] for _, t in cls._fields_) + "0P")
+    assert layout.size == ctypes.sizeof(cls), cls.__name__
+    return layout.pack
+
+
 class RopeArgs(ctypes.Structure):
     _fields_ = [("type", _I), ("layout", _I), ("heads", _I), ("kv_heads", _I), ("dh", _I), ("pairs", _I), ("rows", _L),
                 ("q", _P), ("ldq", _L), ("q_out", _P), ("ldqo", _L), ("k", _P), ("ldk", _L), ("k_out", _P), ("ldko", _L),
@@ -105,6 +117,9 @@ class PackedArgs(ctypes.Structure):
                 ("q", _P), ("ldq", _L), ("k", _P), ("ldk", _L), ("v", _P), ("ldv", _L), ("o", _P), ("ldo", _L),
                 ("lse", _P), ("q_start", _P), ("k_start", _P), ("k_len", _P), ("max_q", _L), ("max_k", _L),
                 ("causal", _I), ("scale", _F), ("work", _P), ("work_bytes", _Z)]
+
+
+_pack_rope, _pack_packed = _packer(RopeArgs), _packer(PackedArgs)
 
 
 def load(path=None):
@@ -149,9 +164,9 @@ def load(path=None):
         "bag_block_pool": ([_P, _P, _I, _L, _L, _I, _P, _P, _L], _I),
         "bag_block_select": ([_P, _P, _I, _L, _L, _I, _P, _P, _L, _L, _I, _I, _P], _I),
         "bag_attention_blocks": ([_P, _P, _L, _P, _L, _P, _L, _I, _L, _L, _I, _I, _P, _I, _P, _L], _I),
-        "bag_rope": ([_P, ctypes.POINTER(RopeArgs)], _I),
-        "bag_attention_packed": ([_P, ctypes.POINTER(PackedArgs)], _I),
-        "bag_attention_prefix": ([_P, ctypes.POINTER(PackedArgs), _P, _L, _P, _L, _L], _I),
+        "bag_rope": ([_P, _P], _I),
+        "bag_attention_packed": ([_P, _P], _I),
+        "bag_attention_prefix": ([_P, _P, _P, _L, _P, _L, _L], _I),
         "bag_attention_work": ([_P, _L, _I, _I, _I, _L, _L, _L, _L, ctypes.POINTER(_Z)], _I),
         "bag_rel_l1": ([_P, _P, _P, _I, _L, _L, _P, _P], _I),
         "bag_rel_l1_noalloc": ([_P, _P, _I, _L, _L, _P, _P], _I),
@@ -501,10 +516,10 @@ class Context:
             kv_heads, capacity = v_heads, v_cap
         elif v is not None and (v_heads != kv_heads or v_cap != capacity):
             raise ValueError(f"v {tuple(v.shape)} and v_out {tuple(v_out.shape)} differ from k and k_out")
-        args = RopeArgs(_T32[dt], kind, heads, kv_heads, dh, f.size, rows, *q_a, *k_a, *v_a,
-                        _vec(slots, "slots", rows, "int32"), capacity, _vec(pos, "pos", rows, "int32"), pos0,
-                        f.ctypes.data, scale, int(inverse))
-        self._chk(self.lib.bag_rope(self.h, ctypes.byref(args)))
+        self._chk(self.lib.bag_rope(self.h, _pack_rope(
+            _T32[dt], kind, heads, kv_heads, dh, f.size, rows, *q_a, *k_a, *v_a,
+            _vec(slots, "slots", rows, "int32") or 0, capacity, _vec(pos, "pos", rows, "int32") or 0, pos0, f.ctypes.data,
+            scale, int(inverse))))
 
     @staticmethod
     def _packed(q, k, v, o, q_start, heads, kv_heads, k_start, k_len, max_q, max_k, causal, scale, lse, work):
@@ -524,10 +539,10 @@ class Context:
             _want(lse, "lse", f"dense float32 [{nq}, {heads}] on the device")
         if work is not None and not (work.is_cuda and work.is_contiguous()):
             _want(work, "work", "dense memory on the device")
-        return PackedArgs(_T16[kind], heads, kv_heads, dh, nq, nk, seqs, qp, ldq, kp, ldk, vp, ldv, op, ldo, _dp(lse),
-                          _vec(q_start, "q_start", seqs + 1, "int32"), _vec(k_start, "k_start", seqs, "int32"),
-                          _vec(k_len, "k_len", seqs, "int32"), max_q or 0, max_k or 0, int(causal), scale or 0.0,
-                          _dp(work), 0 if work is None else work.numel() * work.element_size()), kind, wk
+        return _pack_packed(_T16[kind], heads, kv_heads, dh, nq, nk, seqs, qp, ldq, kp, ldk, vp, ldv, op, ldo, _dp(lse) or 0,
+                            _vec(q_start, "q_start", seqs + 1, "int32"), _vec(k_start, "k_start", seqs, "int32") or 0,
+                            _vec(k_len, "k_len", seqs, "int32") or 0, max_q or 0, max_k or 0, int(causal), scale or 0.0,
+                            _dp(work) or 0, 0 if work is None else work.numel() * work.element_size()), kind, wk
 
     def attention_packed(self, q, k, v, o, q_start, heads, kv_heads=None, k_start=None, k_len=None, max_q=None,
                          max_k=None, causal=True, scale=None, lse=None, work=None):
@@ -538,7 +553,7 @@ class Context:
         CTAs."""
         a, _, _ = self._packed(q, k, v, o, q_start, heads, heads if kv_heads is None else kv_heads, k_start, k_len,
                                max_q, max_k, causal, scale, lse, work)
-        self._chk(self.lib.bag_attention_packed(self.h, ctypes.byref(a)))
+        self._chk(self.lib.bag_attention_packed(self.h, a))
 
     def attention_prefix(self, q, k, v, o, q_start, prefix_k, prefix_v, heads, kv_heads=None, k_start=None,
                          k_len=None, max_q=None, max_k=None, causal=True, scale=None, lse=None, work=None):
@@ -550,7 +565,7 @@ class Context:
         vp, ldv, nv, cv, _ = _mat(prefix_v, "prefix_v", (kind,))
         if ck != wk or cv != wk or n != nv:
             raise ValueError(f"prefix_k {tuple(prefix_k.shape)} and prefix_v {tuple(prefix_v.shape)} do not fit rows of {wk}")
-        self._chk(self.lib.bag_attention_prefix(self.h, ctypes.byref(a), kp, ldk, vp, ldv, n))
+        self._chk(self.lib.bag_attention_prefix(self.h, a, kp, ldk, vp, ldv, n))
 
     def attention_work(self, nq, heads, dh, kv_heads, seqs, max_q, max_k, n_prefix=0):
         """Bytes of workspace for attention_packed, or with n_prefix for attention_prefix, of these sizes."""
@@ -592,7 +607,7 @@ def _mat(t, name, types=None):
     return t.data_ptr(), ld if rows > 1 else max(ld, cols), rows, cols, kind
 
 
-_NO_ROWS = (None, 0, None, 0)
+_NO_ROWS = (0, 0, 0, 0)
 
 
 def _in_out(x, y, name, dh, rows, kind, same_rows):

@@ -41,6 +41,14 @@ def test_structures_match_the_header(tmp_path):
     assert [int(x) for x in source_parts.run(code + "}\n", tmp_path).split()] == want
 
 
+def test_packed_bytes_are_the_structures():
+    """The bytes handed to the library hold every field where the structure has it."""
+    for cls, pack in ((bag.RopeArgs, bag._pack_rope), (bag.PackedArgs, bag._pack_packed)):
+        values = [i + 1 for i in range(len(cls._fields_))]
+        got = cls.from_buffer_copy(pack(*values))
+        assert [getattr(got, f) for f, _ in cls._fields_] == values
+
+
 def test_host_tensors_are_refused():
     ctx = bag.Context.__new__(bag.Context)  # refused before the library is reached
     x = torch.zeros(3, 128)
