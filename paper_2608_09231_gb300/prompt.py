@@ -123,11 +123,11 @@ class TextAttention:
         n = h.shape[0]
         if n != self.pk.shape[0] or n > self.q.shape[0]:
             raise ValueError(f"a prefix of {n} tokens, and a layer for {self.pk.shape[0]} of at most {self.q.shape[0]}")
+        start = torch.tensor([0, n], device=DEV, dtype=torch.int32)
         with ordered(self.ctx):
             q, k, v = self._project(h)
             self.ctx.rope(q, self.q[:n], self.freqs, self.dh, k=k, k_out=self.pk, v=v, v_out=self.pv, layout=self.layout,
                           scale=self.scale)
-            start = torch.tensor([0, n], device=DEV, dtype=torch.int32)
             self.ctx.attention_packed(self.q[:n], self.pk, self.pv, self.o[:n], start, self.heads, self.kv_heads,
                                       work=self.work)
             self._out(h)
@@ -142,9 +142,9 @@ class TextAttention:
             raise ValueError("the prefix comes first")
         if n == 0:
             return
+        pos = step["pos"] + self.seen if self.seen else step["pos"]  # torch's work, before the context's waits for it
         with ordered(c):
             q, k, v = self._project(h)
-            pos = step["pos"] + self.seen if self.seen else step["pos"]
             c.rope(q, self.q[:n], self.freqs, self.dh, pos=pos, k=k, k_out=self.k, v=v, v_out=self.v, slots=step["slots"],
                    layout=self.layout, scale=self.scale)
             args = [self.q[:n], self.k, self.v, self.o[:n], step["q_start"]]

@@ -1,6 +1,7 @@
 """Rotary positions, cache and attention as a text layer uses them together: prompts, more tokens, single ones,
 with and without a shared prefix."""
 
+import contextlib
 import math
 
 import pytest
@@ -106,6 +107,39 @@ def test_on_another_stream(ctx):
         got = got.clone()
     s.synchronize()
     assert torch.equal(got, want)
+
+
+def test_no_work_of_torch_once_the_context_waits(ctx, monkeypatch):
+    """Behind a prefix, on another stream: what torch makes for a step is there when the context's stream has waited
+    for torch's (which is kept busy from then on)."""
+    n = 40
+    h, first = texts(6, 30), texts(7, n)
+    outs, real = [], prompt.ordered
+
+    @contextlib.contextmanager
+    def busy(c):
+        with real(c):
+            torch.cuda._sleep(50_000_000)  # some 25 ms
+            yield
+
+    for late in (False, True):
+        cache = prompt.TextCache(2, 64)
+        layer = layer_of(ctx, cache, 64, n)
+        got = h.clone()
+        if late:
+            monkeypatch.setattr(prompt, "ordered", busy)
+            s = torch.cuda.Stream()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                layer.prefix(first.clone())
+                layer.step(got, cache.extend([10, 20]))
+            s.synchronize()
+        else:
+            layer.prefix(first.clone())
+            layer.step(got, cache.extend([10, 20]))
+        outs.append((got, layer.q[:30].clone()))
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][0], outs[1][0])
 
 
 def test_refusals(ctx):
