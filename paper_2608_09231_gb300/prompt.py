@@ -123,6 +123,8 @@ class TextAttention:
         n = h.shape[0]
         if n != self.pk.shape[0] or n > self.q.shape[0]:
             raise ValueError(f"a prefix of {n} tokens, and a layer for {self.pk.shape[0]} of at most {self.q.shape[0]}")
+        if n == 0:
+            return
         start = torch.tensor([0, n], device=DEV, dtype=torch.int32)
         with ordered(self.ctx):
             q, k, v = self._project(h)

@@ -142,6 +142,15 @@ def test_no_work_of_torch_once_the_context_waits(ctx, monkeypatch):
     assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][0], outs[1][0])
 
 
+def test_an_empty_prefix(ctx):
+    cache = prompt.TextCache(2, 16)
+    layer = layer_of(ctx, cache, 16)
+    layer.prefix(texts(1, 0))
+    h = texts(1, 3)
+    layer.step(h, cache.extend([1, 2]))
+    assert bool(torch.isfinite(h).all())
+
+
 def test_refusals(ctx):
     cache = prompt.TextCache(2, 16)
     layer = layer_of(ctx, cache, 16, prefix=8)
