@@ -527,7 +527,7 @@ class Context:
         op, ldo, no, wo, _ = _mat(o, "o", (kind,))
         kp, ldk, nk, wk, _ = _mat(k, "k", (kind,))
         vp, ldv, nv, wv, _ = _mat(v, "v", (kind,))
-        dh = wq // heads
+        dh = wq // heads if heads else 0
         if wq != heads * dh or wk != kv_heads * dh or wv != wk or nv != nk or no != nq or wo != wq:
             raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)} and o {tuple(o.shape)} do not "
                              f"fit {heads} and {kv_heads} heads")

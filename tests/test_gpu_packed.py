@@ -461,3 +461,11 @@ def test_refusals(ctx):
     ctx.attention_packed(q[:0], k, v, o[:0], st, 4, 2, **b.dev)
     ctx.attention_packed(q, k, v, o, st[:1], 4, 2, k_start=st[:0], k_len=st[:0])
     assert bool((o == 9).all())
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(0, 2), (4, 0), (0, 0), (-4, -2)])
+def test_heads_that_are_none(heads, kv_heads, ctx):
+    b = Batch([(4, 9)], 4, 2, 128, "bf16", pad=0)
+    with pytest.raises((ValueError, bag.BagError)):
+        ctx.attention_packed(b.q, b.k, b.v, b.o, i32(b.starts), heads, kv_heads, **b.dev)
+    assert bool((b.o == 9).all())
