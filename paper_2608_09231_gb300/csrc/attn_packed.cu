@@ -40,6 +40,7 @@ struct PackedParams {
   // tokens of all sequences and of each
   int together, tokens, slots1, slots2;
   int by_head;  // order of the units: a head after the other, or all heads of a slot
+  int beside;   // the kernel before is attn_few_kernel of the same call, which it has nothing to wait for from
   int* err;
   // few-row kernel: whether a unit's keys may be shared among CTAs, their sums (see attn_few_kernel)
   int few, split;
@@ -754,7 +755,13 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     tmem_alloc(tmem_slot, M::TMEM_COLS);
     tmem_relinquish();
   }
-  grid_dep_sync();
+  // Beside the few-row kernel of a call, whose sums only the join reads: it let this one start when all of its CTAs
+  // had waited for what came before the call, so this one has CTAs wherever an SM is done with those, and waits
+  // for it at the end, for the kernels that follow.
+  if (p.beside)
+    grid_dep_launch();
+  else
+    grid_dep_sync();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1154,6 +1161,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
     tc_fence_after();
     tmem_dealloc(tmem, M::TMEM_COLS);
   }
+  if (p.beside) grid_dep_wait();
 }
 
 namespace {
@@ -1482,6 +1490,7 @@ cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {
   p.err = a.err;
   const long tiles = (slots1 * t.parts1 + slots2 * t.parts2) * groups;
   const long few = t.few ? t.ctas : 0, joins = a.nq * a.heads;
+  p.beside = few && tiles;
   if (tiles > 0x7fffffffL || joins > 0x7fffffffL || slots1 > 0x7fffffffL || slots2 > 0x7fffffffL)
     return cudaErrorInvalidConfiguration;
   p.slots1 = (int)slots1, p.slots2 = (int)slots2;

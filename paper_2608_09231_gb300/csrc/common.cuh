@@ -22,9 +22,11 @@ namespace bag {
 // early (they wait the same way).  Every kernel calls this before its first access to
 // global memory that a kernel before it on the stream may write (the gate reads its
 // parameters ahead of it); in a kernel launched without the attribute both are no-ops.
+__device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_dep_sync() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  grid_dep_wait();
+  grid_dep_launch();
 }
 
 // ---------------------------------------------------------------------------
