@@ -405,6 +405,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      if (done.r0 + n + 8 * i >= done.rows) continue;  // no such row
       float top = -INFINITY;
 #pragma unroll
       for (int v = 0; v < F_WARPS; ++v) top = fmaxf(top, sml[v * F_ROWS + n + 8 * i].x);
