@@ -136,10 +136,12 @@ BAG_DEV int few_length(int lk) { return (lk + F_TILE - 1) / F_TILE + F_COST; }
 // loads are in flight while the warps' sums are joined.
 // Bound: HBM.  64 tokens over 512 to 32,767 keys each (32 heads, 8 key heads, 2.3 GB) 360 us, 6.4 TB/s or 95 % of the
 // copy rate (a grid of sequences, heads and parts of up to 8192 keys: 392 to 546); one token over 131,071
-// keys 51 us (floor 40, the rest a launch's start and the join).  Four warps a CTA and two CTAs on an SM
+// keys 51 us (floor 40, the rest a launch's start and the join).  Few keys a unit: latency, a unit's loads, the join
+// of its warps; 128 tokens over 10 to 400 keys 20 us, floor 8.  Four warps a CTA and two CTAs on an SM
 // instead of eight and one: 376 -> 363 us, 128 tokens over short own keys 85 -> 65.  bf16 weights enter P V in
 // two parts, whose rounding would otherwise be the largest error (2-norm 1.9e-3 against 1.7e-3, the
-// output's own): 4 % of the time, as the products are not what bounds it.
+// output's own).  With at most eight rows the second parts are rows 8 to 15 of the same product, added up at
+// the end (two products: 16 tokens over 4097 keys 51.7 us, so 50.4), and the softmax takes half.
 template <bool F16, int DH>
 __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const PackedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -300,6 +302,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
   Work w = find();
   begin(w);
   while (true) {
+    const bool eight = w.rows - w.r0 <= 8;  // rows, whose weights' second parts take the place of the other eight
     int lim[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -328,6 +331,10 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
       float alpha[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        if (i == 1 && eight) {
+          alpha[1] = alpha[0];
+          break;
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -362,30 +369,41 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
           o[i][3] *= alpha[1];
         }
       }
-      const uint32_t a0 = pack16<F16>(sc[0][0], sc[0][1]), a1 = pack16<F16>(sc[0][2], sc[0][3]),
-                     a2 = pack16<F16>(sc[1][0], sc[1][1]), a3 = pack16<F16>(sc[1][2], sc[1][3]);
-      // bf16: what its eight bits leave of a weight, as a second operand
+      const uint32_t a0 = pack16<F16>(sc[0][0], sc[0][1]), a2 = pack16<F16>(sc[1][0], sc[1][1]);
+      // bf16: what its eight bits leave of a weight
       auto rest = [](uint32_t w, float a, float b) {
-        return pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+        return F16 ? 0u : pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
       };
-      uint32_t r0, r1, r2, r3;
-      if constexpr (!F16) {
-        r0 = rest(a0, sc[0][0], sc[0][1]), r1 = rest(a1, sc[0][2], sc[0][3]);
-        r2 = rest(a2, sc[1][0], sc[1][1]), r3 = rest(a3, sc[1][2], sc[1][3]);
-      }
+      // P V; both: with a second operand for what is left of the weights
+      auto products = [&](auto both, uint32_t a1, uint32_t a3, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          auto word = [&](const uint4& v) { return t < 2 ? v.x : (t < 4 ? v.y : (t < 6 ? v.z : v.w)); };
-          const uint32_t sel = t & 1 ? 0x7632u : 0x5410u;
-          const uint32_t b0 = __byte_perm(word(vf[0][u]), word(vf[1][u]), sel),
-                         b1 = __byte_perm(word(vf[2][u]), word(vf[3][u]), sel);
-          mma16816<F16>(o[u * 8 + t], a0, a1, a2, a3, b0, b1);
-          if constexpr (!F16) mma16816<F16>(o[u * 8 + t], r0, r1, r2, r3, b0, b1);
+          for (int t = 0; t < 8; ++t) {
+            auto word = [&](const uint4& v) { return t < 2 ? v.x : (t < 4 ? v.y : (t < 6 ? v.z : v.w)); };
+            const uint32_t sel = t & 1 ? 0x7632u : 0x5410u;
+            const uint32_t b0 = __byte_perm(word(vf[0][u]), word(vf[1][u]), sel),
+                           b1 = __byte_perm(word(vf[2][u]), word(vf[3][u]), sel);
+            mma16816<F16>(o[u * 8 + t], a0, a1, a2, a3, b0, b1);
+            if constexpr (decltype(both)::value) mma16816<F16>(o[u * 8 + t], r0, r1, r2, r3, b0, b1);
+          }
         }
+      };
+      const uint32_t r0 = rest(a0, sc[0][0], sc[0][1]), r2 = rest(a2, sc[1][0], sc[1][1]);
+      if (eight) {
+        products(std::false_type{}, r0, r2, 0, 0, 0, 0);
+      } else {
+        const uint32_t a1 = pack16<F16>(sc[0][2], sc[0][3]), a3 = pack16<F16>(sc[1][2], sc[1][3]);
+        products(std::bool_constant<!F16>{}, a1, a3, r0, rest(a1, sc[0][2], sc[0][3]), r2, rest(a3, sc[1][2], sc[1][3]));
       }
       if (k0 + F_TILE < end) load_v(k0 + F_TILE);
+    }
+    if (!F16 && eight) {
+#pragma unroll
+      for (int i = 0; i < U * 8; ++i) {
+        o[i][0] += o[i][2];
+        o[i][1] += o[i][3];
+      }
     }
     // where the sums go, then the next unit's loads
     const Work done = w;
