@@ -129,11 +129,11 @@ BAG_DEV int few_length(int lk) { return (lk + F_TILE - 1) / F_TILE + F_COST; }
 // 2 c + 1, 2 c + 8 and 2 c + 9 for P V, whose pairs of keys a byte permutation makes; its column n of
 // product t is then head column 64 u + 8 n + t, and a lane ends with runs of 8 columns of the output.
 // Keys past the last are loaded as zeros (whatever lies there, NaN included).
-// Split: the key tiles of all units lie in a row, and each CTA takes an equal share of them, so that lengths need
-// not be alike and one wave of CTAs does it all; every CTA adds the lengths up for itself.  A unit that lies in
-// one CTA's share is finished there; of the others a CTA holds at most two pieces, one that starts its
-// unit (piece 1) and one that does not (piece 0), which attn_join_kernel adds up.  The next unit's first
-// loads are in flight while the warps' sums are joined.
+// Units lie in a row, of which each CTA takes an equal share, and finds the next one from the last.  Split: their key
+// tiles do, so that lengths need not be alike and one wave of CTAs does it all; every CTA adds the lengths up
+// for itself.  A unit that lies in one CTA's share is finished there; of the others a CTA holds at most two
+// pieces, one that starts its unit (piece 1) and one that does not (piece 0), which attn_join_kernel adds up.
+// The next unit's first loads are in flight while the warps' sums are joined.
 // Bound: HBM.  64 tokens over 512 to 32,767 keys each (32 heads, 8 key heads, 2.3 GB) 360 us, 6.4 TB/s or 95 % of the
 // copy rate (a grid of sequences, heads and parts of up to 8192 keys: 392 to 546); one token over 131,071
 // keys 51 us (floor 40, the rest a launch's start and the join).  Few keys a unit: latency, a unit's loads, the join
@@ -188,9 +188,9 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
   long here = add_up(0), total = here;
   for (int i = F_TH; i < p.seqs; i += F_TH) total += add_up(i);
   if (p.seqs > F_TH) add_up(0);
-  const long share = p.split ? (total + gridDim.x - 1) / gridDim.x : 1;
+  const long share = (total + gridDim.x - 1) / gridDim.x;
   long pos = (long)blockIdx.x * share;
-  const long stop = p.split ? min(pos + share, total) : total;
+  const long stop = min(pos + share, total);
   if (p.split && blockIdx.x == 0 && threadIdx.x == 0) p.place[0] = share;
 
   // what is done next: a unit, or some tiles of one
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
     w.rows = s.lq * G;
     w.head = blocks == 1 ? (int)unit : (int)(unit / blocks);
     w.r0 = blocks == 1 ? 0 : (int)(unit - (long)w.head * blocks) * F_ROWS;
-    w.length = p.split ? (int)min((long)(all - at), stop - pos) : 1;
+    w.length = (int)min((long)(all - at), stop - pos);
     w.starts = at == 0;
     w.ends = at + w.length == all;
     w.k_lo = max(at - F_COST, 0) * F_TILE;
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
     }
     // where the sums go, then the next unit's loads
     const Work done = w;
-    pos += p.split ? w.length : gridDim.x;
+    pos += w.length;
     const bool more = pos < stop;
     if (more) {
       w = find();
@@ -1464,7 +1464,8 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   t.parts2 = (int)p2;
   if (t.few) {
     const long units16 = a.seqs * a.kv_heads * cdiv(max_q * G, F_ROWS), slots = sms * (a.dh == 64 ? few_ctas<64>() : few_ctas<128>());
-    // equal shares, but for keys too few to be worth a join (128 tokens over 10 to 400 keys: 24 us, in whole units 25)
+    // equal shares, but for keys too few to be worth a join (2 to 3 us).  Of 32 / 8 heads, in whole units and in equal
+    // shares: 64 tokens over 200 keys each 14 and 17 us, 128 over 6 to 200 20 and 17, over 6 to 400 33 and 18
     t.split = max_k > 256;
     t.ctas = (int)std::max(1L, std::min(slots, t.split ? units16 * std::min(cdiv(max_k, 2 * F_TILE), slots) : units16));
     if (t.split && bytes < parts_of(t) * part_bytes(a) + piece_bytes(a, t)) {
