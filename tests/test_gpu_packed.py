@@ -393,6 +393,44 @@ def test_captured_with_lengths_that_change(prefix, ctx):
         ctx.set_stream(0)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_own_keys_that_outlast_the_prefix(captured, ctx):
+    """An estimate of one key leaves 40,000 to a CTA each, which end long after the prefix's kernel has: what follows on
+    the stream, the joined sums and then what overwrites the cache, waits for both."""
+    s = torch.cuda.Stream()
+    try:
+        with torch.cuda.stream(s):
+            ctx.set_stream(s.cuda_stream)
+            b = Batch([(1, 40000), (1, 5), (2, 20000)], 8, 2, 128, "bf16", prefix=130)
+            n = ctx.attention_work(b.q.shape[0], 8, 128, 2, 3, 2, 1, 130)
+            work = torch.full((n // 4,), math.nan, device=DEV)
+            k, v, starts = b.k.clone(), b.v.clone(), i32(b.starts)
+            outs = []
+
+            def call():
+                b.k.copy_(k)
+                b.v.copy_(v)
+                ctx.attention_prefix(b.q, b.k, b.v, b.o, starts, b.pk, b.pv, 8, 2, **b.dev, max_q=2, max_k=1, lse=b.lse,
+                                     work=work)
+                b.k.fill_(7.0)
+                b.v.fill_(math.nan)
+
+            if captured:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=s):
+                    call()
+            for _ in range(4):
+                graph.replay() if captured else call()
+                outs.append(b.o.clone())
+            s.synchronize()
+            b.k.copy_(k)
+            b.v.copy_(v)
+            b.check()
+            assert all(torch.equal(outs[0].view(torch.int16), x.view(torch.int16)) for x in outs)
+    finally:
+        ctx.set_stream(0)
+
+
 def test_on_another_stream(ctx):
     """Inputs made on a stream right before the call, read right after it."""
     s = torch.cuda.Stream()
