@@ -75,7 +75,7 @@ class TextCache:
         n, s = int(first[-1]), self.texts
         q_start, k_start, k_len, pos, slots = dev.split([s + 1, s, s, n, n])
         return dict(q_start=q_start, k_start=k_start, k_len=k_len, pos=pos, slots=slots, rows=n,
-                    max_q=max(new, default=0), max_k=max(self.lens, default=0))
+                    max_q=max(new, default=0), max_k=max(self.lens, default=0), cache=self)
 
 
 class TextAttention:
@@ -85,7 +85,7 @@ class TextAttention:
 
     def __init__(self, ctx, weights, heads, kv_heads, cache, rows, prefix=0, dh=128, theta=10000.0, layout="half", **scaling):
         self.ctx, self.heads, self.kv_heads, self.dh, self.layout = ctx, heads, kv_heads, dh, layout
-        self.texts = cache.texts
+        self.texts, self.room = cache.texts, cache.room
         wq, d = weights["wqkv"].shape
         if wq != (heads + 2 * kv_heads) * dh or weights["wo"].shape != (d, heads * dh):
             raise ValueError(f"weights of {tuple(weights['wqkv'].shape)} and {tuple(weights['wo'].shape)} do not fit "
@@ -137,6 +137,12 @@ class TextAttention:
 
     def step(self, h, step):
         """The tokens h [rows, d] (fp32, updated in place) that TextCache.extend made `step` for."""
+        cache = step["cache"]
+        if (cache.texts, cache.room) != (self.texts, self.room):
+            raise ValueError(f"a step of {cache.texts} texts of {cache.room} tokens, and a layer for {self.texts} of {self.room}")
+        self._run(h, step)
+
+    def _run(self, h, step):
         n, c = step["rows"], self.ctx
         if h.shape[0] != n or n > self.q.shape[0]:
             raise ValueError(f"{h.shape[0]} rows for a step of {n}, of at most {self.q.shape[0]}")
