@@ -57,10 +57,13 @@ def rope_frequencies(pairs, theta=10000.0, factor=1.0, scaling="parts", original
 
 
 class TextCache:
-    """Rows of the texts in a cache: text i has rows [i * room, i * room + its length)."""
+    """Rows of the texts in a cache: text i has rows [i * room, i * room + its length).  Lengths grow when a step is made
+    (extend), so that every step runs through every layer, or is taken back."""
 
     def __init__(self, texts, room):
         self.texts, self.room, self.lens = texts, room, [0] * texts
+        self.made = 0   # steps so far
+        self.gone = []  # ranges of those that were taken back
 
     def extend(self, new):
         """What a step that adds new[i] tokens to text i hands to the operators (rows in the texts' order)."""
@@ -69,13 +72,34 @@ class TextCache:
         first = np.concatenate([[0], np.cumsum(new)])
         pos = np.concatenate([np.arange(m, m + n) for n, m in zip(new, self.lens)] or [[]])
         place = np.repeat(np.arange(self.texts) * self.room, new)
-        self.lens = [n + m for n, m in zip(new, self.lens)]
+        before, self.lens = list(self.lens), [n + m for n, m in zip(new, self.lens)]
+        self.made += 1
         ints = np.concatenate([first, np.arange(self.texts) * self.room, self.lens, pos, place + pos])
         dev = torch.from_numpy(ints.astype(np.int32)).to(DEV)  # one copy for all
         n, s = int(first[-1]), self.texts
         q_start, k_start, k_len, pos, slots = dev.split([s + 1, s, s, n, n])
         return dict(q_start=q_start, k_start=k_start, k_len=k_len, pos=pos, slots=slots, rows=n,
-                    max_q=max(new, default=0), max_k=max(self.lens, default=0), cache=self)
+                    max_q=max(new, default=0), max_k=max(self.lens, default=0), cache=self, number=self.made,
+                    before=before, after=list(self.lens), ran=set())
+
+    def take_back(self, step):
+        """Lengths as before `step`, which does not run, nor do those made after it.  A layer does this itself with a
+        step that it refuses."""
+        if not any(first <= step["number"] < end for first, end in self.gone):
+            self.lens = list(step["before"])
+            self.gone.append((step["number"], self.made + 1))
+
+    def stands(self, step):
+        """Whether `step` may run: one that was taken back does so if no other has been made since, and counts again."""
+        n = step["number"]
+        if not any(first <= n < end for first, end in self.gone):
+            return True
+        first, end = self.gone[-1]
+        if not first <= n < end or end != self.made + 1 or self.lens != step["before"]:
+            return False
+        self.gone[-1] = (n + 1, end)
+        self.lens = list(step["after"])
+        return True
 
 
 class TextAttention:
@@ -136,11 +160,21 @@ class TextAttention:
         self.seen = n
 
     def step(self, h, step):
-        """The tokens h [rows, d] (fp32, updated in place) that TextCache.extend made `step` for."""
+        """The tokens h [rows, d] (fp32, updated in place) that TextCache.extend made `step` for.  A step that is refused is
+        taken back: the texts are as long as before it, and it may be given again unless another is made first."""
         cache = step["cache"]
-        if (cache.texts, cache.room) != (self.texts, self.room):
-            raise ValueError(f"a step of {cache.texts} texts of {cache.room} tokens, and a layer for {self.texts} of {self.room}")
-        self._run(h, step)
+        try:
+            if (cache.texts, cache.room) != (self.texts, self.room):
+                raise ValueError(f"a step of {cache.texts} texts of {cache.room} tokens, and a layer for {self.texts} of "
+                                 f"{self.room}")
+            if not cache.stands(step):
+                raise ValueError("the step was taken back, and others have been made since")
+            self._run(h, step)
+            step["ran"].add(id(self))
+        except Exception:
+            if id(self) not in step["ran"]:
+                cache.take_back(step)
+            raise
 
     def _run(self, h, step):
         n, c = step["rows"], self.ctx

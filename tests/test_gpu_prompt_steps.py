@@ -1,0 +1,53 @@
+"""Text layers whose steps were refused before."""
+
+import math
+
+import pytest
+import torch
+
+import test_gpu_prompt as T
+from paper_2608_09231_gb300 import bag, prompt
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def ctx(lib):
+    c = bag.create("tiny", T=2, B=1)
+    yield c
+    c.operators_status()
+    c.close()
+
+
+@pytest.mark.parametrize("prefix", [0, 30])
+def test_a_refused_step_leaves_no_trace(prefix, ctx):
+    """Refusals for the rows, the type, the layer's size and the texts' places; then the steps give what they give alone."""
+    outs = []
+    for refused in (False, True):
+        cache = prompt.TextCache(2, 64)
+        layer = T.layer_of(ctx, cache, 40, prefix)
+        layer.k.fill_(math.nan)
+        layer.v.fill_(math.nan)
+        if refused and prefix:
+            with pytest.raises(ValueError, match="prefix comes first"):
+                layer.step(T.texts(1, 2), cache.extend([1, 1]))
+        if prefix:
+            layer.prefix(T.texts(9, prefix))
+        got = []
+        for key, new in enumerate(([20, 5], [1, 1], [0, 9])):
+            n = sum(new)
+            if refused:
+                for bad, rows in ((T.texts(1, n + 1), new), (T.texts(1, n).double(), new), (T.texts(1, n)[:, :380], new),
+                                  (T.texts(1, 41), [41 - n, n])):
+                    with pytest.raises((ValueError, bag.BagError)):
+                        layer.step(bad, cache.extend(rows))
+                other = prompt.TextCache(3, 64)
+                with pytest.raises(ValueError, match="a layer for 2"):
+                    layer.step(T.texts(1, 3), other.extend([1, 1, 1]))
+            h = T.texts(key, n)
+            layer.step(h, cache.extend(new))
+            got.append(h)
+        assert cache.lens == [21, 15]
+        outs.append(got)
+    assert all(bool(torch.isfinite(a).all()) and torch.equal(a, b) for a, b in zip(*outs))
