@@ -145,8 +145,9 @@ class TextAttention:
     def prefix(self, h):
         """The tokens h [n, d] (fp32, updated in place) of the prefix that all texts start with, before any of theirs."""
         n = h.shape[0]
-        if n != self.pk.shape[0] or n > self.q.shape[0]:
-            raise ValueError(f"a prefix of {n} tokens, and a layer for {self.pk.shape[0]} of at most {self.q.shape[0]}")
+        if h.shape != (self.pk.shape[0], self.wqkv.cols) or n > self.q.shape[0]:
+            raise ValueError(f"a prefix of {tuple(h.shape)}, and a layer for one of {self.pk.shape[0]} rows of {self.wqkv.cols}, of "
+                             f"at most {self.q.shape[0]}")
         if n == 0:
             return
         start = torch.tensor([0, n], device=DEV, dtype=torch.int32)
@@ -178,8 +179,8 @@ class TextAttention:
 
     def _run(self, h, step):
         n, c = step["rows"], self.ctx
-        if h.shape[0] != n or n > self.q.shape[0]:
-            raise ValueError(f"{h.shape[0]} rows for a step of {n}, of at most {self.q.shape[0]}")
+        if h.shape != (n, self.wqkv.cols) or n > self.q.shape[0]:
+            raise ValueError(f"{tuple(h.shape)} for a step of {n} rows of {self.wqkv.cols}, of at most {self.q.shape[0]}")
         if self.seen != self.pk.shape[0]:
             raise ValueError("the prefix comes first")
         if n == 0:

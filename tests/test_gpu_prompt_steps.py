@@ -51,3 +51,21 @@ def test_a_refused_step_leaves_no_trace(prefix, ctx):
         assert cache.lens == [21, 15]
         outs.append(got)
     assert all(bool(torch.isfinite(a).all()) and torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("prefix", [0, 8])
+def test_rows_of_another_width(prefix, ctx):
+    """Rows that are wider than the weights, but not than the memory for their codes, are refused before anything runs."""
+    weights = prompt.random_weights(380, 6, 2)
+    cache = prompt.TextCache(1, 16)
+    layer = prompt.TextAttention(ctx, weights, 6, 2, cache, 16, prefix)
+    if prefix:
+        with pytest.raises(ValueError):
+            layer.prefix(T.texts(1, prefix))
+        layer.prefix(T.texts(1, prefix)[:, :380].contiguous())
+    layer.k.fill_(9.0)
+    h = T.texts(2, 4)
+    before = h.clone()
+    with pytest.raises(ValueError):
+        layer.step(h, cache.extend([4]))
+    assert torch.equal(h, before) and bool((layer.k == 9).all()) and cache.lens == [0]
