@@ -87,7 +87,7 @@ class TextCache:
         step that it refuses."""
         if not any(first <= step["number"] < end for first, end in self.gone):
             self.lens = list(step["before"])
-            self.gone.append((step["number"], self.made + 1))
+            self.gone = [r for r in self.gone if r[0] < step["number"]] + [(step["number"], self.made + 1)]
 
     def stands(self, step):
         """Whether `step` may run: one that was taken back does so if no other has been made since, and counts again."""

@@ -114,3 +114,23 @@ def test_lengths_set_by_hand():
     cache.lens[0] = 7
     assert s["after"] == [1, 2] and s["before"] == [0, 0]
     assert cache.extend([1, 0])["pos"].tolist() == [7]
+
+
+def test_taken_back_and_given_again_many_times():
+    """A later step and then the one before it; both again; what they are does not depend on how often."""
+    cache = prompt.TextCache(1, 10)
+    layer = Layer(cache)
+    s, t = cache.extend([2]), cache.extend([3])
+    for _ in range(3):
+        cache.take_back(t)
+        assert cache.lens == [2]
+        cache.take_back(s)
+        assert cache.lens == [0]
+        layer.step(h(2), s)
+        layer.step(h(3), t)
+        layer.step(h(3), t)
+        assert cache.lens == [5]
+    assert len(cache.gone) == 1
+    u = cache.extend([1])
+    layer.step(h(1), u)
+    assert cache.lens == [6] and layer.log[-1] == [6]
