@@ -488,8 +488,8 @@ bag_status bag_rope(bag_ctx* ctx, const bag_rope_args* a);
  * (q_start does not decrease); its keys and values are the k_len[i] rows of k and v from row
  * k_start[i] on, or, where k_start and k_len are null, the rows of its queries.  o = softmax(scale q
  * k^T) v; with causal, query t of lq sees keys 0 .. t + lk - lq, so queries are a sequence's last tokens.
- * A row that sees no key gets zeros (lse -inf); rows of q outside every sequence keep what o and lse
- * hold there.  Ranges that leave k's or q's rows are clipped to them.  heads query heads share
+ * A row that sees no key gets zeros (lse -inf), one that sees only scores of minus infinity NaN (lse -inf); rows of q
+ * outside every sequence keep what o and lse hold there.  Ranges that leave k's or q's rows are clipped to them.  heads query heads share
  * kv_heads key heads as in bag_attention_blocks.  Rows of k and v that belong to no sequence may
  * hold anything, NaN included; a NaN in a sequence's own values reaches all of its rows.
  * Scores, softmax and sums are fp32; weights are rounded to `type` before they meet v (bf16 ones of sequences

@@ -5,7 +5,8 @@
 //
 // over the prefix's keys and the own keys j <= t + lk - lq.  Sums over parts of the keys are kept as
 // (m, l, O) with l = sum 2^(s - m), O = sum 2^(s - m) v, s in log2 units; parts are joined by
-// m = max m_i, l = sum 2^(m_i - m) l_i, O likewise.
+// m = max m_i, l = sum 2^(m_i - m) l_i, O likewise.  l = 0: no key is seen; l = 1 with m of minus infinity: keys are
+// seen, but all scores are minus infinity, which weighs nothing beside other parts and makes a row without them NaN.
 //
 // A sequence's rows of a key head are its query tokens times the heads that share it.  At most 16 of them: the
 // keys are what there is to read, and attn_few_kernel streams them.  More: attn_packed_kernel, on the tensor
@@ -74,6 +75,13 @@ BAG_DEV Span span_all(const PackedParams& p) {
 // come from the caller's estimate of the longest sequence).
 BAG_DEV int own_parts(const PackedParams& p, int lk) {
   return (int)min(((long)p.fused * 128 + lk + p.chunk2 - 1) / p.chunk2, (long)p.parts2);
+}
+
+// 2^(m - top) of a part with (m, l) where the parts' largest maximum is top, and what a row's joined sums are
+// multiplied by: zero where no key is seen, NaN where there are only scores of minus infinity.
+BAG_DEV float part_weight(float2 ml, float top) { return ml.y == 0.f ? 0.f : (ml.x == top ? 1.f : ex2(ml.x - top)); }
+BAG_DEV float inverse_sum(float top, float l) {
+  return l == 0.f ? 0.f : (top == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l);
 }
 
 template <bool F16>
@@ -453,18 +461,19 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
 #pragma unroll
       for (int k = 0; k < F_WARPS; ++k) {
         const float2 f = sml[k * F_ROWS + lr];
-        den += f.y == 0.f ? 0.f : ex2(f.x - top) * f.y;
+        den += part_weight(f, top) * f.y;
         const float4* row = reinterpret_cast<const float4*>(so + (k * F_ROWS + lr) * LD + col);
         const float4 a = row[0], b = row[1];
         v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
         v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
       }
       const Row t = done.r0 == 0 ? last_rows[i] : row_of(r);
+      if (den == 0.f && limit(done, r, t.tok) > done.k_lo) den = 1.f;  // all scores are minus infinity
       const long tok = done.q0 + t.tok;
       const int h = done.head * G + t.g;
       const bool whole = done.starts && done.ends;
       if (whole && p.parts1 == 0) {
-        const float inv = den == 0.f ? 0.f : 1.f / den;
+        const float inv = inverse_sum(top, den);
         uint4 x;
         x.x = pack16<F16>(v[0] * inv, v[1] * inv);
         x.y = pack16<F16>(v[2] * inv, v[3] * inv);
@@ -1104,8 +1113,9 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
       steps += tiles;
       // while the last product is on its way: the row's maximum and sum, and where its output goes, for the lanes
       // that store it
+      if (l == 0.f && tiles > 0 && limit > 0) l = 1.f;  // the row sees keys, but all scores are minus infinity
       const bool any = l > 0.f || l != l;  // the row sees a key (or NaN)
-      const float f = 1.f / l;
+      const float f = inverse_sum(m_use, l);
       const bool direct = u.direct;
       {
         const int mine = token(), h = u.head0 + row - of * p.together;
@@ -1281,7 +1291,7 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
       const long at = a.at(i0 + threadIdx.x, &whole);
       const float2 f = (whole ? p.part_ml : p.piece_ml)[at];
       from[threadIdx.x] = (whole ? p.part_o : p.piece_o) + at * DH;
-      weight[threadIdx.x] = make_float2(f.y == 0.f ? 0.f : ex2(f.x - top), f.y);
+      weight[threadIdx.x] = make_float2(part_weight(f, top), f.y);
     }
     __syncthreads();
     const int n = min(JN_TH, a.n - i0);
@@ -1312,7 +1322,7 @@ __global__ void __launch_bounds__(JN_TH) attn_join_kernel(const PackedParams p) 
     acc.z += v.z;
     acc.w += v.w;
   }
-  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const float inv = inverse_sum(top, den);
   uint2 u;
   u.x = pack16<F16>(acc.x * inv, acc.y * inv);
   u.y = pack16<F16>(acc.z * inv, acc.w * inv);
@@ -1362,7 +1372,7 @@ __global__ void __launch_bounds__(JR_TH) attn_join_rows_kernel(const PackedParam
 #pragma unroll
       for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       m = fmaxf(m, top);
-      const float before = den == 0.f ? 0.f : ex2(top - m), w = f.y == 0.f ? 0.f : ex2(f.x - m);
+      const float before = part_weight(make_float2(top, den), m), w = part_weight(f, m);
       top = m;
       den *= before;
 #pragma unroll
@@ -1380,7 +1390,7 @@ __global__ void __launch_bounds__(JR_TH) attn_join_rows_kernel(const PackedParam
         if (i + 4 < n) load(i + 4);
       }
     }
-    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const float inv = inverse_sum(top, den);
     uint16_t* o = p.o + tok * p.ldo + (long)h * DH + lane * C;
     if constexpr (C == 4)
       *reinterpret_cast<uint2*>(o) = make_uint2(pack16<F16>(acc[0] * inv, acc[1] * inv), pack16<F16>(acc[2] * inv, acc[3] * inv));
