@@ -493,7 +493,8 @@ bag_status bag_rope(bag_ctx* ctx, const bag_rope_args* a);
  * kv_heads key heads as in bag_attention_blocks.  Rows of k and v that belong to no sequence may
  * hold anything, NaN included; a NaN in a sequence's own values reaches all of its rows.
  * Scores, softmax and sums are fp32; weights are rounded to `type` before they meet v (bf16 ones of sequences
- * of at most 16 rows a key head, such as single tokens, to twice its bits).
+ * of at most 16 rows a key head, such as single tokens, to twice its bits; fp16 ones to 2^-32 of the largest at
+ * most, below its normal range).
  *
  * max_q and max_k: the most queries and keys of a sequence, as far as the caller knows (0: does not);
  * a wrong number costs time, not correctness.  work: device workspace of work_bytes, 16-byte aligned,

@@ -84,6 +84,12 @@ BAG_DEV float inverse_sum(float top, float l) {
   return l == 0.f ? 0.f : (top == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l);
 }
 
+// fp16 weights: m is kept this much below the largest score, so that a row's largest weight is 2^7 to 2^15 (65504 is
+// the type's end) and weights keep all their bits down to 2^-21 of it, and some down to 2^-32; with the largest at 1,
+// many keys of weights below 2^-25 would vanish from O and stay in l.  bf16 has the range of fp32.
+template <bool F16>
+constexpr float kWeightsUp = F16 ? 7.f : 0.f;
+
 template <bool F16>
 BAG_DEV uint32_t pack16(float a, float b) {
   return F16 ? pack_f16x2(a, b) : pack_bf16x2(a, b);
@@ -350,7 +356,7 @@ __global__ void __launch_bounds__(F_TH, few_ctas<DH>()) attn_few_kernel(const Pa
             if (k0 + 8 * t + 2 * c + e >= lim[i]) sc[t][2 * i + e] = -INFINITY;
         float mx = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) * p.scale_log2;
+        mx = fmaf(fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)), p.scale_log2, -kWeightsUp<F16>);
         alpha[i] = 1.f;
         if (mx > m[i] + 8.f) {  // the maximum moves only by more than 2^8, which P's type holds
           alpha[i] = ex2(m[i] - mx);
@@ -1069,7 +1075,7 @@ __global__ void __launch_bounds__(Pt<DH, NT>::THREADS, 3 - NT)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             mq[k] = max3(mq[k], __uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-        const float mx2 = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * p.scale_log2;
+        const float mx2 = fmaf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])), p.scale_log2, -kWeightsUp<F16>);
         float alpha = 1.f;
         if (mx2 > m_use + 8.f) {
           alpha = ex2(m_use - mx2);

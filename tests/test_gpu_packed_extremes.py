@@ -1,5 +1,5 @@
-"""Attention of packed sequences where scores are minus infinity, in every form of the kernels: few and many rows, keys in
-parts, behind a prefix."""
+"""Attention of packed sequences where scores are minus infinity or weights vanish, in every form of the kernels: few and
+many rows, keys in parts, behind a prefix."""
 
 import math
 
@@ -54,8 +54,8 @@ def plain(b, causal=True):
             products = scale * (q.abs() @ kept.abs().T).amax(1, keepdim=True)
             more = 2 * (dh + 8) * 2.0 ** -23 * products + k.shape[0] * 2.0 ** -23 + 2.0 ** -21
             t = u * a + a * more
-            if f16:  # weights below the normal range: half a step of 2^-24
-                t = t + 2.0 ** -25 * (w > 0).double() @ v.abs() / l.clamp(min=1e-300)
+            if f16:  # weights below the normal range: half a step of 2^-24, where the largest weight is 2^7 or more
+                t = t + 2.0 ** -32 * (w > 0).double() @ v.abs() / l.clamp(min=1e-300)
             o[q0:q0 + lq, h] = got
             tol[q0:q0 + lq, h] = t + u * (got.abs().nan_to_num() + t) + (2.0 ** -25 if f16 else 0.0)
             lse[q0:q0 + lq, h] = (top + torch.log(l)).squeeze(1)
@@ -109,3 +109,34 @@ def test_keys_of_minus_infinity(lens, prefix, dh, dtype, workspace, ctx):
         o = check(b.run(ctx, work="all" if workspace else None))
         if prefix is None or hidden:
             assert bool(o.isnan().any())
+
+
+@pytest.mark.parametrize("lq", [1, 3, 70])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("at", [0, 30000, 59999])
+@pytest.mark.parametrize("prefix", [False, True])
+def test_many_small_weights(lq, dh, at, prefix, ctx):
+    """One key, and 60,000 of 2^-25.5 of its weight with all the values that are not zero: together 1.3e-3 of the result."""
+    n, z = 60000, -17.671875
+    b = P.Batch([(lq, 1 if prefix else n)], 4, 2, dh, "f16", prefix=n if prefix else None, pad=0, behind=0)
+    k, v = (b.pk, b.pv) if prefix else (b.k[b.seqs[0][2]:][:n], b.v[b.seqs[0][2]:][:n])
+    b.q.zero_()
+    b.q[:, [h * dh for h in range(4)]] = 8.0
+    scale = 1.0 / 8.0
+    k.zero_()
+    k[:, [0, dh]] = z
+    k[at] = 0.0
+    v.fill_(1.0)
+    v[at] = 0.0
+    if prefix:  # an own key that weighs nothing
+        k0 = b.seqs[0][2]
+        b.k[k0:k0 + 1] = 0.0
+        b.k[k0:k0 + 1, [0, dh]] = -200.0
+        b.v[k0:k0 + 1] = 0.0
+    b.run(ctx, scale=scale, causal=False)
+    w = math.exp(z)
+    want = (n - 1) * w / (1.0 + (n - 1) * w)
+    # a weight's rounding (2^-32 of the largest at most), the score's few operations on 17.7 twice, sums that may cut,
+    # exp2 and the division; the output's half step
+    tol = n * 2.0 ** -32 + want * (8 * 18 * 2.0 ** -23 + n * 2.0 ** -23 + 2.0 ** -21 + 2.0 ** -11) + 2.0 ** -25
+    assert float((b.o.double() - want).abs().max()) <= tol
