@@ -457,8 +457,8 @@ enum { BAG_ROPE_INTERLEAVED = 0, BAG_ROPE_HALF = 1 };
 /* Rotary positions.  Pair i < pairs of each head of q and k turns by position * freqs[i] radians
  * (backwards with inverse, which is the backward pass of q and k) and is multiplied by scale; pair i
  * is columns (2i, 2i + 1) with BAG_ROPE_INTERLEAVED, (i, i + pairs) with BAG_ROPE_HALF; columns from
- * 2 pairs on, and v, are copied.  Angles are exact to 2^-34 of a turn for any 32-bit position, results
- * computed in fp32 and rounded once.  Row r of k and v goes to row slots[r] of k_out and v_out (a row
+ * 2 pairs on, and v, are copied.  Angles are exact to 2^-34 of a turn for any 32-bit position (2^-65 of a turn
+ * for each step of it); their sine and cosine and the results are computed in fp32, and rounded once.  Row r of k and v goes to row slots[r] of k_out and v_out (a row
  * outside [0, capacity) is skipped; the slots of one call have to be distinct), or to row r where
  * slots is null (then capacity >= rows).  Each of q, k and v may be null (with its output).  q_out
  * may be q, and without slots k_out k and v_out v; other overlaps of an output are refused. */

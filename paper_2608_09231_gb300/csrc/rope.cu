@@ -3,8 +3,10 @@
 // Pair i of a head turns by the angle position * f_i.  The host hands f_i over as turns a position, a
 // 64-bit fraction F_i of a turn: the low 64 bits of position * F_i are the angle modulo a turn, exactly
 // but for F_i's own rounding (2^-65 turns a position, 2^-34 at position 2^31), so far positions lose
-// nothing and nothing is computed in fp64.  Its upper 32 bits, as a signed fraction of a turn, give sine
-// and cosine (sincospif).  A CTA computes a row's table once, in shared memory, for all heads; then a
+// nothing and nothing is computed in fp64.  Its nearest quarter turn is taken off in integers; what is left, at
+// most an eighth of a turn, becomes fp32 with 24 bits of its own whatever its size (slow pairs at near
+// positions turn by very little), and sine and cosine (sincospif) are swapped and signed by the quarter.
+// A CTA computes a row's table once, in shared memory, for all heads; then a
 // thread keeps the entries of its V pairs in registers and walks the heads.
 // Bound: HBM (each element read and written once): 32,760 rows of 40 + 40 heads of 128, bf16, 196.6 us (100 % of the
 // copy rate), 6111 rows of 32 + 8 + 8 heads, half of each rotated, into slots 25.7 (floor 22).  With loads only as
@@ -128,10 +130,13 @@ __global__ void __launch_bounds__(R_TH, 4) rope_kernel(const __grid_constant__ R
     if (row0 + r < a.rows) {
       const uint64_t pos = (uint64_t)(a.pos ? (long)__ldg(a.pos + row0 + r) : a.pos0 + row0 + r);
       const uint64_t angle = pos * a.turns[pair];
-      const float half_turns = (float)(int)((angle + 0x80000000ull) >> 32) * 0x1p-31f;  // [-1, 1]
+      const uint64_t quarter = (angle + (1ull << 61)) >> 62;  // the nearest, 0 to 3
+      const float half_turns = (float)(int64_t)(angle - (quarter << 62)) * 0x1p-63f;  // [-1/4, 1/4]
       float s, c;
       sincospif(half_turns, &s, &c);
-      table[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
+      const float cos = quarter & 1 ? s : c, sin = quarter & 1 ? c : s;
+      table[i] = make_float2((quarter == 1 || quarter == 2 ? -cos : cos) * a.scale,
+                             ((quarter >= 2) != (a.inverse != 0) ? -sin : sin) * a.scale);
     }
   }
   __syncthreads();
