@@ -458,8 +458,8 @@ enum { BAG_ROPE_INTERLEAVED = 0, BAG_ROPE_HALF = 1 };
  * (backwards with inverse, which is the backward pass of q and k) and is multiplied by scale; pair i
  * is columns (2i, 2i + 1) with BAG_ROPE_INTERLEAVED, (i, i + pairs) with BAG_ROPE_HALF; columns from
  * 2 pairs on, and v, are copied.  Angles are exact to 2^-34 of a turn for any 32-bit position (2^-65 of a turn
- * for each step of it); their sine and cosine and the results are computed in fp32, and rounded once.  Row r of k and v goes to row slots[r] of k_out and v_out (a row
- * outside [0, capacity) is skipped; the slots of one call have to be distinct), or to row r where
+ * for each step of it); their sine and cosine and the results are computed in fp32, and rounded once.
+ * Row r of k and v goes to row slots[r] of k_out and v_out (a row outside [0, capacity) is skipped; the slots of one call have to be distinct), or to row r where
  * slots is null (then capacity >= rows).  Each of q, k and v may be null (with its output).  q_out
  * may be q, and without slots k_out k and v_out v; other overlaps of an output are refused. */
 typedef struct {
@@ -498,7 +498,7 @@ bag_status bag_rope(bag_ctx* ctx, const bag_rope_args* a);
  *
  * max_q and max_k: the most queries and keys of a sequence, as far as the caller knows (0: does not);
  * a wrong number costs time, not correctness.  work: device workspace of work_bytes, 16-byte aligned,
- * for sums over parts of the keys: bag_attention_work says how much the fastest form takes; with less
+ * for sums over parts of the keys: bag_attention_work says how much the fastest forms take; with less
  * (or null) fewer CTAs share a sequence.  Its contents before and after a call mean nothing, and calls
  * that may run at the same time need one each.  The order of sums depends on the sizes, max_q,
  * max_k and work_bytes. */
@@ -527,7 +527,9 @@ bag_status bag_attention_packed(bag_ctx* ctx, const bag_packed_args* a);
 bag_status bag_attention_prefix(bag_ctx* ctx, const bag_packed_args* a, const void* pk, long ldpk,
                                 const void* pv, long ldpv, long n_prefix);
 
-/* Bytes of workspace for calls of these sizes (n_prefix 0: bag_attention_packed). */
+/* Bytes of workspace with which every call up to these sizes takes its fastest form: of fewer queries, sequences or keys
+ * or a shorter prefix (n_prefix 0: bag_attention_packed alone) too, where nq <= seqs * max_q.  max_q or max_k 0: any, and
+ * for calls that do not know them. */
 bag_status bag_attention_work(bag_ctx* ctx, long nq, int heads, int kv_heads, int dh, long seqs, long max_q,
                               long max_k, long n_prefix, size_t* bytes);
 

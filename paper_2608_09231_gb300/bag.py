@@ -568,7 +568,8 @@ class Context:
         self._chk(self.lib.bag_attention_prefix(self.h, a, kp, ldk, vp, ldv, n))
 
     def attention_work(self, nq, heads, dh, kv_heads, seqs, max_q, max_k, n_prefix=0):
-        """Bytes of workspace for attention_packed, or with n_prefix for attention_prefix, of these sizes."""
+        """Bytes of workspace with which attention_packed, and with n_prefix attention_prefix, take their fastest form at any
+        sizes up to these (max_q or max_k None: not known)."""
         n = _Z()
         self._chk(self.lib.bag_attention_work(self.h, nq, heads, kv_heads, dh, seqs, max_q or 0, max_k or 0, n_prefix,
                                               ctypes.byref(n)))

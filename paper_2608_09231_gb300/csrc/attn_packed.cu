@@ -1427,7 +1427,7 @@ long parts_of(const Plan& t) { return t.parts1 + t.parts2 > 1 ? t.parts1 + t.par
 Plan plan_of(const PackedArgs& a, size_t bytes) {
   Plan t{};
   const long G = a.heads / a.kv_heads, sms = sm_count();
-  const long max_k = std::max(a.max_k, 1L);  // as the caller says, so that the size told for a call is the call's
+  const long max_k = std::max(a.max_k, 1L);
   const long max_q = std::max(1L, std::min(a.max_q, a.nq)), rows = a.nq * G;
   const long most = (long)std::min<size_t>(bytes / part_bytes(a), 1u << 30);  // parts
   t.few = max_q * G <= F_ROWS;
@@ -1493,9 +1493,34 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
 }
 }  // namespace
 
+// A bound of what any call wants whose sizes are at most these (what one call wants is not monotone in them: few
+// rows want many parts, many want none), for its parts as plan_of counts them before it rounds.
 size_t attention_packed_work(const PackedArgs& a) {
-  const Plan t = plan_of(a, ~(size_t)0 >> 1);
-  return parts_of(t) * part_bytes(a) + piece_bytes(a, t);
+  const long G = a.heads / a.kv_heads, sms = sm_count(), all = a.nq * a.heads;  // rows and heads
+  const long max_q = std::max(1L, std::min(a.max_q, a.nq)), max_k = std::max(a.max_k, 1L);
+  const long tiles = cdiv(max_k, PT), pre = cdiv(a.n_prefix, PT);
+  const bool many = max_q * G > F_ROWS;  // beside calls for the few-row kernel others too
+  // Own keys of units of n rows on the tensor cores: p2 <= tiles / 12, and with x = tiles * units / (4 sms), tiles / max(12,
+  // floor(x)) < 13 / 12 * 4 sms / units, where n * units >= rows of all key heads.
+  auto own = [&](long tiles, long rows, long n) { return many && tiles >= 24 ? std::min(tiles / 12 * rows, 13 * sms * n / 3) : 0L; };
+  long kept = own(tiles + pre, all, a.n_prefix == 0 && max_q * G <= PT ? PT : 2 * PT);
+  if (a.n_prefix) {
+    // The prefix with all rows together: few of each sequence, or so many as make that the faster way (writing and reading
+    // two parts at least takes less time than the key tiles that it saves, at most one tile of rows a sequence).
+    const long some = many ? std::min((double)all, (double)a.kv_heads * a.seqs * std::max((double)F_ROWS, pre * 7.8 * 2500.0 / (8.0 * a.dh + 16.0)))
+                           : all;
+    const long p1 = std::max(some, std::min(cdiv(a.n_prefix, 512) * some, 2 * PT * sms));
+    kept = std::max(kept, p1 + std::max(some, own(tiles, some, 2 * PT)));
+  }
+  size_t bytes = (size_t)kept * ((size_t)a.dh * 4 + 8);
+  if (G <= F_ROWS && max_k > 256) {  // equal shares of single tokens' keys
+    const long slots = sms * (a.dh == 64 ? few_ctas<64>() : few_ctas<128>());
+    Plan t{};
+    t.split = 1;
+    t.ctas = (int)std::min(slots, a.seqs * a.kv_heads * std::min(cdiv(max_k, 2 * F_TILE), slots));
+    bytes += piece_bytes(a, t);
+  }
+  return bytes;
 }
 
 cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s) {

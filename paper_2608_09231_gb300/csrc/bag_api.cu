@@ -2167,9 +2167,9 @@ static bag_status bag_attention_work_impl(bag_ctx* ctx, long nq, int heads, int 
   CKS(check_packed(ctx, nq, heads, kv_heads, dh, seqs, max_q, max_k, n_prefix));
   PackedArgs g{};
   g.nq = nq, g.heads = heads, g.kv_heads = kv_heads, g.dh = dh, g.seqs = seqs;
-  g.k_rows = kMaxRows, g.n_prefix = n_prefix;
+  g.n_prefix = n_prefix;
   g.max_q = max_q ? std::min(max_q, nq) : nq;
-  g.max_k = max_k ? std::min(max_k, kMaxRows) : nq;
+  g.max_k = max_k ? std::min(max_k, kMaxRows) : kMaxRows;  // a call takes its number of rows of k for it
   *bytes = nq && seqs ? attention_packed_work(g) : 0;
   return BAG_OK;
 }

@@ -353,7 +353,7 @@ struct PackedArgs {
   int* err;
 };
 cudaError_t attention_packed(const PackedArgs& a, cudaStream_t s);
-// bytes of workspace with which a call takes its fastest form
+// bytes of workspace with which any call up to these sizes takes its fastest form
 size_t attention_packed_work(const PackedArgs& a);
 cudaError_t attention_packed_init();  // part of kernels_init
 
