@@ -123,11 +123,9 @@ class TextAttention:
         self.k, self.v = (torch.empty(cache.texts * cache.room, kv_heads * dh, **bf16) for _ in range(2))
         self.pk, self.pv = (torch.empty(prefix, kv_heads * dh, **bf16) for _ in range(2))
         self.seen = 0  # tokens of the prefix so far
-        room = cache.room
-        self.work = torch.empty(max(ctx.attention_work(n, heads, dh, kv_heads, texts, max_q, max_k, p)
-                                    for n, texts, max_q, max_k, p in ((rows, cache.texts, rows, room, 0), (rows, cache.texts, rows, room, prefix),
-                                                                      (min(rows, cache.texts), cache.texts, 1, room, prefix),
-                                                                      (min(rows, cache.texts), cache.texts, 1, room, 0), (rows, 1, rows, prefix, 0))),
+        # for steps of any number of tokens, and for the prefix
+        self.work = torch.empty(max(ctx.attention_work(rows, heads, dh, kv_heads, cache.texts, min(rows, cache.room), cache.room, prefix),
+                                    ctx.attention_work(prefix, heads, dh, kv_heads, 1, prefix, prefix)),
                                 device=DEV, dtype=torch.uint8)
 
     def _project(self, h):

@@ -1,4 +1,4 @@
-"""Text layers whose steps were refused before."""
+"""Text layers whose steps were refused before, and the workspace that a layer keeps for all of its steps."""
 
 import math
 
@@ -69,3 +69,18 @@ def test_rows_of_another_width(prefix, ctx):
     with pytest.raises(ValueError):
         layer.step(h, cache.extend([4]))
     assert torch.equal(h, before) and bool((layer.k == 9).all()) and cache.lens == [0]
+
+
+@pytest.mark.parametrize("texts,room,rows,prefix,heads,kv_heads", [(8, 16384, 1024, 0, 32, 8), (1, 32768, 512, 0, 28, 4),
+                                                                  (1, 16384, 512, 700, 28, 4), (16, 600, 2048, 1024, 6, 2)])
+def test_a_layer_keeps_memory_for_every_step(texts, room, rows, prefix, heads, kv_heads, ctx):
+    """What the library asks for a step's own sizes, and for the sizes of any that the layer may take, the layer has."""
+    cache = prompt.TextCache(texts, room)
+    layer = prompt.TextAttention(ctx, prompt.random_weights(256, heads, kv_heads), heads, kv_heads, cache, rows, prefix)
+    for n in (1, 2, 3, 8, 31, 32, 64, 128, 129, 256, 500, rows):
+        for q in {min(n, room), -(-n // texts)}:
+            for k in {q, min(room, q + room // 2), room}:
+                for p in {0, prefix}:
+                    assert ctx.attention_work(n, heads, 128, kv_heads, texts, q, k, p) <= layer.work.numel()
+    assert ctx.attention_work(prefix, heads, 128, kv_heads, 1, None, prefix) <= layer.work.numel()
+    assert layer.work.numel() < 200e6
