@@ -1502,14 +1502,15 @@ size_t attention_packed_work(const PackedArgs& a) {
   const bool many = max_q * G > F_ROWS;  // beside calls for the few-row kernel others too
   // Own keys of units of n rows on the tensor cores: p2 <= tiles / 12, and with x = tiles * units / (4 sms), tiles / max(12,
   // floor(x)) < 13 / 12 * 4 sms / units, where n * units >= rows of all key heads.
-  auto own = [&](long tiles, long rows, long n) { return many && tiles >= 24 ? std::min(tiles / 12 * rows, 13 * sms * n / 3) : 0L; };
+  auto up_to = [](long times, long rows, long cap) { return rows >= cap ? cap : std::min(times * rows, cap); };  // times >= 1
+  auto own = [&](long tiles, long rows, long n) { return many && tiles >= 24 ? up_to(tiles / 12, rows, 13 * sms * n / 3) : 0L; };
   long kept = own(tiles + pre, all, a.n_prefix == 0 && max_q * G <= PT ? PT : 2 * PT);
   if (a.n_prefix) {
     // The prefix with all rows together: few of each sequence, or so many as make that the faster way (writing and reading
     // two parts at least takes less time than the key tiles that it saves, at most one tile of rows a sequence).
     const long some = many ? std::min((double)all, (double)a.kv_heads * a.seqs * std::max((double)F_ROWS, pre * 7.8 * 2500.0 / (8.0 * a.dh + 16.0)))
                            : all;
-    const long p1 = std::max(some, std::min(cdiv(a.n_prefix, 512) * some, 2 * PT * sms));
+    const long p1 = std::max(some, up_to(cdiv(a.n_prefix, 512), some, 2 * PT * sms));
     kept = std::max(kept, p1 + std::max(some, own(tiles, some, 2 * PT)));
   }
   size_t bytes = (size_t)kept * ((size_t)a.dh * 4 + 8);

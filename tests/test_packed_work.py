@@ -127,3 +127,15 @@ def test_nothing_where_no_call_shares(tmp_path):
         texts, room, rows, prefix, heads, kv = layer
         (_, told, _, _, _), = run(tmp_path, [(152, heads, kv, 128, rows, prefix, texts, rows, room, 1, 1, 0, 1, 1, 1)])
         assert told < 250e6, (layer, told)
+
+
+def test_sizes_that_no_memory_holds(tmp_path):
+    """The largest sizes that are accepted: the size told is that of the formula, whatever it is."""
+    rows, kv = 0x7fffff00, 65535
+    cases = [(152, kv, kv, 128, rows, p, rows, q, 0, 1, 1, 0, 1, 1, 1) for p in (0, rows) for q in (0, 1, 1000)]
+    for c, (_, told, _, _, _) in zip(cases, run(tmp_path, cases)):
+        cap, few = 13 * 152 * 256 // 3, 304 * 2 * 16 * 520 + (rows + 1) * 8
+        if c[5] == 0:
+            assert told == (0 if c[7] == 1 else cap * 520) + few
+        else:
+            assert told >= 2 * rows * kv * 520 + few and told < 2 ** 62
