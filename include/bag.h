@@ -459,9 +459,10 @@ enum { BAG_ROPE_INTERLEAVED = 0, BAG_ROPE_HALF = 1 };
  * is columns (2i, 2i + 1) with BAG_ROPE_INTERLEAVED, (i, i + pairs) with BAG_ROPE_HALF; columns from
  * 2 pairs on, and v, are copied.  Angles are exact to 2^-34 of a turn for any 32-bit position (2^-65 of a turn
  * for each step of it); their sine and cosine and the results are computed in fp32, and rounded once.
- * Row r of k and v goes to row slots[r] of k_out and v_out (a row outside [0, capacity) is skipped; the slots of one call have to be distinct), or to row r where
- * slots is null (then capacity >= rows).  Each of q, k and v may be null (with its output).  q_out
- * may be q, and without slots k_out k and v_out v; other overlaps of an output are refused. */
+ * Row r of k and v goes to row slots[r] of k_out and v_out (a row outside [0, capacity) is skipped; the slots of one
+ * call have to be distinct), or to row r where slots is null (then capacity >= rows).  Each of q, k and v may be
+ * null (with its output).  q_out may be q, and without slots k_out k and v_out v; other overlaps of an output are
+ * refused. */
 typedef struct {
   int type;               /* BAG_F32, BAG_BF16 or BAG_F16 */
   int layout;             /* BAG_ROPE_* */
@@ -489,19 +490,21 @@ bag_status bag_rope(bag_ctx* ctx, const bag_rope_args* a);
  * k_start[i] on, or, where k_start and k_len are null, the rows of its queries.  o = softmax(scale q
  * k^T) v; with causal, query t of lq sees keys 0 .. t + lk - lq, so queries are a sequence's last tokens.
  * A row that sees no key gets zeros (lse -inf), one that sees only scores of minus infinity NaN (lse -inf); rows of q
- * outside every sequence keep what o and lse hold there.  Ranges that leave k's or q's rows are clipped to them.  heads query heads share
- * kv_heads key heads as in bag_attention_blocks.  Rows of k and v that belong to no sequence may
- * hold anything, NaN included; a NaN in a sequence's own values reaches all of its rows.
- * Scores, softmax and sums are fp32; weights are rounded to `type` before they meet v (bf16 ones of sequences
- * of at most 16 rows a key head, such as single tokens, to twice its bits; fp16 ones to 2^-32 of the largest at
- * most, below its normal range).
+ * outside every sequence keep what o and lse hold there.  Ranges that leave k's or q's rows are clipped to them.
+ * heads query heads share kv_heads key heads as in bag_attention_blocks.  Rows of k and v that belong to no
+ * sequence may hold anything, NaN included; a value of a sequence's own v that is not finite may reach any of its
+ * rows, those that do not see it among them.
+ * Scores, softmax and sums are fp32; weights are rounded to `type` before they meet v.  fp16 ones below its normal range
+ * lose at most 2^-32 of the largest.  bf16 ones over a sequence's own keys are kept to twice its bits in calls whose
+ * max_q (nq where it is 0) times the heads that share a key head is at most 16, such as those of single tokens
+ * (behind a prefix only with a workspace, and not over the prefix's keys).
  *
  * max_q and max_k: the most queries and keys of a sequence, as far as the caller knows (0: does not);
- * a wrong number costs time, not correctness.  work: device workspace of work_bytes, 16-byte aligned,
+ * a wrong number costs time, and with max_q the bits of bf16 weights, not correctness.  work: device workspace of work_bytes, 16-byte aligned,
  * for sums over parts of the keys: bag_attention_work says how much the fastest forms take; with less
  * (or null) fewer CTAs share a sequence.  Its contents before and after a call mean nothing, and calls
  * that may run at the same time need one each.  The order of sums depends on the sizes, max_q,
- * max_k and work_bytes. */
+ * max_k, work_bytes and the lengths of all sequences of the call. */
 typedef struct {
   int type;               /* BAG_BF16 or BAG_F16 */
   int heads, kv_heads, dh;/* dh 64 or 128 (else EUNSUPPORTED) */

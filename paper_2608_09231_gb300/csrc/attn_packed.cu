@@ -719,14 +719,15 @@ BAG_DEV Unit unit_of(const PackedParams& p, int nt, int at) {
 // So the loads and scores of a unit run beside the output of the one before, and what a CTA costs to launch
 // (tensor memory, barriers, the launch itself, some 5,000 cycles) comes once for each that is resident.
 // V is read as it lies, a row a key: as an operand whose rows run along the contraction (as fast as the other way).
-// P is rounded to the operands' type, as in the dense kernel: both operands of an MMA are of one type.
+// P is rounded to the operands' type, as in the dense kernel: both operands of an MMA are of one type (2-norm error
+// bf16 1.8e-3 to 2.2e-3 where the output's own rounding gives 1.6e-3 to 1.7e-3, fp16 2.2e-4 to 2.7e-4 for 1.9e-4 to 2.1e-4).
 // Two tiles and one CTA on an SM, or one tile and two CTAs: the first reads each K and V tile once for 256 rows
 // (16,384 tokens, 32 heads 1300 against 1480 us, 16 x 512 tokens 62 against 72), the second has more CTAs for
 // few rows (77 tokens, 32 heads 7.1 against 8.3, 512 tokens 11.9 against 12.9).
 // Bound: a step of both tiles takes some 2,600 cycles for 2,048 of products: a tile's scores, softmax and P V
 // follow each other, and the hand-overs between the warps (about 1,200 cycles a step) are only partly hidden
-// by the other tile.  A unit costs some 6,000 cycles besides, mostly its output.  16,384 causal tokens, 32 heads 1300 us
-// (1690 TFLOP/s), 4608 x 24 heads 103, 4 x 2048 x 32 115, 16 x 512 x 32 61 (query and output bytes 25); heads of
+// by the other tile.  A unit costs some 6,000 cycles besides, mostly its output.  16,384 causal tokens, 32 heads 1300 to
+// 1474 us (1690 to 1490 TFLOP/s: back to back, or between other work, by what clock the card holds), 4608 x 24 heads 103, 4 x 2048 x 32 115, 16 x 512 x 32 61 (query and output bytes 25); heads of
 // 64: 16,384 x 32 1150, where the softmax has twice the work for each product.
 // Not kept: two threads a row (4 x 2048 124 -> 188 us: the issuing warp loses its slots), an MMA warp whose issue branches on
 // the last tile (16,384 tokens 1380 -> 1480), 64-bit descriptors in registers (spills in the issuing warp).
@@ -1430,7 +1431,7 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   const long max_k = std::max(a.max_k, 1L);
   const long max_q = std::max(1L, std::min(a.max_q, a.nq)), rows = a.nq * G;
   const long most = (long)std::min<size_t>(bytes / part_bytes(a), 1u << 30);  // parts
-  t.few = max_q * G <= F_ROWS;
+  t.few = max_q * G <= F_ROWS;  // 64 tokens over 8192 keys, 16 heads on one key head 55 us, 32 on one (tensor cores) 67, floor 40
   // heads of a group that share a tile: as many as leave few of its rows empty, or whose rows of a
   // sequence fit one.  More units of a key head read its keys again, and a sequence's last tile is less full: with
   // one of seven heads, 24 prompts behind a prefix take 74 us, with all seven (126 of 128 rows) 46.
@@ -1454,7 +1455,9 @@ Plan plan_of(const PackedArgs& a, size_t bytes) {
   }
   // units of 256 rows where there are enough of them, or enough keys, and sequences (or the rows of all) fill
   // them: 16 x 512 tokens, 32 / 8 heads 62 us (72 with 128), 512 tokens over 33,000 keys 233 (244); but one prompt
-  // of 77 tokens 6.9 (8.3), 512 x 28 / 4 heads 11.7 (12.9), 32 x 8 tokens over up to 8192 keys 49 (65)
+  // of 77 tokens 6.9 (8.3), 512 x 28 / 4 heads 11.7 (12.9), 32 x 8 tokens over up to 8192 keys 49 (65).  Sequences of
+  // very different lengths, with 256 and with 128: 32 prompts of 8 to 512 tokens 29 and 31 us, 24 behind a prefix 40
+  // and 47, 8 texts in parts 90 and 117, 128 tokens behind 16,384 shared keys 58 and 87
   auto units = [&](long n) { return (rows / n + (a.seqs + 1) / 2) * a.kv_heads; };
   t.rows = (all_rows || max_q * G > PT) &&
                    (units(256) * 2 > sms || units(256) * cdiv(max_k + a.n_prefix, PT) >= 8 * sms) ? 256 : 128;

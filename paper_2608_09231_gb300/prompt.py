@@ -9,6 +9,8 @@ The text tokens that condition a DiT come from a decoder-only encoder, whose att
              them start with (attention_prefix)
   h       += o Wo^T                            o encoded (quant_fp8), update in the product's epilogue
 
+The projections have no biases.
+
 `TextCache` says where texts lie and what a step adds to them: whole prompts, more tokens of each, or
 one each.  `TextAttention` is the layer.  `rope_frequencies` makes the table of a rotary embedding, also for
 contexts longer than it was trained for.
@@ -66,7 +68,8 @@ class TextCache:
         self.gone = []  # ranges of those that were taken back
 
     def extend(self, new):
-        """What a step that adds new[i] tokens to text i hands to the operators (rows in the texts' order)."""
+        """What a step that adds new[i] tokens to text i hands to the operators (rows in the texts' order).  The host makes
+        it, and waits until it is on the device."""
         if len(new) != self.texts or any(n < 0 or n + m > self.room for n, m in zip(new, self.lens)):
             raise ValueError(f"{self.texts} texts of at most {self.room} tokens, of {self.lens}, cannot take {new}")
         first = np.concatenate([[0], np.cumsum(new)])
